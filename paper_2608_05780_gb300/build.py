@@ -28,8 +28,11 @@ LIB = os.path.join(HERE, "libevisel.so")
 
 SOURCES = ["probe_attn.cu", "attn_combine.cu", "evidence.cu", "evisel_capi.cpp", "evisel_noalloc.cu", "evisel_selftest.cu", "intra_frame.cu",
            "cross_frame.cu", "text_evidence.cu", "topp_mask.cu",
-           "coarse_evidence.cu"]
-HEADERS = ["evisel_internal.h", "evisel_plan.h", "sm103_ptx.cuh"]
+           "coarse_evidence.cu", "evisel_cache.cpp", "cache_attn.cu", "cache_evidence.cu", "cache_evict.cu",
+           "cache_append.cu", "cache_select.cu"]
+HEADERS = ["evisel_internal.h", "evisel_plan.h", "sm103_ptx.cuh", "cache_internal.h", "cache_common.cuh",
+           "cache_choose.cuh", "cache_pages.cuh"]
+PUBLIC = ["evisel.h", "evisel_cache.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", "-I" + INCLUDE, "-I" + CSRC]
@@ -48,7 +51,7 @@ ID_PREFIX = b"evisel-build-id:"
 def build_id() -> str:
     """SHA-256 (first 24 hex digits) of everything that determines the binary."""
     h = hashlib.sha256()
-    for f in [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.join(INCLUDE, "evisel.h"), __file__]:
+    for f in [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.join(INCLUDE, f) for f in PUBLIC] + [__file__]:
         h.update(os.path.basename(f).encode() + b"\0")
         with open(f, "rb") as fh:
             h.update(fh.read())

@@ -1,0 +1,83 @@
+// Eviction: the tokens of a (sequence, KV head) with the most accumulated
+// weight, its sinks and its recent ones, compacted into other pages.
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "cache_choose.cuh"
+#include "cache_pages.cuh"
+
+namespace evisel {
+namespace {
+
+constexpr int kChooseThreads = 1024;
+
+__global__ void __launch_bounds__(kChooseThreads) cache_evict_choose_kernel(const __grid_constant__ CacheEvictLaunch L) {
+  __shared__ ChooseScratch sc;
+  const int b = blockIdx.x / L.c.hkv, h = blockIdx.x % L.c.hkv;
+  int len = cache_len(L.c, b, h, L.status);
+  if (len > L.acc_len) {
+    record_bounds(L.status);
+    len = static_cast<int>(L.acc_len);
+  }
+  const int count = min(len, L.budget);
+  const bool all = len <= L.budget;
+  const int sink = all ? count : L.sink, recent = all ? 0 : L.recent;
+  const float* acc = L.acc + (static_cast<int64_t>(b) * L.c.hkv + h) * L.acc_len;
+  int32_t* kept = L.kept + (static_cast<int64_t>(b) * L.c.hkv + h) * L.budget;
+  float* out = L.acc_out + (static_cast<int64_t>(b) * L.c.hkv + h) * L.acc_out_len;
+  auto put = [&](int rank, int i) {
+    kept[rank] = i;
+    out[rank] = acc[i];
+  };
+  for (int i = threadIdx.x; i < sink; i += kChooseThreads) put(i, i);
+  for (int i = threadIdx.x; i < recent; i += kChooseThreads) put(count - recent + i, len - recent + i);
+  for (int i = count + threadIdx.x; i < L.budget; i += kChooseThreads) kept[i] = -1;
+  for (int64_t i = count + threadIdx.x; i < L.acc_out_len; i += kChooseThreads) out[i] = 0.f;
+  choose_top(sink, len - recent, count - sink - recent, [&](int i) { return order_key(__ldg(acc + i)); }, sc,
+             [&](int rank, int i) { put(sink + rank, i); });
+  if (threadIdx.x == 0) L.out_lens[b * L.out.ls[0] + h * L.out.ls[1]] = count;
+}
+
+// The source of an evicted cache's page: the kept tokens, in order.
+struct KeptTokens {
+  const CacheEvictLaunch& L;
+  int b, h, count;
+  const int32_t* kept;
+  __device__ __forceinline__ KeptTokens(const CacheEvictLaunch& L_, int b_, int h_) : L(L_), b(b_), h(h_) {
+    count = min(cache_len(L.c, b, h, L.status), L.budget);
+    if (count > L.acc_len) count = static_cast<int>(L.acc_len);
+    kept = L.kept + (static_cast<int64_t>(b) * L.c.hkv + h) * L.budget;
+  }
+  __device__ __forceinline__ int first() const { return 0; }             // positions written: [first, end)
+  __device__ __forceinline__ int end() const { return count; }
+  __device__ __forceinline__ void rows(int pos, const uint4*& k, const uint4*& v) const {
+    const int i = __ldg(kept + pos);
+    const int64_t id = cache_page(L.c, b, h, i >> L.c.log_page, L.status), slot = i & (L.c.page - 1);
+    k = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.c.k) + id * L.c.ks[0] + h * L.c.ks[1] + slot * L.c.ks[2]);
+    v = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.c.v) + id * L.c.vs[0] + h * L.c.vs[1] + slot * L.c.vs[2]);
+  }
+};
+
+template <class T, int D>
+__global__ void __launch_bounds__(kPageThreads) cache_evict_copy_kernel(const __grid_constant__ CacheEvictLaunch L) {
+  const int h = blockIdx.y, b = blockIdx.z;
+  fill_page<T, D>(L.out, L.out_k, L.out_v, L.out_mean, b, h, blockIdx.x, KeptTokens(L, b, h), L.status);
+}
+
+template <class T, int D>
+cudaError_t launch_d(const CacheEvictLaunch& L, cudaStream_t stream) {
+  cache_evict_choose_kernel<<<L.c.batch * L.c.hkv, kChooseThreads, 0, stream>>>(L);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  cache_evict_copy_kernel<T, D><<<dim3((L.budget + L.out.page - 1) / L.out.page, L.c.hkv, L.c.batch), kPageThreads, 0, stream>>>(L);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_cache_evict(const CacheEvictLaunch& L, cudaStream_t stream) {
+  if (L.c.dtype == 0) return L.c.head_dim == 128 ? launch_d<BF16, 128>(L, stream) : launch_d<BF16, 64>(L, stream);
+  return L.c.head_dim == 128 ? launch_d<FP16, 128>(L, stream) : launch_d<FP16, 64>(L, stream);
+}
+
+}  // namespace evisel

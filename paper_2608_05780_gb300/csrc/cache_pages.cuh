@@ -1,0 +1,61 @@
+// One page of a cache filled from a source of tokens, with its mean key.
+#pragma once
+
+#include "cache_common.cuh"
+
+namespace evisel {
+
+constexpr int kPageThreads = 256;
+
+// Writes the page's slots at positions [src.first(), src.end()) and, with
+// `mean`, the mean of all its keys before src.end() (the older ones read back
+// from the page). A block of kPageThreads threads per (page, head, sequence); D / 8
+// threads share a token, 16 bytes of it each.
+template <class T, int D, class Source>
+__device__ __forceinline__ void fill_page(const CacheView& c, void* k_out, void* v_out, void* mean, int b, int h, int page,
+                                          const Source& src, int* status) {
+  constexpr int LANES = D / 8, GROUPS = kPageThreads / LANES;
+  __shared__ float sums[GROUPS][D];
+  const int p0 = page << c.log_page, p1 = min(p0 + c.page, src.end());
+  if (p1 <= p0 || p1 <= src.first()) return;     // (the whole block)
+  const int64_t id = cache_page(c, b, h, page, status);
+  uint16_t* k = static_cast<uint16_t*>(k_out) + id * c.ks[0] + h * c.ks[1];
+  uint16_t* v = static_cast<uint16_t*>(v_out) + id * c.vs[0] + h * c.vs[1];
+  const int x = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+  float sum[8] = {};
+  for (int pos = p0 + grp; pos < p1; pos += GROUPS) {
+    uint4* kd = reinterpret_cast<uint4*>(k + (pos - p0) * c.ks[2]) + x;
+    uint4 key;
+    if (pos >= src.first()) {
+      const uint4 *ks, *vs;
+      src.rows(pos, ks, vs);
+      key = __ldg(ks + x);
+      const uint4 value = __ldg(vs + x);
+      *kd = key;
+      *(reinterpret_cast<uint4*>(v + (pos - p0) * c.vs[2]) + x) = value;
+    } else {
+      if (!mean) continue;
+      key = *kd;
+    }
+    float f[8];
+    unpack8<T>(key, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += f[e];
+  }
+  if (!mean) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[grp][x * 8 + e] = sum[e];
+  __syncthreads();
+  const float n = static_cast<float>(p1 - p0);
+  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(mean) + (id * c.hkv + h) * D);
+  for (int i = threadIdx.x; i < D / 2; i += kPageThreads) {
+    float lo = 0.f, hi = 0.f;
+    for (int g = 0; g < GROUPS; ++g) {
+      lo += sums[g][2 * i];
+      hi += sums[g][2 * i + 1];
+    }
+    dst[i] = T::pack(lo / n, hi / n);
+  }
+}
+
+}  // namespace evisel

@@ -14,6 +14,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "../../include/evisel.h"
+#include "cache_internal.h"
 #include "evisel_internal.h"
 #include "evisel_plan.h"
 
@@ -438,6 +439,7 @@ struct evisel_ws {
   // coarse map scratch: block affinities and row normalisers of the text rows
   void* coarse_buf = nullptr;
   size_t coarse_bytes = 0;
+  WsCache cache;                    // scratch of the paged-cache calls
 };
 
 namespace {
@@ -633,6 +635,30 @@ int launch_text_sums(evisel_ws* ws, float* tok, float* frame, int accumulate, co
 }
 
 }  // namespace
+
+// What the paged-cache calls (evisel_cache.cpp) use of a workspace.
+namespace evisel {
+int ws_acquire(evisel_ws** inout) { return *inout ? EVISEL_OK : create_ws(inout); }
+WsCache& ws_cache(evisel_ws* ws) { return ws->cache; }
+int* ws_status(evisel_ws* ws) { return ws->status; }
+cudaStream_t ws_last_stream(evisel_ws* ws) { return ws->last_stream; }
+void ws_ran_on(evisel_ws* ws, cudaStream_t stream) { ws->last_stream = stream; }
+
+int encode_map4(CUtensorMap* map, const void* base, int dtype, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
+                const uint32_t (&box)[4]) {
+  auto enc = tensor_map_encoder();
+  if (!enc) return fail(EVISEL_ECUDA, "cuTensorMapEncodeTiled unavailable from the driver");
+  cuuint64_t d[4], st[3];
+  cuuint32_t bx[4], estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) d[i] = dims[i], bx[i] = box[i];
+  for (int i = 0; i < 3; ++i) st[i] = strides[i];
+  const CUresult r = enc(map, dtype == 0 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                         const_cast<void*>(base), d, st, bx, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(EVISEL_ECUDA, "cuTensorMapEncodeTiled failed: " + std::to_string(r));
+  return EVISEL_OK;
+}
+}  // namespace evisel
 
 extern "C" {
 
@@ -1125,6 +1151,7 @@ void evisel_free(evisel_ws* ws) {
   if (ws->topp_done) cudaEventSynchronize(ws->topp_done);
   if (ws->topp_buf) cudaFree(ws->topp_buf);
   if (ws->coarse_buf) cudaFree(ws->coarse_buf);
+  if (ws->cache.buf) cudaFree(ws->cache.buf);
   if (ws->topp_stage) cudaFreeHost(ws->topp_stage);
   if (ws->topp_done) cudaEventDestroy(ws->topp_done);
   if (prev >= 0 && prev != ws->device) cudaSetDevice(prev);

@@ -1,0 +1,442 @@
+"""The paged-cache calls against their float64 definitions (oracle/cache.py), at
+the sizes, masks and layouts where they can go wrong. Bounds: cache_helpers.
+"""
+import numpy as np
+import pytest
+
+from cache_helpers import check_attention, make_cache, random_tree, tensor, tree_words, u_of
+from oracle import cache as ref_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def _types():
+    import torch
+    return {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def _status(ev, ws):
+    assert ev.evisel_status(ws) == 0
+
+
+# --- attention ------------------------------------------------------------------
+
+# lens, T, hq, hkv, d, page, dtype, layout, gain
+ATTEND = [
+    ([0], 1, 1, 1, 64, 16, "bf16", "hnd", 1.0),                        # nothing cached
+    ([1], 1, 7, 1, 128, 64, "bf16", "hnd", 1.0),
+    ([63, 64, 65], 1, 4, 2, 64, 64, "bf16", "nhd", 1.0),               # unit edges
+    ([127, 128, 129, 0, 300], 1, 28, 4, 128, 128, "bf16", "hnd", 1.0),
+    ([1000, 17], 1, 28, 4, 128, 16, "fp16", "nhd", 4.0),               # pages inside units, sharp logits
+    ([777], 2, 14, 2, 128, 32, "bf16", "hnd", 4.0),                    # 14 rows
+    ([200, 0, 5], 3, 16, 8, 64, 16, "fp16", "hnd", 1.0),
+    ([500], 16, 2, 2, 128, 64, "bf16", "hnd", 1.0),                    # 16 rows
+    ([500], 17, 1, 1, 64, 64, "bf16", "nhd", 1.0),                     # 17
+    ([333, 1], 9, 8, 2, 128, 32, "bf16", "hnd", 4.0),                  # 36 rows
+    ([129, 700], 33, 7, 1, 64, 64, "fp16", "hnd", 1.0),                # 231 rows, two mask words
+    ([260], 64, 14, 2, 128, 128, "bf16", "hnd", 4.0),                  # 448 rows
+    ([640, 64], 37, 4, 1, 128, 16, "bf16", "nhd", 1.0),                # 148 rows
+    ([40], 5, 128, 1, 64, 16, "bf16", "hnd", 1.0),                     # a group of 128 heads
+]
+
+
+@pytest.mark.parametrize("lens,t,hq,hkv,d,page,dtype,layout,gain", ATTEND)
+def test_attention_of_drafted_trees(cuda_lib, lens, t, hq, hkv, d, page, dtype, layout, gain):
+    """Random trees, ragged numbers of drafted tokens, NaN in every slot past a sequence's length."""
+    import torch
+    rng = np.random.default_rng(len(lens) * 1000 + t)
+    ty = _types()[dtype]
+    cache, ref = make_cache(rng, lens, hkv, d, page, ty, layout, gain=gain)
+    batch = len(lens)
+    q, q_ref = tensor(rng, (batch, t, hq, d), ty)
+    k, k_ref = tensor(rng, (batch, t, hkv, d), ty, gain)
+    v, v_ref = tensor(rng, (batch, t, hkv, d), ty)
+    allowed = random_tree(rng, batch, t)
+    drafted = rng.integers(0 if t > 1 else 1, t + 1, batch)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, tree=tree_words(allowed),
+                                                 drafted=torch.from_numpy(drafted.astype(np.int32)).cuda())
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref, allowed, drafted), d, ty)
+
+
+@pytest.mark.parametrize("t", [1, 5, 40])
+def test_attention_defaults(cuda_lib, t):
+    """A chain without a tree; every token without counts; one tree for all; the cache alone; a scale of its own."""
+    rng = np.random.default_rng(t)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [90, 0, 257], 2, 128, 32, ty)
+    q, q_ref = tensor(rng, (3, t, 6, 128), ty)
+    k, k_ref = tensor(rng, (3, t, 2, 128), ty)
+    v, v_ref = tensor(rng, (3, t, 2, 128), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref), 128, ty, "chain")
+    tree = random_tree(rng, 1, t)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, tree=tree_words(tree)[0], ws=ws, softmax_scale=0.25)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref, np.repeat(tree, 3, 0), scale=0.25), 128, ty, "one tree")
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, ws=ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), 128, ty, "cache alone")
+    _status(cuda_lib, ws)
+
+
+def test_attention_rows_without_any_key(cuda_lib):
+    """Bits that leave a row nothing, over an empty cache and over one token; and values that no row may see."""
+    import torch
+    rng = np.random.default_rng(5)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [0, 1], 1, 64, 16, ty)
+    q, q_ref = tensor(rng, (2, 4, 3, 64), ty)
+    k, k_ref = tensor(rng, (2, 4, 1, 64), ty)
+    v, v_ref = tensor(rng, (2, 4, 1, 64), ty)
+    allowed = np.zeros((2, 4, 4), bool)
+    allowed[0, 1, 1] = allowed[0, 2, 0] = True
+    allowed[1, 3, 1] = True
+    want = ref_cache.attention(ref, q_ref, k_ref, v_ref, allowed)
+    bad = ~allowed.any(1)                                    # drafted tokens that nobody attends
+    k[torch.from_numpy(bad).cuda()] = float("inf")
+    v[torch.from_numpy(bad).cuda()] = float("nan")
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, tree=tree_words(allowed))
+    check_attention(o, lse, want, 64, ty)
+    assert torch.all(o[0, 0] == 0) and torch.all(o[0, 3] == 0)
+    # Token 1's value spoils the rows that attend it and no others.
+    v[0, 1] = float("nan")
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, tree=tree_words(allowed), ws=ws)
+    assert torch.isnan(o[0, 1]).all() and not torch.isnan(o[0, [0, 2, 3]]).any() and not torch.isnan(o[1]).any()
+
+
+def test_attention_of_strided_inputs(cuda_lib):
+    """q, k and v as views of one fused projection, outputs given, another stream than the default."""
+    import torch
+    rng = np.random.default_rng(8)
+    ty = _types()["fp16"]
+    cache, ref = make_cache(rng, [100, 33], 2, 64, 16, ty)
+    x, x_ref = tensor(rng, (2, 6, 8 + 2 + 2, 64), ty)
+    o = torch.empty((2, 6, 8, 64), dtype=ty, device="cuda")
+    lse = torch.empty((8, 2, 6), device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    got = cuda_lib.evisel_cache_attention(cache, x[:, :, :8], x[:, :, 8:10], x[:, :, 10:], o=o, lse=lse, stream=stream)
+    assert got[0] is o and got[1] is lse
+    stream.synchronize()
+    check_attention(o, lse, ref_cache.attention(ref, x_ref[:, :, :8], x_ref[:, :, 8:10], x_ref[:, :, 10:]), 64, ty)
+    # batch and heads in another order in memory
+    q = x[:, :, :8].permute(2, 0, 1, 3).contiguous().permute(1, 2, 0, 3)
+    o2, lse2, _ = cuda_lib.evisel_cache_attention(cache, q, x[:, :, 8:10], x[:, :, 10:])
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_attention_of_pages_in_a_larger_pool(cuda_lib):
+    """Keys and values interleaved in one pool [P, 2, hkv, page, d], and heads outside the pages."""
+    import torch
+    rng = np.random.default_rng(9)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [150, 70], 2, 128, 32, ty)
+    q, q_ref = tensor(rng, (2, 1, 8, 128), ty)
+    want = ref_cache.attention(ref, q_ref)
+    pool = torch.stack([cache.k, cache.v], 1)
+    one = cuda_lib.Cache(pool[:, 0], pool[:, 1], cache.table, cache.lens)
+    heads = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in (cache.k, cache.v)]
+    two = cuda_lib.Cache(*heads, cache.table, cache.lens)
+    for c in (one, two):
+        o, lse, ws = cuda_lib.evisel_cache_attention(c, q)
+        check_attention(o, lse, want, 128, ty)
+        _status(cuda_lib, ws)
+
+
+@pytest.mark.parametrize("t", [1, 12])
+def test_attention_of_lengths_per_head(cuda_lib, t):
+    rng = np.random.default_rng(10)
+    ty = _types()["bf16"]
+    lens = [[70, 0, 129], [1, 64, 500]]
+    cache, ref = make_cache(rng, lens, 3, 64, 16, ty, per_head=True)
+    q, q_ref = tensor(rng, (2, t, 6, 64), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), 64, ty)
+
+
+def test_attention_is_the_same_twice_and_in_a_graph(cuda_lib):
+    """Same bits again, alone, among others and replayed with new lengths."""
+    import torch
+    rng = np.random.default_rng(11)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [2000, 900, 3], 4, 128, 64, ty, poison=False)
+    q, q_ref = tensor(rng, (3, 2, 28, 128), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q)
+    o2, lse2, _ = cuda_lib.evisel_cache_attention(cache, q, ws=ws)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cuda_lib.evisel_cache_attention(cache, q, ws=ws, o=o2, lse=lse2, stream=torch.cuda.current_stream())
+    for lens in ([2000, 900, 3], [1, 555, 0], [1999, 64, 64]):
+        cache.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        graph.replay()
+        ref["lens"] = np.array(lens)
+        check_attention(o2, lse2, ref_cache.attention(ref, q_ref), 128, ty, str(lens))
+
+
+# --- evidence -------------------------------------------------------------------
+
+@pytest.mark.parametrize("lens,t,hq,hkv,d,page,dtype,layout", [
+    ([0], 1, 1, 1, 64, 16, "bf16", "hnd"),
+    ([1, 127, 128, 129], 1, 14, 2, 128, 64, "bf16", "nhd"),
+    ([300, 0, 77], 5, 16, 8, 64, 16, "fp16", "hnd"),
+    ([1000], 33, 7, 1, 128, 128, "bf16", "hnd"),           # 231 rows
+    ([200, 513], 40, 12, 2, 64, 32, "bf16", "hnd"),        # 240 rows
+    ([140], 130, 3, 1, 128, 32, "fp16", "nhd"),            # 390 rows
+    ([260], 2, 128, 1, 64, 16, "bf16", "hnd"),             # a group of 128 heads
+])
+def test_evidence(cuda_lib, lens, t, hq, hkv, d, page, dtype, layout):
+    """Weights of the attention's own LSE; rows left out by ``use`` and by counts, whose queries are not finite;
+    NaN in the slots past each length; written, added to, and entries past a length left alone."""
+    import torch
+    rng = np.random.default_rng(t * 7 + len(lens))
+    ty = _types()[dtype]
+    cache, ref = make_cache(rng, lens, hkv, d, page, ty, layout)
+    batch = len(lens)
+    q, q_ref = tensor(rng, (batch, t, hq, d), ty)
+    drafted = rng.integers(1, t + 1, batch)
+    n_dev = torch.from_numpy(drafted.astype(np.int32)).cuda()
+    use = rng.random((batch, t)) < 0.8
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, drafted=n_dev)
+    lse_ref = lse.cpu().numpy()
+    want = ref_cache.evidence(ref, q_ref, lse_ref, use, drafted)
+    dead = ~use | (np.arange(t) >= drafted[:, None])
+    q[torch.from_numpy(dead).cuda()] = float("nan")
+    acc = torch.full((batch, hkv, cache.max_tokens + 3), 0.5, device="cuda")
+    use_dev = torch.from_numpy(use).cuda()
+    logit = np.abs(q_ref).max() * np.sqrt(d) * np.nanmax(np.abs(ref["k"]))     # sum |q k| scale is below this
+    rel = (d + 8) * 2.0 ** -24 * logit + 2.0 ** -20 + 2.0 ** -22 * 12
+    for add in (False, True):
+        got, ws = cuda_lib.evisel_cache_evidence(cache, q, lse, acc=acc, use=use_dev, drafted=n_dev, accumulate=add, ws=ws)
+        _status(cuda_lib, ws)
+        assert got is acc
+        host = acc.double().cpu().numpy()
+        for b in range(batch):
+            for h in range(hkv):
+                n = lens[b]
+                err = np.abs(host[b, h, :n] - (2.0 if add else 1.0) * want[b][h])
+                assert np.all(err <= rel * 2 * want[b][h] + 1e-30), (b, h, add, err.max())
+                assert np.all(host[b, h, n:] == 0.5)
+
+
+def test_evidence_of_all_rows_sums_to_the_cached_share(cuda_lib):
+    """Without drafted keys a row's weights sum to 1, so that all of them sum to rows x heads of the group."""
+    import torch
+    rng = np.random.default_rng(3)
+    ty = _types()["bf16"]
+    cache, _ = make_cache(rng, [4000, 1234], 4, 128, 64, ty)
+    q, _ = tensor(rng, (2, 20, 28, 128), ty, 2.0)
+    _, lse, ws = cuda_lib.evisel_cache_attention(cache, q)
+    acc, ws = cuda_lib.evisel_cache_evidence(cache, q, lse, ws=ws)
+    assert acc.shape == (2, 4, cache.max_tokens)
+    # 140 rows' LSEs, each within the bound of cache_helpers at A <= 128 here
+    assert torch.all((acc.double().sum(2) - 140).abs() <= 140 * (136 * 2.0 ** -24 * 128 + 2.0 ** -19))
+
+
+# --- eviction -------------------------------------------------------------------
+
+def _scores(rng, kind, batch, hkv, n):
+    x = rng.random((batch, hkv, n)).astype(np.float32)
+    if kind == "ties":
+        x = np.floor(x * 4).astype(np.float32)
+    elif kind == "equal":
+        x[:] = 0.25
+    elif kind == "signs":
+        x = np.where(x < 0.2, -0.0, np.where(x < 0.4, 0.0, (x - 0.7) * 1e-30)).astype(np.float32)
+    elif kind == "nan":
+        x[x < 0.3] = np.nan
+        x[x > 0.9] = np.inf
+        x[(x > 0.5) & (x < 0.6)] = -np.inf
+    return x
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "equal", "signs", "nan"])
+@pytest.mark.parametrize("lens,hkv,d,page,out_page,budget,sink,recent,dtype", [
+    ([0, 1, 5, 64, 65], 2, 64, 16, 32, 8, 1, 3, "bf16"),
+    ([100, 101, 99], 1, 128, 64, 16, 100, 0, 0, "fp16"),          # all, one less, fewer
+    ([1500, 3000], 3, 64, 32, 128, 257, 4, 33, "bf16"),
+    ([2049], 2, 128, 128, 64, 1, 0, 0, "bf16"),                   # a single token
+    ([1025, 40], 2, 128, 16, 16, 40, 10, 30, "bf16"),             # nothing left to choose
+])
+def test_evict(cuda_lib, kind, lens, hkv, d, page, out_page, budget, sink, recent, dtype):
+    import torch
+    rng = np.random.default_rng(budget)
+    ty = _types()[dtype]
+    cache, ref = make_cache(rng, lens, hkv, d, page, ty, poison=False)
+    batch = len(lens)
+    out, out_ref = make_cache(rng, [0] * batch, hkv, d, out_page, ty, "nhd", room=budget, mean=True, poison=False)
+    acc = _scores(rng, kind, batch, hkv, cache.max_tokens + 1)
+    before = out.k.clone()
+    kept, acc_out, ws = cuda_lib.evisel_cache_evict(cache, torch.from_numpy(acc).cuda(), out, budget, sink=sink, recent=recent)
+    _status(cuda_lib, ws)
+    kept, acc_out = kept.cpu().numpy(), acc_out.cpu().numpy()
+    k, v, mean = (x.double().cpu().numpy() for x in (out.k, out.v, out.k_mean))
+    table, touched = out_ref["table"], np.zeros(tuple(out.k.shape[:3]), bool)
+    for b in range(batch):
+        assert int(out.lens[b]) == min(lens[b], budget)
+        for h in range(hkv):
+            want = ref_cache.choose(acc[b, h], lens[b], budget, sink, recent)
+            n = len(want)
+            assert kept[b, h, :n].tolist() == want and np.all(kept[b, h, n:] == -1)
+            np.testing.assert_array_equal(acc_out[b, h, :n], acc[b, h, want])
+            assert np.all(acc_out[b, h, n:] == 0)
+            old_k, old_v = ref_cache.tokens(ref, "k", b, h)[want], ref_cache.tokens(ref, "v", b, h)[want]
+            for j in range(-(-n // out_page)):
+                m = min(out_page, n - j * out_page)
+                at = table[b, j]
+                touched[at, h, :m] = True
+                np.testing.assert_array_equal(k[at, h, :m], old_k[j * out_page:j * out_page + m])
+                np.testing.assert_array_equal(v[at, h, :m], old_v[j * out_page:j * out_page + m])
+                part = old_k[j * out_page:j * out_page + m]
+                bound = (u_of(ty) + out_page * 2.0 ** -23) * np.abs(part).mean(0)
+                assert np.all(np.abs(mean[at, h] - part.mean(0)) <= bound)
+    np.testing.assert_array_equal(k[~touched], before.double().cpu().numpy()[~touched])    # nothing else is written
+
+
+# --- append ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("lens,counts,t,hkv,d,page,dtype,layout,own", [
+    ([0, 15, 16, 17], [1, 1, 1, 0], 1, 2, 64, 16, "bf16", "hnd", True),
+    ([0, 100, 63], [5, 0, 8], 8, 1, 128, 64, "fp16", "nhd", False),
+    ([3], [300], 300, 3, 64, 32, "bf16", "hnd", True),
+    ([0, 7], None, 129, 2, 128, 128, "bf16", "nhd", True),
+])
+def test_append(cuda_lib, lens, counts, t, hkv, d, page, dtype, layout, own):
+    """Runs and picked tokens, onto page edges; nothing else of the pool changes; means over old and new tokens."""
+    import torch
+    rng = np.random.default_rng(t)
+    ty = _types()[dtype]
+    cache, ref = make_cache(rng, lens, hkv, d, page, ty, layout, room=t, mean=True, poison=False)
+    batch = len(lens)
+    took = counts or [t] * batch
+    x, x_ref = tensor(rng, (batch, t, 2 * hkv, d), ty)       # k and v beside each other
+    src = None if own else np.stack([rng.permutation(t) for _ in range(batch)]).astype(np.int32)
+    k_before, v_before = cache.k.clone(), cache.v.clone()
+    new, ws = cuda_lib.evisel_cache_append(
+        cache, x[:, :, :hkv], x[:, :, hkv:], src=None if own else torch.from_numpy(src).cuda(),
+        counts=None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda"))
+    _status(cuda_lib, ws)
+    assert new.tolist() == [n + c for n, c in zip(lens, took)] and cache.lens.tolist() == list(lens)
+    k, v = ref["k"].copy(), ref["v"].copy()
+    for b in range(batch):
+        for i in range(took[b]):
+            pos, s = lens[b] + i, i if own else src[b, i]
+            k[ref["table"][b, pos // page], :, pos % page] = x_ref[b, s, :hkv]
+            v[ref["table"][b, pos // page], :, pos % page] = x_ref[b, s, hkv:]
+    np.testing.assert_array_equal(cache.k.double().cpu().numpy(), k)
+    np.testing.assert_array_equal(cache.v.double().cpu().numpy(), v)
+    mean = cache.k_mean.double().cpu().numpy()
+    touched = np.zeros(len(k), bool)
+    for b in range(batch):
+        end = lens[b] + took[b]
+        for j in range(lens[b] // page, -(-end // page) if took[b] else 0):
+            at, m = ref["table"][b, j], min(page, end - j * page)
+            touched[at] = True
+            part = k[at, :, :m]
+            bound = (u_of(ty) + page * 2.0 ** -23) * np.abs(part).mean(1)
+            assert np.all(np.abs(mean[at] - part.mean(1)) <= bound)
+    assert np.all(mean[~touched] == 0)
+
+
+def test_append_then_attend_with_new_lengths(cuda_lib):
+    """The lengths that an append returns, assigned to the handle, are the ones the next call reads."""
+    rng = np.random.default_rng(1)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [10, 0], 2, 64, 16, ty, room=8, poison=False)
+    k, k_ref = tensor(rng, (2, 8, 2, 64), ty)
+    v, v_ref = tensor(rng, (2, 8, 2, 64), ty)
+    cache.lens, ws = cuda_lib.evisel_cache_append(cache, k, v)
+    q, q_ref = tensor(rng, (2, 1, 4, 64), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, ws=ws)
+    ref.update(k=cache.k.double().cpu().numpy(), v=cache.v.double().cpu().numpy(), lens=np.array([18, 8]))
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), 64, ty)
+
+
+# --- selection ------------------------------------------------------------------
+
+@pytest.mark.parametrize("lens,t,hq,hkv,d,page,n,sink,recent,dtype", [
+    ([0, 1, 16, 17, 160], 1, 2, 1, 64, 16, 4, 0, 1, "bf16"),
+    ([1000, 300], 1, 28, 4, 128, 16, 9, 2, 3, "bf16"),
+    ([2000], 5, 6, 2, 64, 32, 8, 1, 7, "fp16"),               # nothing left to choose
+    ([4096, 4033], 12, 14, 2, 128, 64, 64, 1, 1, "bf16"),     # all; one short page
+    ([16 * 2100 + 5], 1, 2, 2, 64, 16, 100, 0, 1, "bf16"),    # more pages than a block has threads
+])
+def test_select(cuda_lib, lens, t, hq, hkv, d, page, n, sink, recent, dtype):
+    """Chosen pages against the exact scores (numbers on a grid: no rounding in any order), and the attention over
+    them against the attention over those tokens."""
+    import torch
+    rng = np.random.default_rng(n)
+    ty = _types()[dtype]
+    cache, ref = make_cache(rng, lens, hkv, d, page, ty, mean=True, poison=False)
+    batch = len(lens)
+    grid = lambda x: np.clip(np.round(x * 16), -128, 128) / 16  # noqa: E731
+    q_ref = grid(rng.standard_normal((batch, t, hq, d)))
+    mean = grid(rng.standard_normal((len(ref["k"]), hkv, d)))
+    cache.k_mean.copy_(torch.from_numpy(mean))
+    q = torch.from_numpy(q_ref).to(ty).cuda()
+    drafted = rng.integers(1, t + 1, batch)
+    n_dev = torch.from_numpy(drafted.astype(np.int32)).cuda()
+    view, pages, ws = cuda_lib.evisel_cache_select(cache, q, n, sink=sink, recent=recent, drafted=n_dev)
+    _status(cuda_lib, ws)
+    pages = pages.cpu().numpy()
+    sel = dict(ref, table=np.zeros((batch, hkv, n), np.int32), lens=np.zeros((batch, hkv), np.int64))
+    for b in range(batch):
+        count = -(-lens[b] // page)
+        for h in range(hkv):
+            want = ref_cache.choose(ref_cache.page_scores(ref, mean, q_ref, b, h, drafted), count, n, sink, recent)
+            assert pages[b, h, :len(want)].tolist() == want and np.all(pages[b, h, len(want):] == -1)
+            sel["table"][b, h, :len(want)] = ref["table"][b, want]
+            sel["lens"][b, h] = sum(min(page, lens[b] - j * page) for j in want)
+    np.testing.assert_array_equal(view.lens.cpu().numpy(), sel["lens"])
+    o, lse, ws = cuda_lib.evisel_cache_attention(view, q, drafted=n_dev, ws=ws)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(sel, q_ref, drafted=drafted), d, ty)
+
+
+# --- what the kernels catch --------------------------------------------------------
+
+def test_out_of_range_device_values_are_reported(cuda_lib):
+    """Lengths, page ids, source indices and counts out of range: no access leaves the buffers, the status says so,
+    and the next call is as good as new."""
+    import torch
+    rng = np.random.default_rng(2)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [40, 20], 2, 64, 16, ty, room=16, mean=True, poison=False)
+    q, q_ref = tensor(rng, (2, 2, 4, 64), ty)
+    kv, _ = tensor(rng, (2, 2, 2, 64), ty)
+    out, _ = make_cache(rng, [0, 0], 2, 64, 16, ty, room=16, mean=True, poison=False)
+    acc = torch.rand((2, 2, cache.max_tokens), device="cuda")
+    good_table, good_lens = cache.table.clone(), cache.lens.clone()
+    i32 = dict(dtype=torch.int32, device="cuda")
+
+    def calls(c, **kw):
+        o, lse, ws = cuda_lib.evisel_cache_attention(c, q)
+        yield ws
+        yield cuda_lib.evisel_cache_evidence(c, q, lse, acc=acc.clone())[1]
+        yield cuda_lib.evisel_cache_evict(c, acc, out, 8)[2]
+        yield cuda_lib.evisel_cache_select(c, q, 2)[2]
+        yield cuda_lib.evisel_cache_append(c, kv, kv)[1]
+
+    for table, lens in ((good_table + len(ref["k"]), good_lens), (-good_table - 1, good_lens),
+                        (good_table, good_lens + 10_000), (good_table, -good_lens)):
+        for ws in calls(cache.view(table, lens)):
+            assert cuda_lib.evisel_status(ws) == -7
+            assert cuda_lib.evisel_status(ws) == 0
+    for kw in (dict(src=torch.full((2, 2), 2, **i32)), dict(src=torch.full((2, 2), -1, **i32)),
+               dict(counts=torch.tensor([3, 1], **i32)), dict(counts=torch.tensor([-1, 1], **i32))):
+        _, ws = cuda_lib.evisel_cache_append(cache, kv, kv, **kw)
+        assert cuda_lib.evisel_status(ws) == -7
+    full = torch.tensor([cache.max_tokens, 0], **i32)
+    new, ws = cuda_lib.evisel_cache_append(cache.view(good_table, full), kv, kv)
+    assert new.tolist() == [cache.max_tokens, 2] and cuda_lib.evisel_status(ws) == -7
+    # acc shorter than a sequence
+    _, lse, ws = cuda_lib.evisel_cache_attention(cache, q, ws=ws)
+    short = torch.full((2, 2, 30), -1.0, device="cuda")
+    cuda_lib.evisel_cache_evidence(cache, q, lse, acc=short, ws=ws)
+    assert cuda_lib.evisel_status(ws) == -7
+    cuda_lib.evisel_cache_evict(cache, short, out, 8, ws=ws)
+    assert cuda_lib.evisel_status(ws) == -7
+    good, ref = make_cache(rng, [40, 20], 2, 64, 16, ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(good, q, ws=ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), 64, ty)
+    _status(cuda_lib, ws)
