@@ -7,54 +7,15 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
-#include "cache_common.cuh"
+#include "cache_attn.cuh"
 
 namespace evisel {
 namespace {
 
 constexpr float kLn2 = 0.69314718055994531f;
-constexpr float kRescaleThreshold = 8.0f;        // log2 units: a running max moves only when it grows by more
 constexpr int kKeys = 64;                        // keys of a unit
 constexpr int kKeyWarps = 4;                     // warps over a unit's keys, 16 each
 constexpr int kStages = 3;
-
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  const bool ok = ptx::mbar_wait(bar, parity, abort_flag, kWaitTimeoutNs);
-  return __all_sync(0xffffffffu, ok);
-}
-
-__device__ __forceinline__ void record_timeout(volatile int* abort_flag, int* status) {
-  *abort_flag = 1;
-  atomicExch(status, kStatusTimeout);
-}
-
-// A CTA's part of one problem: units [t0, t1) of a (sequence, KV head, row tile).
-struct Segment {
-  int b, h, rt, t0, t1, len, problem;
-};
-
-// A CTA's segments in order, from unit u on.
-struct Walk {
-  int u, end, entry, first;
-  __device__ __forceinline__ bool next(const CacheAttnLaunch& L, const UnitCount& uc, Segment& s) {
-    if (u >= end) return false;
-    int tiles = uc.tiles(entry);
-    while (u >= first + tiles * uc.mult) {
-      first += tiles * uc.mult;
-      tiles = uc.tiles(++entry);
-    }
-    const int inner = (u - first) / tiles;
-    s.t0 = (u - first) % tiles;
-    s.t1 = min(tiles, s.t0 + (end - u));
-    s.b = uc.per_head ? entry / L.c.hkv : entry;
-    s.h = uc.per_head ? entry % L.c.hkv : inner / L.row_tiles;
-    s.rt = inner % L.row_tiles;
-    s.len = cache_len(L.c, s.b, s.h, L.status);
-    s.problem = (s.b * L.c.hkv + s.h) * L.row_tiles + s.rt;
-    u += s.t1 - s.t0;
-    return true;
-  }
-};
 
 // ---------------------------------------------------------------- few rows
 // Up to 16 * MG rows of a (sequence, KV head) at a time. Every warp takes 16 of
@@ -78,7 +39,7 @@ struct FewCfg {
 };
 
 template <class T, int D, int MG>
-__global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), 2) cache_attn_few_kernel(const __grid_constant__ CacheAttnLaunch L) {
+__global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) cache_attn_few_kernel(const __grid_constant__ CacheAttnLaunch L) {
   using C = FewCfg<D, MG>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -352,7 +313,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
   };
 
   if (live && tiles > 0) {
-    const int rt = r / L.tile_rows, row = r % L.tile_rows;
+    const int slot = r / L.slot_rows, rt = slot / L.slots;
+    const int row = (slot % L.slots) * (L.tile_rows / L.slots) + r % L.slot_rows;
     const int u0 = first + rt * tiles, i0 = split_owner(u0, sp.total, ctas), i1 = split_owner(u0 + tiles - 1, sp.total, ctas);
     const int problem = bh * L.row_tiles + rt;
     const int n = (i1 - i0 + 1 - wi + wpr - 1) / wpr;            // partials of this warp
@@ -465,7 +427,9 @@ cudaError_t launch_few(const CacheAttnLaunch& L, cudaStream_t stream) {
 
 template <class T, int D>
 cudaError_t launch_d(const CacheAttnLaunch& L, cudaStream_t stream) {
-  const cudaError_t e = L.tile_rows == 16 ? launch_few<T, D, 1>(L, stream) : launch_few<T, D, 2>(L, stream);
+  const cudaError_t e = L.wide               ? launch_cache_attn_wide(L, stream)
+                        : L.tile_rows == 16 ? launch_few<T, D, 1>(L, stream)
+                                            : launch_few<T, D, 2>(L, stream);
   if (e != cudaSuccess) return e;
   // Warps per row: as many as keep the rows' blocks within about two per SM.
   const int64_t rows = static_cast<int64_t>(L.c.batch) * L.c.hkv * L.rows;
@@ -477,9 +441,23 @@ cudaError_t launch_d(const CacheAttnLaunch& L, cudaStream_t stream) {
 
 }  // namespace
 
-CacheAttnShape cache_attn_shape(int rows, int head_dim, int n_sm) {
+CacheAttnShape cache_attn_shape(int rows, int gq, bool q_map, int n_sm) {
   CacheAttnShape s;
-  s.tile_rows = rows <= 16 ? 16 : 32;
+  if (rows > 32 && q_map) {
+    s.wide = true;
+    s.slot_rows = 128 / gq * gq;
+    const int slots = (rows + s.slot_rows - 1) / s.slot_rows;
+    s.slots = slots > 1 ? 2 : 1;
+    s.tile_rows = 128 * s.slots;
+    s.row_tiles = (slots + s.slots - 1) / s.slots;
+    s.key_tile = 128;
+    s.n_ctas = n_sm;
+    s.min_units = 1;
+    return s;
+  }
+  s.wide = false;
+  s.slots = 1;
+  s.slot_rows = s.tile_rows = rows <= 16 ? 16 : 32;
   s.row_tiles = (rows + s.tile_rows - 1) / s.tile_rows;
   s.key_tile = kKeys;
   s.n_ctas = 2 * n_sm;

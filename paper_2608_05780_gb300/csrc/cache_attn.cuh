@@ -1,0 +1,49 @@
+// What the attention kernels over a paged cache share: bounded waits and a
+// CTA's walk over its part of the units.
+#pragma once
+
+#include "cache_common.cuh"
+
+namespace evisel {
+
+constexpr float kRescaleThreshold = 8.0f;        // log2 units: a running max moves only when it grows by more
+
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  const bool ok = ptx::mbar_wait(bar, parity, abort_flag, kWaitTimeoutNs);
+  return __all_sync(0xffffffffu, ok);
+}
+
+__device__ __forceinline__ void record_timeout(volatile int* abort_flag, int* status) {
+  *abort_flag = 1;
+  atomicExch(status, kStatusTimeout);
+}
+
+// A CTA's part of one problem: units [t0, t1) of a (sequence, KV head, row tile).
+struct Segment {
+  int b, h, rt, t0, t1, len, problem;
+};
+
+// A CTA's segments in order, from unit u on.
+struct Walk {
+  int u, end, entry, first;
+  __device__ __forceinline__ bool next(const CacheAttnLaunch& L, const UnitCount& uc, Segment& s) {
+    if (u >= end) return false;
+    int tiles = uc.tiles(entry);
+    while (u >= first + tiles * uc.mult) {
+      first += tiles * uc.mult;
+      tiles = uc.tiles(++entry);
+    }
+    const int inner = (u - first) / tiles;
+    s.t0 = (u - first) % tiles;
+    s.t1 = min(tiles, s.t0 + (end - u));
+    s.b = uc.per_head ? entry / L.c.hkv : entry;
+    s.h = uc.per_head ? entry % L.c.hkv : inner / L.row_tiles;
+    s.rt = inner % L.row_tiles;
+    s.len = cache_len(L.c, s.b, s.h, L.status);
+    s.problem = (s.b * L.c.hkv + s.h) * L.row_tiles + s.rt;
+    u += s.t1 - s.t0;
+    return true;
+  }
+};
+
+}  // namespace evisel

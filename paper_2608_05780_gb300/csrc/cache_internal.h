@@ -41,6 +41,7 @@ struct DraftView {
 // units, so no two are the same).
 struct CacheAttnLaunch {
   CUtensorMap tm_k, tm_v;           // pages; box {64, box_rows, 1, 1} in the order of `perm`
+  CUtensorMap tm_q;                 // wide: {d, hq, T, B}, box {64, gq, 128 / gq, 1}
   CacheView c;
   DraftView d;
   void* o;
@@ -50,8 +51,10 @@ struct CacheAttnLaunch {
   int* status;
   int k_perm, v_perm;               // where token, head and page stand in the maps' coordinates
   int box_rows;
-  int rows, tile_rows, row_tiles;   // rows = tokens * gq
+  int rows, tile_rows, row_tiles;   // rows = tokens * gq; tile_rows rows of a partial
+  int slots, slot_rows;             // a row tile is `slots` slots of slot_rows rows, tile_rows / slots places each
   int n_ctas, key_tile, min_units;  // units a CTA takes at least
+  int wide;                         // 128-row slots on tcgen05 (else mma.sync)
 };
 
 struct CacheEvidenceLaunch {
@@ -110,9 +113,11 @@ cudaError_t launch_cache_select(const CacheSelectLaunch& L, cudaStream_t stream)
 
 // Row tile and CTAs of a call with `rows` rows per (sequence, KV head).
 struct CacheAttnShape {
-  int tile_rows, row_tiles, key_tile, n_ctas, min_units;
+  int tile_rows, row_tiles, slots, slot_rows, key_tile, n_ctas, min_units;
+  bool wide;
 };
-CacheAttnShape cache_attn_shape(int rows, int head_dim, int n_sm);
+CacheAttnShape cache_attn_shape(int rows, int gq, bool q_map, int n_sm);
+cudaError_t launch_cache_attn_wide(const CacheAttnLaunch& L, cudaStream_t stream);
 
 // What the cache calls use of a workspace (evisel_capi.cpp).
 struct WsCache {

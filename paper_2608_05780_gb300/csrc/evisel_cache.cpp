@@ -165,6 +165,25 @@ int encode_pages(CUtensorMap* map, int* perm, const void* base, const evisel_cac
   return encode_map4(map, base, c->dtype, dims, strides, box);
 }
 
+// Whether a TMA map can describe q: no repeated (stride 0) dimension.
+bool has_query_map(const evisel_cache* c, const evisel_draft* d) {
+  const int64_t sizes[3] = {c->batch, d->tokens, d->hq};
+  for (int i = 0; i < 3; ++i)
+    if (sizes[i] > 1 && d->q_stride[i] == 0) return false;
+  return true;
+}
+
+// Map of q {d, hq, T, B}, box of `box_tokens` tokens of one KV group: rows (token, head).
+int encode_queries(CUtensorMap* map, const evisel_cache* c, const evisel_draft* d, int box_tokens) {
+  auto bytes = [&](int64_t stride, int64_t size) { return static_cast<uint64_t>(size > 1 ? stride : c->head_dim) * 2; };
+  const uint64_t dims[4] = {static_cast<uint64_t>(c->head_dim), static_cast<uint64_t>(d->hq),
+                            static_cast<uint64_t>(d->tokens), static_cast<uint64_t>(c->batch)};
+  const uint64_t strides[3] = {bytes(d->q_stride[2], d->hq), bytes(d->q_stride[1], d->tokens),
+                               bytes(d->q_stride[0], c->batch)};
+  const uint32_t box[4] = {64u, static_cast<uint32_t>(d->hq / c->hkv), static_cast<uint32_t>(box_tokens), 1u};
+  return encode_map4(map, d->q, c->dtype, dims, strides, box);
+}
+
 int grow(evisel_ws* ws, size_t need, cudaStream_t stream) {
   WsCache& w = ws_cache(ws);
   if (need <= w.bytes) return EVISEL_OK;
@@ -217,7 +236,10 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     L.c = view_of(cache);
     L.d = view_of(cache, draft);
     L.rows = draft->tokens * L.d.gq;
-    const CacheAttnShape shape = cache_attn_shape(L.rows, cache->head_dim, n_sm);
+    const CacheAttnShape shape = cache_attn_shape(L.rows, L.d.gq, has_query_map(cache, draft), n_sm);
+    L.wide = shape.wide;
+    L.slots = shape.slots;
+    L.slot_rows = shape.slot_rows;
     L.tile_rows = shape.tile_rows;
     L.row_tiles = shape.row_tiles;
     L.key_tile = shape.key_tile;
@@ -234,6 +256,8 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     if (rc == EVISEL_OK) rc = grow(*ws_inout, ml_bytes + parts * L.tile_rows * cache->head_dim * sizeof(float), stream);
     if (rc == EVISEL_OK && cache->max_pages > 0) rc = encode_pages(&L.tm_k, &L.k_perm, cache->k, cache, cache->k_stride, L.box_rows);
     if (rc == EVISEL_OK && cache->max_pages > 0) rc = encode_pages(&L.tm_v, &L.v_perm, cache->v, cache, cache->v_stride, L.box_rows);
+    if (rc != EVISEL_OK) return rc;
+    if (L.wide) rc = encode_queries(&L.tm_q, cache, draft, 128 / L.d.gq);
     if (rc != EVISEL_OK) return rc;
     char* buf = static_cast<char*>(ws_cache(*ws_inout).buf);
     L.part_ml = reinterpret_cast<float2*>(buf);
