@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) ca
     const CUtensorMap* map = is_v ? &L.tm_v : &L.tm_k;
     const int perm = is_v ? L.v_perm : L.k_perm;
     const uint64_t pol = ptx::l2_policy_evict_first();
-    while (ok && walk.next(L, uc, s)) {
+    while (ok && walk.next(L.c, L.row_tiles, uc, s, L.status)) {
       for (int t = s.t0; t < s.t1; ++t, ++n) {
         const int st = n % kStages, key0 = t * kKeys + sub * L.box_rows;
         const bool mine = lane < n_loads && key0 < s.len;
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) ca
   float4* join = reinterpret_cast<float4*>(smem + C::OFF_JOIN) + mg * 16 * D / 4;
   float2* ml = reinterpret_cast<float2*>(smem + C::OFF_ML) + mg * kKeyWarps * 16;
 
-  while (walk.next(L, uc, s)) {
+  while (walk.next(L.c, L.row_tiles, uc, s, L.status)) {
     // Q fragments of this warp's 16 rows (rows past the last one: zeros).
     uint32_t qf[D / 16][4];
     const int row0 = s.rt * L.tile_rows + mg * 16 + fr;
@@ -314,7 +314,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
 
   if (live && tiles > 0) {
     const int slot = r / L.slot_rows, rt = slot / L.slots;
-    const int row = (slot % L.slots) * (L.tile_rows / L.slots) + r % L.slot_rows;
+    const int in_slot = L.wide && !L.qt.head_inner ? g * L.qt.tokens + t % L.qt.tokens : r % L.slot_rows;
+    const int row = (slot % L.slots) * (L.tile_rows / L.slots) + in_slot;
     const int u0 = first + rt * tiles, i0 = split_owner(u0, sp.total, ctas), i1 = split_owner(u0 + tiles - 1, sp.total, ctas);
     const int problem = bh * L.row_tiles + rt;
     const int n = (i1 - i0 + 1 - wi + wpr - 1) / wpr;            // partials of this warp
@@ -441,11 +442,11 @@ cudaError_t launch_d(const CacheAttnLaunch& L, cudaStream_t stream) {
 
 }  // namespace
 
-CacheAttnShape cache_attn_shape(int rows, int gq, bool q_map, int n_sm) {
+CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n_sm) {
   CacheAttnShape s;
   if (rows > 32 && q_map) {
     s.wide = true;
-    s.slot_rows = 128 / gq * gq;
+    s.slot_rows = qt.rows;
     const int slots = (rows + s.slot_rows - 1) / s.slot_rows;
     s.slots = slots > 1 ? 2 : 1;
     s.tile_rows = 128 * s.slots;

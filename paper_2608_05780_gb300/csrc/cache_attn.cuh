@@ -26,7 +26,7 @@ struct Segment {
 // A CTA's segments in order, from unit u on.
 struct Walk {
   int u, end, entry, first;
-  __device__ __forceinline__ bool next(const CacheAttnLaunch& L, const UnitCount& uc, Segment& s) {
+  __device__ __forceinline__ bool next(const CacheView& c, int row_tiles, const UnitCount& uc, Segment& s, int* status) {
     if (u >= end) return false;
     int tiles = uc.tiles(entry);
     while (u >= first + tiles * uc.mult) {
@@ -36,11 +36,11 @@ struct Walk {
     const int inner = (u - first) / tiles;
     s.t0 = (u - first) % tiles;
     s.t1 = min(tiles, s.t0 + (end - u));
-    s.b = uc.per_head ? entry / L.c.hkv : entry;
-    s.h = uc.per_head ? entry % L.c.hkv : inner / L.row_tiles;
-    s.rt = inner % L.row_tiles;
-    s.len = cache_len(L.c, s.b, s.h, L.status);
-    s.problem = (s.b * L.c.hkv + s.h) * L.row_tiles + s.rt;
+    s.b = uc.per_head ? entry / c.hkv : entry;
+    s.h = uc.per_head ? entry % c.hkv : inner / row_tiles;
+    s.rt = inner % row_tiles;
+    s.len = cache_len(c, s.b, s.h, status);
+    s.problem = (s.b * c.hkv + s.h) * row_tiles + s.rt;
     u += s.t1 - s.t0;
     return true;
   }

@@ -9,7 +9,7 @@
 //   warp 9          S = Q K^T and O += P V (A = P from TMEM, over S)
 //   warp 10         V pages into a 2-deep ring
 //   warp 11         Q of the segment's slots, by a map whose box is the group's
-//                   heads of 128 / gq tokens
+//                   heads of as many tokens as 128 rows hold
 // Per key tile: P0.V, S0 of the next tile, P1.V, S1 of the next tile, so that the
 // tensor pipe works on one slot while the softmax works on the other. With one
 // slot the other slot's S columns are a second S buffer.
@@ -44,7 +44,8 @@ struct WideCfg {
   static constexpr int B_DRAIN = B_OF + 2;
   static constexpr int N_BARS = B_DRAIN + 1;
   static constexpr int OFF_MISC = OFF_BAR + N_BARS * 8;   // TMEM address, abort flag, split scratch
-  static constexpr int SMEM = OFF_MISC + 8 + 40 * 4 + 1024;
+  static constexpr int SMEM_USED = OFF_MISC + 8 + 40 * 4 + 1024;
+  static constexpr int SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA per SM: TMEM is taken whole
   static constexpr int COL_O = 128;              // per slot: S (128 columns) | O (D)
   static constexpr int SLOT_COLS = 128 + D;
   static_assert(SMEM <= 232448, "shared memory budget");
@@ -76,7 +77,7 @@ __device__ __forceinline__ void load_pages(const CacheAttnLaunch& L, const UnitC
   Segment s;
   uint32_t n = 0;
   bool ok = true;
-  while (ok && walk.next(L, uc, s)) {
+  while (ok && walk.next(L.c, L.row_tiles, uc, s, L.status)) {
     for (int t = s.t0; t < s.t1; ++t, ++n) {
       const int st = n % R, key0 = t * kKeys + sub * L.box_rows;
       const bool mine = sub < subs && key0 < s.len;
@@ -104,12 +105,12 @@ __device__ __forceinline__ void load_queries(const CacheAttnLaunch& L, const Uni
                                              volatile int* abort_flag) {
   using C = WideCfg<D>;
   auto bar = [&](int i) { return sbase + C::OFF_BAR + 8u * i; };
-  const int lane = threadIdx.x & 31, tokens = kRows / L.d.gq;      // of a slot
+  const int lane = threadIdx.x & 31, tokens = L.qt.tokens;         // of a slot
   const uint64_t pol = ptx::l2_policy_evict_last();
   Segment s;
   uint32_t n = 0;                                // segments
   bool ok = true;
-  for (; ok && walk.next(L, uc, s); ++n) {
+  for (; ok && walk.next(L.c, L.row_tiles, uc, s, L.status); ++n) {
     if (n >= 1 && !warp_wait(bar(C::B_QE), (n - 1) & 1, abort_flag)) {
       ok = false;
       break;
@@ -119,8 +120,8 @@ __device__ __forceinline__ void load_queries(const CacheAttnLaunch& L, const Uni
       ptx::mbar_arrive_expect_tx(bar(C::B_QF), ns * C::KB * L.slot_rows * 128);
       for (int i = 0; i < ns; ++i)
         for (int kb = 0; kb < C::KB; ++kb)
-          ptx::tma_load_4d(sbase + C::OFF_Q + i * C::TILE + kb * C::BLOCK, &L.tm_q, bar(C::B_QF), kb * 64, s.h * L.d.gq,
-                           (s.rt * L.slots + i) * tokens, s.b, pol);
+          ptx::tma_load_page(sbase + C::OFF_Q + i * C::TILE + kb * C::BLOCK, &L.tm_q, bar(C::B_QF), L.q_perm, kb * 64,
+                             (s.rt * L.slots + i) * tokens, s.h * L.d.gq, s.b, pol);
     }
     __syncwarp();
   }
@@ -188,7 +189,7 @@ __device__ __forceinline__ void issue_mmas(const CacheAttnLaunch& L, const UnitC
 
   Segment s;
   uint32_t n = 0, seg = 0, pf = 0;               // tiles and segments so far; parity of the P waits, a bit per buffer
-  while (ok && walk.next(L, uc, s)) {
+  while (ok && walk.next(L.c, L.row_tiles, uc, s, L.status)) {
     const bool two = slots_of(L, s) == 2;
     const int cnt = s.t1 - s.t0;
     ok = warp_wait(bar(C::B_QF), seg & 1, abort_flag) && warp_wait(bar(C::B_KF + n % NK), (n / NK) & 1, abort_flag);
@@ -277,7 +278,7 @@ __device__ __forceinline__ void softmax_rows(const CacheAttnLaunch& L, const Uni
   Segment s;
   uint32_t n = 0, sf = 0, of = 0;                // tiles so far; parity of the S waits, a bit per buffer (this slot's or not); O waits
   bool ok = true;
-  while (ok && walk.next(L, uc, s)) {
+  while (ok && walk.next(L.c, L.row_tiles, uc, s, L.status)) {
     const bool two = slots_of(L, s) == 2;
     const int cnt = s.t1 - s.t0;
     if (slot == 1 && !two) {                     // the other slot's S takes both buffers
@@ -389,7 +390,8 @@ __device__ __forceinline__ void softmax_rows(const CacheAttnLaunch& L, const Uni
     if (!ok) break;
     ptx::tc_fence_after();
     const int64_t at = (static_cast<int64_t>(blockIdx.x) + s.problem) * L.tile_rows + slot * kRows + row;
-    const bool live = row < L.slot_rows && (s.rt * L.slots + slot) * L.slot_rows + row < L.rows;
+    const int token = (s.rt * L.slots + slot) * L.qt.tokens + (L.qt.head_inner ? row / L.d.gq : row % L.qt.tokens);
+    const bool live = row < L.slot_rows && token < L.d.tokens;
     float4* dst = reinterpret_cast<float4*>(L.part_o + at * D);
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {

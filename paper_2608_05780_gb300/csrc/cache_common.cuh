@@ -71,7 +71,7 @@ __device__ __forceinline__ void unpack8(const uint4& w, float (&f)[8]) {
 
 namespace ptx {
 
-// 4-D tiled load whose token, head and page coordinates stand at the places that
+// 4-D tiled load whose token, head and page (or sequence) coordinates stand at the places that
 // `perm` names: two bits each for the coordinate (1..3) of token, head and page.
 __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, uint32_t bar, int perm, int c0,
                                               int token, int head, int page, uint64_t cache_hint) {
@@ -79,15 +79,6 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* m
   const int c1 = pt == 1 ? token : ph == 1 ? head : page;
   const int c2 = pt == 2 ? token : ph == 2 ? head : page;
   const int c3 = pt == 3 ? token : ph == 3 ? head : page;
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar), "l"(cache_hint)
-      : "memory");
-}
-
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2,
-                                            int c3, uint64_t cache_hint) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
       " [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),

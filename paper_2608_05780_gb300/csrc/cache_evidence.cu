@@ -1,20 +1,339 @@
 // Attention weight per cached token:
 //   acc[b, h, m] (+)= sum_{t used} sum_{heads g of group h} exp(scale q . k_m - LSE).
-// One thread per key: its key in registers, the rows' queries by broadcast loads.
+//
+// S^T = K Q^T on tcgen05 with the keys as the 128 TMEM lanes and the rows as
+// columns, so that a thread adds one key's columns and nothing crosses lanes.
+// A persistent CTA per SM walks its even share of the units (128 keys of a
+// sequence and KV head), four at a time:
+//   warps 0-15  four groups of 128 threads, a key each; the CTA's n-th unit is
+//               in K stage n % 4, S buffer n % 4 and goes to group n % 4
+//   warp 16     K pages by TMA, four stages
+//   warp 17     the queries' tiles (up to 128 rows), three stages, read once per
+//               four units
+//   warp 18     the MMAs: tile by tile, for each the four units
+//   warp 19     each tile's -LSE log2e, beside it in its stage
+// Few rows (decoding) leave the K stream as the bound; with many a tile's
+// 128 x 128 products and exponentials are, and a query tile loaded once per four
+// units keeps its traffic (32 KB for four products) out of the way.
 #include <cstdint>
 #include <cuda_runtime.h>
 
-#include "cache_common.cuh"
+#include "cache_attn.cuh"
 
 namespace evisel {
 namespace {
 
-constexpr int kThreads = 128;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kKeys = 128;
+constexpr int kGroups = 4;
+constexpr int kKeyWarps = kGroups * 4;
+constexpr int kWarpK = kKeyWarps, kWarpQ = kWarpK + 1, kWarpMma = kWarpK + 2, kWarpLse = kWarpK + 3;
+constexpr int kThreads = 32 * (kKeyWarps + 4);
+constexpr int QS = 3;
+
+template <int D>
+struct EvCfg {
+  static constexpr int KB = D / 64;
+  static constexpr int BLOCK = kKeys * 128;
+  static constexpr int TILE = KB * BLOCK;
+  static constexpr int OFF_K = 0;
+  static constexpr int OFF_Q = kGroups * TILE;
+  static constexpr int OFF_LSE = OFF_Q + QS * TILE;          // [QS][128] fp32
+  static constexpr int OFF_PART = OFF_LSE + QS * 128 * 4;    // [QS] whether some row of the tile does not count
+  static constexpr int OFF_BAR = OFF_PART + 16;
+  static constexpr int B_KF = 0, B_KE = B_KF + kGroups, B_QF = B_KE + kGroups, B_QE = B_QF + QS, B_SF = B_QE + QS,
+                       B_SE = B_SF + kGroups, B_DRAIN = B_SE + kGroups, N_BARS = B_DRAIN + 1;
+  static constexpr int OFF_MISC = OFF_BAR + N_BARS * 8;      // TMEM address, abort flag, split scratch
+  static constexpr int SMEM_USED = OFF_MISC + 8 + 40 * 4 + 1024;
+  static constexpr int SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA per SM: TMEM is taken whole
+  static_assert(SMEM <= 232448, "shared memory budget");
+};
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) cache_evidence_kernel(const __grid_constant__ CacheEvidenceLaunch L) {
-  const int h = blockIdx.y, b = blockIdx.z, key = blockIdx.x * kThreads + threadIdx.x;
+__global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __grid_constant__ CacheEvidenceLaunch L) {
+  using C = EvCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sbase = ptx::smem_addr(smem);
+  auto bar = [&](int i) { return sbase + C::OFF_BAR + 8u * i; };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
+  int* scratch = reinterpret_cast<int*>(smem + C::OFF_MISC + 8);
+  float* lse_s = reinterpret_cast<float*>(smem + C::OFF_LSE);
+  volatile int* part_s = reinterpret_cast<volatile int*>(smem + C::OFF_PART);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  const UnitCount uc(L.c, kKeys, 1, L.status);
+  int begin = 0, end = 0;
+  const Split sp = split_find_unit(uc, scratch, [&](int total) {
+    const int ctas = split_ctas(total, L.n_ctas, 1), i = blockIdx.x;
+    begin = i < ctas ? split_begin(i, total, ctas) : total;
+    end = i < ctas ? split_begin(i + 1, total, ctas) : total;
+    return begin;
+  });
+  if (begin >= end) return;                      // (the whole block, before anything is started)
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::N_BARS; ++i)
+      ptx::mbar_init(bar(i), i >= C::B_QF && i < C::B_QF + QS                ? 2u        // the copy and the LSE warp
+                             : i >= C::B_QE && i < C::B_QE + QS              ? 1u + kKeyWarps
+                             : i >= C::B_SE && i < C::B_SE + kGroups         ? 4u
+                                                                             : 1u);
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 0) {
+    ptx::tmem_alloc<512>(sbase + C::OFF_MISC);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  Walk walk{begin, end, sp.entry, sp.first};
+  Segment s;
+  const int n_tiles = (L.d.tokens + L.qt.tokens - 1) / L.qt.tokens;   // query tiles
+  bool ok = true;
+
+  if (warp == kWarpK) {
+    const int kb = lane % C::KB, sub = lane / C::KB, subs = kKeys / L.box_rows;
+    const uint64_t pol = ptx::l2_policy_evict_first();
+    uint32_t n = 0;
+    while (ok && walk.next(L.c, 1, uc, s, L.status)) {
+      for (int t = s.t0; t < s.t1; ++t, ++n) {
+        const int st = n % kGroups, key0 = t * kKeys + sub * L.box_rows;
+        const bool mine = sub < subs && key0 < s.len;
+        const int id = mine ? cache_page(L.c, s.b, s.h, key0 >> L.c.log_page, L.status) : 0;
+        if (n >= kGroups && !warp_wait(bar(C::B_KE + st), (n / kGroups - 1) & 1, abort_flag)) {
+          ok = false;
+          break;
+        }
+        const int boxes = min(subs, (s.len - t * kKeys + L.box_rows - 1) / L.box_rows) * C::KB;
+        if (lane == 0) ptx::mbar_arrive_expect_tx(bar(C::B_KF + st), boxes * L.box_rows * 128);
+        __syncwarp();
+        if (mine)
+          ptx::tma_load_page(sbase + C::OFF_K + st * C::TILE + kb * C::BLOCK + sub * L.box_rows * 128, &L.tm_k,
+                             bar(C::B_KF + st), L.k_perm, kb * 64, key0 & (L.c.page - 1), s.h, id, pol);
+      }
+    }
+    if (!ok && lane == 0) record_timeout(abort_flag, L.status);
+    const volatile int never = 0;                // no copy in flight at exit
+    for (uint32_t i = 0; i < kGroups && i < n; ++i)
+      ptx::mbar_wait(bar(C::B_KF + (n - 1 - i) % kGroups), ((n - 1 - i) / kGroups) & 1, &never, kWaitTimeoutNs);
+  } else if (warp == kWarpQ) {
+    const uint64_t pol = ptx::l2_policy_evict_last();
+    uint32_t n = 0;
+    while (ok && walk.next(L.c, 1, uc, s, L.status))
+      for (int t = s.t0; ok && t < s.t1; t += kGroups)
+        for (int q = 0; q < n_tiles; ++q, ++n) {
+          const int st = n % QS;
+          if (n >= QS && !warp_wait(bar(C::B_QE + st), (n / QS - 1) & 1, abort_flag)) {
+            ok = false;
+            break;
+          }
+          if (lane == 0) {
+            ptx::mbar_arrive_expect_tx(bar(C::B_QF + st), C::KB * L.qt.rows * 128);
+            for (int kb = 0; kb < C::KB; ++kb)
+              ptx::tma_load_page(sbase + C::OFF_Q + st * C::TILE + kb * C::BLOCK, &L.tm_q, bar(C::B_QF + st), L.q_perm,
+                                 kb * 64, q * L.qt.tokens, s.h * L.d.gq, s.b, pol);
+          }
+          __syncwarp();
+        }
+    if (!ok && lane == 0) record_timeout(abort_flag, L.status);
+    // Every tile issued has landed at exit (its phase also needs the LSE warp's arrival, which may be
+    // missing after a failure: then the wait ends by its limit).
+    const volatile int never = 0;
+    for (uint32_t i = 0; i < QS && i < n; ++i)
+      ptx::mbar_wait(bar(C::B_QF + (n - 1 - i) % QS), ((n - 1 - i) / QS) & 1, &never, kWaitTimeoutNs);
+  } else if (warp == kWarpMma) {
+    const int n_cols = (L.qt.rows + 15) & ~15;
+    const uint32_t idesc = (1u << 4) | (T::kFormat << 7) | (T::kFormat << 10) | (static_cast<uint32_t>(n_cols >> 3) << 17) |
+                           (static_cast<uint32_t>(kKeys >> 4) << 24);
+    const uint64_t dk = ptx::sdesc_sw128(sbase + C::OFF_K, 16, 1024), dq = ptx::sdesc_sw128(sbase + C::OFF_Q, 16, 1024);
+    uint32_t leader = 0, n = 0, nq = 0, se = 0;  // units, query tiles; parity of the S-empty waits, a bit per group
+    int first_leader = -1;
+    bool same = true, issued = false;
+    while (ok && walk.next(L.c, 1, uc, s, L.status))
+      for (int t = s.t0; ok && t < s.t1; t += kGroups) {
+        const int count = min(kGroups, s.t1 - t);
+        for (int q = 0; ok && q < n_tiles; ++q, ++nq) {
+          const int qs = nq % QS;
+          ok = warp_wait(bar(C::B_QF + qs), (nq / QS) & 1, abort_flag);
+          for (int i = 0; ok && i < count; ++i) {
+            const uint32_t st = (n + i) % kGroups;
+            // A group's first step finds its buffer free (parity 1 of a fresh barrier passes).
+            ok = (q > 0 || warp_wait(bar(C::B_KF + st), ((n + i) / kGroups) & 1, abort_flag)) &&
+                 warp_wait(bar(C::B_SE + st), ((se >> st) & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            se ^= 1u << st;
+            ptx::tc_fence_after();
+            const bool me = ptx::elect_one(leader);
+            if (first_leader < 0) first_leader = static_cast<int>(leader);
+            same = same && static_cast<int>(leader) == first_leader;
+            if (me && same) {
+              const uint64_t kd = dk + static_cast<uint64_t>(st * C::TILE >> 4);
+              const uint64_t qd = dq + static_cast<uint64_t>(qs * C::TILE >> 4);
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint64_t off = static_cast<uint64_t>(((kk / 4) * C::BLOCK + (kk % 4) * 32) >> 4);
+                ptx::mma_ss(tmem + st * 128, kd + off, qd + off, idesc, kk > 0 ? 1u : 0u);
+              }
+              ptx::mma_commit(bar(C::B_SF + st));
+              if (q + 1 == n_tiles) ptx::mma_commit(bar(C::B_KE + st));
+              if (i + 1 == count) ptx::mma_commit(bar(C::B_QE + qs));
+            }
+            __syncwarp();
+            issued = true;
+            ok = same;
+          }
+        }
+        n += count;
+      }
+    if (!ok) {
+      if (lane == 0) record_timeout(abort_flag, L.status);
+      if (issued && lane == first_leader) {      // every MMA ends before TMEM is released
+        const volatile int never = 0;
+        ptx::mma_commit(bar(C::B_DRAIN));
+        ptx::mbar_wait(bar(C::B_DRAIN), 0, &never, kWaitTimeoutNs);
+      }
+    }
+    __syncwarp();
+  } else if (warp == kWarpLse) {
+    // -LSE log2e per row of a tile, -inf for a row that does not count (those add
+    // 0; their queries may be anything, so that the tile is marked).
+    uint32_t n = 0;
+    while (ok && walk.next(L.c, 1, uc, s, L.status)) {
+      const int drafted = drafted_tokens(L.d, s.b);
+      for (int t = s.t0; ok && t < s.t1; t += kGroups)
+        for (int q = 0; q < n_tiles; ++q, ++n) {
+          const int st = n % QS;
+          float v[4];
+          bool part = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = i * 32 + lane;
+            const int tok = q * L.qt.tokens + (L.qt.head_inner ? r / L.d.gq : r % L.qt.tokens);
+            const int head = s.h * L.d.gq + (L.qt.head_inner ? r % L.d.gq : r / L.qt.tokens);
+            const bool in = r < L.qt.rows && tok < drafted &&
+                            (!L.use || __ldg(L.use + static_cast<int64_t>(s.b) * L.d.tokens + tok) != 0);
+            const float lse = in ? __ldg(L.lse + (static_cast<int64_t>(head) * L.c.batch + s.b) * L.d.tokens + tok) : -INFINITY;
+            v[i] = lse == -INFINITY ? -INFINITY : -kLog2e * lse;
+            part = part || (lse == -INFINITY && r < L.qt.rows);
+          }
+          part = __any_sync(0xffffffffu, part);
+          if (n >= QS && !warp_wait(bar(C::B_QE + st), (n / QS - 1) & 1, abort_flag)) {
+            ok = false;
+            break;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lse_s[st * 128 + i * 32 + lane] = v[i];
+          if (lane == 0) part_s[st] = part;
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(C::B_QF + st));
+        }
+    }
+    if (!ok && lane == 0) record_timeout(abort_flag, L.status);
+  } else {
+    const int grp = warp >> 2, key = threadIdx.x & 127;
+    const uint32_t tS = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + grp * 128;
+    const uint64_t scale2 = ptx::f2(L.d.scale_log2, L.d.scale_log2);
+    uint32_t n = 0, nq = 0, step = 0;
+    while (walk.next(L.c, 1, uc, s, L.status))
+      for (int t = s.t0; t < s.t1; t += kGroups) {
+        const int count = min(kGroups, s.t1 - t), mine = (grp - n) & (kGroups - 1);
+        n += count;
+        const bool active = mine < count;
+        const int64_t pos = static_cast<int64_t>(t + mine) * kKeys + key;
+        const bool live = active && pos < s.len && pos < L.acc_len;
+        if (active && pos < s.len && pos >= L.acc_len) record_bounds(L.status);
+        float* dst = L.acc + (static_cast<int64_t>(s.b) * L.c.hkv + s.h) * L.acc_len + pos;
+        const float old = live && L.accumulate ? *dst : 0.f;
+        uint64_t a2[4] = {0, 0, 0, 0};
+        for (int q = 0; q < n_tiles; ++q, ++nq) {
+          const int qs = nq % QS;
+          ok = ok && warp_wait(bar(C::B_QF + qs), (nq / QS) & 1, abort_flag);
+          if (active) {
+            ok = ok && warp_wait(bar(C::B_SF + grp), step & 1, abort_flag);
+            ++step;
+            if (ok) {
+              ptx::tc_fence_after();
+              const float* lrow = lse_s + qs * 128;
+              const int valid = L.qt.head_inner ? min(L.qt.rows, (L.d.tokens - q * L.qt.tokens) * L.d.gq) : L.qt.rows;
+              const bool part = part_s[qs] != 0;
+              auto add4 = [&](const uint32_t* r, const float4& nl, int e) {
+                float x0, x1, x2, x3;
+                ptx::unf2(ptx::fma2(ptx::f2(__uint_as_float(r[0]), __uint_as_float(r[1])), scale2, ptx::f2(nl.x, nl.y)), x0, x1);
+                ptx::unf2(ptx::fma2(ptx::f2(__uint_as_float(r[2]), __uint_as_float(r[3])), scale2, ptx::f2(nl.z, nl.w)), x2, x3);
+                a2[(2 * e) & 3] = ptx::add2(a2[(2 * e) & 3], ptx::f2(ptx::ex2(x0), ptx::ex2(x1)));
+                a2[(2 * e + 1) & 3] = ptx::add2(a2[(2 * e + 1) & 3], ptx::f2(ptx::ex2(x2), ptx::ex2(x3)));
+              };
+              // A row that does not count adds 0 whatever its logit is.
+              auto drop4 = [&](uint32_t* r, const float4& nl) {
+                if (nl.x == -INFINITY) r[0] = 0u;
+                if (nl.y == -INFINITY) r[1] = 0u;
+                if (nl.z == -INFINITY) r[2] = 0u;
+                if (nl.w == -INFINITY) r[3] = 0u;
+              };
+              int c0 = 0;
+#pragma unroll 1
+              for (; c0 + 32 <= valid; c0 += 32) {
+                float4 l4[8];                    // read before the TMEM wait, which covers their latency
+                uint32_t r[32];
+                ptx::tmem_ld32(tS + c0, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) l4[e] = reinterpret_cast<const float4*>(lrow + c0)[e];
+                ptx::tmem_wait_ld();
+                if (part) {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) drop4(r + 4 * e, l4[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) add4(r + 4 * e, l4[e], e);
+              }
+              // The last columns by 16; past the tile's rows they are whatever its stage held.
+#pragma unroll 1
+              for (; c0 < valid; c0 += 16) {
+                float4 l4[4];
+                uint32_t r[16];
+                ptx::tmem_ld16(tS + c0, r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l4[e] = reinterpret_cast<const float4*>(lrow + c0)[e];
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) drop4(r + 4 * e, l4[e]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) add4(r + 4 * e, l4[e], e);
+              }
+              ptx::tc_fence_before();
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(C::B_SE + grp));
+          }
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(C::B_QE + qs));
+        }
+        float s0, s1, s2, s3;
+        ptx::unf2(ptx::add2(a2[0], a2[1]), s0, s1);
+        ptx::unf2(ptx::add2(a2[2], a2[3]), s2, s3);
+        if (ok && live) *dst = old + ((s0 + s1) + (s2 + s3));
+      }
+    if (!ok && lane == 0) record_timeout(abort_flag, L.status);
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc<512>(tmem);
+  }
+}
+
+// Queries that a TMA map cannot describe (a dimension repeated by a stride of 0),
+// or none at all: one thread per key, its key in registers, the rows' queries by broadcast loads.
+constexpr int kPlainThreads = 128;
+
+template <class T, int D>
+__global__ void __launch_bounds__(kPlainThreads) cache_evidence_plain_kernel(const __grid_constant__ CacheEvidenceLaunch L) {
+  const int h = blockIdx.y, b = blockIdx.z, key = blockIdx.x * kPlainThreads + threadIdx.x;
   int len = cache_len(L.c, b, h, L.status);
   if (len > L.acc_len) {
     record_bounds(L.status);
@@ -55,9 +374,18 @@ __global__ void __launch_bounds__(kThreads) cache_evidence_kernel(const __grid_c
 
 template <class T, int D>
 cudaError_t launch_d(const CacheEvidenceLaunch& L, cudaStream_t stream) {
+  if (L.has_q_map) {
+    using C = EvCfg<D>;
+    auto kern = cache_evidence_kernel<T, D>;
+    static PerDeviceAttr once;
+    const cudaError_t e = raise_smem_limit(once, reinterpret_cast<const void*>(kern), C::SMEM);
+    if (e != cudaSuccess) return e;
+    kern<<<L.n_ctas, kThreads, C::SMEM, stream>>>(L);
+    return cudaGetLastError();
+  }
   const int64_t room = static_cast<int64_t>(L.c.max_pages) * L.c.page;
-  const dim3 grid(static_cast<unsigned>((room + kThreads - 1) / kThreads), L.c.hkv, L.c.batch);
-  cache_evidence_kernel<T, D><<<grid, kThreads, 0, stream>>>(L);
+  const dim3 grid(static_cast<unsigned>((room + kPlainThreads - 1) / kPlainThreads), L.c.hkv, L.c.batch);
+  cache_evidence_plain_kernel<T, D><<<grid, kPlainThreads, 0, stream>>>(L);
   return cudaGetLastError();
 }
 

@@ -34,6 +34,14 @@ struct DraftView {
   float scale_log2;                 // softmax_scale * log2(e)
 };
 
+// Rows of a tile of queries of one (sequence, KV head), as their map's box lays
+// them out: all gq heads of `tokens` tokens, the heads inside a token's rows or
+// the tokens inside a head's.
+struct QueryTile {
+  int tokens, rows;                 // rows = tokens * gq <= 128
+  int head_inner;
+};
+
 // Attention: the cached keys of every (sequence, KV head, tile of tile_rows
 // rows), a problem, are cut into units of kKeyTile keys, and all units are dealt
 // evenly over n_ctas CTAs in order. A CTA's part of a problem leaves a partial:
@@ -41,7 +49,7 @@ struct DraftView {
 // units, so no two are the same).
 struct CacheAttnLaunch {
   CUtensorMap tm_k, tm_v;           // pages; box {64, box_rows, 1, 1} in the order of `perm`
-  CUtensorMap tm_q;                 // wide: {d, hq, T, B}, box {64, gq, 128 / gq, 1}
+  CUtensorMap tm_q;                 // wide: queries, box of gq heads of tile_tokens tokens
   CacheView c;
   DraftView d;
   void* o;
@@ -49,24 +57,27 @@ struct CacheAttnLaunch {
   float* part_o;                    // [partials, tile_rows, d], unnormalised
   float2* part_ml;                  // [partials, tile_rows]: running max (log2 units), row sum
   int* status;
-  int k_perm, v_perm;               // where token, head and page stand in the maps' coordinates
+  int k_perm, v_perm, q_perm;       // where token, head and page (sequence) stand in the maps' coordinates
   int box_rows;
   int rows, tile_rows, row_tiles;   // rows = tokens * gq; tile_rows rows of a partial
   int slots, slot_rows;             // a row tile is `slots` slots of slot_rows rows, tile_rows / slots places each
+  QueryTile qt;                     // wide: the rows of a slot
   int n_ctas, key_tile, min_units;  // units a CTA takes at least
   int wide;                         // 128-row slots on tcgen05 (else mma.sync)
 };
 
 struct CacheEvidenceLaunch {
-  CUtensorMap tm_k, tm_q;
+  CUtensorMap tm_k, tm_q;           // pages, queries
   CacheView c;
   DraftView d;
+  QueryTile qt;
+  int has_q_map;                    // tm_q and qt describe q
   const float* lse;                 // [hq, B, T]
   const uint8_t* use;               // [B, T] or null
   float* acc;                       // [B, hkv, acc_len]
   int64_t acc_len;
   int* status;
-  int k_perm, q_perm, box_rows;
+  int k_perm, q_perm, box_rows, n_ctas;
   int accumulate;
 };
 
@@ -116,7 +127,7 @@ struct CacheAttnShape {
   int tile_rows, row_tiles, slots, slot_rows, key_tile, n_ctas, min_units;
   bool wide;
 };
-CacheAttnShape cache_attn_shape(int rows, int gq, bool q_map, int n_sm);
+CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n_sm);
 cudaError_t launch_cache_attn_wide(const CacheAttnLaunch& L, cudaStream_t stream);
 
 // What the cache calls use of a workspace (evisel_capi.cpp).

@@ -142,27 +142,39 @@ DraftView view_of(const evisel_cache* c, const evisel_draft* d) {
   return v;
 }
 
-// Map of the pages of k or v: {d, ...} with token, head and page in the order of
-// their strides (a dimension of one entry takes any), box of box_rows tokens of one page and head.
-int encode_pages(CUtensorMap* map, int* perm, const void* base, const evisel_cache* c, const int64_t* stride, int box_rows) {
-  struct Dim {
-    int64_t stride;
-    uint64_t size;
-    uint32_t box;
-    int what;                       // 0 token, 1 head, 2 page
-  } dim[3] = {{stride[2], static_cast<uint64_t>(c->page), static_cast<uint32_t>(box_rows), 0},
-              {stride[1], static_cast<uint64_t>(c->hkv), 1u, 1},
-              {stride[0], static_cast<uint64_t>(c->n_pages), 1u, 2}};
-  for (Dim& x : dim)
-    if (x.size == 1) x.stride = c->head_dim;
-  std::stable_sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
-  const uint64_t dims[4] = {static_cast<uint64_t>(c->head_dim), dim[0].size, dim[1].size, dim[2].size};
-  const uint64_t strides[3] = {static_cast<uint64_t>(dim[0].stride) * 2, static_cast<uint64_t>(dim[1].stride) * 2,
-                               static_cast<uint64_t>(dim[2].stride) * 2};
-  const uint32_t box[4] = {64u, dim[0].box, dim[1].box, dim[2].box};
+// 4-D map {d, ...} of a tensor whose other dimensions are token, head and page (or
+// sequence), placed in the order of their strides (a dimension of one entry
+// takes any); `perm` gets the place, 1..3, of each: two bits, in that order.
+struct MapDim {
+  int64_t stride;                   // elements
+  int64_t size;
+  int box;
+};
+
+int encode_sorted(CUtensorMap* map, int* perm, const void* base, int head_dim, int dtype, const MapDim (&in)[3]) {
+  struct {
+    MapDim x;
+    int what;
+  } dim[3] = {{in[0], 0}, {in[1], 1}, {in[2], 2}};
+  for (auto& d : dim)
+    if (d.x.size == 1) d.x.stride = head_dim;
+  std::stable_sort(dim, dim + 3, [](const auto& a, const auto& b) { return a.x.stride < b.x.stride; });
+  uint64_t dims[4] = {static_cast<uint64_t>(head_dim)}, strides[3];
+  uint32_t box[4] = {64u};
   *perm = 0;
-  for (int i = 0; i < 3; ++i) *perm |= (i + 1) << (2 * dim[i].what);
-  return encode_map4(map, base, c->dtype, dims, strides, box);
+  for (int i = 0; i < 3; ++i) {
+    dims[i + 1] = static_cast<uint64_t>(dim[i].x.size);
+    strides[i] = static_cast<uint64_t>(dim[i].x.stride) * 2;
+    box[i + 1] = static_cast<uint32_t>(dim[i].x.box);
+    *perm |= (i + 1) << (2 * dim[i].what);
+  }
+  return encode_map4(map, base, dtype, dims, strides, box);
+}
+
+// The pages of k or v, box of box_rows tokens of one page and head.
+int encode_pages(CUtensorMap* map, int* perm, const void* base, const evisel_cache* c, const int64_t* stride, int box_rows) {
+  return encode_sorted(map, perm, base, c->head_dim, c->dtype,
+                       {{stride[2], c->page, box_rows}, {stride[1], c->hkv, 1}, {stride[0], c->n_pages, 1}});
 }
 
 // Whether a TMA map can describe q: no repeated (stride 0) dimension.
@@ -173,15 +185,23 @@ bool has_query_map(const evisel_cache* c, const evisel_draft* d) {
   return true;
 }
 
-// Map of q {d, hq, T, B}, box of `box_tokens` tokens of one KV group: rows (token, head).
-int encode_queries(CUtensorMap* map, const evisel_cache* c, const evisel_draft* d, int box_tokens) {
-  auto bytes = [&](int64_t stride, int64_t size) { return static_cast<uint64_t>(size > 1 ? stride : c->head_dim) * 2; };
-  const uint64_t dims[4] = {static_cast<uint64_t>(c->head_dim), static_cast<uint64_t>(d->hq),
-                            static_cast<uint64_t>(d->tokens), static_cast<uint64_t>(c->batch)};
-  const uint64_t strides[3] = {bytes(d->q_stride[2], d->hq), bytes(d->q_stride[1], d->tokens),
-                               bytes(d->q_stride[0], c->batch)};
-  const uint32_t box[4] = {64u, static_cast<uint32_t>(d->hq / c->hkv), static_cast<uint32_t>(box_tokens), 1u};
-  return encode_map4(map, d->q, c->dtype, dims, strides, box);
+// The tokens cut evenly into as few tiles of at most 128 rows as hold them.
+QueryTile query_tile(const evisel_cache* c, const evisel_draft* d) {
+  const int gq = d->hq / c->hkv, most = 128 / gq;
+  QueryTile t{};
+  const int tiles = std::max(1, (d->tokens + most - 1) / most);
+  t.tokens = std::max(1, (d->tokens + tiles - 1) / tiles);
+  t.rows = t.tokens * gq;
+  return t;
+}
+
+// The queries, box of a tile. The rows follow the order of the strides.
+int encode_queries(CUtensorMap* map, int* perm, QueryTile* tile, const evisel_cache* c, const evisel_draft* d) {
+  const int rc = encode_sorted(map, perm, d->q, c->head_dim, c->dtype,
+                               {{d->q_stride[1], d->tokens, tile->tokens}, {d->q_stride[2], d->hq, d->hq / c->hkv},
+                                {d->q_stride[0], c->batch, 1}});
+  tile->head_inner = ((*perm >> 2) & 3) < (*perm & 3);
+  return rc;
 }
 
 int grow(evisel_ws* ws, size_t need, cudaStream_t stream) {
@@ -236,7 +256,8 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     L.c = view_of(cache);
     L.d = view_of(cache, draft);
     L.rows = draft->tokens * L.d.gq;
-    const CacheAttnShape shape = cache_attn_shape(L.rows, L.d.gq, has_query_map(cache, draft), n_sm);
+    L.qt = query_tile(cache, draft);
+    const CacheAttnShape shape = cache_attn_shape(L.rows, L.qt, has_query_map(cache, draft), n_sm);
     L.wide = shape.wide;
     L.slots = shape.slots;
     L.slot_rows = shape.slot_rows;
@@ -256,8 +277,7 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     if (rc == EVISEL_OK) rc = grow(*ws_inout, ml_bytes + parts * L.tile_rows * cache->head_dim * sizeof(float), stream);
     if (rc == EVISEL_OK && cache->max_pages > 0) rc = encode_pages(&L.tm_k, &L.k_perm, cache->k, cache, cache->k_stride, L.box_rows);
     if (rc == EVISEL_OK && cache->max_pages > 0) rc = encode_pages(&L.tm_v, &L.v_perm, cache->v, cache, cache->v_stride, L.box_rows);
-    if (rc != EVISEL_OK) return rc;
-    if (L.wide) rc = encode_queries(&L.tm_q, cache, draft, 128 / L.d.gq);
+    if (rc == EVISEL_OK && L.wide) rc = encode_queries(&L.tm_q, &L.q_perm, &L.qt, cache, draft);
     if (rc != EVISEL_OK) return rc;
     char* buf = static_cast<char*>(ws_cache(*ws_inout).buf);
     L.part_ml = reinterpret_cast<float2*>(buf);
@@ -286,7 +306,16 @@ int evisel_cache_evidence(const evisel_cache* cache, const evisel_draft* draft, 
     CacheEvidenceLaunch L{};
     L.c = view_of(cache);
     L.d = view_of(cache, draft);
+    L.n_ctas = sm_count();
+    if (L.n_ctas <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
+    L.box_rows = std::min(cache->page, 128);
+    L.qt = query_tile(cache, draft);
+    L.has_q_map = draft->tokens > 0 && has_query_map(cache, draft);
+    if (static_cast<int64_t>(cache->batch) * cache->hkv * ((static_cast<int64_t>(cache->max_pages) * cache->page + 127) / 128) > INT32_MAX)
+      return fail(EVISEL_EUNSUPPORTED, "too many units of work");
     rc = ws_acquire(ws_inout);
+    if (rc == EVISEL_OK && L.has_q_map) rc = encode_pages(&L.tm_k, &L.k_perm, cache->k, cache, cache->k_stride, L.box_rows);
+    if (rc == EVISEL_OK && L.has_q_map) rc = encode_queries(&L.tm_q, &L.q_perm, &L.qt, cache, draft);
     if (rc != EVISEL_OK) return rc;
     L.lse = lse;
     L.use = use;

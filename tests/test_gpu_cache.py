@@ -124,6 +124,37 @@ def test_attention_of_strided_inputs(cuda_lib):
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("order", ["heads outside tokens", "one query for all sequences", "one token for all"])
+def test_many_rows_of_queries_in_other_orders(cuda_lib, order):
+    """Queries stored [B, hq, T, d], and ones repeated by a stride of 0: attention and evidence."""
+    rng = np.random.default_rng(12)
+    ty = _types()["bf16"]
+    lens = [300, 129]
+    cache, ref = make_cache(rng, lens, 2, 64, 32, ty)
+    if order == "heads outside tokens":
+        q, _ = tensor(rng, (2, 14, 45, 64), ty)
+        q = q.transpose(1, 2)
+    elif order == "one query for all sequences":
+        q, _ = tensor(rng, (1, 45, 14, 64), ty)
+        q = q.expand(2, -1, -1, -1)
+    else:
+        q, _ = tensor(rng, (2, 1, 14, 64), ty)
+        q = q.expand(-1, 45, -1, -1)
+    q_ref = q.double().cpu().numpy()
+    k, k_ref = tensor(rng, (2, 45, 2, 64), ty)
+    v, v_ref = tensor(rng, (2, 45, 2, 64), ty)
+    allowed = random_tree(rng, 2, 45)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, tree=tree_words(allowed))
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref, allowed), 64, ty)
+    acc, ws = cuda_lib.evisel_cache_evidence(cache, q, lse, ws=ws)
+    _status(cuda_lib, ws)
+    want = ref_cache.evidence(ref, q_ref, lse.cpu().numpy())
+    for b in range(2):
+        for h in range(2):                       # A <= 40 here, |LSE| <= 10
+            got = acc[b, h, :lens[b]].double().cpu().numpy()
+            assert np.all(np.abs(got - want[b][h]) <= (72 * 2.0 ** -24 * 40 + 2.0 ** -18) * want[b][h])
+
+
 def test_attention_of_pages_in_a_larger_pool(cuda_lib):
     """Keys and values interleaved in one pool [P, 2, hkv, page, d], and heads outside the pages."""
     import torch
