@@ -1,10 +1,35 @@
-// Choice of the highest of many scores by one block: a radix select on their
-// order keys, then their positions in ascending order.
+// Choice of the highest of many scores by one cluster of CTAs: a radix select on
+// their order keys over shared-memory histograms (read across the cluster),
+// then their positions in ascending order.
 #pragma once
 
 #include "cache_common.cuh"
 
 namespace evisel {
+
+namespace ptx {
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The int at shared address `addr` of CTA `rank` of the cluster.
+__device__ __forceinline__ int ld_cluster(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  int v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+}  // namespace ptx
 
 // Ascending with the float (-0 equal to 0), NaN lowest.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -13,53 +38,164 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-struct ChooseScratch {
-  int hist[256];
-  int digit, left;
-  int sums[34];
+struct ChooseMem {
+  int hist[4][256];                 // per pass: the keys of this CTA by digit
+  int tot[256];
+  int digit, left, done;
+  int above[32], tie[32];           // per warp
+  int sum[2];                       // this CTA's keys above the boundary, and on it
+};
+
+// A CTA's part [a, b) of [lo, hi): whole groups of 32 in order of rank.
+struct ChoosePart {
+  int a, b;
+  __device__ __forceinline__ ChoosePart(int lo, int hi, int rank, int size) {
+    const int chunk = (max(hi - lo, 0) + 32 * size - 1) / (32 * size) * 32;
+    a = min(hi, lo + rank * chunk);
+    b = min(hi, a + chunk);
+  }
 };
 
 // The `want` highest of key(i), lo <= i < hi (0 <= want <= hi - lo; ties: the
-// lower i): emit(rank, i) for each, ranks ascending with i. The whole block calls.
-template <class Key, class Emit>
-__device__ __forceinline__ void choose_top(int lo, int hi, int want, Key key, ChooseScratch& sc, Emit emit) {
+// lower i): emit(rank, i) for each, ranks ascending with i. Every thread of every
+// CTA of the cluster calls, with the same lo, hi and want; key(i) is asked for
+// the i of the CTA's own ChoosePart only. The last cluster barrier is the
+// caller's: no CTA may leave before the others have read its sums. THREADS: the block's.
+template <int THREADS, class Key, class Emit>
+__device__ __forceinline__ void choose_top(int lo, int hi, int want, Key key, ChooseMem& m, Emit emit) {
   if (want <= 0) return;
-  const int n = hi - lo, threads = blockDim.x;
-  uint32_t prefix = 0, mask = 0;                 // the boundary key's digits so far
+  const int rank = static_cast<int>(ptx::cluster_rank()), size = static_cast<int>(ptx::cluster_size());
+  const ChoosePart part(lo, hi, rank, size);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t prefix = 0, mask = 0;                 // the boundary's digits so far
   int left = want;                               // to take among the keys with that prefix
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += threads) sc.hist[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += threads) {
-      const uint32_t k = key(lo + i);
-      if ((k & mask) == prefix) atomicAdd(&sc.hist[(k >> shift) & 255u], 1);
+  for (int i = threadIdx.x; i < 4 * 256; i += THREADS) m.hist[i >> 8][i & 255] = 0;
+  __syncthreads();
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass;
+#pragma unroll 4
+    for (int i = part.a + static_cast<int>(threadIdx.x); i < part.b; i += THREADS) {
+      const uint32_t k = key(i);
+      if ((k & mask) == prefix) atomicAdd(&m.hist[pass][(k >> shift) & 255u], 1);
+    }
+    if (size > 1) ptx::cluster_sync();
+    else __syncthreads();
+    if (threadIdx.x < 256) {
+      int x = m.hist[pass][threadIdx.x];
+      if (size > 1) {
+        x = 0;
+        for (int r = 0; r < size; ++r) x += ptx::ld_cluster(ptx::smem_addr(&m.hist[pass][threadIdx.x]), r);
+      }
+      m.tot[threadIdx.x] = x;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      int d = 255, rest = left;
-      while (d > 0 && sc.hist[d] < rest) rest -= sc.hist[d--];
-      sc.digit = d;
-      sc.left = rest;
+    if (warp == 0) {
+      // Digits from the highest: a lane holds eight, the one where the sum reaches `left` walks them.
+      int x[8], sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += x[e] = m.tot[255 - 8 * lane - e];
+      int inc = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      int rest = left - (inc - sum);
+      if (rest > 0 && rest <= sum) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (rest > 0 && rest <= x[e]) {
+            m.digit = 255 - 8 * lane - e;
+            m.left = rest;
+            m.done = rest == x[e];               // all keys with this prefix are taken: no digit below it matters
+          }
+          rest -= x[e];
+        }
+      }
     }
     __syncthreads();
-    prefix |= static_cast<uint32_t>(sc.digit) << shift;
+    prefix |= static_cast<uint32_t>(m.digit) << shift;
     mask |= 255u << shift;
-    left = sc.left;
+    left = m.left;
+    if (m.done) break;
   }
-  // Keys above the boundary key, and the first `left` equal to it.
-  int rank = 0, equal = 0;
-  for (int base = 0; base < n; base += threads) {
-    const int i = base + static_cast<int>(threadIdx.x);
-    const uint32_t k = i < n ? key(lo + i) : 0u;
-    const bool above = i < n && k > prefix, tie = i < n && k == prefix;
-    int total, total_eq;
-    const int eq = equal + block_prefix(tie, sc.sums, total_eq);
-    const bool take = above || (tie && eq < left);
-    const int at = rank + block_prefix(take, sc.sums, total);
-    if (take) emit(at, lo + i);
-    rank += total;
-    equal += total_eq;
+  // Keys above the boundary, and the first `left` on it: counted per warp over
+  // its own run of keys, then placed.
+  const int run = ((part.b - part.a + THREADS - 1) / THREADS) * 32;
+  const int wa = min(part.b, part.a + warp * run), wb = min(part.b, wa + run);
+  int above = 0, tie = 0;
+#pragma unroll 4
+  for (int i = wa; i < wb; i += 32) {
+    const uint32_t k = i + lane < wb ? key(i + lane) & mask : 0u;
+    above += __popc(__ballot_sync(0xffffffffu, i + lane < wb && k > prefix));
+    tie += __popc(__ballot_sync(0xffffffffu, i + lane < wb && k == prefix));
   }
+  if (lane == 0) {
+    m.above[warp] = above;
+    m.tie[warp] = tie;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    const int xa = lane < THREADS / 32 ? m.above[lane] : 0, xt = lane < THREADS / 32 ? m.tie[lane] : 0;
+    int ia = xa, it = xt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int ya = __shfl_up_sync(0xffffffffu, ia, o), yt = __shfl_up_sync(0xffffffffu, it, o);
+      if (lane >= o) {
+        ia += ya;
+        it += yt;
+      }
+    }
+    m.above[lane] = ia - xa;
+    m.tie[lane] = it - xt;
+    if (lane == 31) {
+      m.sum[0] = ia;
+      m.sum[1] = it;
+    }
+  }
+  if (size > 1) ptx::cluster_sync();
+  else __syncthreads();
+  int na = m.above[warp], nt = m.tie[warp];      // before this warp's run
+  for (int r = 0; r < rank; ++r) {
+    na += ptx::ld_cluster(ptx::smem_addr(&m.sum[0]), r);
+    nt += ptx::ld_cluster(ptx::smem_addr(&m.sum[1]), r);
+  }
+#pragma unroll 2
+  for (int i = wa; i < wb; i += 32) {
+    const uint32_t k = i + lane < wb ? key(i + lane) & mask : 0u;
+    const bool is_above = i + lane < wb && k > prefix, is_tie = i + lane < wb && k == prefix;
+    const uint32_t ba = __ballot_sync(0xffffffffu, is_above), bt = __ballot_sync(0xffffffffu, is_tie);
+    const uint32_t low = (1u << lane) - 1u;
+    const int ta = na + __popc(ba & low), tt = nt + __popc(bt & low);
+    if (is_above || (is_tie && tt < left)) emit(ta + min(tt, left), i + lane);
+    na += __popc(ba);
+    nt += __popc(bt);
+  }
+}
+
+// CTAs per problem: so many that each has `least` scores, and the grid stays within about one CTA per SM.
+inline int choose_cluster(int64_t problems, int64_t scores, int64_t least, int n_sm) {
+  int c = 8;
+  while (c > 1 && (problems * c > n_sm || scores < least * c)) c /= 2;
+  return c;
+}
+
+// Launches `kern` with clusters of `cluster` CTAs (grid.x a multiple of it).
+template <class Launch>
+cudaError_t launch_clusters(void (*kern)(Launch), const Launch& L, unsigned grid, unsigned threads, int cluster,
+                            cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, L);
 }
 
 }  // namespace evisel

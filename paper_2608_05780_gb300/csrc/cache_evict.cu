@@ -12,8 +12,9 @@ namespace {
 constexpr int kChooseThreads = 1024;
 
 __global__ void __launch_bounds__(kChooseThreads) cache_evict_choose_kernel(const __grid_constant__ CacheEvictLaunch L) {
-  __shared__ ChooseScratch sc;
-  const int b = blockIdx.x / L.c.hkv, h = blockIdx.x % L.c.hkv;
+  __shared__ ChooseMem mem;
+  const int rank = static_cast<int>(ptx::cluster_rank()), size = static_cast<int>(ptx::cluster_size());
+  const int problem = blockIdx.x / size, b = problem / L.c.hkv, h = problem % L.c.hkv;
   int len = cache_len(L.c, b, h, L.status);
   if (len > L.acc_len) {
     record_bounds(L.status);
@@ -22,20 +23,22 @@ __global__ void __launch_bounds__(kChooseThreads) cache_evict_choose_kernel(cons
   const int count = min(len, L.budget);
   const bool all = len <= L.budget;
   const int sink = all ? count : L.sink, recent = all ? 0 : L.recent;
-  const float* acc = L.acc + (static_cast<int64_t>(b) * L.c.hkv + h) * L.acc_len;
-  int32_t* kept = L.kept + (static_cast<int64_t>(b) * L.c.hkv + h) * L.budget;
-  float* out = L.acc_out + (static_cast<int64_t>(b) * L.c.hkv + h) * L.acc_out_len;
-  auto put = [&](int rank, int i) {
-    kept[rank] = i;
-    out[rank] = acc[i];
+  const float* acc = L.acc + static_cast<int64_t>(problem) * L.acc_len;
+  int32_t* kept = L.kept + static_cast<int64_t>(problem) * L.budget;
+  float* out = L.acc_out + static_cast<int64_t>(problem) * L.acc_out_len;
+  auto put = [&](int place, int i) {
+    kept[place] = i;
+    out[place] = acc[i];
   };
-  for (int i = threadIdx.x; i < sink; i += kChooseThreads) put(i, i);
-  for (int i = threadIdx.x; i < recent; i += kChooseThreads) put(count - recent + i, len - recent + i);
-  for (int i = count + threadIdx.x; i < L.budget; i += kChooseThreads) kept[i] = -1;
-  for (int64_t i = count + threadIdx.x; i < L.acc_out_len; i += kChooseThreads) out[i] = 0.f;
-  choose_top(sink, len - recent, count - sink - recent, [&](int i) { return order_key(__ldg(acc + i)); }, sc,
-             [&](int rank, int i) { put(sink + rank, i); });
-  if (threadIdx.x == 0) L.out_lens[b * L.out.ls[0] + h * L.out.ls[1]] = count;
+  const int first = rank * kChooseThreads + static_cast<int>(threadIdx.x), step = size * kChooseThreads;
+  for (int i = first; i < sink; i += step) put(i, i);
+  for (int i = first; i < recent; i += step) put(count - recent + i, len - recent + i);
+  for (int i = count + first; i < L.budget; i += step) kept[i] = -1;
+  for (int64_t i = count + first; i < L.acc_out_len; i += step) out[i] = 0.f;
+  choose_top<kChooseThreads>(sink, len - recent, count - sink - recent, [&](int i) { return order_key(__ldg(acc + i)); }, mem,
+             [&](int place, int i) { put(sink + place, i); });
+  if (first == 0) L.out_lens[b * L.out.ls[0] + h * L.out.ls[1]] = count;
+  if (size > 1) ptx::cluster_sync();
 }
 
 // The source of an evicted cache's page: the kept tokens, in order.
@@ -66,8 +69,11 @@ __global__ void __launch_bounds__(kPageThreads) cache_evict_copy_kernel(const __
 
 template <class T, int D>
 cudaError_t launch_d(const CacheEvictLaunch& L, cudaStream_t stream) {
-  cache_evict_choose_kernel<<<L.c.batch * L.c.hkv, kChooseThreads, 0, stream>>>(L);
-  cudaError_t e = cudaGetLastError();
+  const int problems = L.c.batch * L.c.hkv;
+  const int64_t room = static_cast<int64_t>(L.c.max_pages) * L.c.page;
+  const int cluster = choose_cluster(problems, room < L.acc_len ? room : L.acc_len, 2048, sm_count());
+  const cudaError_t e = launch_clusters(cache_evict_choose_kernel, L, static_cast<unsigned>(problems * cluster), kChooseThreads,
+                                        cluster, stream);
   if (e != cudaSuccess) return e;
   cache_evict_copy_kernel<T, D><<<dim3((L.budget + L.out.page - 1) / L.out.page, L.c.hkv, L.c.batch), kPageThreads, 0, stream>>>(L);
   return cudaGetLastError();

@@ -111,7 +111,6 @@ struct CacheSelectLaunch {
   int32_t* pages;
   int32_t* sel_table;
   int32_t* sel_lens;
-  float* scores;                    // [B, hkv, max_pages] scratch
   int* status;
   int n_select, sink, recent;
 };

@@ -23,24 +23,36 @@ __device__ __forceinline__ void fill_page(const CacheView& c, void* k_out, void*
   uint16_t* v = static_cast<uint16_t*>(v_out) + id * c.vs[0] + h * c.vs[1];
   const int x = threadIdx.x % LANES, grp = threadIdx.x / LANES;
   float sum[8] = {};
-  for (int pos = p0 + grp; pos < p1; pos += GROUPS) {
-    uint4* kd = reinterpret_cast<uint4*>(k + (pos - p0) * c.ks[2]) + x;
-    uint4 key;
-    if (pos >= src.first()) {
-      const uint4 *ks, *vs;
-      src.rows(pos, ks, vs);
-      key = __ldg(ks + x);
-      const uint4 value = __ldg(vs + x);
-      *kd = key;
-      *(reinterpret_cast<uint4*>(v + (pos - p0) * c.vs[2]) + x) = value;
-    } else {
-      if (!mean) continue;
-      key = *kd;
-    }
-    float f[8];
-    unpack8<T>(key, f);
+  // Four tokens a thread at a time: their places, then all loads, then all stores.
+  for (int base = p0 + grp; base < p1; base += 4 * GROUPS) {
+    const uint4 *ks[4], *vs[4];
+    uint4 key[4], value[4];
+    bool in[4], fresh[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += f[e];
+    for (int i = 0; i < 4; ++i) {
+      const int pos = base + i * GROUPS;
+      fresh[i] = pos < p1 && pos >= src.first();
+      in[i] = fresh[i] || (pos < p1 && mean);    // an older token is read for the mean only
+      ks[i] = vs[i] = reinterpret_cast<const uint4*>(k + (pos - p0) * c.ks[2]);
+      if (fresh[i]) src.rows(pos, ks[i], vs[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      key[i] = in[i] ? ks[i][x] : make_uint4(0, 0, 0, 0);
+      if (fresh[i]) value[i] = vs[i][x];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int slot = base + i * GROUPS - p0;
+      if (fresh[i]) {
+        reinterpret_cast<uint4*>(k + slot * c.ks[2])[x] = key[i];
+        reinterpret_cast<uint4*>(v + slot * c.vs[2])[x] = value[i];
+      }
+      float f[8];
+      unpack8<T>(key[i], f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += in[i] ? f[e] : 0.f;
+    }
   }
   if (!mean) return;
 #pragma unroll

@@ -1,5 +1,10 @@
 // Pages chosen for the queries of a (sequence, KV head) by their mean keys:
 //   score_j = max over the rows of q . k_mean_j.
+//
+// One launch, a cluster of CTAs per (sequence, KV head): each CTA forms the scores
+// of its part of the pages (16 pages against 8 rows per mma.sync, both read from
+// global memory 16 bytes a lane, the products' order along d permuted alike on
+// both sides) in shared memory, and the cluster chooses among them.
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -8,73 +13,85 @@
 namespace evisel {
 namespace {
 
-constexpr int kScoreThreads = 256;
-constexpr int kChooseThreads = 1024;
+constexpr int kChooseThreads = 512;
+constexpr int kMaxPages = 8192;                  // scores of a (sequence, KV head), over its cluster
+constexpr float kNone = -INFINITY;
 
-// A warp per page, a lane per D / 32 channels.
 template <class T, int D>
-__global__ void __launch_bounds__(kScoreThreads) cache_score_kernel(const __grid_constant__ CacheSelectLaunch L) {
-  constexpr int E = D / 32;
-  const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31;
-  const int page = blockIdx.x * (kScoreThreads / 32) + (threadIdx.x >> 5);
-  const int n = (cache_len(L.c, b, h, L.status) + L.c.page - 1) >> L.c.log_page;
-  if (page >= n) return;
-  const int64_t id = cache_page(L.c, b, h, page, L.status);
-  auto load = [&](const uint16_t* p, float (&x)[E]) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(p + lane * E);
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) {
-      const uint32_t y = __ldg(w + e);
-      x[2 * e] = T::lo(y), x[2 * e + 1] = T::hi(y);
-    }
-  };
-  float k[E];
-  load(static_cast<const uint16_t*>(L.c.k_mean) + (id * L.c.hkv + h) * D, k);
-  const int drafted = drafted_tokens(L.d, b);
-  float top = -INFINITY;
-  for (int t = 0; t < drafted; ++t)
-    for (int g = 0; g < L.d.gq; ++g) {
-      float q[E], x = 0.f;
-      load(static_cast<const uint16_t*>(L.d.q) + b * L.d.qs[0] + t * L.d.qs[1] + (h * L.d.gq + g) * L.d.qs[2], q);
-#pragma unroll
-      for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-      top = fmaxf(top, x);
-    }
-  if (lane == 0) L.scores[(static_cast<int64_t>(b) * L.c.hkv + h) * L.c.max_pages + page] = top;
-}
-
 __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __grid_constant__ CacheSelectLaunch L) {
-  __shared__ ChooseScratch sc;
-  const int b = blockIdx.x / L.c.hkv, h = blockIdx.x % L.c.hkv;
+  __shared__ ChooseMem mem;
+  __shared__ float score[kMaxPages];             // of the CTA's part, from its first page on
+  constexpr int J = D / 32;                      // 16-byte chunks of a row per lane
+  const int rank = static_cast<int>(ptx::cluster_rank()), size = static_cast<int>(ptx::cluster_size());
+  const int problem = blockIdx.x / size, b = problem / L.c.hkv, h = problem % L.c.hkv;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, fr = lane >> 2, fc = (lane & 3) * 8;
   const int len = cache_len(L.c, b, h, L.status), n = (len + L.c.page - 1) >> L.c.log_page;
   const int count = min(n, L.n_select);
   const bool all = n <= L.n_select;
-  const int sink = all ? count : L.sink, recent = all ? 0 : L.recent;
-  const float* score = L.scores + (static_cast<int64_t>(b) * L.c.hkv + h) * L.c.max_pages;
-  const int64_t at = (static_cast<int64_t>(b) * L.c.hkv + h) * L.n_select;
-  auto put = [&](int rank, int page) {
-    L.pages[at + rank] = page;
-    L.sel_table[at + rank] = cache_page(L.c, b, h, page, L.status);
+  const int sink = all ? count : L.sink, recent = all ? 0 : L.recent, want = count - sink - recent;
+  const int lo = sink, hi = n - recent;
+  const ChoosePart part(lo, hi, rank, size);
+
+  if (want > 0) {
+    const int rows = drafted_tokens(L.d, b) * L.d.gq;
+    const uint16_t* q0 = static_cast<const uint16_t*>(L.d.q) + b * L.d.qs[0] + h * L.d.gq * L.d.qs[2] + fc;
+    for (int p0 = part.a + warp * 16; p0 < part.b; p0 += kChooseThreads / 32 * 16) {
+      uint4 a[2][J];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int p = min(p0 + fr + 8 * half, part.b - 1);       // past the part: its last page again, not kept
+        const int64_t id = cache_page(L.c, b, h, p, L.status);
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.c.k_mean) + (id * L.c.hkv + h) * D + fc);
+#pragma unroll
+        for (int j = 0; j < J; ++j) a[half][j] = __ldg(src + 4 * j);
+      }
+      float top[2] = {kNone, kNone};
+#pragma unroll 2
+      for (int r0 = 0; r0 < rows; r0 += 8) {
+        const int r = min(r0 + fr, rows - 1), t = r / L.d.gq, g = r % L.d.gq;   // past the rows: the last one again
+        const uint4* src = reinterpret_cast<const uint4*>(q0 + t * L.d.qs[1] + g * L.d.qs[2]);
+        float c[4] = {};
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const uint4 x = __ldg(src + 4 * j);
+          const uint32_t f0[4] = {a[0][j].x, a[1][j].x, a[0][j].y, a[1][j].y};
+          const uint32_t f1[4] = {a[0][j].z, a[1][j].z, a[0][j].w, a[1][j].w};
+          ptx::mma16816<T>(c, f0, x.x, x.y);
+          ptx::mma16816<T>(c, f1, x.z, x.w);
+        }
+        top[0] = fmaxf(top[0], fmaxf(c[0], c[1]));
+        top[1] = fmaxf(top[1], fmaxf(c[2], c[3]));
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
+        top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
+        const int p = p0 + fr + 8 * half;
+        if ((lane & 3) == 0 && p < part.b) score[p - part.a] = top[half];
+      }
+    }
+    __syncthreads();
+  }
+
+  const int64_t at = static_cast<int64_t>(problem) * L.n_select;
+  auto put = [&](int place, int page) {
+    L.pages[at + place] = page;
+    L.sel_table[at + place] = cache_page(L.c, b, h, page, L.status);
   };
-  for (int i = threadIdx.x; i < sink; i += kChooseThreads) put(i, i);
-  for (int i = threadIdx.x; i < recent; i += kChooseThreads) put(count - recent + i, n - recent + i);
-  for (int i = count + threadIdx.x; i < L.n_select; i += kChooseThreads) L.pages[at + i] = L.sel_table[at + i] = -1;
-  choose_top(sink, n - recent, count - sink - recent, [&](int i) { return order_key(__ldg(score + i)); }, sc,
-             [&](int rank, int i) { put(sink + rank, i); });
-  if (threadIdx.x == 0)
-    L.sel_lens[b * L.c.hkv + h] = count > 0 ? (count - 1) * L.c.page + (len - (n - 1) * L.c.page) : 0;
+  const int first = rank * kChooseThreads + static_cast<int>(threadIdx.x), step = size * kChooseThreads;
+  for (int i = first; i < sink; i += step) put(i, i);
+  for (int i = first; i < recent; i += step) put(count - recent + i, n - recent + i);
+  for (int i = count + first; i < L.n_select; i += step) L.pages[at + i] = L.sel_table[at + i] = -1;
+  choose_top<kChooseThreads>(lo, hi, want, [&](int i) { return order_key(score[i - part.a]); }, mem,
+             [&](int place, int i) { put(sink + place, i); });
+  if (first == 0) L.sel_lens[problem] = count > 0 ? (count - 1) * L.c.page + (len - (n - 1) * L.c.page) : 0;
+  if (size > 1) ptx::cluster_sync();
 }
 
 template <class T, int D>
 cudaError_t launch_d(const CacheSelectLaunch& L, cudaStream_t stream) {
-  constexpr int W = kScoreThreads / 32;
-  cache_score_kernel<T, D><<<dim3((L.c.max_pages + W - 1) / W, L.c.hkv, L.c.batch), kScoreThreads, 0, stream>>>(L);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  cache_select_kernel<<<L.c.batch * L.c.hkv, kChooseThreads, 0, stream>>>(L);
-  return cudaGetLastError();
+  const int problems = L.c.batch * L.c.hkv, cluster = choose_cluster(problems, L.c.max_pages, 64, sm_count());
+  return launch_clusters(cache_select_kernel<T, D>, L, static_cast<unsigned>(problems * cluster), kChooseThreads, cluster, stream);
 }
 
 }  // namespace

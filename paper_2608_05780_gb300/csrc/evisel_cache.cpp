@@ -443,8 +443,6 @@ int evisel_cache_select(const evisel_cache* cache, const evisel_draft* draft, in
     if (cache->max_pages > 0 && !cache->k_mean) return fail(EVISEL_EINVAL, "the cache has no k_mean");
     rc = ws_acquire(ws_inout);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
-    const size_t scores = static_cast<size_t>(cache->batch) * cache->hkv * cache->max_pages;
-    if (rc == EVISEL_OK) rc = grow(*ws_inout, scores * sizeof(float), stream);
     if (rc != EVISEL_OK) return rc;
     CacheSelectLaunch L{};
     L.c = view_of(cache);
@@ -452,7 +450,6 @@ int evisel_cache_select(const evisel_cache* cache, const evisel_draft* draft, in
     L.pages = pages;
     L.sel_table = sel_table;
     L.sel_lens = sel_lens;
-    L.scores = static_cast<float*>(ws_cache(*ws_inout).buf);
     L.n_select = n_select;
     L.sink = sink;
     L.recent = recent;
