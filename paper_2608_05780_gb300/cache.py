@@ -5,25 +5,27 @@ names and, like the probe's, take an optional workspace and return it last.
 Lengths, tables, tree bits and counts stay on the device: no call waits for it,
 and what they hold is checked by the kernels (``evisel_status(ws)`` answers
 EVISEL_EBOUNDS, -7, where a length, page id or index was out of range).
+
+A decoding step's calls take a few microseconds on the device, so that the
+checks here are plain comparisons, their messages formed only when one fails.
 """
 from __future__ import annotations
 
 import ctypes
 import struct
 
-from ._binding import Workspace, _check, _stream_handle, load
+from ._binding import Workspace, _check, load
 
 _CACHE = struct.Struct("@8i10q5P")
 _DRAFT = struct.Struct("@iifi11q5P")
-_declared = False
-_DTYPES = {}
+_NONE = (0, 0, 0, 0)
+_calls = None           # the library's functions, torch's names and lookups: filled by the first call
 
 
-def _lib():
-    global _declared
-    lib = load()
-    if not _declared:
+class _Calls:
+    def __init__(self):
         import torch
+        lib = load()
         vp, i32, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
         ws = ctypes.POINTER(vp)
         for name, args in (("attention", [vp, vp, vp, vp, vp, ws]),
@@ -33,14 +35,24 @@ def _lib():
                            ("select", [vp, vp, i32, i32, i32, vp, vp, vp, vp, ws])):
             f = getattr(lib, "evisel_cache_" + name)
             f.argtypes, f.restype = args, i32
-        _DTYPES.update({torch.bfloat16: 0, torch.float16: 1})
-        _declared = True
-    return lib
+            setattr(self, name, f)
+        self.empty, self.i32, self.f32 = torch.empty, torch.int32, torch.float32
+        self.dtypes = {torch.bfloat16: 0, torch.float16: 1}
+        self.masks = (torch.bool, torch.uint8)
+        self.current_device = torch.cuda.current_device
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _get():
+    global _calls
+    if _calls is None:
+        _calls = _Calls()
+    return _calls
+
+
+def _refuse(what):
+    raise ValueError(what)
 
 
 class Cache:
@@ -51,37 +63,43 @@ class Cache:
     The handle holds the tensors; assign ``lens`` or ``table`` to replace one.
     """
 
-    __slots__ = ("k", "v", "k_mean", "device", "shape", "_table", "_lens", "_packed")
+    __slots__ = ("k", "v", "k_mean", "device", "dtype", "batch", "hkv", "page", "head_dim", "max_tokens", "_pool",
+                 "_table", "_lens", "_packed")
 
     def __init__(self, k, v, table, lens, k_mean=None):
-        import torch
-        _lib()
-        _need(k.dim() == 4 and k.shape == v.shape, "k and v must be pages [P, hkv, page, d] of one shape")
-        _need(k.is_cuda and k.dtype in _DTYPES and v.dtype == k.dtype and v.device == k.device,
-              "k and v must be CUDA tensors of bf16 or fp16 on one device")
-        _need(k.stride(3) == 1 and v.stride(3) == 1, "d must be contiguous in k and v")
-        if k_mean is not None:
-            _need(k_mean.shape == (k.shape[0], k.shape[1], k.shape[3]) and k_mean.dtype == k.dtype
-                  and k_mean.device == k.device and k_mean.is_contiguous(),
-                  "k_mean must be contiguous [P, hkv, d], of k's type and device")
-        self.k, self.v, self.k_mean, self.device = k, v, k_mean, k.device
-        self.shape = tuple(k.shape)
-        self._set(table, lens, torch.int32)
+        c = _get()
+        if not (k.dim() == 4 and k.shape == v.shape):
+            _refuse("k and v must be pages [P, hkv, page, d] of one shape")
+        if not (k.is_cuda and k.dtype in c.dtypes and v.dtype == k.dtype and v.device == k.device):
+            _refuse("k and v must be CUDA tensors of bf16 or fp16 on one device")
+        ks, vs = k.stride(), v.stride()
+        if not (ks[3] == 1 and vs[3] == 1):
+            _refuse("d must be contiguous in k and v")
+        pages, hkv, page, d = k.shape
+        if k_mean is not None and not (k_mean.shape == (pages, hkv, d) and k_mean.dtype == k.dtype
+                                       and k_mean.device == k.device and k_mean.is_contiguous()):
+            _refuse("k_mean must be contiguous [P, hkv, d], of k's type and device")
+        self.k, self.v, self.k_mean, self.device, self.dtype = k, v, k_mean, k.device, k.dtype
+        self.hkv, self.page, self.head_dim = hkv, page, d
+        self._pool = (pages, c.dtypes[k.dtype], ks[:3], vs[:3], k.data_ptr(), v.data_ptr(),
+                      0 if k_mean is None else k_mean.data_ptr())
+        self._set(table, lens)
 
-    def _set(self, table, lens, i32):
-        n_pages, hkv, page, d = self.shape
-        for x, dim, what in ((table, 2, "table"), (lens, 1, "lens")):
-            _need(x.dtype == i32 and x.device == self.device and x.dim() in (dim, dim + 1)
-                  and x.shape[0] == lens.shape[0] and (x.dim() == dim or x.shape[1] == hkv),
-                  f"{what} must be int32 [B{', n' * (dim - 1)}] or [B, hkv{', n' * (dim - 1)}] on the cache's device")
-        _need(table.stride(-1) == 1 or table.shape[-1] <= 1, "table rows must be contiguous")
-        k, v, km = self.k, self.v, self.k_mean
-        self._table, self._lens = table, lens
-        self._packed = _CACHE.pack(
-            lens.shape[0], hkv, d, page, n_pages, table.shape[-1], _DTYPES[k.dtype], 0, *k.stride()[:3],
-            *v.stride()[:3], table.stride(0), table.stride(1) if table.dim() == 3 else 0, lens.stride(0),
-            lens.stride(1) if lens.dim() == 2 else 0, k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(),
-            0 if km is None else km.data_ptr())
+    def _set(self, table, lens):
+        i32 = _calls.i32
+        ts, ls, batch, hkv = table.stride(), lens.stride(), lens.shape[0] if lens.dim() else -1, self.hkv
+        if not (lens.dtype == i32 and lens.device == self.device and (lens.shape == (batch,) or lens.shape == (batch, hkv))):
+            _refuse("lens must be int32 [B] or [B, hkv] on the cache's device")
+        n = table.shape[-1] if table.dim() else -1
+        if not (table.dtype == i32 and table.device == self.device and (table.shape == (batch, n) or table.shape == (batch, hkv, n))):
+            _refuse("table must be int32 [B, n] or [B, hkv, n] on the cache's device")
+        if not (ts[-1] == 1 or n <= 1):
+            _refuse("table rows must be contiguous")
+        pages, dtype, ks, vs, kp, vp, mp = self._pool
+        self._table, self._lens, self.batch, self.max_tokens = table, lens, batch, n * self.page
+        self._packed = _CACHE.pack(batch, hkv, self.head_dim, self.page, pages, n, dtype, 0, *ks, *vs,
+                                   ts[0], ts[1] if len(ts) == 3 else 0, ls[0], ls[1] if len(ls) == 2 else 0,
+                                   kp, vp, table.data_ptr(), lens.data_ptr(), mp)
 
     @property
     def table(self):
@@ -89,7 +107,7 @@ class Cache:
 
     @table.setter
     def table(self, table):
-        self._set(table, self._lens, self._lens.dtype)
+        self._set(table, self._lens)
 
     @property
     def lens(self):
@@ -97,84 +115,68 @@ class Cache:
 
     @lens.setter
     def lens(self, lens):
-        self._set(self._table, lens, self._table.dtype)
-
-    @property
-    def batch(self):
-        return self._lens.shape[0]
-
-    @property
-    def hkv(self):
-        return self.shape[1]
-
-    @property
-    def max_tokens(self):
-        """Tokens that a table row can hold."""
-        return self._table.shape[-1] * self.shape[2]
+        self._set(self._table, lens)
 
     def view(self, table, lens):
         """The same pages under another table and lengths."""
         c = object.__new__(Cache)
-        c.k, c.v, c.k_mean, c.device, c.shape = self.k, self.v, self.k_mean, self.device, self.shape
-        c._set(table, lens, self._lens.dtype)
+        c.k, c.v, c.k_mean, c.device, c.dtype = self.k, self.v, self.k_mean, self.device, self.dtype
+        c.hkv, c.page, c.head_dim, c._pool = self.hkv, self.page, self.head_dim, self._pool
+        c._set(table, lens)
         return c
 
 
-def _check_new(cache, x, tokens, what):
-    _need(x.dim() == 4 and x.shape[0] == cache.batch and x.shape[2:] == (cache.shape[1], cache.shape[3])
-          and (tokens is None or x.shape[1] == tokens), f"{what} must be [B, T, hkv, d]")
-    _need(x.dtype == cache.k.dtype and x.device == cache.device and x.stride(3) == 1,
-          f"{what} must have the cache's type and device, d contiguous")
+def _new(cache, x, shape, what):
+    """Strides and address of new keys or values."""
+    s = x.stride()
+    if not (x.shape == shape and x.dtype == cache.dtype and x.device == cache.device and s[3] == 1):
+        _refuse(f"{what} must be [B, T, hkv, d] = {list(shape)} of the cache's type and device, d contiguous")
+    return s, x.data_ptr()
 
 
-def _i32(cache, x, shape, what):
-    import torch
-    _need(x.dtype == torch.int32 and x.shape == shape and x.device == cache.device and x.is_contiguous(),
-          f"{what} must be contiguous int32 {list(shape)} on the cache's device")
-    return x.data_ptr()
-
-
-def _f32(cache, x, shape, what):
-    import torch
-    _need(x.dtype == torch.float32 and x.shape == shape and x.device == cache.device and x.is_contiguous(),
-          f"{what} must be contiguous float32 {list(shape)} on the cache's device")
+def _plain(cache, x, dtype, shape, what):
+    """Address of a contiguous tensor of this type and shape."""
+    if not (x.dtype == dtype and x.shape == shape and x.device == cache.device and x.is_contiguous()):
+        _refuse(f"{what} must be contiguous {dtype} {list(shape)} on the cache's device")
     return x.data_ptr()
 
 
 def _draft(cache, q, k_new, v_new, tree, drafted, scale):
-    import torch
-    _need(q.dim() == 4 and q.shape[0] == cache.batch and q.shape[3] == cache.shape[3] and q.dtype == cache.k.dtype
-          and q.device == cache.device and q.stride(3) == 1,
-          "q must be [B, T, hq, d] of the cache's type and device, d contiguous")
-    tokens, hq = q.shape[1], q.shape[2]
-    qs = q.stride()
-    ks = vs = (0, 0, 0)
+    qs, sh = q.stride(), q.shape
+    if not (len(sh) == 4 and sh[0] == cache.batch and sh[3] == cache.head_dim and q.dtype == cache.dtype
+            and q.device == cache.device and qs[3] == 1):
+        _refuse("q must be [B, T, hq, d] of the cache's type and device, d contiguous")
+    batch, tokens, hq, d = sh
+    ks = vs = _NONE
     kp = vp = tp = dp = t0 = t1 = 0
-    _need((k_new is None) == (v_new is None), "k_new and v_new go together")
-    if k_new is not None:
-        _check_new(cache, k_new, tokens, "k_new")
-        _check_new(cache, v_new, tokens, "v_new")
-        ks, vs, kp, vp = k_new.stride(), v_new.stride(), k_new.data_ptr(), v_new.data_ptr()
+    if k_new is not None or v_new is not None:
+        if k_new is None or v_new is None:
+            _refuse("k_new and v_new go together")
+        shape = (batch, tokens, cache.hkv, d)
+        ks, kp = _new(cache, k_new, shape, "k_new")
+        vs, vp = _new(cache, v_new, shape, "v_new")
     if tree is not None:
-        words = -(-tokens // 32)
-        _need(tree.dtype == torch.int32 and tree.device == cache.device and tree.dim() in (2, 3)
-              and tree.shape[-2:] == (tokens, words) and (tree.dim() == 2 or tree.shape[0] == cache.batch)
-              and (tree.stride(-1) == 1 or words <= 1),
-              f"tree must be int32 bit words [B, {tokens}, {words}] or [{tokens}, {words}] on the cache's device")
-        tp, t1, t0 = tree.data_ptr(), tree.stride(-2), tree.stride(0) if tree.dim() == 3 else 0
+        words, ts = (tokens + 31) // 32, tree.stride()
+        if tree.shape == (batch, tokens, words):
+            t0, t1 = ts[0], ts[1]
+        elif tree.shape == (tokens, words):
+            t1 = ts[0]
+        else:
+            _refuse(f"tree must be int32 bit words [B, {tokens}, {words}] or [{tokens}, {words}]")
+        if not (tree.dtype == _calls.i32 and tree.device == cache.device and (ts[-1] == 1 or words <= 1)):
+            _refuse("tree must be int32 with contiguous rows on the cache's device")
+        tp = tree.data_ptr()
     if drafted is not None:
-        dp = _i32(cache, drafted, (cache.batch,), "drafted")
+        dp = _plain(cache, drafted, _calls.i32, (batch,), "drafted")
     return _DRAFT.pack(tokens, hq, scale, 0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], t0, t1,
                        q.data_ptr(), kp, vp, tp, dp)
 
 
-def _call(cache, name, ws, stream, *args):
-    import torch
-    lib = _lib()
-    _need(cache.device.index == torch.cuda.current_device(), "the cache's device must be the current one")
-    ws = Workspace() if ws is None else ws
-    _check(getattr(lib, name)(*args, _stream_handle(stream), ctypes.byref(ws.ptr)))
-    return ws
+def _stream(cache, stream):
+    index = cache.device.index
+    if index != _calls.current_device():
+        _refuse("the cache's device must be the current one")
+    return _calls.raw_stream(index) if stream is None else stream.cuda_stream
 
 
 def evisel_cache_attention(cache, q, k_new=None, v_new=None, tree=None, drafted=None, ws=None, o=None, lse=None,
@@ -185,45 +187,46 @@ def evisel_cache_attention(cache, q, k_new=None, v_new=None, tree=None, drafted=
     tokens that a sequence has drafted, T each by default. The strides of q, k_new and v_new are free but for d's.
 
     Returns (o [B, T, hq, d], lse [hq, B, T] fp32, ws)."""
-    import torch
     draft = _draft(cache, q, k_new, v_new, tree, drafted, softmax_scale)
     batch, tokens, hq, d = q.shape
-    if o is None:
-        o = torch.empty((batch, tokens, hq, d), dtype=q.dtype, device=q.device)
-    else:
-        _need(o.shape == q.shape and o.dtype == q.dtype and o.device == q.device and o.is_contiguous(),
-              "o must be contiguous [B, T, hq, d] of q's type")
-    if lse is None:
-        lse = torch.empty((hq, batch, tokens), dtype=torch.float32, device=q.device)
-    else:
-        _f32(cache, lse, (hq, batch, tokens), "lse")
-    ws = _call(cache, "evisel_cache_attention", ws, stream, cache._packed, draft, o.data_ptr(), lse.data_ptr())
-    return o, lse, ws
+    o_p = (_calls.empty((batch, tokens, hq, d), dtype=cache.dtype, device=cache.device) if o is None else o)
+    lse_p = (_calls.empty((hq, batch, tokens), dtype=_calls.f32, device=cache.device) if lse is None else lse)
+    if o is not None:
+        _plain(cache, o, cache.dtype, q.shape, "o")
+    if lse is not None:
+        _plain(cache, lse, _calls.f32, (hq, batch, tokens), "lse")
+    ws = Workspace() if ws is None else ws
+    rc = _calls.attention(cache._packed, draft, o_p.data_ptr(), lse_p.data_ptr(), _stream(cache, stream), ctypes.byref(ws.ptr))
+    if rc:
+        _check(rc)
+    return o_p, lse_p, ws
 
 
 def evisel_cache_evidence(cache, q, lse, acc=None, use=None, drafted=None, accumulate=False, ws=None,
                           softmax_scale=0.0, stream=None):
     """Attention weight of the queries q [B, T, hq, d] per cached token, summed over the rows and the heads of each
     KV group, from the row normalisers ``lse`` [hq, B, T] of evisel_cache_attention. ``use`` bool [B, T]: the rows
-    that count. ``acc`` fp32 [B, hkv, n] (cache.max_tokens by default) is overwritten, or with ``accumulate`` added
-    to, up to each sequence's length.
+    that count. ``acc`` fp32 [B, hkv, n] (zeros up to cache.max_tokens by default) is overwritten, or with
+    ``accumulate`` added to, up to each sequence's length.
 
     Returns (acc, ws)."""
-    import torch
     draft = _draft(cache, q, None, None, None, drafted, softmax_scale)
     batch, tokens, hq, _ = q.shape
-    lse_p = _f32(cache, lse, (hq, batch, tokens), "lse")
+    lse_p = _plain(cache, lse, _calls.f32, (hq, batch, tokens), "lse")
     if acc is None:
-        acc = torch.zeros((batch, cache.hkv, cache.max_tokens), dtype=torch.float32, device=q.device)
-    _need(acc.dim() == 3, "acc must be [B, hkv, n]")
-    acc_p = _f32(cache, acc, (batch, cache.hkv, acc.shape[2]), "acc")
+        acc = _calls.empty((batch, cache.hkv, cache.max_tokens), dtype=_calls.f32, device=cache.device).zero_()
+    n = acc.shape[-1] if acc.dim() else 0
+    acc_p = _plain(cache, acc, _calls.f32, (batch, cache.hkv, n), "acc")
     use_p = 0
     if use is not None:
-        _need(use.dtype in (torch.bool, torch.uint8) and use.shape == (batch, tokens) and use.device == cache.device
-              and use.is_contiguous(), "use must be contiguous bool [B, T] on the cache's device")
-        use_p = use.data_ptr()
-    ws = _call(cache, "evisel_cache_evidence", ws, stream, cache._packed, draft, lse_p, use_p, acc_p, acc.shape[2],
-               int(bool(accumulate)))
+        if use.dtype not in _calls.masks:
+            _refuse("use must be bool or uint8")
+        use_p = _plain(cache, use, use.dtype, (batch, tokens), "use")
+    ws = Workspace() if ws is None else ws
+    rc = _calls.evidence(cache._packed, draft, lse_p, use_p, acc_p, n, 1 if accumulate else 0, _stream(cache, stream),
+                         ctypes.byref(ws.ptr))
+    if rc:
+        _check(rc)
     return acc, ws
 
 
@@ -233,19 +236,29 @@ def evisel_cache_evict(cache, acc, out, budget, sink=0, recent=0, kept=None, acc
     out.lens, and out.k_mean where there is one, are written.
 
     Returns (kept int32 [B, hkv, budget] with -1 past the tokens kept, acc_out [B, hkv, out.max_tokens], ws)."""
-    import torch
-    _need(acc.dim() == 3, "acc must be [B, hkv, n]")
-    acc_p = _f32(cache, acc, (cache.batch, cache.hkv, acc.shape[2]), "acc")
-    _need(out.device == cache.device, "out must be on the cache's device")
-    _need(out.batch == cache.batch and out.hkv == cache.hkv, "out must have the cache's batch and heads")
+    batch, hkv, budget = cache.batch, cache.hkv, int(budget)
+    n = acc.shape[-1] if acc.dim() else 0
+    acc_p = _plain(cache, acc, _calls.f32, (batch, hkv, n), "acc")
+    if not (out.device == cache.device and out.batch == batch and out.hkv == hkv):
+        _refuse("out must have the cache's batch, heads and device")
+    shape = (batch, hkv, budget if budget > 0 else 0)
     if kept is None:
-        kept = torch.empty((cache.batch, cache.hkv, max(0, int(budget))), dtype=torch.int32, device=cache.device)
+        kept = _calls.empty(shape, dtype=_calls.i32, device=cache.device)
+        kept_p = kept.data_ptr()
+    else:
+        kept_p = _plain(cache, kept, _calls.i32, shape, "kept")
     if acc_out is None:
-        acc_out = torch.empty((cache.batch, cache.hkv, out.max_tokens), dtype=torch.float32, device=cache.device)
-    _need(acc_out.dim() == 3, "acc_out must be [B, hkv, n]")
-    ws = _call(cache, "evisel_cache_evict", ws, stream, cache._packed, acc_p, acc.shape[2], out._packed, int(budget),
-               int(sink), int(recent), _i32(cache, kept, (cache.batch, cache.hkv, max(0, int(budget))), "kept"),
-               _f32(cache, acc_out, (cache.batch, cache.hkv, acc_out.shape[2]), "acc_out"), acc_out.shape[2])
+        m = out.max_tokens
+        acc_out = _calls.empty((batch, hkv, m), dtype=_calls.f32, device=cache.device)
+        acc_out_p = acc_out.data_ptr()
+    else:
+        m = acc_out.shape[-1] if acc_out.dim() else 0
+        acc_out_p = _plain(cache, acc_out, _calls.f32, (batch, hkv, m), "acc_out")
+    ws = Workspace() if ws is None else ws
+    rc = _calls.evict(cache._packed, acc_p, n, out._packed, budget, int(sink), int(recent), kept_p, acc_out_p, m,
+                      _stream(cache, stream), ctypes.byref(ws.ptr))
+    if rc:
+        _check(rc)
     return kept, acc_out, ws
 
 
@@ -255,19 +268,23 @@ def evisel_cache_append(cache, k_new, v_new, src=None, counts=None, lens_out=Non
     cache.lens is not written: the new lengths are returned, to be assigned to it.
 
     Returns (lens int32 [B], ws)."""
-    import torch
-    _check_new(cache, k_new, None, "k_new")
-    tokens = k_new.shape[1]
-    _check_new(cache, v_new, tokens, "v_new")
+    batch = cache.batch
+    shape = (batch, k_new.shape[1] if k_new.dim() > 1 else -1, cache.hkv, cache.head_dim)
+    ks, kp = _new(cache, k_new, shape, "k_new")
+    vs, vp = _new(cache, v_new, shape, "v_new")
     if lens_out is None:
-        lens_out = torch.empty((cache.batch,), dtype=torch.int32, device=cache.device)
-    ks, vs = k_new.stride(), v_new.stride()
-    draft = _DRAFT.pack(tokens, cache.hkv, 0.0, 0, 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0,
-                        0, k_new.data_ptr(), v_new.data_ptr(), 0, 0)
-    ws = _call(cache, "evisel_cache_append", ws, stream, cache._packed, draft,
-               0 if src is None else _i32(cache, src, (cache.batch, tokens), "src"),
-               0 if counts is None else _i32(cache, counts, (cache.batch,), "counts"),
-               _i32(cache, lens_out, (cache.batch,), "lens_out"))
+        lens_out = _calls.empty((batch,), dtype=_calls.i32, device=cache.device)
+        out_p = lens_out.data_ptr()
+    else:
+        out_p = _plain(cache, lens_out, _calls.i32, (batch,), "lens_out")
+    src_p = 0 if src is None else _plain(cache, src, _calls.i32, shape[:2], "src")
+    counts_p = 0 if counts is None else _plain(cache, counts, _calls.i32, (batch,), "counts")
+    draft = _DRAFT.pack(shape[1], cache.hkv, 0.0, 0, 0, 0, 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], 0, 0,
+                        0, kp, vp, 0, 0)
+    ws = Workspace() if ws is None else ws
+    rc = _calls.append(cache._packed, draft, src_p, counts_p, out_p, _stream(cache, stream), ctypes.byref(ws.ptr))
+    if rc:
+        _check(rc)
     return lens_out, ws
 
 
@@ -277,12 +294,14 @@ def evisel_cache_select(cache, q, n_select, sink=0, recent=1, drafted=None, ws=N
 
     Returns (view, pages, ws): a Cache of the chosen pages for evisel_cache_attention, and their logical numbers
     int32 [B, hkv, n_select], ascending, -1 past them."""
-    import torch
     draft = _draft(cache, q, None, None, None, drafted, 0.0)
-    batch, hkv = cache.batch, cache.hkv
-    out = torch.empty((2, batch, hkv, max(0, int(n_select))), dtype=torch.int32, device=cache.device)
-    lens = torch.empty((batch, hkv), dtype=torch.int32, device=cache.device)
-    pages, table = out[0], out[1]
-    ws = _call(cache, "evisel_cache_select", ws, stream, cache._packed, draft, int(n_select), int(sink), int(recent),
-               pages.data_ptr(), table.data_ptr(), lens.data_ptr())
+    n, empty, i32, dev = int(n_select), _calls.empty, _calls.i32, cache.device
+    shape = (cache.batch, cache.hkv, n if n > 0 else 0)
+    pages, table = empty(shape, dtype=i32, device=dev), empty(shape, dtype=i32, device=dev)
+    lens = empty(shape[:2], dtype=i32, device=dev)
+    ws = Workspace() if ws is None else ws
+    rc = _calls.select(cache._packed, draft, n, int(sink), int(recent), pages.data_ptr(), table.data_ptr(),
+                       lens.data_ptr(), _stream(cache, stream), ctypes.byref(ws.ptr))
+    if rc:
+        _check(rc)
     return cache.view(table, lens), pages, ws
