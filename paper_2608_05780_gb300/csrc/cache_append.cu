@@ -38,6 +38,8 @@ struct NewTokens {
 template <class T, int D>
 __global__ void __launch_bounds__(kPageThreads) cache_append_kernel(const __grid_constant__ CacheAppendLaunch L) {
   const int h = blockIdx.y, b = blockIdx.z;
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   const NewTokens src(L, b, h);
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) L.lens_out[b] = src.end();
   fill_page<T, D>(L.c, const_cast<void*>(L.c.k), const_cast<void*>(L.c.v), const_cast<void*>(L.c.k_mean), b, h,
@@ -47,8 +49,7 @@ __global__ void __launch_bounds__(kPageThreads) cache_append_kernel(const __grid
 template <class T, int D>
 cudaError_t launch_d(const CacheAppendLaunch& L, cudaStream_t stream) {
   const int pages = (L.d.tokens + L.c.page - 1) / L.c.page + 1;  // that T tokens can touch
-  cache_append_kernel<T, D><<<dim3(pages, L.c.hkv, L.c.batch), kPageThreads, 0, stream>>>(L);
-  return cudaGetLastError();
+  return launch_after(cache_append_kernel<T, D>, dim3(pages, L.c.hkv, L.c.batch), kPageThreads, 0, stream, L);
 }
 
 }  // namespace

@@ -18,10 +18,10 @@ constexpr int kKeyWarps = 4;                     // warps over a unit's keys, 16
 constexpr int kStages = 3;
 
 // ---------------------------------------------------------------- few rows
-// Up to 16 * MG rows of a (sequence, KV head) at a time. Every warp takes 16 of
-// a unit's 64 keys against 16 rows with a running max, row sum and O of its own
-// (mma.sync, fp32 accumulators in registers); the four key warps are joined when
-// the CTA leaves the problem. A producer warp streams the pages by TMA.
+// Up to 16 * MG rows of a (sequence, KV head) at a time. Each of four warps takes
+// 16 of a unit's 64 keys against all rows with a running max, row sum and O of
+// its own (mma.sync, fp32 accumulators in registers, two CTAs per SM); they are
+// joined when the CTA leaves the problem. A producer warp streams the pages by TMA.
 template <int D, int MG>
 struct FewCfg {
   static constexpr int KB = D / 64;                          // 128-byte column blocks
@@ -29,17 +29,20 @@ struct FewCfg {
   static constexpr int TILE = KB * BLOCK;
   static constexpr int OFF_K = 0;
   static constexpr int OFF_V = kStages * TILE;
-  static constexpr int OFF_JOIN = 2 * kStages * TILE;        // per row group: 16 rows x D fp32
-  static constexpr int OFF_ML = OFF_JOIN + MG * 16 * D * 4;  // per row group, key warp: 16 x (max, sum)
+  // MG = 2: a segment's 32 queries, swizzled like K; then, at its end, 16 rows x D fp32.
+  static constexpr int OFF_Q = 2 * kStages * TILE, OFF_JOIN = OFF_Q;
+  static constexpr int OFF_ML = OFF_JOIN + 16 * D * 4;       // per key warp: 16 MG x (max, sum)
+  static_assert(16 * MG * D * 2 <= 16 * D * 4, "the queries fit where the join goes");
   static constexpr int OFF_BAR = OFF_ML + MG * kKeyWarps * 16 * 8;
   static constexpr int B_FULL = 0, B_EMPTY = kStages;
   static constexpr int OFF_MISC = OFF_BAR + 2 * kStages * 8; // abort flag, split scratch
   static constexpr int SMEM = OFF_MISC + 8 + 40 * 4 + 1024;
-  static constexpr int THREADS = 32 * (MG * kKeyWarps + 1);
+  static constexpr int THREADS = 32 * (kKeyWarps + 1);
+  static_assert(2 * (SMEM + 1024) <= 233472, "two CTAs per SM");
 };
 
 template <class T, int D, int MG>
-__global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) cache_attn_few_kernel(const __grid_constant__ CacheAttnLaunch L) {
+__global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel(const __grid_constant__ CacheAttnLaunch L) {
   using C = FewCfg<D, MG>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -52,11 +55,13 @@ __global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) ca
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       ptx::mbar_init(bar(C::B_FULL + i), 1);
-      ptx::mbar_init(bar(C::B_EMPTY + i), MG * kKeyWarps);
+      ptx::mbar_init(bar(C::B_EMPTY + i), kKeyWarps);
     }
     *abort_flag = 0;
     ptx::fence_mbar_init();
   }
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   const UnitCount uc(L.c, kKeys, L.row_tiles, L.status);
   int ctas = 1, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
@@ -72,7 +77,7 @@ __global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) ca
   uint32_t n = 0;                                // units so far
   bool ok = true;
 
-  if (warp == MG * kKeyWarps) {
+  if (warp == kKeyWarps) {
     // Producer: lane i sends one box of K or V.
     const int subs = kKeys / L.box_rows, n_loads = subs * C::KB * 2;
     const int sub = lane / (2 * C::KB), kb = (lane >> 1) % C::KB, is_v = lane & 1;
@@ -104,36 +109,55 @@ __global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) ca
     return;
   }
 
-  const int mg = warp / kKeyWarps, kw = warp % kKeyWarps;
+  const int kw = warp;
   const int r8 = lane & 7, mi = lane >> 3;
   // ldmatrix addresses within a tile: this lane's row, and its 16-byte chunk at even k-steps (^ swizzle).
   const int k_row = kw * 16 + (mi >> 1) * 8 + r8, k_chunk = mi & 1;
   const int v_row = kw * 16 + (mi & 1) * 8 + r8, v_chunk = mi >> 1;
+  const int q_row = (mi & 1) * 8 + r8, q_chunk = mi >> 1;
   const int fr = lane >> 2, fc = (lane & 3) * 2;  // fragment row (and row + 8) and first column
-  float4* join = reinterpret_cast<float4*>(smem + C::OFF_JOIN) + mg * 16 * D / 4;
-  float2* ml = reinterpret_cast<float2*>(smem + C::OFF_ML) + mg * kKeyWarps * 16;
+  constexpr int QBLOCK = 16 * MG * 128;
+  float4* join = reinterpret_cast<float4*>(smem + C::OFF_JOIN);
+  float2* ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
 
   while (walk.next(L.c, L.row_tiles, uc, s, L.status)) {
-    // Q fragments of this warp's 16 rows (rows past the last one: zeros).
-    uint32_t qf[D / 16][4];
-    const int row0 = s.rt * L.tile_rows + mg * 16 + fr;
+    // The rows' queries (zeros past the last row): 16 rows as fragments in
+    // registers, 32 in shared memory, where their fragments are read per unit.
+    [[maybe_unused]] uint32_t qf[MG == 1 ? D / 16 : 1][4];
+    const uint16_t* qb = static_cast<const uint16_t*>(L.d.q) + s.b * L.d.qs[0] + s.h * L.d.gq * L.d.qs[2];
+    if constexpr (MG == 1) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int r = row0 + half * 8;
-      const bool in = r < L.rows;
-      const int t = in ? r / L.d.gq : 0, g = in ? r % L.d.gq : 0;
-      const uint32_t* q = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(L.d.q) + s.b * L.d.qs[0] +
-                                                            t * L.d.qs[1] + (s.h * L.d.gq + g) * L.d.qs[2] + fc);
+      for (int half = 0; half < 2; ++half) {
+        const int r = s.rt * L.tile_rows + fr + half * 8;
+        const bool in = r < L.rows;
+        const int t = in ? r / L.d.gq : 0, g = in ? r % L.d.gq : 0;
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(qb + t * L.d.qs[1] + g * L.d.qs[2] + fc);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        qf[ks][half] = in ? __ldg(q + ks * 8) : 0u;
-        qf[ks][half + 2] = in ? __ldg(q + ks * 8 + 4) : 0u;
+        for (int ks = 0; ks < D / 16; ++ks) {
+          qf[ks][half] = in ? __ldg(q + ks * 8) : 0u;
+          qf[ks][half + 2] = in ? __ldg(q + ks * 8 + 4) : 0u;
+        }
       }
+    } else {
+      ptx::bar_sync(1, 32 * kKeyWarps);          // the last segment's queries have been read
+      for (int i = threadIdx.x; i < 16 * MG * D / 8; i += 32 * kKeyWarps) {
+        const int row = i / (D / 8), ch = i % (D / 8), r = s.rt * L.tile_rows + row;
+        const bool in = r < L.rows;
+        const int t = in ? r / L.d.gq : 0, g = in ? r % L.d.gq : 0;
+        const uint4 x = in ? __ldg(reinterpret_cast<const uint4*>(qb + t * L.d.qs[1] + g * L.d.qs[2]) + ch) : make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(smem + C::OFF_Q + (ch / 8) * QBLOCK + row * 128 + ((ch & 7) ^ (row & 7)) * 16) = x;
+      }
+      ptx::bar_sync(1, 32 * kKeyWarps);
     }
-    float o[D / 8][4];
+    float o[MG][D / 8][4];
+    float m[MG][2], l[MG][2];
 #pragma unroll
-    for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int g = 0; g < MG; ++g) {
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) o[g][j][0] = o[g][j][1] = o[g][j][2] = o[g][j][3] = 0.f;
+      m[g][0] = m[g][1] = -INFINITY;
+      l[g][0] = l[g][1] = 0.f;
+    }
 
     for (int t = s.t0; t < s.t1; ++t, ++n) {
       const int st = n % kStages;
@@ -141,24 +165,36 @@ __global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) ca
       const int left = s.len - t * kKeys - kw * 16;   // keys of this warp that exist
       if (ok && left > 0) {
         const uint32_t kt = sbase + C::OFF_K + st * C::TILE, vt = sbase + C::OFF_V + st * C::TILE;
-        float sc[2][4] = {};
+        float sc[MG][2][4] = {};
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
           uint32_t kf[4];
           const int ch = (ks % 4) * 2 + k_chunk;
           ptx::ldmatrix4(kf, kt + (ks / 4) * C::BLOCK + k_row * 128 + ((ch ^ r8) << 4));
-          ptx::mma16816<T>(sc[0], qf[ks], kf[0], kf[1]);
-          ptx::mma16816<T>(sc[1], qf[ks], kf[2], kf[3]);
+#pragma unroll
+          for (int g = 0; g < MG; ++g) {
+            uint32_t qr[4];
+            if constexpr (MG == 1) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) qr[e] = qf[ks][e];
+            } else {
+              const int qch = (ks % 4) * 2 + q_chunk;
+              ptx::ldmatrix4(qr, sbase + C::OFF_Q + (ks / 4) * QBLOCK + (g * 16 + q_row) * 128 + ((qch ^ r8) << 4));
+            }
+            ptx::mma16816<T>(sc[g][0], qr, kf[0], kf[1]);
+            ptx::mma16816<T>(sc[g][1], qr, kf[2], kf[3]);
+          }
         }
         if (left < 16) {
           // Past the sequence's end: the keys are masked, and their values, which
-          // may be anything, are zeroed (each warp reads its own 16 rows only;
-          // warps of other row groups write the same zeros).
+          // may be anything, are zeroed (each warp reads its own 16 rows only).
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int g = 0; g < MG; ++g)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (j * 8 + fc + (e & 1) >= left) sc[j][e] = -INFINITY;
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (j * 8 + fc + (e & 1) >= left) sc[g][j][e] = -INFINITY;
           for (int i = lane; i < (16 - left) * C::KB * 8; i += 32) {
             const int row = kw * 16 + left + i / (C::KB * 8), x = i % (C::KB * 8);
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vt + (x / 8) * C::BLOCK + row * 128 + (x % 8) * 16),
@@ -169,104 +205,124 @@ __global__ void __launch_bounds__(32 * (MG * kKeyWarps + 1), MG == 1 ? 2 : 1) ca
           __syncwarp();
         }
         // Running max (log2 units), moved only when it grows by more than 2^8.
-        float tm[2];
+        float tm[MG][2];
+        bool grows = false;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float x = fmaxf(fmaxf(sc[0][2 * half], sc[0][2 * half + 1]), fmaxf(sc[1][2 * half], sc[1][2 * half + 1]));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-          tm[half] = x * L.d.scale_log2;
-        }
-        if (__any_sync(0xffffffffu, tm[0] > m[0] + kRescaleThreshold || tm[1] > m[1] + kRescaleThreshold)) {
+        for (int g = 0; g < MG; ++g)
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const bool need = tm[half] > m[half] + kRescaleThreshold;
-            const float alpha = need ? ptx::ex2(m[half] - tm[half]) : 1.f;
-            if (need) m[half] = tm[half];
-            l[half] *= alpha;
+            float x = fmaxf(fmaxf(sc[g][0][2 * half], sc[g][0][2 * half + 1]), fmaxf(sc[g][1][2 * half], sc[g][1][2 * half + 1]));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            tm[g][half] = x * L.d.scale_log2;
+            grows = grows || tm[g][half] > m[g][half] + kRescaleThreshold;
+          }
+        if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
-            for (int j = 0; j < D / 8; ++j) {
-              o[j][2 * half] *= alpha;
-              o[j][2 * half + 1] *= alpha;
+          for (int g = 0; g < MG; ++g)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const bool need = tm[g][half] > m[g][half] + kRescaleThreshold;
+              const float alpha = need ? ptx::ex2(m[g][half] - tm[g][half]) : 1.f;
+              if (need) m[g][half] = tm[g][half];
+              l[g][half] *= alpha;
+#pragma unroll
+              for (int j = 0; j < D / 8; ++j) {
+                o[g][j][2 * half] *= alpha;
+                o[g][j][2 * half + 1] *= alpha;
+              }
             }
-          }
         }
-        const float ms[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-        float p[2][4];
+        uint32_t pa[MG][4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int g = 0; g < MG; ++g) {
+          const float ms[2] = {m[g][0] == -INFINITY ? 0.f : m[g][0], m[g][1] == -INFINITY ? 0.f : m[g][1]};
+          float p[2][4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            p[j][e] = ptx::ex2(fmaf(sc[j][e], L.d.scale_log2, -ms[e >> 1]));
-            l[e >> 1] += p[j][e];
-          }
-        const uint32_t pa[4] = {T::pack(p[0][0], p[0][1]), T::pack(p[0][2], p[0][3]), T::pack(p[1][0], p[1][1]),
-                                T::pack(p[1][2], p[1][3])};
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              p[j][e] = ptx::ex2(fmaf(sc[g][j][e], L.d.scale_log2, -ms[e >> 1]));
+              l[g][e >> 1] += p[j][e];
+            }
+          pa[g][0] = T::pack(p[0][0], p[0][1]);
+          pa[g][1] = T::pack(p[0][2], p[0][3]);
+          pa[g][2] = T::pack(p[1][0], p[1][1]);
+          pa[g][3] = T::pack(p[1][2], p[1][3]);
+        }
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
           uint32_t vf[4];
           const int ch = (j % 4) * 2 + v_chunk;
           ptx::ldmatrix4_t(vf, vt + (j / 4) * C::BLOCK + v_row * 128 + ((ch ^ r8) << 4));
-          ptx::mma16816<T>(o[2 * j], pa, vf[0], vf[1]);
-          ptx::mma16816<T>(o[2 * j + 1], pa, vf[2], vf[3]);
+#pragma unroll
+          for (int g = 0; g < MG; ++g) {
+            ptx::mma16816<T>(o[g][2 * j], pa[g], vf[0], vf[1]);
+            ptx::mma16816<T>(o[g][2 * j + 1], pa[g], vf[2], vf[3]);
+          }
         }
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(C::B_EMPTY + st));
     }
 
-    // Join of the four key warps of this row group (every warp passes every
-    // barrier, also after a failure), and the partial of this segment.
+    // Join of the four key warps (every warp passes every barrier, also after a
+    // failure), and the partial of this segment.
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
-      l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
-      if ((lane & 3) == 0) ml[kw * 16 + fr + 8 * half] = make_float2(m[half], l[half]);
-    }
-    ptx::bar_sync(1 + mg, 32 * kKeyWarps);
-    float top[2], sum[2], f[2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      top[half] = -INFINITY;
-      sum[half] = 0.f;
-#pragma unroll
-      for (int w = 0; w < kKeyWarps; ++w) top[half] = fmaxf(top[half], ml[w * 16 + fr + 8 * half].x);
-      const float ref = top[half] == -INFINITY ? 0.f : top[half];
-#pragma unroll
-      for (int w = 0; w < kKeyWarps; ++w) {
-        const float2 x = ml[w * 16 + fr + 8 * half];
-        sum[half] += x.y * ptx::ex2(x.x - ref);
-      }
-      f[half] = ptx::ex2(m[half] - ref);
-    }
-#pragma unroll
-    for (int j = 0; j < D / 8; ++j) {
-      o[j][0] *= f[0], o[j][1] *= f[0], o[j][2] *= f[1], o[j][3] *= f[1];
-    }
-#pragma unroll
-    for (int w = kKeyWarps - 1; w >= 0; --w) {
-      if (kw == w) {
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j) {
-          if (w < kKeyWarps - 1) {
-            const float4 x = join[j * 32 + lane];
-            o[j][0] += x.x, o[j][1] += x.y, o[j][2] += x.z, o[j][3] += x.w;
-          }
-          if (w > 0) join[j * 32 + lane] = make_float4(o[j][0], o[j][1], o[j][2], o[j][3]);
-        }
-      }
-      if (w > 0) ptx::bar_sync(1 + mg, 32 * kKeyWarps);
-    }
-    if (kw == 0 && ok) {
-      const int64_t part = static_cast<int64_t>(blockIdx.x) + s.problem;
+    for (int g = 0; g < MG; ++g)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const int64_t row = part * L.tile_rows + mg * 16 + fr + 8 * half;
-        float* dst = L.part_o + row * D + fc;
+        l[g][half] += __shfl_xor_sync(0xffffffffu, l[g][half], 1);
+        l[g][half] += __shfl_xor_sync(0xffffffffu, l[g][half], 2);
+        if ((lane & 3) == 0) ml[(kw * MG + g) * 16 + fr + 8 * half] = make_float2(m[g][half], l[g][half]);
+      }
+    ptx::bar_sync(1, 32 * kKeyWarps);
+    const int64_t part0 = (static_cast<int64_t>(blockIdx.x) + s.problem) * L.tile_rows;
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j)
-          *reinterpret_cast<float2*>(dst + j * 8) = make_float2(o[j][2 * half], o[j][2 * half + 1]);
-        if ((lane & 3) == 0) L.part_ml[row] = make_float2(top[half], sum[half]);
+    for (int g = 0; g < MG; ++g) {
+      float top[2], sum[2], f[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        top[half] = -INFINITY;
+        sum[half] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kKeyWarps; ++w) top[half] = fmaxf(top[half], ml[(w * MG + g) * 16 + fr + 8 * half].x);
+        const float ref = top[half] == -INFINITY ? 0.f : top[half];
+#pragma unroll
+        for (int w = 0; w < kKeyWarps; ++w) {
+          const float2 x = ml[(w * MG + g) * 16 + fr + 8 * half];
+          sum[half] += x.y * ptx::ex2(x.x - ref);
+        }
+        f[half] = ptx::ex2(m[g][half] - ref);
+      }
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) {
+        o[g][j][0] *= f[0], o[g][j][1] *= f[0], o[g][j][2] *= f[1], o[g][j][3] *= f[1];
+      }
+#pragma unroll
+      for (int w = kKeyWarps - 1; w >= 0; --w) {
+        if (kw == w) {
+#pragma unroll
+          for (int j = 0; j < D / 8; ++j) {
+            if (w < kKeyWarps - 1) {
+              const float4 x = join[j * 32 + lane];
+              o[g][j][0] += x.x, o[g][j][1] += x.y, o[g][j][2] += x.z, o[g][j][3] += x.w;
+            }
+            if (w > 0) join[j * 32 + lane] = make_float4(o[g][j][0], o[g][j][1], o[g][j][2], o[g][j][3]);
+          }
+        }
+        if (w > 0 || g + 1 < MG) ptx::bar_sync(1, 32 * kKeyWarps);
+      }
+      if (kw == 0 && ok) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int64_t row = part0 + g * 16 + fr + 8 * half;
+          float* dst = L.part_o + row * D + fc;
+#pragma unroll
+          for (int j = 0; j < D / 8; ++j)
+            *reinterpret_cast<float2*>(dst + j * 8) = make_float2(o[g][j][2 * half], o[g][j][2 * half + 1]);
+          if ((lane & 3) == 0) L.part_ml[row] = make_float2(top[half], sum[half]);
+        }
       }
     }
   }
@@ -288,6 +344,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
   __shared__ float2 join_ml[kJoinWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int bh = blockIdx.y, b = bh / L.c.hkv, h = bh % L.c.hkv;
+  // Everything but the partials was there before the kernel that this one follows began.
   const UnitCount uc(L.c, L.key_tile, L.row_tiles, L.status);
   const Split sp = split_find_entry(uc, scratch, uc.per_head ? bh : b);
   const int tiles = uc.tiles(sp.entry);
@@ -312,6 +369,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
     }
   };
 
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   if (live && tiles > 0) {
     const int slot = r / L.slot_rows, rt = slot / L.slots;
     const int in_slot = L.wide && !L.qt.head_inner ? g * L.qt.tokens + t % L.qt.tokens : r % L.slot_rows;
@@ -422,8 +481,7 @@ cudaError_t launch_few(const CacheAttnLaunch& L, cudaStream_t stream) {
   static PerDeviceAttr once;
   const cudaError_t e = raise_smem_limit(once, reinterpret_cast<const void*>(kern), C::SMEM);
   if (e != cudaSuccess) return e;
-  kern<<<L.n_ctas, C::THREADS, C::SMEM, stream>>>(L);
-  return cudaGetLastError();
+  return launch_after(kern, dim3(L.n_ctas), C::THREADS, C::SMEM, stream, L);
 }
 
 template <class T, int D>
@@ -436,8 +494,8 @@ cudaError_t launch_d(const CacheAttnLaunch& L, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(L.c.batch) * L.c.hkv * L.rows;
   const int wpr = rows >= 2048 ? 1 : rows >= 1024 ? 2 : rows >= 512 ? 4 : 8;
   const int per = kJoinWarps / wpr;
-  cache_join_kernel<T, D><<<dim3((L.rows + per - 1) / per, L.c.batch * L.c.hkv), 32 * kJoinWarps, 0, stream>>>(L, wpr);
-  return cudaGetLastError();
+  return launch_after(cache_join_kernel<T, D>, dim3((L.rows + per - 1) / per, L.c.batch * L.c.hkv), 32 * kJoinWarps, 0, stream,
+                      L, wpr);
 }
 
 }  // namespace

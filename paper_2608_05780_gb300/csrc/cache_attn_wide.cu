@@ -422,6 +422,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attn_wide_kernel(const __gr
   int* scratch = reinterpret_cast<int*>(smem + C::OFF_MISC + 8);
   const int warp = threadIdx.x >> 5;
 
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   const UnitCount uc(L.c, kKeys, L.row_tiles, L.status);
   int ctas = 1, begin = 0, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
@@ -469,8 +471,7 @@ cudaError_t launch_d(const CacheAttnLaunch& L, cudaStream_t stream) {
   static PerDeviceAttr once;
   const cudaError_t e = raise_smem_limit(once, reinterpret_cast<const void*>(kern), C::SMEM);
   if (e != cudaSuccess) return e;
-  kern<<<L.n_ctas, kThreads, C::SMEM, stream>>>(L);
-  return cudaGetLastError();
+  return launch_after(kern, dim3(L.n_ctas), kThreads, C::SMEM, stream, L);
 }
 
 }  // namespace

@@ -180,22 +180,4 @@ inline int choose_cluster(int64_t problems, int64_t scores, int64_t least, int n
   return c;
 }
 
-// Launches `kern` with clusters of `cluster` CTAs (grid.x a multiple of it).
-template <class Launch>
-cudaError_t launch_clusters(void (*kern)(Launch), const Launch& L, unsigned grid, unsigned threads, int cluster,
-                            cudaStream_t stream) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cluster;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, L);
-}
-
 }  // namespace evisel

@@ -71,6 +71,13 @@ __device__ __forceinline__ void unpack8(const uint4& w, float (&f)[8]) {
 
 namespace ptx {
 
+// Programmatic dependent launch: grid_wait() returns when the kernels before this
+// one in the stream have ended and their writes are visible; a kernel calls
+// grid_launch_next() after it, so that whatever may start early finds everything
+// before the kernel it follows done.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // 4-D tiled load whose token, head and page (or sequence) coordinates stand at the places that
 // `perm` names: two bits each for the coordinate (1..3) of token, head and page.
 __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, uint32_t bar, int perm, int c0,
@@ -221,6 +228,45 @@ __device__ __forceinline__ int split_begin(int i, int total, int ctas) {
 // The CTA that holds unit u.
 __device__ __forceinline__ int split_owner(int u, int total, int ctas) {
   return static_cast<int>((static_cast<int64_t>(u + 1) * ctas - 1) / total);
+}
+
+// ---------------------------------------------------------------- launch
+// Launches a kernel that begins with grid_wait() (or waits before it reads what
+// the kernel before it writes).
+template <class... Params>
+cudaError_t launch_after(void (*kern)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream,
+                         const Params&... params) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, params...);
+}
+
+// The same in clusters of `cluster` CTAs, one per problem.
+template <class Launch>
+cudaError_t launch_clusters(void (*kern)(Launch), const Launch& L, int problems, unsigned threads, int cluster,
+                            cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(problems * cluster);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, L);
 }
 
 }  // namespace evisel

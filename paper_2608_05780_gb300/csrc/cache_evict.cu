@@ -13,6 +13,8 @@ constexpr int kChooseThreads = 1024;
 
 __global__ void __launch_bounds__(kChooseThreads) cache_evict_choose_kernel(const __grid_constant__ CacheEvictLaunch L) {
   __shared__ ChooseMem mem;
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   const int rank = static_cast<int>(ptx::cluster_rank()), size = static_cast<int>(ptx::cluster_size());
   const int problem = blockIdx.x / size, b = problem / L.c.hkv, h = problem % L.c.hkv;
   int len = cache_len(L.c, b, h, L.status);
@@ -64,6 +66,8 @@ struct KeptTokens {
 template <class T, int D>
 __global__ void __launch_bounds__(kPageThreads) cache_evict_copy_kernel(const __grid_constant__ CacheEvictLaunch L) {
   const int h = blockIdx.y, b = blockIdx.z;
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   fill_page<T, D>(L.out, L.out_k, L.out_v, L.out_mean, b, h, blockIdx.x, KeptTokens(L, b, h), L.status);
 }
 
@@ -72,11 +76,10 @@ cudaError_t launch_d(const CacheEvictLaunch& L, cudaStream_t stream) {
   const int problems = L.c.batch * L.c.hkv;
   const int64_t room = static_cast<int64_t>(L.c.max_pages) * L.c.page;
   const int cluster = choose_cluster(problems, room < L.acc_len ? room : L.acc_len, 2048, sm_count());
-  const cudaError_t e = launch_clusters(cache_evict_choose_kernel, L, static_cast<unsigned>(problems * cluster), kChooseThreads,
-                                        cluster, stream);
+  const cudaError_t e = launch_clusters(cache_evict_choose_kernel, L, problems, kChooseThreads, cluster, stream);
   if (e != cudaSuccess) return e;
-  cache_evict_copy_kernel<T, D><<<dim3((L.budget + L.out.page - 1) / L.out.page, L.c.hkv, L.c.batch), kPageThreads, 0, stream>>>(L);
-  return cudaGetLastError();
+  return launch_after(cache_evict_copy_kernel<T, D>, dim3((L.budget + L.out.page - 1) / L.out.page, L.c.hkv, L.c.batch),
+                      kPageThreads, 0, stream, L);
 }
 
 }  // namespace

@@ -63,6 +63,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
   volatile int* part_s = reinterpret_cast<volatile int*>(smem + C::OFF_PART);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   const UnitCount uc(L.c, kKeys, 1, L.status);
   int begin = 0, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
@@ -380,8 +382,7 @@ cudaError_t launch_d(const CacheEvidenceLaunch& L, cudaStream_t stream) {
     static PerDeviceAttr once;
     const cudaError_t e = raise_smem_limit(once, reinterpret_cast<const void*>(kern), C::SMEM);
     if (e != cudaSuccess) return e;
-    kern<<<L.n_ctas, kThreads, C::SMEM, stream>>>(L);
-    return cudaGetLastError();
+    return launch_after(kern, dim3(L.n_ctas), kThreads, C::SMEM, stream, L);
   }
   const int64_t room = static_cast<int64_t>(L.c.max_pages) * L.c.page;
   const dim3 grid(static_cast<unsigned>((room + kPlainThreads - 1) / kPlainThreads), L.c.hkv, L.c.batch);

@@ -21,6 +21,8 @@ template <class T, int D>
 __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __grid_constant__ CacheSelectLaunch L) {
   __shared__ ChooseMem mem;
   __shared__ float score[kMaxPages];             // of the CTA's part, from its first page on
+  ptx::grid_wait();
+  ptx::grid_launch_next();
   constexpr int J = D / 32;                      // 16-byte chunks of a row per lane
   const int rank = static_cast<int>(ptx::cluster_rank()), size = static_cast<int>(ptx::cluster_size());
   const int problem = blockIdx.x / size, b = problem / L.c.hkv, h = problem % L.c.hkv;
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
 template <class T, int D>
 cudaError_t launch_d(const CacheSelectLaunch& L, cudaStream_t stream) {
   const int problems = L.c.batch * L.c.hkv, cluster = choose_cluster(problems, L.c.max_pages, 64, sm_count());
-  return launch_clusters(cache_select_kernel<T, D>, L, static_cast<unsigned>(problems * cluster), kChooseThreads, cluster, stream);
+  return launch_clusters(cache_select_kernel<T, D>, L, problems, kChooseThreads, cluster, stream);
 }
 
 }  // namespace
