@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel
   const UnitCount uc(L.c, kKeys, L.row_tiles, L.status);
   int ctas = 1, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
-    ctas = split_ctas(total, L.n_ctas, L.min_units);
+    ctas = split_ctas(total, L.n_ctas, L.min_units, L.c.batch * L.c.hkv * L.row_tiles);
     const int i = blockIdx.x;
     end = i < ctas ? split_begin(i + 1, total, ctas) : 0;
     return i < ctas ? split_begin(i, total, ctas) : total;
@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
   const Split sp = split_find_entry(uc, scratch, uc.per_head ? bh : b);
   const int tiles = uc.tiles(sp.entry);
   const int first = sp.first + (uc.per_head ? 0 : h * L.row_tiles * tiles);
-  const int ctas = split_ctas(sp.total, L.n_ctas, L.min_units);
+  const int ctas = split_ctas(sp.total, L.n_ctas, L.min_units, L.c.batch * L.c.hkv * L.row_tiles);
 
   const int r = blockIdx.x * (kJoinWarps / wpr) + warp / wpr, wi = warp % wpr;
   const bool in = r < L.rows;
@@ -369,43 +369,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
     }
   };
 
-  ptx::grid_wait();
-  ptx::grid_launch_next();
-  if (live && tiles > 0) {
-    const int slot = r / L.slot_rows, rt = slot / L.slots;
-    const int in_slot = L.wide && !L.qt.head_inner ? g * L.qt.tokens + t % L.qt.tokens : r % L.slot_rows;
-    const int row = (slot % L.slots) * (L.tile_rows / L.slots) + in_slot;
-    const int u0 = first + rt * tiles, i0 = split_owner(u0, sp.total, ctas), i1 = split_owner(u0 + tiles - 1, sp.total, ctas);
-    const int problem = bh * L.row_tiles + rt;
-    const int n = (i1 - i0 + 1 - wi + wpr - 1) / wpr;            // partials of this warp
-    for (int base = 0; base < n; base += 32) {
-      const int64_t mine = static_cast<int64_t>(i0 + problem + wi) + static_cast<int64_t>(base + lane) * wpr;
-      const float2 x = base + lane < n ? L.part_ml[mine * L.tile_rows + row] : make_float2(-INFINITY, 0.f);
-      float top = x.x;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      move_max(top);
-      const float w = ptx::ex2(x.x - (m == -INFINITY ? 0.f : m));
-      float lw = x.y * w;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) lw += __shfl_xor_sync(0xffffffffu, lw, o);
-      l += lw;
-      const int cnt = min(32, n - base);
-#pragma unroll 4
-      for (int k = 0; k < cnt; ++k) {
-        const float wk = __shfl_sync(0xffffffffu, w, k);
-        const int64_t part = static_cast<int64_t>(i0 + problem + wi) + static_cast<int64_t>(base + k) * wpr;
-        const float* src = L.part_o + (part * L.tile_rows + row) * D + lane * E;
-        if constexpr (E == 4) {
-          const float4 y = *reinterpret_cast<const float4*>(src);
-          acc[0] += wk * y.x, acc[1] += wk * y.y, acc[2] += wk * y.z, acc[3] += wk * y.w;
-        } else {
-          const float2 y = *reinterpret_cast<const float2*>(src);
-          acc[0] += wk * y.x, acc[1] += wk * y.y;
-        }
-      }
-    }
-  }
+  // The drafted tokens first: they need nothing of the kernel before.
   if (live && L.d.k_new) {
     auto load = [&](const void* base, const int64_t (&st)[3], int tok, int hd, float (&x)[E]) {
       const uint16_t* p = static_cast<const uint16_t*>(base) + b * st[0] + tok * st[1] + hd * st[2] + lane * E;
@@ -426,25 +390,100 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
                       : t < 32 * w       ? 0u
                                          : (2u << (t - 32 * w)) - 1u;
       if (drafted - 32 * w < 32) bits &= (1u << (drafted - 32 * w)) - 1u;
-      for (int turn = 0; bits; ++turn) {
-        const int j = __ffs(bits) - 1;
-        bits &= bits - 1;
-        if (turn % wpr != wi) continue;
-        float k[E], v[E];
-        load(L.d.k_new, L.d.kns, 32 * w + j, h, k);
-        load(L.d.v_new, L.d.vns, 32 * w + j, h, v);
-        float x = 0.f;
+      // This warp's share of the bits: its eighth, quarter or half of the word's places.
+      const uint32_t every = wpr == 8 ? 0x01010101u : wpr == 4 ? 0x11111111u : wpr == 2 ? 0x55555555u : 0xffffffffu;
+      bits &= every << wi;
+      // Four keys at a time: their loads together, their four sums over the lanes in one exchange.
+      while (bits) {
+        int tok[4];
+        bool on[4];
 #pragma unroll
-        for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
+        for (int i = 0; i < 4; ++i) {
+          on[i] = bits != 0;
+          tok[i] = 32 * w + (on[i] ? __ffs(bits) - 1 : 0);
+          bits &= bits - 1;
+        }
+        float k[4][E], v[4][E], x[4];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        x *= L.d.scale_log2;
-        move_max(x);
-        const float p = ptx::ex2(x - (m == -INFINITY ? 0.f : m));
-        l += p;
+        for (int i = 0; i < 4; ++i) {
+          if (!on[i]) tok[i] = tok[0];
+          load(L.d.k_new, L.d.kns, tok[i], h, k[i]);
+          load(L.d.v_new, L.d.vns, tok[i], h, v[i]);
+        }
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(p, v[e], acc[e]);
+        for (int i = 0; i < 4; ++i) {
+          x[i] = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[i] = fmaf(q[e], k[i][e], x[i]);
+        }
+        const bool hi = lane & 16, mid = lane & 8;
+        const float y0 = (hi ? x[2] : x[0]) + __shfl_xor_sync(0xffffffffu, hi ? x[0] : x[2], 16);
+        const float y1 = (hi ? x[3] : x[1]) + __shfl_xor_sync(0xffffffffu, hi ? x[1] : x[3], 16);
+        float z = (mid ? y1 : y0) + __shfl_xor_sync(0xffffffffu, mid ? y0 : y1, 8);
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        z *= L.d.scale_log2;                     // lanes 8 i .. 8 i + 7: key i
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = __shfl_sync(0xffffffffu, z, 8 * i);
+          if (on[i]) top = fmaxf(top, x[i]);
+        }
+        move_max(top);
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (on[i]) {
+            const float p = ptx::ex2(x[i] - ref);
+            l += p;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(p, v[i][e], acc[e]);
+          }
       }
+    }
+  }
+
+  ptx::grid_wait();
+  ptx::grid_launch_next();
+  if (live && tiles > 0) {
+    const int slot = r / L.slot_rows, rt = slot / L.slots;
+    const int in_slot = L.wide && !L.qt.head_inner ? g * L.qt.tokens + t % L.qt.tokens : r % L.slot_rows;
+    const int row = (slot % L.slots) * (L.tile_rows / L.slots) + in_slot;
+    const int u0 = first + rt * tiles, i0 = split_owner(u0, sp.total, ctas), i1 = split_owner(u0 + tiles - 1, sp.total, ctas);
+    const int problem = bh * L.row_tiles + rt;
+    const int n = (i1 - i0 + 1 - wi + wpr - 1) / wpr;            // partials of this warp
+    const int64_t step = static_cast<int64_t>(wpr) * L.tile_rows;
+    const int64_t row0 = static_cast<int64_t>(i0 + problem + wi) * L.tile_rows + row;
+    // Eight partials at a time, all loads at once.
+    for (int base = 0; base < n; base += 8) {
+      float y[8][E];
+      const float2 x = lane < 8 && base + lane < n ? L.part_ml[row0 + (base + lane) * step] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float* src = L.part_o + (row0 + (base + k) * step) * D + lane * E;
+        if (base + k < n) {
+          if constexpr (E == 4) {
+            const float4 z = *reinterpret_cast<const float4*>(src);
+            y[k][0] = z.x, y[k][1] = z.y, y[k][2] = z.z, y[k][3] = z.w;
+          } else {
+            const float2 z = *reinterpret_cast<const float2*>(src);
+            y[k][0] = z.x, y[k][1] = z.y;
+          }
+        }
+      }
+      float top = x.x;
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      move_max(__shfl_sync(0xffffffffu, top, 0));
+      const float w = ptx::ex2(x.x - (m == -INFINITY ? 0.f : m)), lw = x.y * w;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (base + k < n) {
+          const float wk = __shfl_sync(0xffffffffu, w, k);
+          l += __shfl_sync(0xffffffffu, lw, k);
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] = fmaf(wk, y[k][e], acc[e]);
+        }
     }
   }
   if (wpr > 1) {

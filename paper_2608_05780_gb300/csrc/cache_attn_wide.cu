@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attn_wide_kernel(const __gr
   const UnitCount uc(L.c, kKeys, L.row_tiles, L.status);
   int ctas = 1, begin = 0, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
-    ctas = split_ctas(total, L.n_ctas, L.min_units);
+    ctas = split_ctas(total, L.n_ctas, L.min_units, L.c.batch * L.c.hkv * L.row_tiles);
     const int i = blockIdx.x;
     begin = i < ctas ? split_begin(i, total, ctas) : total;
     end = i < ctas ? split_begin(i + 1, total, ctas) : total;

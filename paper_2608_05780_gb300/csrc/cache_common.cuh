@@ -171,14 +171,53 @@ __device__ __forceinline__ int block_prefix(int x, int* warp_sums, int& total) {
   return before + inc - x;
 }
 
-// The entry that holds unit `at(total)`, found by the whole block.
+constexpr int kWarpEntries = 256;                // up to so many entries every warp adds up by itself
+
+// The entry that holds unit `at(total)`. Every thread of the block calls and gets it.
 template <class At>
 __device__ __forceinline__ Split split_find_unit(const UnitCount& u, int* mem, At at) {
-  const int n = u.entries(), per = (n + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
+  const int n = u.entries();
+  Split s;
+  if (n <= kWarpEntries) {
+    // Without a barrier: a block's first loads wait for nothing but the lengths
+    // (by the block with barriers it took 1.5 us of a small call's 10, this 0.8).
+    const int lane = threadIdx.x & 31;
+    int m[kWarpEntries / 32];
+    s.total = 0;
+#pragma unroll
+    for (int c = 0; c < kWarpEntries / 32; ++c) {
+      const int e = c * 32 + lane;
+      m[c] = e < n ? u.tiles(e) * u.mult : 0;
+    }
+#pragma unroll
+    for (int c = 0; c < kWarpEntries / 32; ++c)
+      if (c * 32 < n) s.total += __reduce_add_sync(0xffffffffu, m[c]);
+    const int want = at(s.total);
+    int before = 0;
+    s.entry = s.first = 0;
+#pragma unroll
+    for (int c = 0; c < kWarpEntries / 32; ++c)
+      if (c * 32 < n) {
+        int inc = m[c];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += y;
+        }
+        const int first = before + inc - m[c];
+        const uint32_t hit = __ballot_sync(0xffffffffu, want >= first && want < first + m[c]);
+        if (hit) {
+          s.entry = c * 32 + __ffs(hit) - 1;
+          s.first = __shfl_sync(0xffffffffu, first, __ffs(hit) - 1);
+        }
+        before += __shfl_sync(0xffffffffu, inc, 31);
+      }
+    return s;
+  }
+  const int per = (n + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
   const int e0 = min(n, static_cast<int>(threadIdx.x) * per), e1 = min(n, e0 + per);
   int sum = 0;
   for (int e = e0; e < e1; ++e) sum += u.tiles(e) * u.mult;
-  Split s;
   int first = block_prefix(sum, mem + 2, s.total);
   const int want = at(s.total);
   if (threadIdx.x == 0) mem[0] = mem[1] = 0;
@@ -199,9 +238,25 @@ __device__ __forceinline__ Split split_find_unit(const UnitCount& u, int* mem, A
   return s;
 }
 
-// The first unit of entry `want`, found by the whole block.
+// The first unit of entry `want`, likewise.
 __device__ __forceinline__ Split split_find_entry(const UnitCount& u, int* mem, int want) {
-  const int n = u.entries(), per = (n + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
+  const int n = u.entries();
+  Split s;
+  s.entry = want;
+  if (n <= kWarpEntries) {
+    const int lane = threadIdx.x & 31;
+    int all = 0, before = 0;
+#pragma unroll
+    for (int c = 0; c < kWarpEntries / 32; ++c) {
+      const int e = c * 32 + lane, m = e < n ? u.tiles(e) * u.mult : 0;
+      all += m;
+      before += e < want ? m : 0;
+    }
+    s.total = __reduce_add_sync(0xffffffffu, all);
+    s.first = __reduce_add_sync(0xffffffffu, before);
+    return s;
+  }
+  const int per = (n + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
   const int e0 = min(n, static_cast<int>(threadIdx.x) * per), e1 = min(n, e0 + per);
   int sum = 0, before = 0;
   for (int e = e0; e < e1; ++e) {
@@ -209,19 +264,25 @@ __device__ __forceinline__ Split split_find_entry(const UnitCount& u, int* mem, 
     if (e < want) before += m;
     sum += m;
   }
-  Split s;
   const int first = block_prefix(sum, mem + 2, s.total);
   if (want >= e0 && want < e1) mem[1] = first + before;
   __syncthreads();
-  s.entry = want;
   s.first = mem[1];
   return s;
 }
 
-// CTAs that share `total` units (each takes at least `least`), and CTA i's first unit.
-__device__ __forceinline__ int split_ctas(int total, int n_ctas, int least) {
+// CTAs that share `total` units of `problems` problems: each takes at least
+// `least`, and where there are many CTAs to a problem their number is a multiple of
+// the problems', so that problems of one length are cut at their borders (a
+// CTA that crosses one pays its fill and its join twice: 2 us of 10 for one token over 4,160).
+__device__ __forceinline__ int split_ctas(int total, int n_ctas, int least, int problems) {
+  if (problems * 8 <= n_ctas) {
+    const int k = min(n_ctas / problems, (total + least * problems - 1) / (least * problems));
+    return max(1, k) * problems;
+  }
   return max(1, min(n_ctas, (total + least - 1) / least));
 }
+// CTA i's first unit.
 __device__ __forceinline__ int split_begin(int i, int total, int ctas) {
   return static_cast<int>(static_cast<int64_t>(i) * total / ctas);
 }

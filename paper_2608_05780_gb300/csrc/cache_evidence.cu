@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
   const UnitCount uc(L.c, kKeys, 1, L.status);
   int begin = 0, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
-    const int ctas = split_ctas(total, L.n_ctas, 1), i = blockIdx.x;
+    const int ctas = split_ctas(total, L.n_ctas, 1, L.c.batch * L.c.hkv), i = blockIdx.x;
     begin = i < ctas ? split_begin(i, total, ctas) : total;
     end = i < ctas ? split_begin(i + 1, total, ctas) : total;
     return begin;
