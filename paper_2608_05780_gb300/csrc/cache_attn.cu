@@ -60,9 +60,13 @@ __global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel
     *abort_flag = 0;
     ptx::fence_mbar_init();
   }
+  if (threadIdx.x == 0) {
+    ptx::tma_prefetch_desc(&L.tm_k);
+    ptx::tma_prefetch_desc(&L.tm_v);
+  }
   ptx::grid_wait();
   ptx::grid_launch_next();
-  const UnitCount uc(L.c, kKeys, L.row_tiles, L.status);
+  const UnitCount uc(L.c, kKeys, L.lead, L.row_tiles, L.status);
   int ctas = 1, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
     ctas = split_ctas(total, L.n_ctas, L.min_units, L.c.batch * L.c.hkv * L.row_tiles);
@@ -345,10 +349,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int bh = blockIdx.y, b = bh / L.c.hkv, h = bh % L.c.hkv;
   // Everything but the partials was there before the kernel that this one follows began.
-  const UnitCount uc(L.c, L.key_tile, L.row_tiles, L.status);
+  const UnitCount uc(L.c, L.key_tile, L.lead, L.row_tiles, L.status);
   const Split sp = split_find_entry(uc, scratch, uc.per_head ? bh : b);
   const int tiles = uc.tiles(sp.entry);
-  const int first = sp.first + (uc.per_head ? 0 : h * L.row_tiles * tiles);
+  const int first = sp.first + (uc.per_head ? 0 : h * L.row_tiles * uc.units(tiles));
   const int ctas = split_ctas(sp.total, L.n_ctas, L.min_units, L.c.batch * L.c.hkv * L.row_tiles);
 
   const int r = blockIdx.x * (kJoinWarps / wpr) + warp / wpr, wi = warp % wpr;
@@ -449,7 +453,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
     const int slot = r / L.slot_rows, rt = slot / L.slots;
     const int in_slot = L.wide && !L.qt.head_inner ? g * L.qt.tokens + t % L.qt.tokens : r % L.slot_rows;
     const int row = (slot % L.slots) * (L.tile_rows / L.slots) + in_slot;
-    const int u0 = first + rt * tiles, i0 = split_owner(u0, sp.total, ctas), i1 = split_owner(u0 + tiles - 1, sp.total, ctas);
+    const int u0 = first + rt * uc.units(tiles) + uc.lead, i0 = split_owner(u0, sp.total, ctas), i1 = split_owner(u0 + tiles - 1, sp.total, ctas);
     const int problem = bh * L.row_tiles + rt;
     const int n = (i1 - i0 + 1 - wi + wpr - 1) / wpr;            // partials of this warp
     const int64_t step = static_cast<int64_t>(wpr) * L.tile_rows;
@@ -551,6 +555,7 @@ CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n
     s.key_tile = 128;
     s.n_ctas = n_sm;
     s.min_units = 1;
+    s.lead = 1;
     return s;
   }
   s.wide = false;
@@ -559,7 +564,8 @@ CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n
   s.row_tiles = (rows + s.tile_rows - 1) / s.tile_rows;
   s.key_tile = kKeys;
   s.n_ctas = 2 * n_sm;
-  s.min_units = 2;
+  s.min_units = 3;
+  s.lead = 2;
   return s;
 }
 

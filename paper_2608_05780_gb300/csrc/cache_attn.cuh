@@ -18,7 +18,7 @@ __device__ __forceinline__ void record_timeout(volatile int* abort_flag, int* st
   atomicExch(status, kStatusTimeout);
 }
 
-// A CTA's part of one problem: units [t0, t1) of a (sequence, KV head, row tile).
+// A CTA's part of one problem: key tiles [t0, t1) of a (sequence, KV head, row tile).
 struct Segment {
   int b, h, rt, t0, t1, len, problem;
 };
@@ -27,22 +27,26 @@ struct Segment {
 struct Walk {
   int u, end, entry, first;
   __device__ __forceinline__ bool next(const CacheView& c, int row_tiles, const UnitCount& uc, Segment& s, int* status) {
-    if (u >= end) return false;
-    int tiles = uc.tiles(entry);
-    while (u >= first + tiles * uc.mult) {
-      first += tiles * uc.mult;
-      tiles = uc.tiles(++entry);
+    for (;;) {
+      if (u >= end) return false;
+      int tiles = uc.tiles(entry), n = uc.units(tiles);
+      while (u >= first + n * uc.mult) {
+        first += n * uc.mult;
+        tiles = uc.tiles(++entry);
+        n = uc.units(tiles);
+      }
+      const int inner = (u - first) / n, from = (u - first) % n, to = min(n, from + (end - u));
+      u += to - from;
+      s.t0 = max(0, from - uc.lead);
+      s.t1 = max(0, to - uc.lead);
+      if (s.t0 == s.t1) continue;                // a problem's lead alone: its keys are the next CTA's
+      s.b = uc.per_head ? entry / c.hkv : entry;
+      s.h = uc.per_head ? entry % c.hkv : inner / row_tiles;
+      s.rt = inner % row_tiles;
+      s.len = cache_len(c, s.b, s.h, status);
+      s.problem = (s.b * c.hkv + s.h) * row_tiles + s.rt;
+      return true;
     }
-    const int inner = (u - first) / tiles;
-    s.t0 = (u - first) % tiles;
-    s.t1 = min(tiles, s.t0 + (end - u));
-    s.b = uc.per_head ? entry / c.hkv : entry;
-    s.h = uc.per_head ? entry % c.hkv : inner / row_tiles;
-    s.rt = inner % row_tiles;
-    s.len = cache_len(c, s.b, s.h, status);
-    s.problem = (s.b * c.hkv + s.h) * row_tiles + s.rt;
-    u += s.t1 - s.t0;
-    return true;
   }
 };
 

@@ -422,9 +422,14 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attn_wide_kernel(const __gr
   int* scratch = reinterpret_cast<int*>(smem + C::OFF_MISC + 8);
   const int warp = threadIdx.x >> 5;
 
+  if (threadIdx.x == 0) {
+    ptx::tma_prefetch_desc(&L.tm_k);
+    ptx::tma_prefetch_desc(&L.tm_v);
+    ptx::tma_prefetch_desc(&L.tm_q);
+  }
   ptx::grid_wait();
   ptx::grid_launch_next();
-  const UnitCount uc(L.c, kKeys, L.row_tiles, L.status);
+  const UnitCount uc(L.c, kKeys, L.lead, L.row_tiles, L.status);
   int ctas = 1, begin = 0, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
     ctas = split_ctas(total, L.n_ctas, L.min_units, L.c.batch * L.c.hkv * L.row_tiles);

@@ -124,9 +124,9 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 }  // namespace ptx
 
 // ---------------------------------------------------------------- even split of ragged work
-// Sequences (or (sequence, head) pairs, where each has its length) are entries;
-// an entry holds ceil(len / key_tile) * mult units, mult of which tile the other
-// dimensions. Every thread of the block calls; `mem` holds 2 + 32 ints.
+// Sequences (or (sequence, head) pairs, where each has its length) are entries of
+// `mult` problems each. A problem holds `lead` units for its fill and its join,
+// then one per key_tile keys; nothing where it has no key. Every thread of the block calls; `mem` holds 2 + 32 ints.
 struct Split {
   int total;        // units of all entries
   int entry;        // the entry that was looked for ...
@@ -135,11 +135,11 @@ struct Split {
 
 struct UnitCount {
   const CacheView& c;
-  int key_tile, mult;
+  int key_tile, lead, mult;
   int* status;
   bool per_head;
-  __device__ __forceinline__ UnitCount(const CacheView& c_, int key_tile_, int row_tiles, int* status_)
-      : c(c_), key_tile(key_tile_), mult(0), status(status_), per_head(c_.ls[1] != 0) {
+  __device__ __forceinline__ UnitCount(const CacheView& c_, int key_tile_, int lead_, int row_tiles, int* status_)
+      : c(c_), key_tile(key_tile_), lead(lead_), mult(0), status(status_), per_head(c_.ls[1] != 0) {
     mult = per_head ? row_tiles : row_tiles * c.hkv;
   }
   __device__ __forceinline__ int entries() const { return per_head ? c.batch * c.hkv : c.batch; }
@@ -147,6 +147,7 @@ struct UnitCount {
     const int len = per_head ? cache_len(c, e / c.hkv, e % c.hkv, status) : cache_len(c, e, 0, status);
     return (len + key_tile - 1) / key_tile;
   }
+  __device__ __forceinline__ int units(int tiles) const { return tiles > 0 ? tiles + lead : 0; }   // of a problem
 };
 
 // Exclusive prefix over the block of one int per thread; `total` gets the sum. Two barriers.
@@ -182,12 +183,27 @@ __device__ __forceinline__ Split split_find_unit(const UnitCount& u, int* mem, A
     // Without a barrier: a block's first loads wait for nothing but the lengths
     // (by the block with barriers it took 1.5 us of a small call's 10, this 0.8).
     const int lane = threadIdx.x & 31;
+    if (n <= 32) {                               // (little code: it is fetched cold)
+      const int m = lane < n ? u.units(u.tiles(lane)) * u.mult : 0;
+      int inc = m;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      s.total = __shfl_sync(0xffffffffu, inc, 31);
+      const int want = at(s.total);
+      const uint32_t hit = __ballot_sync(0xffffffffu, want >= inc - m && want < inc);
+      s.entry = hit ? __ffs(hit) - 1 : 0;
+      s.first = __shfl_sync(0xffffffffu, inc - m, s.entry);
+      return s;
+    }
     int m[kWarpEntries / 32];
     s.total = 0;
 #pragma unroll
     for (int c = 0; c < kWarpEntries / 32; ++c) {
       const int e = c * 32 + lane;
-      m[c] = e < n ? u.tiles(e) * u.mult : 0;
+      m[c] = e < n ? u.units(u.tiles(e)) * u.mult : 0;
     }
 #pragma unroll
     for (int c = 0; c < kWarpEntries / 32; ++c)
@@ -217,14 +233,14 @@ __device__ __forceinline__ Split split_find_unit(const UnitCount& u, int* mem, A
   const int per = (n + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
   const int e0 = min(n, static_cast<int>(threadIdx.x) * per), e1 = min(n, e0 + per);
   int sum = 0;
-  for (int e = e0; e < e1; ++e) sum += u.tiles(e) * u.mult;
+  for (int e = e0; e < e1; ++e) sum += u.units(u.tiles(e)) * u.mult;
   int first = block_prefix(sum, mem + 2, s.total);
   const int want = at(s.total);
   if (threadIdx.x == 0) mem[0] = mem[1] = 0;
   __syncthreads();
   if (want >= first && want < first + sum)
     for (int e = e0; e < e1; ++e) {
-      const int m = u.tiles(e) * u.mult;
+      const int m = u.units(u.tiles(e)) * u.mult;
       if (want < first + m) {
         mem[0] = e;
         mem[1] = first;
@@ -248,7 +264,7 @@ __device__ __forceinline__ Split split_find_entry(const UnitCount& u, int* mem, 
     int all = 0, before = 0;
 #pragma unroll
     for (int c = 0; c < kWarpEntries / 32; ++c) {
-      const int e = c * 32 + lane, m = e < n ? u.tiles(e) * u.mult : 0;
+      const int e = c * 32 + lane, m = e < n ? u.units(u.tiles(e)) * u.mult : 0;
       all += m;
       before += e < want ? m : 0;
     }
@@ -260,7 +276,7 @@ __device__ __forceinline__ Split split_find_entry(const UnitCount& u, int* mem, 
   const int e0 = min(n, static_cast<int>(threadIdx.x) * per), e1 = min(n, e0 + per);
   int sum = 0, before = 0;
   for (int e = e0; e < e1; ++e) {
-    const int m = u.tiles(e) * u.mult;
+    const int m = u.units(u.tiles(e)) * u.mult;
     if (e < want) before += m;
     sum += m;
   }
@@ -282,9 +298,10 @@ __device__ __forceinline__ int split_ctas(int total, int n_ctas, int least, int 
   }
   return max(1, min(n_ctas, (total + least - 1) / least));
 }
-// CTA i's first unit.
+// CTA i's first unit: floor(i total / ctas), in 32 bits.
 __device__ __forceinline__ int split_begin(int i, int total, int ctas) {
-  return static_cast<int>(static_cast<int64_t>(i) * total / ctas);
+  const uint32_t q = static_cast<uint32_t>(total) / ctas, r = static_cast<uint32_t>(total) % ctas;
+  return static_cast<int>(i * q + i * r / ctas);     // i, r <= ctas, the CTAs of a grid
 }
 // The CTA that holds unit u.
 __device__ __forceinline__ int split_owner(int u, int total, int ctas) {

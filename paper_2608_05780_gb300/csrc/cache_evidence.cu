@@ -63,9 +63,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
   volatile int* part_s = reinterpret_cast<volatile int*>(smem + C::OFF_PART);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  if (threadIdx.x == 0) {
+    ptx::tma_prefetch_desc(&L.tm_k);
+    ptx::tma_prefetch_desc(&L.tm_q);
+  }
   ptx::grid_wait();
   ptx::grid_launch_next();
-  const UnitCount uc(L.c, kKeys, 1, L.status);
+  const UnitCount uc(L.c, kKeys, 0, 1, L.status);
   int begin = 0, end = 0;
   const Split sp = split_find_unit(uc, scratch, [&](int total) {
     const int ctas = split_ctas(total, L.n_ctas, 1, L.c.batch * L.c.hkv), i = blockIdx.x;

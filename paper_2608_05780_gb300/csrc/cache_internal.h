@@ -43,10 +43,10 @@ struct QueryTile {
 };
 
 // Attention: the cached keys of every (sequence, KV head, tile of tile_rows
-// rows), a problem, are cut into units of kKeyTile keys, and all units are dealt
-// evenly over n_ctas CTAs in order. A CTA's part of a problem leaves a partial:
-// the one of CTA i and problem p is partial i + p (both never fall along the
-// units, so no two are the same).
+// rows), a problem, are cut into units of key_tile keys; `lead` units without keys
+// stand before them. All units are dealt evenly over n_ctas CTAs in order. A
+// CTA's part of a problem leaves a partial: the one of CTA i and problem p is
+// partial i + p (both never fall along the units, so no two are the same).
 struct CacheAttnLaunch {
   CUtensorMap tm_k, tm_v;           // pages; box {64, box_rows, 1, 1} in the order of `perm`
   CUtensorMap tm_q;                 // wide: queries, box of gq heads of tile_tokens tokens
@@ -62,7 +62,9 @@ struct CacheAttnLaunch {
   int rows, tile_rows, row_tiles;   // rows = tokens * gq; tile_rows rows of a partial
   int slots, slot_rows;             // a row tile is `slots` slots of slot_rows rows, tile_rows / slots places each
   QueryTile qt;                     // wide: the rows of a slot
-  int n_ctas, key_tile, min_units;  // units a CTA takes at least
+  int n_ctas, key_tile;
+  int min_units;                    // that a CTA takes at least
+  int lead;                         // units that stand for a problem's fill and join
   int wide;                         // 128-row slots on tcgen05 (else mma.sync)
 };
 
@@ -123,7 +125,7 @@ cudaError_t launch_cache_select(const CacheSelectLaunch& L, cudaStream_t stream)
 
 // Row tile and CTAs of a call with `rows` rows per (sequence, KV head).
 struct CacheAttnShape {
-  int tile_rows, row_tiles, slots, slot_rows, key_tile, n_ctas, min_units;
+  int tile_rows, row_tiles, slots, slot_rows, key_tile, n_ctas, min_units, lead;
   bool wide;
 };
 CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n_sm);

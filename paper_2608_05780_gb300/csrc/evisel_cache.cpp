@@ -266,10 +266,11 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     L.key_tile = shape.key_tile;
     L.n_ctas = shape.n_ctas;
     L.min_units = shape.min_units;
+    L.lead = shape.lead;
     L.box_rows = std::min(cache->page, L.key_tile);
     const int64_t problems = static_cast<int64_t>(cache->batch) * cache->hkv * L.row_tiles;
     const int64_t tiles = (static_cast<int64_t>(cache->max_pages) * cache->page + L.key_tile - 1) / L.key_tile;
-    if (problems * std::max<int64_t>(tiles, 1) > INT32_MAX) return fail(EVISEL_EUNSUPPORTED, "too many units of work");
+    if (problems * (tiles + L.lead) > INT32_MAX) return fail(EVISEL_EUNSUPPORTED, "too many units of work");
     const size_t parts = static_cast<size_t>(L.n_ctas) + problems;
     const size_t ml_bytes = align_up(parts * L.tile_rows * sizeof(float2), 256);
     rc = ws_acquire(ws_inout);
