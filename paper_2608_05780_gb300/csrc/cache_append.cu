@@ -36,7 +36,7 @@ struct NewTokens {
 };
 
 template <class T, int D>
-__global__ void __launch_bounds__(kPageThreads) cache_append_kernel(const __grid_constant__ CacheAppendLaunch L) {
+__global__ void __launch_bounds__(kPageThreads, kPageBlocks) cache_append_kernel(const __grid_constant__ CacheAppendLaunch L) {
   const int h = blockIdx.y, b = blockIdx.z;
   ptx::grid_wait();
   ptx::grid_launch_next();

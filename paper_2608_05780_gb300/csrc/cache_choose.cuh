@@ -56,44 +56,68 @@ struct ChoosePart {
   }
 };
 
+// The sum over the cluster of the int at `p`, read from every CTA at once.
+__device__ __forceinline__ int sum_cluster(const int* p, int size) {
+  int x[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) x[r] = r < size ? ptx::ld_cluster(ptx::smem_addr(p), r) : 0;
+  return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
+
 // The `want` highest of key(i), lo <= i < hi (0 <= want <= hi - lo; ties: the
 // lower i): emit(rank, i) for each, ranks ascending with i. Every thread of every
 // CTA of the cluster calls, with the same lo, hi and want; key(i) is asked for
 // the i of the CTA's own ChoosePart only. The last cluster barrier is the
 // caller's: no CTA may leave before the others have read its sums. THREADS: the block's.
-template <int THREADS, class Key, class Emit>
+// A warp owns a run of the part; a thread keeps up to ITEMS keys of its run in
+// registers, so that a part of up to ITEMS * THREADS scores is read once.
+template <int THREADS, int ITEMS, class Key, class Emit>
 __device__ __forceinline__ void choose_top(int lo, int hi, int want, Key key, ChooseMem& m, Emit emit) {
   if (want <= 0) return;
   const int rank = static_cast<int>(ptx::cluster_rank()), size = static_cast<int>(ptx::cluster_size());
   const ChoosePart part(lo, hi, rank, size);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int run = ((part.b - part.a + THREADS - 1) / THREADS) * 32;
+  const int wa = min(part.b, part.a + warp * run), wb = min(part.b, wa + run);
+  const bool held = run <= 32 * ITEMS;
+  uint32_t keys[ITEMS];
+  if (held) {
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const int i = wa + 32 * it + lane;
+      keys[it] = i < wb ? key(i) : 0u;
+    }
+  }
+  // f(key, i, whether i is of the run) for the run's keys in order, 32 at a time.
+  auto each = [&](auto f) {
+    if (held) {
+#pragma unroll
+      for (int it = 0; it < ITEMS; ++it)
+        if (wa + 32 * it < wb) f(keys[it], wa + 32 * it + lane, wa + 32 * it + lane < wb);
+    } else {
+#pragma unroll 4
+      for (int i = wa + lane; i - lane < wb; i += 32) f(i < wb ? key(i) : 0u, i, i < wb);
+    }
+  };
   uint32_t prefix = 0, mask = 0;                 // the boundary's digits so far
   int left = want;                               // to take among the keys with that prefix
   for (int i = threadIdx.x; i < 4 * 256; i += THREADS) m.hist[i >> 8][i & 255] = 0;
   __syncthreads();
   for (int pass = 0; pass < 4; ++pass) {
     const int shift = 24 - 8 * pass;
-#pragma unroll 4
-    for (int i = part.a + static_cast<int>(threadIdx.x); i < part.b; i += THREADS) {
-      const uint32_t k = key(i);
-      if ((k & mask) == prefix) atomicAdd(&m.hist[pass][(k >> shift) & 255u], 1);
-    }
+    each([&](uint32_t k, int, bool in) {
+      if (in && (k & mask) == prefix) atomicAdd(&m.hist[pass][(k >> shift) & 255u], 1);
+    });
     if (size > 1) ptx::cluster_sync();
     else __syncthreads();
-    if (threadIdx.x < 256) {
-      int x = m.hist[pass][threadIdx.x];
-      if (size > 1) {
-        x = 0;
-        for (int r = 0; r < size; ++r) x += ptx::ld_cluster(ptx::smem_addr(&m.hist[pass][threadIdx.x]), r);
-      }
-      m.tot[threadIdx.x] = x;
-    }
-    __syncthreads();
+    if (size > 1 && threadIdx.x < 256) m.tot[threadIdx.x] = sum_cluster(&m.hist[pass][threadIdx.x], size);
+    if (size > 1) __syncthreads();
     if (warp == 0) {
       // Digits from the highest: a lane holds eight, the one where the sum reaches `left` walks them.
+      const int* tot = size > 1 ? m.tot : m.hist[pass];
       int x[8], sum = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += x[e] = m.tot[255 - 8 * lane - e];
+      for (int e = 0; e < 8; ++e) sum += x[e] = tot[255 - 8 * lane - e];
       int inc = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -119,17 +143,12 @@ __device__ __forceinline__ void choose_top(int lo, int hi, int want, Key key, Ch
     left = m.left;
     if (m.done) break;
   }
-  // Keys above the boundary, and the first `left` on it: counted per warp over
-  // its own run of keys, then placed.
-  const int run = ((part.b - part.a + THREADS - 1) / THREADS) * 32;
-  const int wa = min(part.b, part.a + warp * run), wb = min(part.b, wa + run);
+  // Keys above the boundary, and the first `left` on it: counted per run, then placed.
   int above = 0, tie = 0;
-#pragma unroll 4
-  for (int i = wa; i < wb; i += 32) {
-    const uint32_t k = i + lane < wb ? key(i + lane) & mask : 0u;
-    above += __popc(__ballot_sync(0xffffffffu, i + lane < wb && k > prefix));
-    tie += __popc(__ballot_sync(0xffffffffu, i + lane < wb && k == prefix));
-  }
+  each([&](uint32_t k, int, bool in) {
+    above += __popc(__ballot_sync(0xffffffffu, in && (k & mask) > prefix));
+    tie += __popc(__ballot_sync(0xffffffffu, in && (k & mask) == prefix));
+  });
   if (lane == 0) {
     m.above[warp] = above;
     m.tie[warp] = tie;
@@ -155,22 +174,27 @@ __device__ __forceinline__ void choose_top(int lo, int hi, int want, Key key, Ch
   }
   if (size > 1) ptx::cluster_sync();
   else __syncthreads();
-  int na = m.above[warp], nt = m.tie[warp];      // before this warp's run
-  for (int r = 0; r < rank; ++r) {
-    na += ptx::ld_cluster(ptx::smem_addr(&m.sum[0]), r);
-    nt += ptx::ld_cluster(ptx::smem_addr(&m.sum[1]), r);
+  // Before this warp's run: the runs before it, and the CTAs before this one (a lane each).
+  int na = 0, nt = 0;
+  if (size > 1) {
+    if (lane < rank) {
+      na = ptx::ld_cluster(ptx::smem_addr(&m.sum[0]), lane);
+      nt = ptx::ld_cluster(ptx::smem_addr(&m.sum[1]), lane);
+    }
+    na = __reduce_add_sync(0xffffffffu, na);
+    nt = __reduce_add_sync(0xffffffffu, nt);
   }
-#pragma unroll 2
-  for (int i = wa; i < wb; i += 32) {
-    const uint32_t k = i + lane < wb ? key(i + lane) & mask : 0u;
-    const bool is_above = i + lane < wb && k > prefix, is_tie = i + lane < wb && k == prefix;
+  na += m.above[warp];
+  nt += m.tie[warp];
+  each([&](uint32_t k, int i, bool in) {
+    const bool is_above = in && (k & mask) > prefix, is_tie = in && (k & mask) == prefix;
     const uint32_t ba = __ballot_sync(0xffffffffu, is_above), bt = __ballot_sync(0xffffffffu, is_tie);
     const uint32_t low = (1u << lane) - 1u;
     const int ta = na + __popc(ba & low), tt = nt + __popc(bt & low);
-    if (is_above || (is_tie && tt < left)) emit(ta + min(tt, left), i + lane);
+    if (is_above || (is_tie && tt < left)) emit(ta + min(tt, left), i);
     na += __popc(ba);
     nt += __popc(bt);
-  }
+  });
 }
 
 // CTAs per problem: so many that each has `least` scores, and the grid stays within about one CTA per SM.

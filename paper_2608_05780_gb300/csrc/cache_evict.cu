@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(kChooseThreads) cache_evict_choose_kernel(cons
   for (int i = first; i < recent; i += step) put(count - recent + i, len - recent + i);
   for (int i = count + first; i < L.budget; i += step) kept[i] = -1;
   for (int64_t i = count + first; i < L.acc_out_len; i += step) out[i] = 0.f;
-  choose_top<kChooseThreads>(sink, len - recent, count - sink - recent, [&](int i) { return order_key(__ldg(acc + i)); }, mem,
+  choose_top<kChooseThreads, 8>(sink, len - recent, count - sink - recent, [&](int i) { return order_key(__ldg(acc + i)); }, mem,
              [&](int place, int i) { put(sink + place, i); });
   if (first == 0) L.out_lens[b * L.out.ls[0] + h * L.out.ls[1]] = count;
   if (size > 1) ptx::cluster_sync();
@@ -64,7 +64,7 @@ struct KeptTokens {
 };
 
 template <class T, int D>
-__global__ void __launch_bounds__(kPageThreads) cache_evict_copy_kernel(const __grid_constant__ CacheEvictLaunch L) {
+__global__ void __launch_bounds__(kPageThreads, kPageBlocks) cache_evict_copy_kernel(const __grid_constant__ CacheEvictLaunch L) {
   const int h = blockIdx.y, b = blockIdx.z;
   ptx::grid_wait();
   ptx::grid_launch_next();

@@ -9,9 +9,10 @@
 //               in K stage n % 4, S buffer n % 4 and goes to group n % 4
 //   warp 16     K pages by TMA, four stages
 //   warp 17     the queries' tiles (up to 128 rows), three stages, read once per
-//               four units
-//   warp 18     the MMAs: tile by tile, for each the four units
-//   warp 19     each tile's -LSE log2e, beside it in its stage
+//               four units, each with its rows' -LSE log2e
+//   warps 18-19 the MMAs: tile by tile, for each the four units, every other one
+//               each (issuing blocks while the tensor pipe is busy: one warp's
+//               waits fall into the other's products)
 // Few rows (decoding) leave the K stream as the bound; with many a tile's
 // 128 x 128 products and exponentials are, and a query tile loaded once per four
 // units keeps its traffic (32 KB for four products) out of the way.
@@ -27,8 +28,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKeys = 128;
 constexpr int kGroups = 4;
 constexpr int kKeyWarps = kGroups * 4;
-constexpr int kWarpK = kKeyWarps, kWarpQ = kWarpK + 1, kWarpMma = kWarpK + 2, kWarpLse = kWarpK + 3;
-constexpr int kThreads = 32 * (kKeyWarps + 4);
+constexpr int kWarpK = kKeyWarps, kWarpQ = kWarpK + 1, kWarpMma = kWarpK + 2;
+constexpr int kMmaWarps = 2;
+constexpr int kThreads = 32 * (kKeyWarps + 2 + kMmaWarps);
 constexpr int QS = 3;
 
 template <int D>
@@ -42,7 +44,7 @@ struct EvCfg {
   static constexpr int OFF_PART = OFF_LSE + QS * 128 * 4;    // [QS] whether some row of the tile does not count
   static constexpr int OFF_BAR = OFF_PART + 16;
   static constexpr int B_KF = 0, B_KE = B_KF + kGroups, B_QF = B_KE + kGroups, B_QE = B_QF + QS, B_SF = B_QE + QS,
-                       B_SE = B_SF + kGroups, B_DRAIN = B_SE + kGroups, N_BARS = B_DRAIN + 1;
+                       B_SE = B_SF + kGroups, B_DRAIN = B_SE + kGroups, N_BARS = B_DRAIN + kMmaWarps;
   static constexpr int OFF_MISC = OFF_BAR + N_BARS * 8;      // TMEM address, abort flag, split scratch
   static constexpr int SMEM_USED = OFF_MISC + 8 + 40 * 4 + 1024;
   static constexpr int SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA per SM: TMEM is taken whole
@@ -81,7 +83,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::N_BARS; ++i)
       ptx::mbar_init(bar(i), i >= C::B_QF && i < C::B_QF + QS                ? 2u        // the copy and the LSE warp
-                             : i >= C::B_QE && i < C::B_QE + QS              ? 1u + kKeyWarps
+                             : i >= C::B_QE && i < C::B_QE + QS              ? kMmaWarps + kKeyWarps + 0u
                              : i >= C::B_SE && i < C::B_SE + kGroups         ? 4u
                                                                              : 1u);
     *abort_flag = 0;
@@ -126,32 +128,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
     const volatile int never = 0;                // no copy in flight at exit
     for (uint32_t i = 0; i < kGroups && i < n; ++i)
       ptx::mbar_wait(bar(C::B_KF + (n - 1 - i) % kGroups), ((n - 1 - i) / kGroups) & 1, &never, kWaitTimeoutNs);
-  } else if (warp == kWarpQ) {
-    const uint64_t pol = ptx::l2_policy_evict_last();
-    uint32_t n = 0;
-    while (ok && walk.next(L.c, 1, uc, s, L.status))
-      for (int t = s.t0; ok && t < s.t1; t += kGroups)
-        for (int q = 0; q < n_tiles; ++q, ++n) {
-          const int st = n % QS;
-          if (n >= QS && !warp_wait(bar(C::B_QE + st), (n / QS - 1) & 1, abort_flag)) {
-            ok = false;
-            break;
-          }
-          if (lane == 0) {
-            ptx::mbar_arrive_expect_tx(bar(C::B_QF + st), C::KB * L.qt.rows * 128);
-            for (int kb = 0; kb < C::KB; ++kb)
-              ptx::tma_load_page(sbase + C::OFF_Q + st * C::TILE + kb * C::BLOCK, &L.tm_q, bar(C::B_QF + st), L.q_perm,
-                                 kb * 64, q * L.qt.tokens, s.h * L.d.gq, s.b, pol);
-          }
-          __syncwarp();
-        }
-    if (!ok && lane == 0) record_timeout(abort_flag, L.status);
-    // Every tile issued has landed at exit (its phase also needs the LSE warp's arrival, which may be
-    // missing after a failure: then the wait ends by its limit).
-    const volatile int never = 0;
-    for (uint32_t i = 0; i < QS && i < n; ++i)
-      ptx::mbar_wait(bar(C::B_QF + (n - 1 - i) % QS), ((n - 1 - i) / QS) & 1, &never, kWaitTimeoutNs);
-  } else if (warp == kWarpMma) {
+  } else if (warp >= kWarpMma) {
+    const int me_w = warp - kWarpMma;            // the units n with n % 2 == me_w
     const int n_cols = (L.qt.rows + 15) & ~15;
     const uint32_t idesc = (1u << 4) | (T::kFormat << 7) | (T::kFormat << 10) | (static_cast<uint32_t>(n_cols >> 3) << 17) |
                            (static_cast<uint32_t>(kKeys >> 4) << 24);
@@ -167,6 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
           ok = warp_wait(bar(C::B_QF + qs), (nq / QS) & 1, abort_flag);
           for (int i = 0; ok && i < count; ++i) {
             const uint32_t st = (n + i) % kGroups;
+            if (static_cast<int>(st % kMmaWarps) != me_w) continue;
             // A group's first step finds its buffer free (parity 1 of a fresh barrier passes).
             ok = (q > 0 || warp_wait(bar(C::B_KF + st), ((n + i) / kGroups) & 1, abort_flag)) &&
                  warp_wait(bar(C::B_SE + st), ((se >> st) & 1) ^ 1, abort_flag);
@@ -186,10 +165,16 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
               }
               ptx::mma_commit(bar(C::B_SF + st));
               if (q + 1 == n_tiles) ptx::mma_commit(bar(C::B_KE + st));
-              if (i + 1 == count) ptx::mma_commit(bar(C::B_QE + qs));
             }
             __syncwarp();
             issued = true;
+            ok = same;
+          }
+          // The tile is free once this warp's products with it are done (at once where it had none).
+          if (ok) {
+            if (ptx::elect_one(leader)) ptx::mma_commit(bar(C::B_QE + qs));
+            same = same && (first_leader < 0 || static_cast<int>(leader) == first_leader);
+            __syncwarp();
             ok = same;
           }
         }
@@ -199,14 +184,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
       if (lane == 0) record_timeout(abort_flag, L.status);
       if (issued && lane == first_leader) {      // every MMA ends before TMEM is released
         const volatile int never = 0;
-        ptx::mma_commit(bar(C::B_DRAIN));
-        ptx::mbar_wait(bar(C::B_DRAIN), 0, &never, kWaitTimeoutNs);
+        ptx::mma_commit(bar(C::B_DRAIN + me_w));
+        ptx::mbar_wait(bar(C::B_DRAIN + me_w), 0, &never, kWaitTimeoutNs);
       }
     }
     __syncwarp();
-  } else if (warp == kWarpLse) {
+  } else if (warp == kWarpQ) {
     // -LSE log2e per row of a tile, -inf for a row that does not count (those add
     // 0; their queries may be anything, so that the tile is marked).
+    const uint64_t pol = ptx::l2_policy_evict_last();
     uint32_t n = 0;
     while (ok && walk.next(L.c, 1, uc, s, L.status)) {
       const int drafted = drafted_tokens(L.d, s.b);
@@ -231,6 +217,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
             ok = false;
             break;
           }
+          if (lane == 0) {
+            ptx::mbar_arrive_expect_tx(bar(C::B_QF + st), C::KB * L.qt.rows * 128);
+            for (int kb = 0; kb < C::KB; ++kb)
+              ptx::tma_load_page(sbase + C::OFF_Q + st * C::TILE + kb * C::BLOCK, &L.tm_q, bar(C::B_QF + st), L.q_perm,
+                                 kb * 64, q * L.qt.tokens, s.h * L.d.gq, s.b, pol);
+          }
+          __syncwarp();
 #pragma unroll
           for (int i = 0; i < 4; ++i) lse_s[st * 128 + i * 32 + lane] = v[i];
           if (lane == 0) part_s[st] = part;
@@ -239,6 +232,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
         }
     }
     if (!ok && lane == 0) record_timeout(abort_flag, L.status);
+    const volatile int never = 0;                // no copy in flight at exit
+    for (uint32_t i = 0; i < QS && i < n; ++i)
+      ptx::mbar_wait(bar(C::B_QF + (n - 1 - i) % QS), ((n - 1 - i) / QS) & 1, &never, kWaitTimeoutNs);
   } else {
     const int grp = warp >> 2, key = threadIdx.x & 127;
     const uint32_t tS = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + grp * 128;

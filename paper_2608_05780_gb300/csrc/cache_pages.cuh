@@ -6,6 +6,7 @@
 namespace evisel {
 
 constexpr int kPageThreads = 256;
+constexpr int kAtOnce = 2, kPageBlocks = 5;       // tokens of a thread in flight, blocks per SM
 
 // Writes the page's slots at positions [src.first(), src.end()) and, with
 // `mean`, the mean of all its keys before src.end() (the older ones read back
@@ -23,13 +24,13 @@ __device__ __forceinline__ void fill_page(const CacheView& c, void* k_out, void*
   uint16_t* v = static_cast<uint16_t*>(v_out) + id * c.vs[0] + h * c.vs[1];
   const int x = threadIdx.x % LANES, grp = threadIdx.x / LANES;
   float sum[8] = {};
-  // Four tokens a thread at a time: their places, then all loads, then all stores.
-  for (int base = p0 + grp; base < p1; base += 4 * GROUPS) {
-    const uint4 *ks[4], *vs[4];
-    uint4 key[4], value[4];
-    bool in[4], fresh[4];
+  // kAtOnce tokens a thread at a time: their places, then all loads, then all stores.
+  for (int base = p0 + grp; base < p1; base += kAtOnce * GROUPS) {
+    const uint4 *ks[kAtOnce], *vs[kAtOnce];
+    uint4 key[kAtOnce], value[kAtOnce];
+    bool in[kAtOnce], fresh[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kAtOnce; ++i) {
       const int pos = base + i * GROUPS;
       fresh[i] = pos < p1 && pos >= src.first();
       in[i] = fresh[i] || (pos < p1 && mean);    // an older token is read for the mean only
@@ -37,12 +38,12 @@ __device__ __forceinline__ void fill_page(const CacheView& c, void* k_out, void*
       if (fresh[i]) src.rows(pos, ks[i], vs[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kAtOnce; ++i) {
       key[i] = in[i] ? ks[i][x] : make_uint4(0, 0, 0, 0);
       if (fresh[i]) value[i] = vs[i][x];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kAtOnce; ++i) {
       const int slot = base + i * GROUPS - p0;
       if (fresh[i]) {
         reinterpret_cast<uint4*>(k + slot * c.ks[2])[x] = key[i];

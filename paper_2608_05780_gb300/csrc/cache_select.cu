@@ -20,7 +20,7 @@ constexpr float kNone = -INFINITY;
 template <class T, int D>
 __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __grid_constant__ CacheSelectLaunch L) {
   __shared__ ChooseMem mem;
-  __shared__ float score[kMaxPages];             // of the CTA's part, from its first page on
+  __shared__ uint32_t score[kMaxPages];          // order keys of the CTA's part, from its first page on
   ptx::grid_wait();
   ptx::grid_launch_next();
   constexpr int J = D / 32;                      // 16-byte chunks of a row per lane
@@ -35,9 +35,16 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
   const ChoosePart part(lo, hi, rank, size);
 
   if (want > 0) {
-    const int rows = drafted_tokens(L.d, b) * L.d.gq;
+    const int rows = drafted_tokens(L.d, b) * L.d.gq, n_part = part.b - part.a;
+    for (int i = threadIdx.x; i < n_part; i += kChooseThreads) score[i] = order_key(-INFINITY);
+    __syncthreads();
+    // Tasks of 16 pages against a share of the rows, so many shares that every warp has a task.
+    const int page_tiles = (n_part + 15) / 16, row_tiles = (rows + 7) / 8;
+    const int shares = page_tiles > 0 ? min(row_tiles, (kChooseThreads / 32 + page_tiles - 1) / page_tiles) : 0;
     const uint16_t* q0 = static_cast<const uint16_t*>(L.d.q) + b * L.d.qs[0] + h * L.d.gq * L.d.qs[2] + fc;
-    for (int p0 = part.a + warp * 16; p0 < part.b; p0 += kChooseThreads / 32 * 16) {
+    for (int task = warp; task < page_tiles * shares; task += kChooseThreads / 32) {
+      const int p0 = part.a + task / shares * 16, share = task % shares;
+      const int first_row = row_tiles * share / shares * 8, end_row = min(rows, row_tiles * (share + 1) / shares * 8);
       uint4 a[2][J];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -49,7 +56,7 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
       }
       float top[2] = {kNone, kNone};
 #pragma unroll 2
-      for (int r0 = 0; r0 < rows; r0 += 8) {
+      for (int r0 = first_row; r0 < end_row; r0 += 8) {
         const int r = min(r0 + fr, rows - 1), t = r / L.d.gq, g = r % L.d.gq;   // past the rows: the last one again
         const uint4* src = reinterpret_cast<const uint4*>(q0 + t * L.d.qs[1] + g * L.d.qs[2]);
         float c[4] = {};
@@ -69,7 +76,8 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
         top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
         top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
         const int p = p0 + fr + 8 * half;
-        if ((lane & 3) == 0 && p < part.b) score[p - part.a] = top[half];
+        // (the order of the maxima does not matter: the keys are whole numbers)
+        if ((lane & 3) == 0 && p < part.b) atomicMax(&score[p - part.a], order_key(top[half]));
       }
     }
     __syncthreads();
@@ -84,7 +92,7 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
   for (int i = first; i < sink; i += step) put(i, i);
   for (int i = first; i < recent; i += step) put(count - recent + i, n - recent + i);
   for (int i = count + first; i < L.n_select; i += step) L.pages[at + i] = L.sel_table[at + i] = -1;
-  choose_top<kChooseThreads>(lo, hi, want, [&](int i) { return order_key(score[i - part.a]); }, mem,
+  choose_top<kChooseThreads, 4>(lo, hi, want, [&](int i) { return score[i - part.a]; }, mem,
              [&](int place, int i) { put(sink + place, i); });
   if (first == 0) L.sel_lens[problem] = count > 0 ? (count - 1) * L.c.page + (len - (n - 1) * L.c.page) : 0;
   if (size > 1) ptx::cluster_sync();
