@@ -41,15 +41,46 @@ struct EvCfg {
   static constexpr int OFF_K = 0;
   static constexpr int OFF_Q = kGroups * TILE;
   static constexpr int OFF_LSE = OFF_Q + QS * TILE;          // [QS][128] fp32
-  static constexpr int OFF_PART = OFF_LSE + QS * 128 * 4;    // [QS] whether some row of the tile does not count
-  static constexpr int OFF_BAR = OFF_PART + 16;
+  static constexpr int OFF_BAR = OFF_LSE + QS * 128 * 4;
   static constexpr int B_KF = 0, B_KE = B_KF + kGroups, B_QF = B_KE + kGroups, B_QE = B_QF + QS, B_SF = B_QE + QS,
-                       B_SE = B_SF + kGroups, B_DRAIN = B_SE + kGroups, N_BARS = B_DRAIN + kMmaWarps;
+                       B_SE = B_SF + kGroups, B_DRAIN = B_SE + kGroups, B_QL = B_DRAIN + kMmaWarps, N_BARS = B_QL + QS;
   static constexpr int OFF_MISC = OFF_BAR + N_BARS * 8;      // TMEM address, abort flag, split scratch
   static constexpr int SMEM_USED = OFF_MISC + 8 + 40 * 4 + 1024;
   static constexpr int SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA per SM: TMEM is taken whole
   static_assert(SMEM <= 232448, "shared memory budget");
 };
+
+// One key's sum over the rows that count, from global memory. A zeroed row's
+// product with a non-finite key is NaN, so that a sum that came out NaN is formed
+// again here; and all of them where no TMA map can describe the queries.
+template <class T, int D>
+__device__ __noinline__ float counted_sum(const CacheEvidenceLaunch& L, int b, int h, int key) {
+  const int64_t id = cache_page(L.c, b, h, key >> L.c.log_page, L.status);
+  const uint4* k = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.c.k) + id * L.c.ks[0] + h * L.c.ks[1] +
+                                                  (key & (L.c.page - 1)) * L.c.ks[2]);
+  const int drafted = drafted_tokens(L.d, b);
+  float sum = 0.f;
+  for (int t = 0; t < drafted; ++t) {
+    if (L.use && !__ldg(L.use + static_cast<int64_t>(b) * L.d.tokens + t)) continue;
+    for (int g = 0; g < L.d.gq && !isnan(sum); ++g) {
+      const int head = h * L.d.gq + g;
+      const float lse = __ldg(L.lse + (static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t);
+      if (lse == -INFINITY) continue;
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.q) + b * L.d.qs[0] +
+                                                      t * L.d.qs[1] + head * L.d.qs[2]);
+      float s = 0.f;
+      for (int i = 0; i < D / 8; ++i) {
+        float x[8], y[8];
+        unpack8<T>(__ldg(k + i), x);
+        unpack8<T>(__ldg(q + i), y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+      }
+      sum += ptx::ex2(fmaf(s, L.d.scale_log2, -kLog2e * lse));
+    }
+  }
+  return sum;
+}
 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __grid_constant__ CacheEvidenceLaunch L) {
@@ -62,7 +93,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
   int* scratch = reinterpret_cast<int*>(smem + C::OFF_MISC + 8);
   float* lse_s = reinterpret_cast<float*>(smem + C::OFF_LSE);
-  volatile int* part_s = reinterpret_cast<volatile int*>(smem + C::OFF_PART);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -190,49 +220,100 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
     }
     __syncwarp();
   } else if (warp == kWarpQ) {
-    // -LSE log2e per row of a tile, -inf for a row that does not count (those add
-    // 0; their queries may be anything, so that the tile is marked).
+    // A tile, and -LSE log2e per row, -inf for a row that does not count. Such a
+    // row adds 0 if its logits are finite: its query, which may be anything, is
+    // zeroed once it has landed (a test per pair in the sums took 12% of the
+    // kernel). A tile's loads are in flight before the tile before it is done, and
+    // without branches (serialised, they were the kernel's bound).
     const uint64_t pol = ptx::l2_policy_evict_last();
-    uint32_t n = 0;
+    int tok_of[4], head_of[4];                   // of this lane's rows, from the tile's first token and head
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = i * 32 + lane;
+      tok_of[i] = L.qt.head_inner ? r / L.d.gq : r % L.qt.tokens;
+      head_of[i] = L.qt.head_inner ? r % L.d.gq : r / L.qt.tokens;
+    }
+    struct Rows {
+      float lse[4];
+      uint8_t use[4];
+    };
+    int drafted = 0;
+    auto load = [&](int q, Rows& x) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int tok = min(q * L.qt.tokens + tok_of[i], L.d.tokens - 1), g = min(head_of[i], L.d.gq - 1);
+        const int64_t row = static_cast<int64_t>(s.b) * L.d.tokens + tok;
+        x.use[i] = L.use ? __ldg(L.use + row) : 1;
+        x.lse[i] = __ldg(L.lse + static_cast<int64_t>(s.h * L.d.gq + g) * L.c.batch * L.d.tokens + row);
+      }
+    };
+    uint32_t n = 0, ql = 0;                      // tiles; parity of the waits for landed ones, a bit per stage
+    int open = -1;                               // stage of a tile whose rows are still to be zeroed,
+    uint32_t zero = 0;                           // bit i: this lane's i-th row of it
+    auto close = [&]() {
+      if (open < 0) return;
+      ok = ok && warp_wait(bar(C::B_QL + open), (ql >> open) & 1, abort_flag);
+      ql ^= 1u << open;
+      for (int i = 0; i < 4; ++i)
+        if ((zero >> i) & 1)
+#pragma unroll
+          for (int x = 0; x < C::KB * 8; ++x)
+            *reinterpret_cast<uint4*>(smem + C::OFF_Q + open * C::TILE + (x / 8) * C::BLOCK + (i * 32 + lane) * 128 + (x % 8) * 16) =
+                make_uint4(0, 0, 0, 0);
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar(C::B_QF + open));
+      open = -1;
+    };
     while (ok && walk.next(L.c, 1, uc, s, L.status)) {
-      const int drafted = drafted_tokens(L.d, s.b);
+      drafted = drafted_tokens(L.d, s.b);
+      Rows now, next;
+      load(0, next);
       for (int t = s.t0; ok && t < s.t1; t += kGroups)
-        for (int q = 0; q < n_tiles; ++q, ++n) {
+        for (int q = 0; ok && q < n_tiles; ++q, ++n) {
           const int st = n % QS;
+          now = next;
+          if (n_tiles > 1) load(q + 1 < n_tiles ? q + 1 : 0, next);
           float v[4];
-          bool part = false;
+          uint32_t drop = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int r = i * 32 + lane;
-            const int tok = q * L.qt.tokens + (L.qt.head_inner ? r / L.d.gq : r % L.qt.tokens);
-            const int head = s.h * L.d.gq + (L.qt.head_inner ? r % L.d.gq : r / L.qt.tokens);
-            const bool in = r < L.qt.rows && tok < drafted &&
-                            (!L.use || __ldg(L.use + static_cast<int64_t>(s.b) * L.d.tokens + tok) != 0);
-            const float lse = in ? __ldg(L.lse + (static_cast<int64_t>(head) * L.c.batch + s.b) * L.d.tokens + tok) : -INFINITY;
-            v[i] = lse == -INFINITY ? -INFINITY : -kLog2e * lse;
-            part = part || (lse == -INFINITY && r < L.qt.rows);
+            const int tok = q * L.qt.tokens + tok_of[i];
+            const bool row = i * 32 + lane < L.qt.rows;
+            const bool in = row && tok < drafted && now.use[i] != 0 && now.lse[i] != -INFINITY;
+            v[i] = in ? -kLog2e * now.lse[i] : -INFINITY;
+            drop |= static_cast<uint32_t>(row && !in) << i;
           }
-          part = __any_sync(0xffffffffu, part);
-          if (n >= QS && !warp_wait(bar(C::B_QE + st), (n / QS - 1) & 1, abort_flag)) {
-            ok = false;
-            break;
+          const bool part = __any_sync(0xffffffffu, drop != 0);
+          if (n >= QS) {
+            if (!__all_sync(0xffffffffu, ptx::mbar_test(bar(C::B_QE + st), (n / QS - 1) & 1))) close();
+            ok = ok && warp_wait(bar(C::B_QE + st), (n / QS - 1) & 1, abort_flag);
+            if (!ok) break;
           }
           if (lane == 0) {
-            ptx::mbar_arrive_expect_tx(bar(C::B_QF + st), C::KB * L.qt.rows * 128);
+            const uint32_t landed = bar((part ? C::B_QL : C::B_QF) + st);
+            ptx::mbar_arrive_expect_tx(landed, C::KB * L.qt.rows * 128);
             for (int kb = 0; kb < C::KB; ++kb)
-              ptx::tma_load_page(sbase + C::OFF_Q + st * C::TILE + kb * C::BLOCK, &L.tm_q, bar(C::B_QF + st), L.q_perm,
-                                 kb * 64, q * L.qt.tokens, s.h * L.d.gq, s.b, pol);
+              ptx::tma_load_page(sbase + C::OFF_Q + st * C::TILE + kb * C::BLOCK, &L.tm_q, landed, L.q_perm, kb * 64,
+                                 q * L.qt.tokens, s.h * L.d.gq, s.b, pol);
           }
           __syncwarp();
 #pragma unroll
           for (int i = 0; i < 4; ++i) lse_s[st * 128 + i * 32 + lane] = v[i];
-          if (lane == 0) part_s[st] = part;
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar(C::B_QF + st));
+          close();
+          if (part) {
+            open = st;
+            zero = drop;
+          }
         }
     }
+    close();
     if (!ok && lane == 0) record_timeout(abort_flag, L.status);
-    const volatile int never = 0;                // no copy in flight at exit
+    // No copy in flight at exit: after a failure the last tiles' phases may never
+    // complete (their other arrival is missing), and these waits end by their limit.
+    const volatile int never = 0;
     for (uint32_t i = 0; i < QS && i < n; ++i)
       ptx::mbar_wait(bar(C::B_QF + (n - 1 - i) % QS), ((n - 1 - i) / QS) & 1, &never, kWaitTimeoutNs);
   } else {
@@ -261,20 +342,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
               ptx::tc_fence_after();
               const float* lrow = lse_s + qs * 128;
               const int valid = L.qt.head_inner ? min(L.qt.rows, (L.d.tokens - q * L.qt.tokens) * L.d.gq) : L.qt.rows;
-              const bool part = part_s[qs] != 0;
               auto add4 = [&](const uint32_t* r, const float4& nl, int e) {
                 float x0, x1, x2, x3;
                 ptx::unf2(ptx::fma2(ptx::f2(__uint_as_float(r[0]), __uint_as_float(r[1])), scale2, ptx::f2(nl.x, nl.y)), x0, x1);
                 ptx::unf2(ptx::fma2(ptx::f2(__uint_as_float(r[2]), __uint_as_float(r[3])), scale2, ptx::f2(nl.z, nl.w)), x2, x3);
                 a2[(2 * e) & 3] = ptx::add2(a2[(2 * e) & 3], ptx::f2(ptx::ex2(x0), ptx::ex2(x1)));
                 a2[(2 * e + 1) & 3] = ptx::add2(a2[(2 * e + 1) & 3], ptx::f2(ptx::ex2(x2), ptx::ex2(x3)));
-              };
-              // A row that does not count adds 0 whatever its logit is.
-              auto drop4 = [&](uint32_t* r, const float4& nl) {
-                if (nl.x == -INFINITY) r[0] = 0u;
-                if (nl.y == -INFINITY) r[1] = 0u;
-                if (nl.z == -INFINITY) r[2] = 0u;
-                if (nl.w == -INFINITY) r[3] = 0u;
               };
               int c0 = 0;
 #pragma unroll 1
@@ -285,10 +358,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
 #pragma unroll
                 for (int e = 0; e < 8; ++e) l4[e] = reinterpret_cast<const float4*>(lrow + c0)[e];
                 ptx::tmem_wait_ld();
-                if (part) {
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) drop4(r + 4 * e, l4[e]);
-                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) add4(r + 4 * e, l4[e], e);
               }
@@ -301,8 +370,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
 #pragma unroll
                 for (int e = 0; e < 4; ++e) l4[e] = reinterpret_cast<const float4*>(lrow + c0)[e];
                 ptx::tmem_wait_ld();
+                if (c0 + 16 > valid) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) drop4(r + 4 * e, l4[e]);
+                  for (int e = 1; e < 16; ++e)
+                    if (c0 + e >= valid) r[e] = 0u;
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) add4(r + 4 * e, l4[e], e);
               }
@@ -317,7 +389,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
         float s0, s1, s2, s3;
         ptx::unf2(ptx::add2(a2[0], a2[1]), s0, s1);
         ptx::unf2(ptx::add2(a2[2], a2[3]), s2, s3);
-        if (ok && live) *dst = old + ((s0 + s1) + (s2 + s3));
+        float sum = (s0 + s1) + (s2 + s3);
+        if (live && isnan(sum)) sum = counted_sum<T, D>(L, s.b, s.h, static_cast<int>(pos));
+        if (ok && live) *dst = old + sum;
       }
     if (!ok && lane == 0) record_timeout(abort_flag, L.status);
   }
@@ -330,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_evidence_kernel(const __gri
 }
 
 // Queries that a TMA map cannot describe (a dimension repeated by a stride of 0),
-// or none at all: one thread per key, its key in registers, the rows' queries by broadcast loads.
+// or none at all: one thread per key.
 constexpr int kPlainThreads = 128;
 
 template <class T, int D>
@@ -342,34 +416,7 @@ __global__ void __launch_bounds__(kPlainThreads) cache_evidence_plain_kernel(con
     len = static_cast<int>(L.acc_len);
   }
   if (key >= len) return;
-  const int id = cache_page(L.c, b, h, key >> L.c.log_page, L.status);
-  const uint4* k = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.c.k) + id * L.c.ks[0] + h * L.c.ks[1] +
-                                                  (key & (L.c.page - 1)) * L.c.ks[2]);
-  uint4 kr[D / 8];
-#pragma unroll
-  for (int i = 0; i < D / 8; ++i) kr[i] = __ldg(k + i);
-  const int drafted = drafted_tokens(L.d, b);
-  float sum = 0.f;
-  for (int t = 0; t < drafted; ++t) {
-    if (L.use && !__ldg(L.use + static_cast<int64_t>(b) * L.d.tokens + t)) continue;
-    for (int g = 0; g < L.d.gq; ++g) {
-      const int head = h * L.d.gq + g;
-      const float lse = __ldg(L.lse + (static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t);
-      if (lse == -INFINITY) continue;
-      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.q) + b * L.d.qs[0] +
-                                                      t * L.d.qs[1] + head * L.d.qs[2]);
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        float x[8], y[8];
-        unpack8<T>(kr[i], x);
-        unpack8<T>(__ldg(q + i), y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
-      }
-      sum += ptx::ex2(fmaf(s, L.d.scale_log2, -kLog2e * lse));
-    }
-  }
+  const float sum = counted_sum<T, D>(L, b, h, key);
   float* dst = L.acc + (static_cast<int64_t>(b) * L.c.hkv + h) * L.acc_len + key;
   *dst = L.accumulate ? *dst + sum : sum;
 }
