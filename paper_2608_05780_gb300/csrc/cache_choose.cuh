@@ -48,9 +48,9 @@ struct ChooseMem {
 
 // A CTA's part [a, b) of [lo, hi): whole groups of 32 in order of rank.
 struct ChoosePart {
-  int a, b;
+  int a, b, chunk;
   __device__ __forceinline__ ChoosePart(int lo, int hi, int rank, int size) {
-    const int chunk = (max(hi - lo, 0) + 32 * size - 1) / (32 * size) * 32;
+    chunk = (max(hi - lo, 0) + 32 * size - 1) / (32 * size) * 32;
     a = min(hi, lo + rank * chunk);
     b = min(hi, a + chunk);
   }
@@ -68,26 +68,29 @@ __device__ __forceinline__ int sum_cluster(const int* p, int size) {
 // lower i): emit(rank, i) for each, ranks ascending with i. Every thread of every
 // CTA of the cluster calls, with the same lo, hi and want; key(i) is asked for
 // the i of the CTA's own ChoosePart only. The last cluster barrier is the
-// caller's: no CTA may leave before the others have read its sums. THREADS: the block's.
+// caller's: no CTA may leave before the others have read its sums. THREADS: the
+// block's; rank, size: the CTA's place in the cluster (0, 1: the block by itself).
+// meanwhile(): what the caller does while the keys are on their way.
 // A warp owns a run of the part; a thread keeps up to ITEMS keys of its run in
 // registers, so that a part of up to ITEMS * THREADS scores is read once.
-template <int THREADS, int ITEMS, class Key, class Emit>
-__device__ __forceinline__ void choose_top(int lo, int hi, int want, Key key, ChooseMem& m, Emit emit) {
-  if (want <= 0) return;
-  const int rank = static_cast<int>(ptx::cluster_rank()), size = static_cast<int>(ptx::cluster_size());
+template <int THREADS, int ITEMS, class Key, class Emit, class Meanwhile>
+__device__ __forceinline__ void choose_top(int lo, int hi, int want, Key key, ChooseMem& m, Emit emit, int rank, int size,
+                                           Meanwhile meanwhile) {
+  if (want <= 0) {
+    meanwhile();
+    return;
+  }
   const ChoosePart part(lo, hi, rank, size);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int run = ((part.b - part.a + THREADS - 1) / THREADS) * 32;
   const int wa = min(part.b, part.a + warp * run), wb = min(part.b, wa + run);
   const bool held = run <= 32 * ITEMS;
   uint32_t keys[ITEMS];
-  if (held) {
+  if (held && wa < wb) {                         // (past the run its last key again: no branch between the loads)
 #pragma unroll
-    for (int it = 0; it < ITEMS; ++it) {
-      const int i = wa + 32 * it + lane;
-      keys[it] = i < wb ? key(i) : 0u;
-    }
+    for (int it = 0; it < ITEMS; ++it) keys[it] = key(min(wa + 32 * it + lane, wb - 1));
   }
+  meanwhile();
   // f(key, i, whether i is of the run) for the run's keys in order, 32 at a time.
   auto each = [&](auto f) {
     if (held) {

@@ -4,7 +4,9 @@
 // One launch, a cluster of CTAs per (sequence, KV head): each CTA forms the scores
 // of its part of the pages (16 pages against 8 rows per mma.sync, both read from
 // global memory 16 bytes a lane, the products' order along d permuted alike on
-// both sides) in shared memory, and the cluster chooses among them.
+// both sides) in shared memory, takes the others' over, chooses among all of them
+// and writes what falls into its part: one exchange, where a choice over the
+// cluster's histograms takes one per digit.
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -20,7 +22,7 @@ constexpr float kNone = -INFINITY;
 template <class T, int D>
 __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __grid_constant__ CacheSelectLaunch L) {
   __shared__ ChooseMem mem;
-  __shared__ uint32_t score[kMaxPages];          // order keys of the CTA's part, from its first page on
+  __shared__ uint32_t score[kMaxPages];          // order keys of the pages from lo on
   ptx::grid_wait();
   ptx::grid_launch_next();
   constexpr int J = D / 32;                      // 16-byte chunks of a row per lane
@@ -36,7 +38,7 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
 
   if (want > 0) {
     const int rows = drafted_tokens(L.d, b) * L.d.gq, n_part = part.b - part.a;
-    for (int i = threadIdx.x; i < n_part; i += kChooseThreads) score[i] = order_key(-INFINITY);
+    for (int i = threadIdx.x; i < n_part; i += kChooseThreads) score[part.a - lo + i] = order_key(-INFINITY);
     __syncthreads();
     // Tasks of 16 pages against a share of the rows, so many shares that every warp has a task.
     const int page_tiles = (n_part + 15) / 16, row_tiles = (rows + 7) / 8;
@@ -77,7 +79,14 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
         top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
         const int p = p0 + fr + 8 * half;
         // (the order of the maxima does not matter: the keys are whole numbers)
-        if ((lane & 3) == 0 && p < part.b) atomicMax(&score[p - part.a], order_key(top[half]));
+        if ((lane & 3) == 0 && p < part.b) atomicMax(&score[p - lo], order_key(top[half]));
+      }
+    }
+    if (size > 1) {
+      ptx::cluster_sync();
+      for (int i = threadIdx.x; i < hi - lo; i += kChooseThreads) {
+        const int owner = i / max(1, part.chunk);
+        if (owner != rank) score[i] = static_cast<uint32_t>(ptx::ld_cluster(ptx::smem_addr(&score[i]), owner));
       }
     }
     __syncthreads();
@@ -92,8 +101,10 @@ __global__ void __launch_bounds__(kChooseThreads) cache_select_kernel(const __gr
   for (int i = first; i < sink; i += step) put(i, i);
   for (int i = first; i < recent; i += step) put(count - recent + i, n - recent + i);
   for (int i = count + first; i < L.n_select; i += step) L.pages[at + i] = L.sel_table[at + i] = -1;
-  choose_top<kChooseThreads, 4>(lo, hi, want, [&](int i) { return score[i - part.a]; }, mem,
-             [&](int place, int i) { put(sink + place, i); });
+  choose_top<kChooseThreads, 4>(lo, hi, want, [&](int i) { return score[i - lo]; }, mem,
+                                [&](int place, int i) {
+                                  if (i >= part.a && i < part.b) put(sink + place, i);
+                                }, 0, 1, [] {});
   if (first == 0) L.sel_lens[problem] = count > 0 ? (count - 1) * L.c.page + (len - (n - 1) * L.c.page) : 0;
   if (size > 1) ptx::cluster_sync();
 }
