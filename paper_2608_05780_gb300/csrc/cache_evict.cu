@@ -80,7 +80,7 @@ template <class T, int D>
 cudaError_t launch_d(const CacheEvictLaunch& L, cudaStream_t stream) {
   const int problems = L.c.batch * L.c.hkv;
   const int64_t room = static_cast<int64_t>(L.c.max_pages) * L.c.page;
-  const int cluster = choose_cluster(problems, room < L.acc_len ? room : L.acc_len, 2048, sm_count());
+  const int cluster = choose_cluster(problems, room < L.acc_len ? room : L.acc_len, 4096, sm_count());
   const cudaError_t e = launch_clusters(cache_evict_choose_kernel, L, problems, kChooseThreads, cluster, stream);
   if (e != cudaSuccess) return e;
   return launch_after(cache_evict_copy_kernel<T, D>, dim3((L.budget + L.out.page - 1) / L.out.page, L.c.hkv, L.c.batch),
