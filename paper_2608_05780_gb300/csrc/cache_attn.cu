@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel
     *abort_flag = 0;
     ptx::fence_mbar_init();
   }
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && L.c.max_pages > 0) {   // (without any page there is no map)
     ptx::tma_prefetch_desc(&L.tm_k);
     ptx::tma_prefetch_desc(&L.tm_v);
   }

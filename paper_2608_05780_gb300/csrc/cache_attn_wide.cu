@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attn_wide_kernel(const __gr
   int* scratch = reinterpret_cast<int*>(smem + C::OFF_MISC + 8);
   const int warp = threadIdx.x >> 5;
 
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && L.c.max_pages > 0) {   // (without any page there is no map)
     ptx::tma_prefetch_desc(&L.tm_k);
     ptx::tma_prefetch_desc(&L.tm_v);
     ptx::tma_prefetch_desc(&L.tm_q);

@@ -34,6 +34,7 @@ constexpr int64_t kMaxStride = int64_t(1) << 38;   // elements: a TMA stride is 
 constexpr int kMaxDrafted = 1024;
 constexpr int kMaxGroup = 128;
 constexpr int kMaxSelectPages = 8192;
+constexpr int64_t kMaxUnits = int64_t(1) << 30;    // of work in a call: the kernels count them in 32 bits
 
 int check_strides(const int64_t* s, const int64_t* sizes, int n, const char* what) {
   for (int i = 0; i < n; ++i)
@@ -270,7 +271,7 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     L.box_rows = std::min(cache->page, L.key_tile);
     const int64_t problems = static_cast<int64_t>(cache->batch) * cache->hkv * L.row_tiles;
     const int64_t tiles = (static_cast<int64_t>(cache->max_pages) * cache->page + L.key_tile - 1) / L.key_tile;
-    if (problems * (tiles + L.lead) > INT32_MAX) return fail(EVISEL_EUNSUPPORTED, "too many units of work");
+    if (problems * (tiles + L.lead) > kMaxUnits) return fail(EVISEL_EUNSUPPORTED, "too many units of work");
     const size_t parts = static_cast<size_t>(L.n_ctas) + problems;
     const size_t ml_bytes = align_up(parts * L.tile_rows * sizeof(float2), 256);
     rc = ws_acquire(ws_inout);
@@ -312,7 +313,7 @@ int evisel_cache_evidence(const evisel_cache* cache, const evisel_draft* draft, 
     L.box_rows = std::min(cache->page, 128);
     L.qt = query_tile(cache, draft);
     L.has_q_map = draft->tokens > 0 && has_query_map(cache, draft);
-    if (static_cast<int64_t>(cache->batch) * cache->hkv * ((static_cast<int64_t>(cache->max_pages) * cache->page + 127) / 128) > INT32_MAX)
+    if (static_cast<int64_t>(cache->batch) * cache->hkv * ((static_cast<int64_t>(cache->max_pages) * cache->page + 127) / 128) > kMaxUnits)
       return fail(EVISEL_EUNSUPPORTED, "too many units of work");
     rc = ws_acquire(ws_inout);
     if (rc == EVISEL_OK && L.has_q_map) rc = encode_pages(&L.tm_k, &L.k_perm, cache->k, cache, cache->k_stride, L.box_rows);

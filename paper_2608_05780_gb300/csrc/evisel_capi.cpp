@@ -638,7 +638,14 @@ int launch_text_sums(evisel_ws* ws, float* tok, float* frame, int accumulate, co
 
 // What the paged-cache calls (evisel_cache.cpp) use of a workspace.
 namespace evisel {
-int ws_acquire(evisel_ws** inout) { return *inout ? EVISEL_OK : create_ws(inout); }
+int ws_acquire(evisel_ws** inout) {
+  if (!*inout) return create_ws(inout);
+  int device = -1;
+  const cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+  if (device != (*inout)->device) return fail(EVISEL_EINVAL, "the workspace belongs to another device");
+  return EVISEL_OK;
+}
 WsCache& ws_cache(evisel_ws* ws) { return ws->cache; }
 int* ws_status(evisel_ws* ws) { return ws->status; }
 cudaStream_t ws_last_stream(evisel_ws* ws) { return ws->last_stream; }
@@ -1200,7 +1207,7 @@ static const char kBuildIdString[] = "evisel-build-id:" EVISEL_BUILD_ID;
 const char* evisel_build_id(void) { return kBuildIdString + sizeof("evisel-build-id:") - 1; }
 
 int64_t evisel_workspace_bytes(const evisel_ws* ws) {
-  return ws ? static_cast<int64_t>(ws->arena_bytes) : 0;
+  return ws ? static_cast<int64_t>(ws->arena_bytes + ws->cache.bytes) : 0;
 }
 
 }  // extern "C"
