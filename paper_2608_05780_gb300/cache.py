@@ -64,7 +64,7 @@ class Cache:
     """
 
     __slots__ = ("k", "v", "k_mean", "device", "dtype", "batch", "hkv", "page", "head_dim", "max_tokens", "_pool",
-                 "_table", "_lens", "_packed")
+                 "_table", "_lens", "_chosen", "_packed")
 
     def __init__(self, k, v, table, lens, k_mean=None):
         c = _get()
@@ -96,34 +96,58 @@ class Cache:
         if not (ts[-1] == 1 or n <= 1):
             _refuse("table rows must be contiguous")
         pages, dtype, ks, vs, kp, vp, mp = self._pool
-        self._table, self._lens, self.batch, self.max_tokens = table, lens, batch, n * self.page
+        self._table, self._lens, self._chosen, self.batch, self.max_tokens = table, lens, None, batch, n * self.page
         self._packed = _CACHE.pack(batch, hkv, self.head_dim, self.page, pages, n, dtype, 0, *ks, *vs,
                                    ts[0], ts[1] if len(ts) == 3 else 0, ls[0], ls[1] if len(ls) == 2 else 0,
                                    kp, vp, table.data_ptr(), lens.data_ptr(), mp)
 
+    def _tensors(self):
+        if self._table is None:                  # a choice's: cut out of its buffer when somebody asks
+            rows, n = self.batch * self.hkv, self.max_tokens // self.page
+            self._table = self._chosen[:rows * n].view(self.batch, self.hkv, n)
+            self._lens = self._chosen[rows * n:].view(self.batch, self.hkv)
+        return self._table, self._lens
+
     @property
     def table(self):
-        return self._table
+        return self._tensors()[0]
 
     @table.setter
     def table(self, table):
-        self._set(table, self._lens)
+        self._set(table, self.lens)
 
     @property
     def lens(self):
-        return self._lens
+        return self._tensors()[1]
 
     @lens.setter
     def lens(self, lens):
-        self._set(self._table, lens)
+        self._set(self.table, lens)
 
-    def view(self, table, lens):
-        """The same pages under another table and lengths."""
+    def _same_pages(self):
         c = object.__new__(Cache)
         c.k, c.v, c.k_mean, c.device, c.dtype = self.k, self.v, self.k_mean, self.device, self.dtype
         c.hkv, c.page, c.head_dim, c._pool = self.hkv, self.page, self.head_dim, self._pool
+        return c
+
+    def view(self, table, lens):
+        """The same pages under another table and lengths."""
+        c = self._same_pages()
         c._set(table, lens)
         return c
+
+    def _choice(self, n):
+        """A view of n pages per (sequence, head), its table and lengths to be written; the addresses of both."""
+        c, batch, hkv = self._same_pages(), self.batch, self.hkv
+        c._table = c._lens = None
+        c._chosen = _calls.empty((batch * hkv * (n + 1),), dtype=_calls.i32, device=self.device)
+        c.batch, c.max_tokens = batch, n * self.page
+        table_p = c._chosen.data_ptr()
+        lens_p = table_p + 4 * batch * hkv * n
+        pages, dtype, ks, vs, kp, vp, mp = self._pool
+        c._packed = _CACHE.pack(batch, hkv, self.head_dim, self.page, pages, n, dtype, 0, *ks, *vs, hkv * n, n, hkv, 1,
+                                kp, vp, table_p, lens_p, mp)
+        return c, table_p, lens_p
 
 
 def _new(cache, x, shape, what):
@@ -295,13 +319,12 @@ def evisel_cache_select(cache, q, n_select, sink=0, recent=1, drafted=None, ws=N
     Returns (view, pages, ws): a Cache of the chosen pages for evisel_cache_attention, and their logical numbers
     int32 [B, hkv, n_select], ascending, -1 past them."""
     draft = _draft(cache, q, None, None, None, drafted, 0.0)
-    n, empty, i32, dev = int(n_select), _calls.empty, _calls.i32, cache.device
-    shape = (cache.batch, cache.hkv, n if n > 0 else 0)
-    pages, table = empty(shape, dtype=i32, device=dev), empty(shape, dtype=i32, device=dev)
-    lens = empty(shape[:2], dtype=i32, device=dev)
+    n = max(0, int(n_select))
+    pages = _calls.empty((cache.batch, cache.hkv, n), dtype=_calls.i32, device=cache.device)
+    view, table_p, lens_p = cache._choice(n)
     ws = Workspace() if ws is None else ws
-    rc = _calls.select(cache._packed, draft, n, int(sink), int(recent), pages.data_ptr(), table.data_ptr(),
-                       lens.data_ptr(), _stream(cache, stream), ctypes.byref(ws.ptr))
+    rc = _calls.select(cache._packed, draft, int(n_select), int(sink), int(recent), pages.data_ptr(), table_p, lens_p,
+                       _stream(cache, stream), ctypes.byref(ws.ptr))
     if rc:
         _check(rc)
-    return cache.view(table, lens), pages, ws
+    return view, pages, ws

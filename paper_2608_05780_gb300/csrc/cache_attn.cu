@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel
 constexpr int kJoinWarps = 8;
 
 template <class T, int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __grid_constant__ CacheAttnLaunch L, int wpr) {
+__global__ void __launch_bounds__(32 * kJoinWarps, 4) cache_join_kernel(const __grid_constant__ CacheAttnLaunch L, int wpr) {
   constexpr int E = D / 32;                      // elements of a row per lane
   __shared__ int scratch[40];
   __shared__ float join_o[kJoinWarps][D];
