@@ -205,6 +205,100 @@ def test_attention_is_the_same_twice_and_in_a_graph(cuda_lib):
         check_attention(o2, lse2, ref_cache.attention(ref, q_ref), 128, ty, str(lens))
 
 
+@pytest.mark.parametrize("batch", [40, 300])
+@pytest.mark.parametrize("t", [1, 20])
+def test_attention_of_many_sequences(cuda_lib, batch, t):
+    """More sequences than a warp, and than the warps add up by themselves; most of them short or empty."""
+    rng = np.random.default_rng(batch)
+    ty = _types()["bf16"]
+    lens = rng.choice([0, 0, 1, 5, 64, 65, 200], batch)
+    cache, ref = make_cache(rng, lens, 1, 64, 16, ty)
+    q, q_ref = tensor(rng, (batch, t, 2, 64), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), 64, ty)
+    acc, ws = cuda_lib.evisel_cache_evidence(cache, q, lse, ws=ws)
+    want = ref_cache.evidence(ref, q_ref, lse.cpu().numpy())
+    for b in range(batch):                       # A <= 40 here
+        got = acc[b, 0, :lens[b]].double().cpu().numpy()
+        assert np.all(np.abs(got - want[b][0]) <= (72 * 2.0 ** -24 * 40 + 2.0 ** -18) * want[b][0])
+
+
+def test_attention_of_the_most_drafted_tokens(cuda_lib):
+    """A chain of 1,024 tokens over a short cache: 32 mask words a row."""
+    rng = np.random.default_rng(4)
+    ty = _types()["fp16"]
+    cache, ref = make_cache(rng, [21], 1, 64, 16, ty)
+    q, q_ref = tensor(rng, (1, 1024, 1, 64), ty)
+    k, k_ref = tensor(rng, (1, 1024, 1, 64), ty)
+    v, v_ref = tensor(rng, (1, 1024, 1, 64), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref), 64, ty)
+    with pytest.raises(cuda_lib.EviselError):
+        cuda_lib.evisel_cache_attention(cache, q.expand(1, -1, -1, -1).repeat(1, 2, 1, 1))
+
+
+@pytest.mark.parametrize("t", [1, 24])
+def test_attention_without_any_page(cuda_lib, t):
+    """A table without columns: only the drafted tokens are there; no drafted token at all; no sequence at all."""
+    import torch
+    rng = np.random.default_rng(6)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [0, 0], 2, 64, 16, ty)
+    bare = cache.view(cache.table[:, :0], cache.lens)
+    q, q_ref = tensor(rng, (2, t, 4, 64), ty)
+    k, k_ref = tensor(rng, (2, t, 2, 64), ty)
+    v, v_ref = tensor(rng, (2, t, 2, 64), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(bare, q, k, v)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref), 64, ty)
+    o, lse, _ = cuda_lib.evisel_cache_attention(cache, q[:, :0], k[:, :0], v[:, :0])
+    assert o.shape == (2, 0, 4, 64) and lse.shape == (4, 2, 0)
+    none = cache.view(cache.table[:0], cache.lens[:0])
+    o, lse, _ = cuda_lib.evisel_cache_attention(none, q[:0])
+    assert o.shape == (0, t, 4, 64)
+    acc, ws = cuda_lib.evisel_cache_evidence(cache.view(cache.table, cache.lens + 3), q[:, :0], lse.new_zeros((4, 2, 0)))
+    assert torch.all(acc == 0)
+
+
+def test_pages_past_4_gb(cuda_lib):
+    """Pages whose byte offsets do not fit 32 bits, in every call."""
+    import torch
+    rng = np.random.default_rng(7)
+    ty = _types()["bf16"]
+    small, ref = make_cache(rng, [300, 70], 4, 128, 64, ty, room=64, mean=True, poison=False)
+    far, n = 70_000, small.k.shape[0]            # a page is 64 KiB
+    pools = []
+    for x in (small.k, small.v):
+        big = torch.empty((far + n, 4, 64, 128), dtype=ty, device="cuda")
+        big[far:] = x
+        pools.append(big)
+    mean = torch.zeros((far + n, 4, 128), dtype=ty, device="cuda")
+    cache = cuda_lib.Cache(*pools, small.table + far * (small.table >= 0).int(), small.lens, mean)
+    q, q_ref = tensor(rng, (2, 5, 28, 128), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), 128, ty)
+    o1, lse1, _ = cuda_lib.evisel_cache_attention(cache, q[:, :1], ws=ws)
+    check_attention(o1, lse1, ref_cache.attention(ref, q_ref[:, :1]), 128, ty)
+    a, _ = cuda_lib.evisel_cache_evidence(cache, q, lse, ws=ws)
+    b, _ = cuda_lib.evisel_cache_evidence(small, q, lse, ws=ws)
+    assert torch.equal(a, b)
+    kv, _ = tensor(rng, (2, 40, 4, 128), ty)
+    for c in (cache, small):
+        c.lens, _ = cuda_lib.evisel_cache_append(c, kv, kv, ws=ws)
+    assert torch.equal(cache.k[far:], small.k) and torch.equal(mean[far:], small.k_mean)
+    out = [make_cache(rng, [0, 0], 4, 128, 64, ty, room=64, mean=True, poison=False)[0] for _ in range(2)]
+    out[1].table.copy_(out[0].table)
+    for c, to in ((cache, out[0]), (small, out[1])):
+        to.k.zero_(), to.v.zero_()
+        cuda_lib.evisel_cache_evict(c, a, to, 64, ws=ws)
+    assert torch.equal(out[0].k, out[1].k) and torch.equal(out[0].v, out[1].v)
+    va, pa, _ = cuda_lib.evisel_cache_select(cache, q, 3, ws=ws)
+    vb, pb, _ = cuda_lib.evisel_cache_select(small, q, 3, ws=ws)
+    assert torch.equal(pa, pb) and torch.equal(va.lens, vb.lens) and torch.equal(va.table, vb.table + far * (vb.table >= 0).int())
+    _status(cuda_lib, ws)
+
+
 # --- evidence -------------------------------------------------------------------
 
 @pytest.mark.parametrize("lens,t,hq,hkv,d,page,dtype,layout", [
@@ -248,6 +342,33 @@ def test_evidence(cuda_lib, lens, t, hq, hkv, d, page, dtype, layout):
                 err = np.abs(host[b, h, :n] - (2.0 if add else 1.0) * want[b][h])
                 assert np.all(err <= rel * 2 * want[b][h] + 1e-30), (b, h, add, err.max())
                 assert np.all(host[b, h, n:] == 0.5)
+
+
+@pytest.mark.parametrize("t", [3, 60])
+def test_evidence_of_a_key_that_is_not_finite(cuda_lib, t):
+    """An infinite key weighs 0 for rows whose logit is -inf, whatever the rows that do not count hold."""
+    import torch
+    rng = np.random.default_rng(13)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [200], 1, 64, 16, ty, poison=False)
+    at = ref["table"][0, 2], 0, 5                # token 37
+    cache.k[at][0] = float("inf")
+    q, _ = tensor(rng, (1, t, 4, 64), ty)
+    q[..., 0] = -q[..., 0].abs() - 0.5           # used rows: logit -inf
+    use = torch.ones((1, t), dtype=torch.bool, device="cuda")
+    use[0, 1] = False
+    q[0, 1] = float("nan")
+    lse = torch.full((4, 1, t), 5.0, device="cuda")
+    acc, ws = cuda_lib.evisel_cache_evidence(cache, q, lse, use=use)
+    ref["k"] = cache.k.double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = ref_cache.evidence(ref, q.double().cpu().numpy(), lse.cpu().numpy(), use.cpu().numpy())[0][0]
+    got = acc[0, 0, :200].double().cpu().numpy()
+    assert want[37] == 0 and got[37] == 0
+    np.testing.assert_allclose(got, want, rtol=72 * 2.0 ** -24 * 40 + 2.0 ** -18)      # A <= 40
+    q[0, 2] = float("nan")                       # a row that counts: every key's sum
+    acc, ws = cuda_lib.evisel_cache_evidence(cache, q, lse, use=use, ws=ws)
+    assert torch.isnan(acc[0, 0, :200]).all()
 
 
 def test_evidence_of_all_rows_sums_to_the_cached_share(cuda_lib):
@@ -322,6 +443,29 @@ def test_evict(cuda_lib, kind, lens, hkv, d, page, out_page, budget, sink, recen
                 bound = (u_of(ty) + out_page * 2.0 ** -23) * np.abs(part).mean(0)
                 assert np.all(np.abs(mean[at, h] - part.mean(0)) <= bound)
     np.testing.assert_array_equal(k[~touched], before.double().cpu().numpy()[~touched])    # nothing else is written
+
+
+@pytest.mark.parametrize("lens,budget", [([70001], 300), ([70001, 9000], 60000), ([8193, 8192, 4097, 4096], 1000)])
+def test_evict_from_long_caches(cuda_lib, lens, budget):
+    """More scores than a CTA's threads hold, a cluster's share of them, one CTA's: equal ones among them."""
+    import torch
+    rng = np.random.default_rng(budget)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, lens, 2, 64, 64, ty, poison=False)
+    out, _ = make_cache(rng, [0] * len(lens), 2, 64, 64, ty, room=budget, poison=False)
+    acc = _scores(rng, "ties", len(lens), 2, cache.max_tokens) + rng.choice([0, 2.0 ** -20], (len(lens), 2, cache.max_tokens)).astype(np.float32)
+    kept, acc_out, ws = cuda_lib.evisel_cache_evict(cache, torch.from_numpy(acc).cuda(), out, budget, sink=3, recent=50)
+    _status(cuda_lib, ws)
+    for b, n in enumerate(lens):
+        for h in range(2):
+            want = ref_cache.choose(acc[b, h], n, budget, 3, 50)
+            got = kept[b, h].cpu().numpy()
+            assert got[:len(want)].tolist() == want and np.all(got[len(want):] == -1)
+            np.testing.assert_array_equal(acc_out[b, h, :len(want)].cpu().numpy(), acc[b, h, want])
+            slot = torch.arange(len(want), device="cuda")
+            src = torch.from_numpy(np.array(want)).cuda()
+            take = lambda c, i: c.k[c.table[b, i // 64].long(), h, i % 64]  # noqa: E731
+            assert torch.equal(take(out, slot), take(cache, src))
 
 
 # --- append ---------------------------------------------------------------------
@@ -422,6 +566,44 @@ def test_select(cuda_lib, lens, t, hq, hkv, d, page, n, sink, recent, dtype):
     o, lse, ws = cuda_lib.evisel_cache_attention(view, q, drafted=n_dev, ws=ws)
     _status(cuda_lib, ws)
     check_attention(o, lse, ref_cache.attention(sel, q_ref, drafted=drafted), d, ty)
+
+
+def test_a_step_in_a_graph(cuda_lib):
+    """Append, attention, choice, attention over it, evidence and eviction captured as one graph: the same as the
+    calls one by one, also with other lengths and inputs at replay."""
+    import torch
+    rng = np.random.default_rng(17)
+    ty = _types()["bf16"]
+    cache, _ = make_cache(rng, [500, 130], 2, 128, 32, ty, room=8, mean=True, poison=False)
+    out, _ = make_cache(rng, [0, 0], 2, 128, 32, ty, room=64, mean=True, poison=False)
+    q, _ = tensor(rng, (2, 4, 14, 128), ty)
+    kv, _ = tensor(rng, (2, 4, 2, 128), ty)
+    after = cuda_lib.Cache(cache.k, cache.v, cache.table, cache.lens.clone(), cache.k_mean)
+
+    def step(ws):
+        lens, ws = cuda_lib.evisel_cache_append(cache, kv, kv, lens_out=after.lens, ws=ws)
+        o, lse, _ = cuda_lib.evisel_cache_attention(after, q, ws=ws)
+        view, pages, _ = cuda_lib.evisel_cache_select(after, q, 5, ws=ws)
+        o2, lse2, _ = cuda_lib.evisel_cache_attention(view, q, ws=ws)
+        acc, _ = cuda_lib.evisel_cache_evidence(after, q, lse, ws=ws)
+        kept, acc_out, _ = cuda_lib.evisel_cache_evict(after, acc, out, 64, sink=1, recent=2, ws=ws)
+        return [lens, o, lse, pages, o2, lse2, acc, kept, acc_out], ws
+
+    _, ws = step(None)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        held, _ = step(ws)
+    for lens in ([500, 130], [1, 33], [0, 499]):
+        cache.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        q.copy_(tensor(rng, (2, 4, 14, 128), ty)[0])
+        graph.replay()
+        got = [x.clone() for x in held]
+        want, _ = step(ws)
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b), (lens, i)
+        # the second sequence has five pages: 499 tokens end beyond them, which the kernels record
+        assert cuda_lib.evisel_status(ws) == (0 if lens[1] + 4 <= 5 * 32 else -7), lens
 
 
 # --- what the kernels catch --------------------------------------------------------
