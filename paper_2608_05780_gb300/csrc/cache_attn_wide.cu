@@ -38,8 +38,10 @@ struct WideCfg {
   static constexpr int OFF_BAR = OFF_V + NV * TILE;
   static constexpr int B_QF = 0, B_QE = 1;       // the segment's Q: landed, read by its last S
   static constexpr int B_KF = 2, B_KE = B_KF + NK, B_VF = B_KE + NK, B_VE = B_VF + NV;
-  static constexpr int B_SF = B_VE + NV;         // 2 S buffers: computed
-  static constexpr int B_PF = B_SF + 2;          // 2: P written (128 arrivals)
+  // S computed: slot 0's, slot 1's, and the second buffer's where there is one slot. Each has one group of waiters,
+  // which waits for every phase: a group that skipped some could take an older phase of the same parity for its own.
+  static constexpr int B_SF = B_VE + NV;
+  static constexpr int B_PF = B_SF + 3;          // 2 S buffers: P written (128 arrivals)
   static constexpr int B_OF = B_PF + 2;          // 2 slots: O complete
   static constexpr int B_DRAIN = B_OF + 2;
   static constexpr int N_BARS = B_DRAIN + 1;
@@ -214,7 +216,7 @@ __device__ __forceinline__ void issue_mmas(const CacheAttnLaunch& L, const UnitC
       if (!ok) break;
       if (elect()) {
         mma_s(0, n + 1, 1);
-        ptx::mma_commit(bar(C::B_SF + 1));
+        ptx::mma_commit(bar(C::B_SF + 2));
         ptx::mma_commit(bar(C::B_KE + (n + 1) % NK));
         if (cnt == 2) ptx::mma_commit(bar(C::B_QE));
       }
@@ -242,7 +244,7 @@ __device__ __forceinline__ void issue_mmas(const CacheAttnLaunch& L, const UnitC
           if (!two || slot == 1) ptx::mma_commit(bar(C::B_VE + n % NV));
           if (more) {
             mma_s(slot, nn, buf);
-            ptx::mma_commit(bar(C::B_SF + buf));
+            ptx::mma_commit(bar(C::B_SF + (two || buf == 0 ? buf : 2)));
             if (!two || slot == 1) {
               ptx::mma_commit(bar(C::B_KE + nn % NK));
               if (j + ahead + 1 == cnt) ptx::mma_commit(bar(C::B_QE));
@@ -276,23 +278,23 @@ __device__ __forceinline__ void softmax_rows(const CacheAttnLaunch& L, const Uni
   const uint32_t tO = tmem_base + lane_base + slot * C::SLOT_COLS + C::COL_O;
   const uint64_t scale2 = ptx::f2(L.d.scale_log2, L.d.scale_log2);
   Segment s;
-  uint32_t n = 0, sf = 0, of = 0;                // tiles so far; parity of the S waits, a bit per buffer (this slot's or not); O waits
+  uint32_t n = 0, sf = 0, of = 0;                // tiles so far; parity of the S waits, a bit per barrier; O waits
   bool ok = true;
   while (ok && walk.next(L.c, L.row_tiles, uc, s, L.status)) {
     const bool two = slots_of(L, s) == 2;
     const int cnt = s.t1 - s.t0;
     if (slot == 1 && !two) {                     // the other slot's S takes both buffers
       n += cnt;
-      sf ^= static_cast<uint32_t>((cnt + 1) / 2 & 1) | static_cast<uint32_t>(cnt / 2 & 1) << 1;
       continue;
     }
     float m = -INFINITY, l = 0.f;                // running max (log2 units), row sum
     for (int j = 0; j < cnt; ++j, ++n) {
       const int b = two ? slot : j & 1;
+      const int sb = two || b == 0 ? b : 2;
       const uint32_t tS = tmem_base + lane_base + b * C::SLOT_COLS;
-      ok = warp_wait(bar(C::B_SF + b), (sf >> b) & 1, abort_flag);
+      ok = warp_wait(bar(C::B_SF + sb), (sf >> sb) & 1, abort_flag);
       if (!ok) break;
-      sf ^= 1u << b;
+      sf ^= 1u << sb;
       ptx::tc_fence_after();
       const int limit = s.len - (s.t0 + j) * kKeys;              // keys from here on do not exist
       float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -384,7 +386,6 @@ __device__ __forceinline__ void softmax_rows(const CacheAttnLaunch& L, const Uni
       ptx::tc_fence_before();
       ptx::mbar_arrive(bar(C::B_PF + b));
     }
-    if (two) sf ^= static_cast<uint32_t>(cnt & 1) << (slot ^ 1);   // the other slot's waits
     ok = ok && warp_wait(bar(C::B_OF + slot), of & 1, abort_flag);
     ++of;
     if (!ok) break;

@@ -224,6 +224,20 @@ def test_attention_of_many_sequences(cuda_lib, batch, t):
         assert np.all(np.abs(got - want[b][0]) <= (72 * 2.0 ** -24 * 40 + 2.0 ** -18) * want[b][0])
 
 
+@pytest.mark.parametrize("t,d", [(37, 64), (23, 128), (80, 64)])
+def test_attention_of_an_odd_number_of_slots(cuda_lib, t, d):
+    """Row tiles of two slots and of one, long enough that a CTA goes from one kind to the other in mid-walk."""
+    rng = np.random.default_rng(t)
+    ty = _types()["bf16"]
+    lens = [4300, 3999, 130, 4000, 4100, 3500, 1, 4200]
+    cache, ref = make_cache(rng, lens, 4, d, 64, ty, poison=False)
+    gq = 7 if d == 64 else 16
+    q, q_ref = tensor(rng, (len(lens), t, 4 * gq, d), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), d, ty)
+
+
 def test_attention_of_the_most_drafted_tokens(cuda_lib):
     """A chain of 1,024 tokens over a short cache: 32 mask words a row."""
     rng = np.random.default_rng(4)
