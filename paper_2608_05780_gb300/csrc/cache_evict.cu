@@ -80,7 +80,9 @@ template <class T, int D>
 cudaError_t launch_d(const CacheEvictLaunch& L, cudaStream_t stream) {
   const int problems = L.c.batch * L.c.hkv;
   const int64_t room = static_cast<int64_t>(L.c.max_pages) * L.c.page;
-  const int cluster = choose_cluster(problems, room < L.acc_len ? room : L.acc_len, 4096, sm_count());
+  // What a CTA's registers hold it chooses from alone: both kernels, four heads, 8,192 scores 14.7 us (a cluster of
+  // eight 14.4, of two 15.7; eight sequences of them 17.8, with two 20.6), 16,384 31.9 us (eight 15.1).
+  const int cluster = choose_cluster(problems, room < L.acc_len ? room : L.acc_len, kChooseThreads * 16, sm_count());
   const cudaError_t e = launch_clusters(cache_evict_choose_kernel, L, problems, kChooseThreads, cluster, stream);
   if (e != cudaSuccess) return e;
   return launch_after(cache_evict_copy_kernel<T, D>, dim3((L.budget + L.out.page - 1) / L.out.page, L.c.hkv, L.c.batch),
