@@ -4,6 +4,7 @@
 //   s_rm = scale q_r . k_m,  O_r = sum_m exp(s_rm - LSE_r) v_m
 //
 // over a (sequence, KV head)'s rows r = (token, head of the group).
+#include <algorithm>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -516,6 +517,265 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 4) cache_join_kernel(const __
     L.lse[(static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t] = l != 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
+// Many rows: 16 of them a warp as one side of mma.sync products, the drafted keys
+// staged in shared memory for the block's rows. Masked keys' products never count;
+// their values meet weights of 0, so a block whose drafted values are not all
+// finite takes its P V value by value, over the allowed ones only. `wpr` warps share 16 rows.
+constexpr int kTileWarps = 4, kChunk = 64;
+
+template <class T>
+__device__ __forceinline__ bool all_finite(const uint4& x) {
+  constexpr uint32_t kExp = T::kFormat == 1 ? 0x7f80u : 0x7c00u;
+  bool ok = true;
+#pragma unroll
+  for (uint32_t w : {x.x, x.y, x.z, x.w}) ok = ok && (w & kExp) != kExp && ((w >> 16) & kExp) != kExp;
+  return ok;
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(32 * kTileWarps, 3) cache_join_tile_kernel(const __grid_constant__ CacheAttnLaunch L, int wpr) {
+  constexpr int BLOCK = kChunk * 128, KB = D / 64;           // a 64-column block of a chunk
+  __shared__ alignas(128) uint8_t tile[2 * KB * BLOCK];      // drafted keys and values, swizzled; then the warps' O
+  __shared__ float2 join_ml[kTileWarps][16];
+  __shared__ int scratch[40];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wi = warp % wpr, group = warp / wpr;
+  const int bh = blockIdx.y, b = bh / L.c.hkv, h = bh % L.c.hkv;
+  // Everything but the partials was there before the kernel that this one follows began.
+  const UnitCount uc(L.c, L.key_tile, L.lead, L.row_tiles, L.status);
+  const Split sp = split_find_entry(uc, scratch, uc.per_head ? bh : b);
+  const int tiles = uc.tiles(sp.entry);
+  const int first = sp.first + (uc.per_head ? 0 : h * L.row_tiles * uc.units(tiles));
+  const int ctas = split_ctas(sp.total, L.n_ctas, L.min_units, L.c.batch * L.c.hkv * L.row_tiles);
+  const int drafted = drafted_tokens(L.d, b);
+
+  const int fr = lane >> 2, fc = (lane & 3) * 2, mi = lane >> 3, r8 = lane & 7;
+  const int block0 = blockIdx.x * (kTileWarps / wpr) * 16;
+  int r[2], t[2];
+  bool in[2], live[2];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    r[half] = block0 + group * 16 + fr + 8 * half;
+    in[half] = r[half] < L.rows;
+    t[half] = in[half] ? r[half] / L.d.gq : 0;
+    live[half] = in[half] && t[half] < drafted;
+  }
+  float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+  auto move_max = [&](int half, float x) {       // the running max is at least x from here on
+    if (x > m[half]) {
+      const float a = ptx::ex2(m[half] - x);
+      l[half] *= a;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) o[j][2 * half] *= a, o[j][2 * half + 1] *= a;
+      m[half] = x;
+    }
+  };
+
+  // The drafted tokens first: they need nothing of the kernel before. Without a tree no row of the block looks past its last token.
+  if (L.d.k_new && block0 / L.d.gq < drafted) {
+    const int last = min(block0 + (kTileWarps / wpr) * 16, L.rows) - 1;
+    const int end = L.d.tree ? drafted : min(drafted, last / L.d.gq + 1);
+    const uint16_t* qb = static_cast<const uint16_t*>(L.d.q) + b * L.d.qs[0] + h * L.d.gq * L.d.qs[2];
+    uint32_t qf[D / 16][4];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(qb + t[half] * L.d.qs[1] + (in[half] ? r[half] % L.d.gq : 0) * L.d.qs[2] + fc);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        qf[ks][half] = live[half] ? __ldg(q + ks * 8) : 0u;
+        qf[ks][half + 2] = live[half] ? __ldg(q + ks * 8 + 4) : 0u;
+      }
+    }
+    const uint32_t kt = ptx::smem_addr(tile), vt = kt + KB * BLOCK;
+    for (int c0 = 0; c0 < end; c0 += kChunk) {
+      const int count = min(kChunk, end - c0), padded = (count + 15) & ~15;
+      uint64_t bits[2];                          // the allowed keys of the chunk
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (L.d.tree) {
+          const int32_t* w = L.d.tree + b * L.d.trs[0] + t[half] * L.d.trs[1] + c0 / 32;
+          bits[half] = static_cast<uint32_t>(__ldg(w));
+          if (count > 32) bits[half] |= static_cast<uint64_t>(static_cast<uint32_t>(__ldg(w + 1))) << 32;
+        } else {
+          bits[half] = t[half] - c0 >= 63 ? ~0ull : t[half] < c0 ? 0ull : (2ull << (t[half] - c0)) - 1ull;
+        }
+        if (count < 64) bits[half] &= (1ull << count) - 1ull;
+        if (!live[half]) bits[half] = 0;
+      }
+      if (c0 > 0) __syncthreads();
+      bool bad = false;
+      for (int i = threadIdx.x; i < padded * (D / 8); i += 32 * kTileWarps) {
+        const int row = i / (D / 8), ch = i % (D / 8);
+        uint4 k = make_uint4(0, 0, 0, 0), v = k;
+        if (row < count) {
+          const int64_t tok = c0 + row;
+          k = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.k_new) + b * L.d.kns[0] + tok * L.d.kns[1] + h * L.d.kns[2]) + ch);
+          v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.v_new) + b * L.d.vns[0] + tok * L.d.vns[1] + h * L.d.vns[2]) + ch);
+        }
+        bad = bad || !all_finite<T>(v);
+        uint8_t* dst = tile + (ch / 8) * BLOCK + row * 128 + ((ch & 7) ^ (row & 7)) * 16;
+        *reinterpret_cast<uint4*>(dst) = k;
+        *reinterpret_cast<uint4*>(dst + KB * BLOCK) = v;
+      }
+      bad = __syncthreads_or(bad);
+      for (int k0 = 16 * wi; k0 < padded; k0 += 16 * wpr) {
+        const uint32_t allow[2] = {static_cast<uint32_t>(bits[0] >> k0) & 0xffffu, static_cast<uint32_t>(bits[1] >> k0) & 0xffffu};
+        if (!__any_sync(0xffffffffu, (allow[0] | allow[1]) != 0)) continue;
+        float p[2][4] = {};
+        const int k_row = k0 + (mi >> 1) * 8 + r8, v_row = k0 + (mi & 1) * 8 + r8;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          uint32_t kf[4];
+          ptx::ldmatrix4(kf, kt + (ks / 4) * BLOCK + k_row * 128 + ((((ks % 4) * 2 + (mi & 1)) ^ r8) << 4));
+          ptx::mma16816<T>(p[0], qf[ks], kf[0], kf[1]);
+          ptx::mma16816<T>(p[1], qf[ks], kf[2], kf[3]);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float& x = p[j][2 * half + e];
+              x = (allow[half] >> (j * 8 + fc + e)) & 1 ? x * L.d.scale_log2 : -INFINITY;
+              top = fmaxf(top, x);
+            }
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          move_max(half, top);
+          const float ref = m[half] == -INFINITY ? 0.f : m[half];
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float& x = p[j][2 * half + e];
+              x = ptx::ex2(x - ref);
+              l[half] += x;
+            }
+        }
+        if (!bad) {
+          const uint32_t pa[4] = {T::pack(p[0][0], p[0][1]), T::pack(p[0][2], p[0][3]), T::pack(p[1][0], p[1][1]), T::pack(p[1][2], p[1][3])};
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) {
+            uint32_t vf[4];
+            ptx::ldmatrix4_t(vf, vt + (j / 4) * BLOCK + v_row * 128 + ((((j % 4) * 2 + (mi >> 1)) ^ r8) << 4));
+            ptx::mma16816<T>(o[2 * j], pa, vf[0], vf[1]);
+            ptx::mma16816<T>(o[2 * j + 1], pa, vf[2], vf[3]);
+          }
+        } else {
+#pragma unroll 1
+          for (int src = 0; src < 4; ++src)      // the lane of the quad that holds the weight
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int half = i & 1, e = (i >> 1) & 1, j8 = (i >> 2) * 8, key = j8 + 2 * src + e;
+              const float w = __shfl_sync(0xffffffffu, p[i >> 2][2 * half + e], (lane & ~3) | src);
+              if ((allow[half] >> key) & 1)
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) {
+                  const uint32_t v = *reinterpret_cast<const uint32_t*>(tile + (KB + j / 8) * BLOCK + (k0 + key) * 128 +
+                                                                        ((j % 8) ^ (key & 7)) * 16 + fc * 2);
+                  o[j][2 * half] = fmaf(w, T::lo(v), o[j][2 * half]);
+                  o[j][2 * half + 1] = fmaf(w, T::hi(v), o[j][2 * half + 1]);
+                }
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
+      l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
+    }
+  }
+
+  ptx::grid_wait();
+  ptx::grid_launch_next();
+  if (tiles > 0) {
+    int n[2];                                    // partials of this warp
+    int64_t row0[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int slot = r[half] / L.slot_rows, rt = slot / L.slots;
+      const int in_slot = L.wide && !L.qt.head_inner ? (r[half] % L.d.gq) * L.qt.tokens + t[half] % L.qt.tokens : r[half] % L.slot_rows;
+      const int row = (slot % L.slots) * (L.tile_rows / L.slots) + in_slot;
+      const int u0 = first + rt * uc.units(tiles) + uc.lead;
+      const int i0 = split_owner(u0, sp.total, ctas), i1 = split_owner(u0 + tiles - 1, sp.total, ctas);
+      n[half] = live[half] ? (i1 - i0 + 1 - wi + wpr - 1) / wpr : 0;
+      row0[half] = static_cast<int64_t>(i0 + bh * L.row_tiles + rt + wi) * L.tile_rows + row;
+    }
+    const int64_t step = static_cast<int64_t>(wpr) * L.tile_rows;
+    for (int i = 0; i < max(n[0], n[1]); ++i) {
+      float2 x[2], y[2][D / 8];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const bool has = i < n[half];
+        const int64_t at = row0[half] + i * step;
+        x[half] = has ? L.part_ml[at] : make_float2(-INFINITY, 0.f);
+        const float2* src = reinterpret_cast<const float2*>(L.part_o + at * D + fc);
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j) y[half][j] = has ? src[4 * j] : make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        move_max(half, x[half].x);
+        const float w = ptx::ex2(x[half].x - (m[half] == -INFINITY ? 0.f : m[half]));
+        l[half] = fmaf(w, x[half].y, l[half]);
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j) {
+          o[j][2 * half] = fmaf(w, y[half][j].x, o[j][2 * half]);
+          o[j][2 * half + 1] = fmaf(w, y[half][j].y, o[j][2 * half + 1]);
+        }
+      }
+    }
+  }
+  if (wpr > 1) {
+    if ((lane & 3) == 0) join_ml[warp][fr] = make_float2(m[0], l[0]), join_ml[warp][fr + 8] = make_float2(m[1], l[1]);
+    __syncthreads();                             // (the chunk's last readers are done too)
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      for (int w = 0; w < wpr; ++w) top[half] = fmaxf(top[half], join_ml[group * wpr + w][fr + 8 * half].x);
+      const float ref = top[half] == -INFINITY ? 0.f : top[half];
+      for (int w = 0; w < wpr; ++w) {
+        const float2 x = join_ml[group * wpr + w][fr + 8 * half];
+        sum[half] = fmaf(x.y, ptx::ex2(x.x - ref), sum[half]);
+      }
+      const float f = ptx::ex2(m[half] - ref);
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) o[j][2 * half] *= f, o[j][2 * half + 1] *= f;
+      m[half] = top[half];
+      l[half] = sum[half];
+    }
+    float4* join = reinterpret_cast<float4*>(tile) + group * (wpr - 1) * (D / 8) * 32 + lane;
+    static_assert((kTileWarps - 1) * (D / 8) * 32 * 16 <= 2 * KB * BLOCK, "three warps' O");
+    if (wi > 0)
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) join[((wi - 1) * (D / 8) + j) * 32] = make_float4(o[j][0], o[j][1], o[j][2], o[j][3]);
+    __syncthreads();
+    if (wi > 0) return;
+    for (int w = 0; w < wpr - 1; ++w)
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) {
+        const float4 x = join[(w * (D / 8) + j) * 32];
+        o[j][0] += x.x, o[j][1] += x.y, o[j][2] += x.z, o[j][3] += x.w;
+      }
+  }
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (!in[half]) continue;
+    const int head = h * L.d.gq + r[half] % L.d.gq;
+    const float inv = l[half] != 0.f ? 1.f / l[half] : 0.f;  // (a NaN sum stays one)
+    uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(L.o) +
+                                                ((static_cast<int64_t>(b) * L.d.tokens + t[half]) * L.d.hq + head) * D + fc);
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j) dst[4 * j] = T::pack(o[j][2 * half] * inv, o[j][2 * half + 1] * inv);
+    if ((lane & 3) == 0)
+      L.lse[(static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t[half]] = l[half] != 0.f ? (m[half] + __log2f(l[half])) * kLn2 : -INFINITY;
+  }
+}
+
 template <class T, int D, int MG>
 cudaError_t launch_few(const CacheAttnLaunch& L, cudaStream_t stream) {
   using C = FewCfg<D, MG>;
@@ -529,23 +789,42 @@ cudaError_t launch_few(const CacheAttnLaunch& L, cudaStream_t stream) {
 
 template <class T, int D>
 cudaError_t launch_d(const CacheAttnLaunch& L, cudaStream_t stream) {
-  const cudaError_t e = L.wide               ? launch_cache_attn_wide(L, stream)
-                        : L.tile_rows == 16 ? launch_few<T, D, 1>(L, stream)
-                                            : launch_few<T, D, 2>(L, stream);
+  cudaError_t e;
+  if (L.wide) e = launch_cache_attn_wide(L, stream);
+  else if (D == 128 || L.tile_rows == 16) e = launch_few<T, D, 1>(L, stream);
+  else e = launch_few<T, 64, 2>(L, stream);
   if (e != cudaSuccess) return e;
-  // Warps per row: as many as keep the rows' blocks within about two per SM.
-  const int64_t rows = static_cast<int64_t>(L.c.batch) * L.c.hkv * L.rows;
-  const int wpr = rows >= 2048 ? 1 : rows >= 1024 ? 2 : rows >= 512 ? 4 : 8;
-  const int per = kJoinWarps / wpr;
+  if (L.join_tile) {
+    const int per_block = 16 * (kTileWarps / L.join_warps);
+    return launch_after(cache_join_tile_kernel<T, D>, dim3((L.rows + per_block - 1) / per_block, L.c.batch * L.c.hkv),
+                        32 * kTileWarps, 0, stream, L, L.join_warps);
+  }
+  const int per = kJoinWarps / L.join_warps;
   return launch_after(cache_join_kernel<T, D>, dim3((L.rows + per - 1) / per, L.c.batch * L.c.hkv), 32 * kJoinWarps, 0, stream,
-                      L, wpr);
+                      L, L.join_warps);
 }
 
 }  // namespace
 
-CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n_sm) {
+// Few rows a CTA or many. A few-rows CTA starts faster and its partials are 16 or
+// 32 rows high; but every 16 rows read the keys again, which the wide one does
+// once for 128 or 256. By the units of 64 keys times 16 rows that the capacity
+// of the tables allows, us with few / wide: 7 heads a KV head of 128, one
+// sequence of 8,192 with 6 tokens (1,536 units) 14.5 / 15.8, 16,384 with 3
+// (2,048) 14.7 / 19.0, 32,768 with 4 (4,096) 19.6 / 22.8, with 6 (6,144) 23.5 / 23.2,
+// with 12 24.8 / 36.6 the other way; 32 of 4,096 with 3 (16,384) 74 / 54. Rows 17 to
+// 32 of heads of 64 have a tile of their own: 32,768 tokens and 8 KV heads take 28.5 us
+// in tiles of 16, 22.3 in one of 32 and 27.1 wide; below 2,048 units 16 is faster
+// (2,048 tokens: 8.6 / 9.9).
+// At least three units a CTA, wide two, for fewer partials in the join: one drafted token
+// over 4,160 takes 9.8 us with one, 9.5 with two, 9.1 with three and 9.6 with four (8,192: 12.2, 9.7, 10.4,
+// 10.6; one KV head over 16,384: 13.7, 11.3, 10.4, 10.5); 24 over 4,160, wide, 22.6, 18.9 and 20.3 with three.
+CacheAttnShape cache_attn_shape(int rows, int tokens, int64_t problems, int64_t capacity, int head_dim, const QueryTile& qt,
+                                bool q_map, int n_sm) {
   CacheAttnShape s;
-  if (rows > 32 && q_map) {
+  const int64_t units = (capacity + kKeys - 1) / kKeys * problems * ((rows + 15) / 16);
+  const bool tall = head_dim == 64 && rows > 16 && units > 14 * n_sm;
+  if (rows > 16 && units > 28 * n_sm && q_map && !(tall && rows <= 32)) {
     s.wide = true;
     s.slot_rows = qt.rows;
     const int slots = (rows + s.slot_rows - 1) / s.slot_rows;
@@ -554,18 +833,32 @@ CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n
     s.row_tiles = (slots + s.slots - 1) / s.slots;
     s.key_tile = 128;
     s.n_ctas = n_sm;
-    s.min_units = 1;
+    s.min_units = 2;
     s.lead = 1;
-    return s;
+  } else {
+    s.wide = false;
+    s.slots = 1;
+    s.slot_rows = s.tile_rows = tall ? 32 : 16;
+    s.row_tiles = (rows + s.tile_rows - 1) / s.tile_rows;
+    s.key_tile = kKeys;
+    s.n_ctas = 2 * n_sm;
+    s.min_units = 3;
+    s.lead = 2;
   }
-  s.wide = false;
-  s.slots = 1;
-  s.slot_rows = s.tile_rows = rows <= 16 ? 16 : 32;
-  s.row_tiles = (rows + s.tile_rows - 1) / s.tile_rows;
-  s.key_tile = kKeys;
-  s.n_ctas = 2 * n_sm;
-  s.min_units = 3;
-  s.lead = 2;
+  // Warps that share a row in the join: each has four partials or more, and the
+  // blocks are not many more than fit. One drafted token over 32,768: 20.8 us with one
+  // warp, 14.6 with eight; 64 sequences of 300: 15.2 with one, 25.4 with eight; 24 drafted
+  // tokens over 4,160: 30.3 with one, 22.4 with four, 23.9 with eight.
+  const int64_t all_rows = problems * rows, tiles = (capacity + s.key_tile - 1) / s.key_tile;
+  const int64_t partials = std::min<int64_t>(s.n_ctas / (problems * s.row_tiles), tiles / s.min_units);
+  // A tile of rows or row by row: by the rows' products with drafted tokens. The whole call, tile / row by row: 64
+  // sequences of 256 with 64 tokens (7.3 million) 108 / 377 us, 8 of 4,096 with 24 (129,024) 36.6 / 39.2, one of 4,160 with 64
+  // (114,688) 33.7 / 33.0, 8 with 12 (32,256) 29.6 / 26.8. Fewer rows are shared by more warps: 5,376 by four
+  // 36.6 us, by one 42.2; 43,008 by four 87, by one 46.3.
+  s.join_tile = all_rows * tokens > 49152;
+  s.join_warps = s.join_tile ? 4 : 8;
+  while (s.join_warps > 1 && (partials < s.join_warps * (s.join_tile ? 1 : 4) || all_rows * s.join_warps > (s.join_tile ? 24576 : 4096)))
+    s.join_warps /= 2;
   return s;
 }
 

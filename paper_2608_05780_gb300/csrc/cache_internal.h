@@ -65,6 +65,7 @@ struct CacheAttnLaunch {
   int n_ctas, key_tile;
   int min_units;                    // that a CTA takes at least
   int lead;                         // units that stand for a problem's fill and join
+  int join_tile, join_warps;        // join by tiles of 16 rows or row by row; the warps (1, 2, 4, 8) that share one
   int wide;                         // 128-row slots on tcgen05 (else mma.sync)
 };
 
@@ -123,12 +124,14 @@ cudaError_t launch_cache_evict(const CacheEvictLaunch& L, cudaStream_t stream);
 cudaError_t launch_cache_append(const CacheAppendLaunch& L, cudaStream_t stream);
 cudaError_t launch_cache_select(const CacheSelectLaunch& L, cudaStream_t stream);
 
-// Row tile and CTAs of a call with `rows` rows per (sequence, KV head).
+// Row tile and CTAs of a call with `rows` rows of `tokens` drafted tokens for each of `problems` (sequence, KV
+// head) pairs, whose tables hold up to `capacity` tokens.
 struct CacheAttnShape {
-  int tile_rows, row_tiles, slots, slot_rows, key_tile, n_ctas, min_units, lead;
-  bool wide;
+  int tile_rows, row_tiles, slots, slot_rows, key_tile, n_ctas, min_units, lead, join_warps;
+  bool wide, join_tile;
 };
-CacheAttnShape cache_attn_shape(int rows, const QueryTile& qt, bool q_map, int n_sm);
+CacheAttnShape cache_attn_shape(int rows, int tokens, int64_t problems, int64_t capacity, int head_dim, const QueryTile& qt,
+                                bool q_map, int n_sm);
 cudaError_t launch_cache_attn_wide(const CacheAttnLaunch& L, cudaStream_t stream);
 
 // What the cache calls use of a workspace (evisel_capi.cpp).

@@ -258,7 +258,9 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     L.d = view_of(cache, draft);
     L.rows = draft->tokens * L.d.gq;
     L.qt = query_tile(cache, draft);
-    const CacheAttnShape shape = cache_attn_shape(L.rows, L.qt, has_query_map(cache, draft), n_sm);
+    const int64_t capacity = static_cast<int64_t>(cache->max_pages) * cache->page;
+    const CacheAttnShape shape = cache_attn_shape(L.rows, draft->tokens, static_cast<int64_t>(cache->batch) * cache->hkv, capacity,
+                                                  cache->head_dim, L.qt, has_query_map(cache, draft), n_sm);
     L.wide = shape.wide;
     L.slots = shape.slots;
     L.slot_rows = shape.slot_rows;
@@ -268,9 +270,11 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     L.n_ctas = shape.n_ctas;
     L.min_units = shape.min_units;
     L.lead = shape.lead;
+    L.join_tile = shape.join_tile;
+    L.join_warps = shape.join_warps;
     L.box_rows = std::min(cache->page, L.key_tile);
     const int64_t problems = static_cast<int64_t>(cache->batch) * cache->hkv * L.row_tiles;
-    const int64_t tiles = (static_cast<int64_t>(cache->max_pages) * cache->page + L.key_tile - 1) / L.key_tile;
+    const int64_t tiles = (capacity + L.key_tile - 1) / L.key_tile;
     if (problems * (tiles + L.lead) > kMaxUnits) return fail(EVISEL_EUNSUPPORTED, "too many units of work");
     const size_t parts = static_cast<size_t>(L.n_ctas) + problems;
     const size_t ml_bytes = align_up(parts * L.tile_rows * sizeof(float2), 256);

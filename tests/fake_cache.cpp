@@ -23,7 +23,7 @@ cudaError_t launch_cache_evidence(const CacheEvidenceLaunch&, cudaStream_t) { re
 cudaError_t launch_cache_evict(const CacheEvictLaunch&, cudaStream_t) { return launched(); }
 cudaError_t launch_cache_append(const CacheAppendLaunch&, cudaStream_t) { return launched(); }
 cudaError_t launch_cache_select(const CacheSelectLaunch&, cudaStream_t) { return launched(); }
-CacheAttnShape cache_attn_shape(int rows, const QueryTile&, bool, int n_sm) {
+CacheAttnShape cache_attn_shape(int rows, int, int64_t, int64_t, int, const QueryTile&, bool, int n_sm) {
   CacheAttnShape s{};
   s.tile_rows = s.slot_rows = 32;
   s.row_tiles = (rows + 31) / 32;

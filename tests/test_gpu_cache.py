@@ -238,6 +238,41 @@ def test_attention_of_an_odd_number_of_slots(cuda_lib, t, d):
     check_attention(o, lse, ref_cache.attention(ref, q_ref), d, ty)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("batch,t,gq,d,tree", [(40, 16, 7, 64, True), (3, 100, 7, 128, True), (1, 333, 2, 64, False),
+                                               (9, 40, 4, 128, False), (300, 9, 2, 128, True)])
+def test_attention_of_many_drafted_rows(cuda_lib, batch, t, gq, d, tree, dtype):
+    """Trees and runs whose joins take rows by tiles: several chunks of drafted keys, odd tails, rows that end early,
+    drafted values that are not finite where no row may look."""
+    import torch
+    rng = np.random.default_rng(batch + t)
+    ty = _types()[dtype]
+    lens = rng.choice([0, 1, 40, 300], batch)
+    cache, ref = make_cache(rng, lens, 2, d, 32, ty)
+    q, q_ref = tensor(rng, (batch, t, 2 * gq, d), ty)
+    k, k_ref = tensor(rng, (batch, t, 2, d), ty)
+    v, v_ref = tensor(rng, (batch, t, 2, d), ty)
+    drafted = rng.integers(0, t + 1, batch)
+    drafted[0] = t
+    allowed = np.zeros((batch, t, t), bool)
+    for b in range(batch):
+        for i in range(t):
+            parent = int(rng.integers(max(0, i - 5), i)) if i and tree else i - 1
+            allowed[b, i] = allowed[b, parent] if parent >= 0 and i else False
+            allowed[b, i, i] = True
+        if tree:
+            allowed[b, :, 3] = False             # a token that nobody looks at, itself neither
+        allowed[b, :, drafted[b]:] = False
+    for b in range(batch):                       # what no row may look at may be anything
+        for tok in np.nonzero(~allowed[b, :drafted[b]].any(0))[0]:
+            k[b, tok], v[b, tok] = float("inf"), float("nan")
+            k_ref[b, tok], v_ref[b, tok] = 0, 0
+    o, lse, ws = cuda_lib.evisel_cache_attention(
+        cache, q, k, v, tree=tree_words(allowed) if tree else None, drafted=torch.from_numpy(drafted.astype(np.int32)).cuda())
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref, allowed, drafted), d, ty)
+
+
 def test_attention_of_the_most_drafted_tokens(cuda_lib):
     """A chain of 1,024 tokens over a short cache: 32 mask words a row."""
     rng = np.random.default_rng(4)
