@@ -180,8 +180,7 @@ __device__ __forceinline__ Split split_find_unit(const UnitCount& u, int* mem, A
   const int n = u.entries();
   Split s;
   if (n <= kWarpEntries) {
-    // Without a barrier: a block's first loads wait for nothing but the lengths
-    // (by the block with barriers it took 1.5 us of a small call's 10, this 0.8).
+    // Without a barrier: a block's first loads wait for nothing but the lengths.
     const int lane = threadIdx.x & 31;
     if (n <= 32) {                               // (little code: it is fetched cold)
       const int m = lane < n ? u.units(u.tiles(lane)) * u.mult : 0;
@@ -198,36 +197,34 @@ __device__ __forceinline__ Split split_find_unit(const UnitCount& u, int* mem, A
       s.first = __shfl_sync(0xffffffffu, inc - m, s.entry);
       return s;
     }
-    int m[kWarpEntries / 32];
-    s.total = 0;
+    // Each lane adds up a run of entries, one scan joins the lanes, and the lane
+    // that holds the unit looks through its run.
+    const int per = (n + 31) / 32, e0 = lane * per;
+    int m[kWarpEntries / 32], sum = 0;
 #pragma unroll
     for (int c = 0; c < kWarpEntries / 32; ++c) {
-      const int e = c * 32 + lane;
-      m[c] = e < n ? u.units(u.tiles(e)) * u.mult : 0;
+      m[c] = c < per && e0 + c < n ? u.units(u.tiles(e0 + c)) * u.mult : 0;
+      sum += m[c];
     }
+    int inc = sum;
 #pragma unroll
-    for (int c = 0; c < kWarpEntries / 32; ++c)
-      if (c * 32 < n) s.total += __reduce_add_sync(0xffffffffu, m[c]);
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    s.total = __shfl_sync(0xffffffffu, inc, 31);
     const int want = at(s.total);
-    int before = 0;
-    s.entry = s.first = 0;
+    int first = inc - sum, entry = e0;
+    bool past = true;                            // the entries so far all end before it
+    const uint32_t hit = __ballot_sync(0xffffffffu, want >= first && want < inc);
 #pragma unroll
-    for (int c = 0; c < kWarpEntries / 32; ++c)
-      if (c * 32 < n) {
-        int inc = m[c];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, inc, o);
-          if (lane >= o) inc += y;
-        }
-        const int first = before + inc - m[c];
-        const uint32_t hit = __ballot_sync(0xffffffffu, want >= first && want < first + m[c]);
-        if (hit) {
-          s.entry = c * 32 + __ffs(hit) - 1;
-          s.first = __shfl_sync(0xffffffffu, first, __ffs(hit) - 1);
-        }
-        before += __shfl_sync(0xffffffffu, inc, 31);
-      }
+    for (int c = 0; c < kWarpEntries / 32; ++c) {
+      past = past && want >= first + m[c];
+      if (past) first += m[c], ++entry;
+    }
+    const int src = hit ? __ffs(hit) - 1 : 0;
+    s.entry = hit ? __shfl_sync(0xffffffffu, entry, src) : 0;
+    s.first = hit ? __shfl_sync(0xffffffffu, first, src) : 0;
     return s;
   }
   const int per = (n + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);

@@ -224,6 +224,31 @@ def test_attention_of_many_sequences(cuda_lib, batch, t):
         assert np.all(np.abs(got - want[b][0]) <= (72 * 2.0 ** -24 * 40 + 2.0 ** -18) * want[b][0])
 
 
+@pytest.mark.parametrize("t", [1, 7])
+def test_attention_of_any_number_of_sequences(cuda_lib, t):
+    """Every way that the lengths are added up: up to a warp's lanes, a few for each lane, the block's."""
+    import torch
+    rng = np.random.default_rng(t)
+    ty = _types()["bf16"]
+    lens = rng.choice([0, 1, 30, 64, 65, 130, 200], 330)
+    cache, ref = make_cache(rng, lens, 1, 64, 16, ty, poison=False)
+    q, q_ref = tensor(rng, (330, t, 2, 64), ty)
+    want = ref_cache.attention(ref, q_ref)
+    weights = None
+    for batch in [*range(1, 40), *range(62, 70), 80, 90, *range(94, 100), *range(126, 132), 160, 161, 200, 255, 256, 257, 300, 330]:
+        part = cache.view(cache.table[:batch], cache.lens[:batch])
+        o, lse, ws = cuda_lib.evisel_cache_attention(part, q[:batch])
+        _status(cuda_lib, ws)
+        check_attention(o, lse, [x[:, :batch] if x.ndim == 3 else x[:batch] for x in want], 64, ty, f"{batch} sequences")
+        acc, ws = cuda_lib.evisel_cache_evidence(part, q[:batch], lse, ws=ws)
+        if weights is None or batch == 330:
+            lse_all, _ = cuda_lib.evisel_cache_attention(cache, q)[1:]
+            weights = cuda_lib.evisel_cache_evidence(cache, q, lse_all)[0]
+        for b in range(batch):
+            got, one = acc[b, 0, :lens[b]], weights[b, 0, :lens[b]]
+            assert torch.all((got - one).abs() <= 1e-4 * one), f"{batch} sequences, {b}"
+
+
 @pytest.mark.parametrize("t,d", [(37, 64), (23, 128), (80, 64)])
 def test_attention_of_an_odd_number_of_slots(cuda_lib, t, d):
     """Row tiles of two slots and of one, long enough that a CTA goes from one kind to the other in mid-walk."""
