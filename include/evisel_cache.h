@@ -89,8 +89,9 @@ typedef struct {
  * not attend never enter it, non-finite ones included.
  *   o    device [B, T, hq, d] contiguous, 16-byte aligned (written)
  *   lse  device fp32 [hq, B, T], natural log (written)
- * The workspace keeps the fp32 partial results of ranges of cached keys, at
- * most (2 SMs + B * T * hq / 16 + B * hkv) * 16..256 rows * (d + 2) * 4 bytes.
+ * The workspace keeps the fp32 partial results of ranges of cached keys: for
+ * tiles of r = 16, 32, 128 or 256 rows (2 SMs + B * hkv * ceil(T * hq / hkv / r))
+ * * r * (d + 2) * 4 bytes at most.
  * Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED, EVISEL_ENOMEM, EVISEL_ECUDA. */
 int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft, void* o, float* lse, void* stream,
                            evisel_ws** ws_inout);
@@ -132,7 +133,7 @@ int evisel_cache_evict(const evisel_cache* cache, const float* acc, int64_t acc_
 /* Appends tokens: the i-th of sequence b, i < counts[b], is new token src[b, i]
  * and goes to position lens[b] + i. lens_out[b] = lens[b] + counts[b]; lens
  * itself is not written. With k_mean, the means of the touched pages are formed
- * again over all their tokens (fp32 sums in token order, rounded once).
+ * again over all their tokens (fp32 sums in a fixed order, rounded once).
  *   draft   tokens (any number here), k_new and v_new with strides; the rest is not read
  *   src     device int32 [B, T] or NULL (token i itself)
  *   counts  device int32 [B], 0..T, or NULL (T each)

@@ -1,5 +1,6 @@
 // Eviction: the tokens of a (sequence, KV head) with the most accumulated
-// weight, its sinks and its recent ones, compacted into other pages.
+// weight, its sinks and its recent ones, compacted into other pages. The copy
+// gathers rows of 256 bytes (d = 128): 134 MB, read and written, in 25 us.
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -11,7 +12,8 @@ namespace {
 
 // 512 threads of at most 64 registers: two CTAs fit an SM, so that clusters of
 // eight find room in every GPC (of 1,024 one in sixteen waited for the others to
-// end: four caches of 65,664 took 33 us, now 16).
+// end: four caches of 65,664 took 33 us, with 512 it is 20). Three or four dependent
+// passes over the digits, 1.5 us each, and not the 4 MB of scores are the bound.
 constexpr int kChooseThreads = 512;
 
 __global__ void __launch_bounds__(kChooseThreads, 2) cache_evict_choose_kernel(const __grid_constant__ CacheEvictLaunch L) {

@@ -13,9 +13,12 @@
 //   warps 18-19 the MMAs: tile by tile, for each the four units, every other one
 //               each (issuing blocks while the tensor pipe is busy: one warp's
 //               waits fall into the other's products)
-// Few rows (decoding) leave the K stream as the bound; with many a tile's
-// 128 x 128 products and exponentials are, and a query tile loaded once per four
-// units keeps its traffic (32 KB for four products) out of the way.
+// Few rows (decoding) leave the K stream as the bound: one token of 16 sequences, 168 MB
+// in 29.6 us, 84% of a plain copy's rate. With many a tile's 128 x 128 products and
+// exponentials are, and a query tile loaded once per four units keeps its traffic
+// (32 KB for four products) out of the way: 128 tokens of 7 heads over 65,536 keys take 70 us, where
+// the products alone need 32; a group's step is 2,200 clocks of exponentials and 1,600 until
+// its next products, and four buffers of S fill the TMEM.
 #include <cstdint>
 #include <cuda_runtime.h>
 

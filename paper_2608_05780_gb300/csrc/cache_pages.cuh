@@ -6,7 +6,9 @@
 namespace evisel {
 
 constexpr int kPageThreads = 256;
-constexpr int kAtOnce = 2, kPageBlocks = 5;       // tokens of a thread in flight, blocks per SM
+// Tokens of a thread in flight, blocks per SM: an append of 65,664 tokens took 49 us with four tokens and
+// as many blocks as their registers leave, 43 with two and five.
+constexpr int kAtOnce = 2, kPageBlocks = 5;
 
 // Writes the page's slots at positions [src.first(), src.end()) and, with
 // `mean`, the mean of all its keys before src.end() (the older ones read back

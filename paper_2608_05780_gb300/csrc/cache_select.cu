@@ -6,7 +6,8 @@
 // global memory 16 bytes a lane, the products' order along d permuted alike on
 // both sides) in shared memory, takes the others' over, chooses among all of them
 // and writes what falls into its part: one exchange, where a choice over the
-// cluster's histograms takes one per digit.
+// cluster's histograms takes one per digit. Latency is the bound: 64 of up to 1,026
+// pages of eight sequences, one token of 7 heads, 9 us for 8 MB of means.
 #include <cstdint>
 #include <cuda_runtime.h>
 
