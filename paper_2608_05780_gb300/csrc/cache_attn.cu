@@ -819,7 +819,7 @@ cudaError_t launch_d(const CacheAttnLaunch& L, cudaStream_t stream) {
 // of the tables allows, us with few / wide: 7 heads a KV head of 128, one
 // sequence of 8,192 with 6 tokens (1,536 units) 14.5 / 15.8, 16,384 with 3
 // (2,048) 14.7 / 19.0, 32,768 with 4 (4,096) 19.6 / 22.8, with 6 (6,144) 23.5 / 23.2,
-// with 12 24.8 / 36.6 the other way; 32 of 4,096 with 3 (16,384) 74 / 54. Rows 17 to
+// with 12 (12,288) 36.6 / 24.8; 32 of 4,096 with 3 (16,384) 74 / 54. Rows 17 to
 // 32 of heads of 64 have a tile of their own: 32,768 tokens and 8 KV heads take 28.5 us
 // in tiles of 16, 22.3 in one of 32 and 27.1 wide; below 2,048 units 16 is faster
 // (2,048 tokens: 8.6 / 9.9).

@@ -59,6 +59,56 @@ def test_attention_of_drafted_trees(cuda_lib, lens, t, hq, hkv, d, page, dtype, 
     check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref, allowed, drafted), d, ty)
 
 
+def _roomy(cache):
+    """The same tokens in a table that could hold a million: what the choice of a kernel goes by."""
+    import torch
+    more = (1 << 20) // cache.page - cache.table.shape[-1]
+    return cache.view(torch.nn.functional.pad(cache.table, (0, more), value=-1), cache.lens)
+
+
+@pytest.mark.parametrize("lens,t,hq,hkv,d,page,dtype,layout,gain", [x for x in ATTEND if x[1] * x[2] // x[3] > 16] + [
+    ([300, 0, 129], 12, 4, 2, 64, 16, "fp16", "nhd", 4.0),             # 24 rows of heads of 64
+    ([1, 65, 511], 16, 14, 2, 64, 32, "bf16", "hnd", 4.0),             # 112 rows, one slot
+    ([2000, 0, 300], 45, 7, 1, 128, 64, "fp16", "hnd", 4.0),           # three slots
+])
+def test_attention_of_drafted_trees_in_roomy_tables(cuda_lib, lens, t, hq, hkv, d, page, dtype, layout, gain):
+    """The same by the kernels that long caches take."""
+    import torch
+    rng = np.random.default_rng(len(lens) * 2000 + t)
+    ty = _types()[dtype]
+    cache, ref = make_cache(rng, lens, hkv, d, page, ty, layout, gain=gain)
+    batch = len(lens)
+    q, q_ref = tensor(rng, (batch, t, hq, d), ty)
+    k, k_ref = tensor(rng, (batch, t, hkv, d), ty, gain)
+    v, v_ref = tensor(rng, (batch, t, hkv, d), ty)
+    allowed = random_tree(rng, batch, t)
+    drafted = rng.integers(0, t + 1, batch)
+    cache = _roomy(cache)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, tree=tree_words(allowed),
+                                                 drafted=torch.from_numpy(drafted.astype(np.int32)).cuda())
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref, allowed, drafted), d, ty)
+    # heads outside tokens in memory, and one query for all sequences
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q.transpose(1, 2).contiguous().transpose(1, 2), ws=ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), d, ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q[:1].expand(batch, -1, -1, -1), ws=ws)
+    check_attention(o, lse, ref_cache.attention(ref, np.repeat(q_ref[:1], batch, 0)), d, ty)
+    _status(cuda_lib, ws)
+
+
+@pytest.mark.parametrize("per_head", [False, True])
+def test_lengths_of_their_own_in_roomy_tables(cuda_lib, per_head):
+    """Lengths per KV head, and a view of chosen pages, by the kernel that long caches take."""
+    rng = np.random.default_rng(31)
+    ty = _types()["bf16"]
+    lens = np.array([[0, 130, 77], [513, 1, 256]])
+    cache, ref = make_cache(rng, lens if per_head else lens[:, 1], 3, 128, 32, ty, per_head=per_head)
+    q, q_ref = tensor(rng, (2, 30, 21, 128), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(_roomy(cache), q)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), 128, ty)
+
+
 @pytest.mark.parametrize("t", [1, 5, 40])
 def test_attention_defaults(cuda_lib, t):
     """A chain without a tree; every token without counts; one tree for all; the cache alone; a scale of its own."""
