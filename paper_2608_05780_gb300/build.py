@@ -30,8 +30,8 @@ SOURCES = ["probe_attn.cu", "attn_combine.cu", "evidence.cu", "evisel_capi.cpp",
            "cross_frame.cu", "text_evidence.cu", "topp_mask.cu",
            "coarse_evidence.cu", "evisel_cache.cpp", "cache_attn.cu", "cache_attn_wide.cu", "cache_evidence.cu", "cache_evict.cu",
            "cache_append.cu", "cache_select.cu"]
-HEADERS = ["evisel_internal.h", "evisel_plan.h", "sm103_ptx.cuh", "cache_internal.h", "cache_common.cuh", "cache_attn.cuh",
-           "cache_choose.cuh", "cache_pages.cuh"]
+HEADERS = ["evisel_internal.h", "evisel_plan.h", "sm103_ptx.cuh", "cache_internal.h", "cache_split.h", "cache_common.cuh",
+           "cache_attn.cuh", "cache_choose.cuh", "cache_pages.cuh"]
 PUBLIC = ["evisel.h", "evisel_cache.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",

@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include "cache_internal.h"
+#include "cache_split.h"
 #include "sm103_ptx.cuh"
 
 namespace evisel {
@@ -282,27 +283,6 @@ __device__ __forceinline__ Split split_find_entry(const UnitCount& u, int* mem, 
   __syncthreads();
   s.first = mem[1];
   return s;
-}
-
-// CTAs that share `total` units of `problems` problems: each takes at least
-// `least`, and where there are many CTAs to a problem their number is a multiple of
-// the problems', so that problems of one length are cut at their borders (a
-// CTA that crosses one pays its fill and its join twice: 2 us of 10 for one token over 4,160).
-__device__ __forceinline__ int split_ctas(int total, int n_ctas, int least, int problems) {
-  if (problems * 8 <= n_ctas) {
-    const int k = min(n_ctas / problems, (total + least * problems - 1) / (least * problems));
-    return max(1, k) * problems;
-  }
-  return max(1, min(n_ctas, (total + least - 1) / least));
-}
-// CTA i's first unit: floor(i total / ctas), in 32 bits.
-__device__ __forceinline__ int split_begin(int i, int total, int ctas) {
-  const uint32_t q = static_cast<uint32_t>(total) / ctas, r = static_cast<uint32_t>(total) % ctas;
-  return static_cast<int>(i * q + i * r / ctas);     // i, r <= ctas, the CTAs of a grid
-}
-// The CTA that holds unit u.
-__device__ __forceinline__ int split_owner(int u, int total, int ctas) {
-  return static_cast<int>((static_cast<int64_t>(u + 1) * ctas - 1) / total);
 }
 
 // ---------------------------------------------------------------- launch

@@ -777,3 +777,33 @@ def test_out_of_range_device_values_are_reported(cuda_lib):
     o, lse, ws = cuda_lib.evisel_cache_attention(good, q, ws=ws)
     check_attention(o, lse, ref_cache.attention(ref, q_ref), 64, ty)
     _status(cuda_lib, ws)
+
+
+# --- batches of mostly empty sequences ------------------------------------------------
+
+@pytest.mark.parametrize("roomy,lens,t,hq,hkv,d", [
+    (False, [100] + 7 * [0], 1, 28, 4, 128),
+    (False, [600] + 31 * [0], 2, 4, 1, 64),
+    (False, 15 * [0] + [130], 3, 4, 2, 64),
+    (True, [513] + 7 * [0], 40, 14, 2, 128),
+    (True, [0, 1100] + 10 * [0], 9, 4, 1, 64),
+    (False, [100] + 7 * [0], 64, 28, 4, 128),              # the join by tiles of rows
+])
+def test_attention_of_mostly_empty_batches(cuda_lib, roomy, lens, t, hq, hkv, d):
+    """Fewer units than (sequence, KV head) pairs, on a workspace whose scratch a larger call has filled."""
+    rng = np.random.default_rng(t)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, lens, hkv, d, 16, ty, room=8)
+    large, _ = make_cache(rng, [900] * len(lens), hkv, d, 64, ty, poison=False)
+    if roomy:
+        cache, large = _roomy(cache), _roomy(large)
+    q, q_ref = tensor(rng, (len(lens), t, hq, d), ty)
+    _, _, ws = cuda_lib.evisel_cache_attention(large, q)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, ws=ws)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref), d, ty)
+    k, k_ref = tensor(rng, (len(lens), t, hkv, d), ty)
+    v, v_ref = tensor(rng, (len(lens), t, hkv, d), ty)
+    o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, ws=ws)
+    _status(cuda_lib, ws)
+    check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref), d, ty, "with drafted keys")
