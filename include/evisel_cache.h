@@ -17,7 +17,8 @@
  *     kernels, so that a captured graph replays with new ones. A length outside
  *     [0, max_pages * page], a page id outside [0, n_pages), a source index
  *     outside the new tokens or an append past the table is caught by the
- *     kernels: no access leaves the buffers, the results of that sequence are
+ *     kernels: no access leaves the buffers, nothing is written to a page that
+ *     the sequence's table does not hold, the results of that sequence are
  *     unspecified, and evisel_status() answers EVISEL_EBOUNDS.
  *   - A call allocates only when its workspace has to grow: not with the same
  *     or smaller sizes again (capture a graph after a first call).

@@ -24,15 +24,17 @@ __device__ __forceinline__ int cache_len(const CacheView& c, int b, int h, int* 
   return n < 0 ? 0 : static_cast<int>(room);
 }
 
-__device__ __forceinline__ int checked_page(const CacheView& c, int id, int* status) {
+// Page id of logical page j (j < max_pages) to write to: -1 where the table holds none of the pool.
+__device__ __forceinline__ int cache_page_to_write(const CacheView& c, int b, int h, int j, int* status) {
+  const int id = __ldg(c.table + b * c.ts[0] + h * c.ts[1] + j);
   if (static_cast<unsigned>(id) < static_cast<unsigned>(c.n_pages)) return id;
   record_bounds(status);
-  return 0;
+  return -1;
 }
 
-// Page id of logical page j (j < max_pages), a page of the pool whatever the table holds.
+// The same to read from: a page of the pool whatever the table holds.
 __device__ __forceinline__ int cache_page(const CacheView& c, int b, int h, int j, int* status) {
-  return checked_page(c, __ldg(c.table + b * c.ts[0] + h * c.ts[1] + j), status);
+  return max(0, cache_page_to_write(c, b, h, j, status));
 }
 
 __device__ __forceinline__ int drafted_tokens(const DraftView& d, int b) {

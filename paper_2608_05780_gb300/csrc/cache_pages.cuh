@@ -21,7 +21,8 @@ __device__ __forceinline__ void fill_page(const CacheView& c, void* k_out, void*
   __shared__ float sums[GROUPS][D];
   const int p0 = page << c.log_page, p1 = min(p0 + c.page, src.end());
   if (p1 <= p0 || p1 <= src.first()) return;     // (the whole block)
-  const int64_t id = cache_page(c, b, h, page, status);
+  const int64_t id = cache_page_to_write(c, b, h, page, status);
+  if (id < 0) return;                            // (the whole block: any other page has its own tokens)
   uint16_t* k = static_cast<uint16_t*>(k_out) + id * c.ks[0] + h * c.ks[1];
   uint16_t* v = static_cast<uint16_t*>(v_out) + id * c.vs[0] + h * c.vs[1];
   const int x = threadIdx.x % LANES, grp = threadIdx.x / LANES;

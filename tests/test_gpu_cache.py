@@ -807,3 +807,50 @@ def test_attention_of_mostly_empty_batches(cuda_lib, roomy, lens, t, hq, hkv, d)
     o, lse, ws = cuda_lib.evisel_cache_attention(cache, q, k, v, ws=ws)
     _status(cuda_lib, ws)
     check_attention(o, lse, ref_cache.attention(ref, q_ref, k_ref, v_ref), d, ty, "with drafted keys")
+
+
+# --- what a bad table or length may not write ------------------------------------------
+
+@pytest.mark.parametrize("bad", [-1, -7, "past"])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 32)])
+def test_a_bad_page_id_writes_nothing(cuda_lib, bad, d, page):
+    """An append onto a page that the table does not have, and an eviction into one: the other sequences' pages (id 0
+    among them) and means stay as they were, their own tokens arrive, and the status says so."""
+    import torch
+    rng = np.random.default_rng(d)
+    ty = _types()["bf16"]
+
+    def two(lens):                               # sequence 0 holds pages 0 and 1; sequence 1 page 2 and then a bad one
+        k, v = (torch.from_numpy(rng.standard_normal((4, 2, page, d))).to(ty).cuda() for _ in range(2))
+        mean = torch.from_numpy(rng.standard_normal((4, 2, d))).to(ty).cuda()
+        table = torch.tensor([[0, 1], [2, 4 if bad == "past" else bad]], dtype=torch.int32, device="cuda")
+        return cuda_lib.Cache(k, v, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), mean)
+
+    cache = two([page - 2, page])
+    before = [x.clone() for x in (cache.k, cache.v, cache.k_mean)]
+    k_new, _ = tensor(rng, (2, 5, 2, d), ty)
+    v_new, _ = tensor(rng, (2, 5, 2, d), ty)
+    _, ws = cuda_lib.evisel_cache_append(cache, k_new, v_new)
+    assert cuda_lib.evisel_status(ws) == -7
+    for pool, old, x in ((cache.k, before[0], k_new), (cache.v, before[1], v_new)):
+        assert torch.equal(pool[0, :, :page - 2], old[0, :, :page - 2]) and torch.equal(pool[0, :, page - 2:], x[0, :2].transpose(0, 1))
+        assert torch.equal(pool[1, :, :3], x[0, 2:].transpose(0, 1)) and torch.equal(pool[1, :, 3:], old[1, :, 3:])
+        assert torch.equal(pool[2:], old[2:])
+    assert torch.equal(cache.k_mean[2:], before[2][2:])
+    for i, m in ((0, page), (1, 3)):
+        part = cache.k[i, :, :m].double()
+        assert torch.all((cache.k_mean[i].double() - part.mean(1)).abs() <= (u_of(ty) + page * 2.0 ** -23) * part.abs().mean(1))
+
+    full, _ = make_cache(rng, [2 * page, 2 * page], 2, d, 16, ty, poison=False)
+    out = two([0, 0])
+    before = [x.clone() for x in (out.k, out.v, out.k_mean)]
+    acc = torch.rand((2, 2, full.max_tokens), device="cuda")
+    kept, _, ws = cuda_lib.evisel_cache_evict(full, acc, out, 2 * page - 1, ws=ws)
+    assert cuda_lib.evisel_status(ws) == -7
+    for pool, old, src in ((out.k, before[0], full.k), (out.v, before[1], full.v)):
+        for h in range(2):
+            pos = kept[0, h].long()
+            want = src[full.table[0, pos // 16].long(), h, pos % 16]
+            assert torch.equal(pool[:2, h].reshape(2 * page, d)[:2 * page - 1], want)
+        assert torch.equal(pool[1, :, page - 1], old[1, :, page - 1]) and torch.equal(pool[3], old[3])
+    assert torch.equal(out.k_mean[3], before[2][3])
