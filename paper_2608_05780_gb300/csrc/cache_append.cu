@@ -19,6 +19,7 @@ struct NewTokens {
       record_bounds(L.status);
       count = count < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(min(count, L.d.tokens)), room));
     }
+    if (__ldg(L.c.lens + b * L.c.ls[0]) < 0) count = 0;   // the first pages may be another sequence's too
   }
   __device__ __forceinline__ int first() const { return len; }
   __device__ __forceinline__ int end() const { return len + count; }

@@ -854,3 +854,20 @@ def test_a_bad_page_id_writes_nothing(cuda_lib, bad, d, page):
             assert torch.equal(pool[:2, h].reshape(2 * page, d)[:2 * page - 1], want)
         assert torch.equal(pool[1, :, page - 1], old[1, :, page - 1]) and torch.equal(pool[3], old[3])
     assert torch.equal(out.k_mean[3], before[2][3])
+
+
+def test_a_negative_length_appends_nothing(cuda_lib):
+    """A page shared as a prefix by two sequences, one of which has a bad length."""
+    import torch
+    rng = np.random.default_rng(3)
+    ty = _types()["bf16"]
+    pools = [torch.from_numpy(rng.standard_normal((3, 1, 16, 64))).to(ty).cuda() for _ in range(2)]
+    table = torch.tensor([[0, 1], [0, 2]], dtype=torch.int32, device="cuda")
+    cache = cuda_lib.Cache(*pools, table, torch.tensor([16, -16], dtype=torch.int32, device="cuda"))
+    before = [x.clone() for x in pools]
+    new, _ = tensor(rng, (2, 2, 1, 64), ty)
+    _, ws = cuda_lib.evisel_cache_append(cache, new, new)
+    assert cuda_lib.evisel_status(ws) == -7
+    for pool, old in zip(pools, before):
+        assert torch.equal(pool[0], old[0]) and torch.equal(pool[2], old[2])
+        assert torch.equal(pool[1, 0, :2], new[0, :, 0]) and torch.equal(pool[1, 0, 2:], old[1, 0, 2:])
