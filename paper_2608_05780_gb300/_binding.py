@@ -145,6 +145,21 @@ def _stream_handle(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _maker(make, stream):
+    """``make`` (torch.empty, torch.zeros) with its tensors on ``stream``, the one that a call runs on: they are filled
+    in its order, and their memory goes back to it."""
+    if stream is None:
+        return make
+    import torch
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+
+    def on_stream(*args, **kw):
+        with torch.cuda.stream(stream):
+            return make(*args, **kw)
+    return on_stream
+
+
 class Workspace:
     """Owner of an evisel_ws* (freed with evisel_free)."""
 

@@ -6,6 +6,9 @@ Lengths, tables, tree bits and counts stay on the device: no call waits for it,
 and what they hold is checked by the kernels (``evisel_status(ws)`` answers
 EVISEL_EBOUNDS, -7, where a length, page id or index was out of range).
 
+``stream`` (a torch.cuda.Stream) takes the place of the current one. What a call
+reads must be ready there; the tensors that it returns are made on it.
+
 A decoding step's calls take a few microseconds on the device, so that the
 checks here are plain comparisons, their messages formed only when one fails.
 """
@@ -14,7 +17,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from ._binding import Workspace, _check, load
+from ._binding import Workspace, _check, _maker, load
 
 _CACHE = struct.Struct("@8i10q5P")
 _DRAFT = struct.Struct("@iifi11q5P")
@@ -36,7 +39,7 @@ class _Calls:
             f = getattr(lib, "evisel_cache_" + name)
             f.argtypes, f.restype = args, i32
             setattr(self, name, f)
-        self.empty, self.i32, self.f32 = torch.empty, torch.int32, torch.float32
+        self.empty, self.zeros, self.i32, self.f32 = torch.empty, torch.zeros, torch.int32, torch.float32
         self.dtypes = {torch.bfloat16: 0, torch.float16: 1}
         self.masks = (torch.bool, torch.uint8)
         self.current_device = torch.cuda.current_device
@@ -136,11 +139,11 @@ class Cache:
         c._set(table, lens)
         return c
 
-    def _choice(self, n):
+    def _choice(self, n, empty):
         """A view of n pages per (sequence, head), its table and lengths to be written; the addresses of both."""
         c, batch, hkv = self._same_pages(), self.batch, self.hkv
         c._table = c._lens = None
-        c._chosen = _calls.empty((batch * hkv * (n + 1),), dtype=_calls.i32, device=self.device)
+        c._chosen = empty((batch * hkv * (n + 1),), dtype=_calls.i32, device=self.device)
         c.batch, c.max_tokens = batch, n * self.page
         table_p = c._chosen.data_ptr()
         lens_p = table_p + 4 * batch * hkv * n
@@ -213,8 +216,9 @@ def evisel_cache_attention(cache, q, k_new=None, v_new=None, tree=None, drafted=
     Returns (o [B, T, hq, d], lse [hq, B, T] fp32, ws)."""
     draft = _draft(cache, q, k_new, v_new, tree, drafted, softmax_scale)
     batch, tokens, hq, d = q.shape
-    o_p = (_calls.empty((batch, tokens, hq, d), dtype=cache.dtype, device=cache.device) if o is None else o)
-    lse_p = (_calls.empty((hq, batch, tokens), dtype=_calls.f32, device=cache.device) if lse is None else lse)
+    empty = _maker(_calls.empty, stream)
+    o_p = (empty((batch, tokens, hq, d), dtype=cache.dtype, device=cache.device) if o is None else o)
+    lse_p = (empty((hq, batch, tokens), dtype=_calls.f32, device=cache.device) if lse is None else lse)
     if o is not None:
         _plain(cache, o, cache.dtype, q.shape, "o")
     if lse is not None:
@@ -238,7 +242,7 @@ def evisel_cache_evidence(cache, q, lse, acc=None, use=None, drafted=None, accum
     batch, tokens, hq, _ = q.shape
     lse_p = _plain(cache, lse, _calls.f32, (hq, batch, tokens), "lse")
     if acc is None:
-        acc = _calls.empty((batch, cache.hkv, cache.max_tokens), dtype=_calls.f32, device=cache.device).zero_()
+        acc = _maker(_calls.zeros, stream)((batch, cache.hkv, cache.max_tokens), dtype=_calls.f32, device=cache.device)
     n = acc.shape[-1] if acc.dim() else 0
     acc_p = _plain(cache, acc, _calls.f32, (batch, cache.hkv, n), "acc")
     use_p = 0
@@ -266,14 +270,15 @@ def evisel_cache_evict(cache, acc, out, budget, sink=0, recent=0, kept=None, acc
     if not (out.device == cache.device and out.batch == batch and out.hkv == hkv):
         _refuse("out must have the cache's batch, heads and device")
     shape = (batch, hkv, budget if budget > 0 else 0)
+    empty = _maker(_calls.empty, stream)
     if kept is None:
-        kept = _calls.empty(shape, dtype=_calls.i32, device=cache.device)
+        kept = empty(shape, dtype=_calls.i32, device=cache.device)
         kept_p = kept.data_ptr()
     else:
         kept_p = _plain(cache, kept, _calls.i32, shape, "kept")
     if acc_out is None:
         m = out.max_tokens
-        acc_out = _calls.empty((batch, hkv, m), dtype=_calls.f32, device=cache.device)
+        acc_out = empty((batch, hkv, m), dtype=_calls.f32, device=cache.device)
         acc_out_p = acc_out.data_ptr()
     else:
         m = acc_out.shape[-1] if acc_out.dim() else 0
@@ -297,7 +302,7 @@ def evisel_cache_append(cache, k_new, v_new, src=None, counts=None, lens_out=Non
     ks, kp = _new(cache, k_new, shape, "k_new")
     vs, vp = _new(cache, v_new, shape, "v_new")
     if lens_out is None:
-        lens_out = _calls.empty((batch,), dtype=_calls.i32, device=cache.device)
+        lens_out = _maker(_calls.empty, stream)((batch,), dtype=_calls.i32, device=cache.device)
         out_p = lens_out.data_ptr()
     else:
         out_p = _plain(cache, lens_out, _calls.i32, (batch,), "lens_out")
@@ -320,8 +325,9 @@ def evisel_cache_select(cache, q, n_select, sink=0, recent=1, drafted=None, ws=N
     int32 [B, hkv, n_select], ascending, -1 past them."""
     draft = _draft(cache, q, None, None, None, drafted, 0.0)
     n = max(0, int(n_select))
-    pages = _calls.empty((cache.batch, cache.hkv, n), dtype=_calls.i32, device=cache.device)
-    view, table_p, lens_p = cache._choice(n)
+    empty = _maker(_calls.empty, stream)
+    pages = empty((cache.batch, cache.hkv, n), dtype=_calls.i32, device=cache.device)
+    view, table_p, lens_p = cache._choice(n, empty)
     ws = Workspace() if ws is None else ws
     rc = _calls.select(cache._packed, draft, int(n_select), int(sink), int(recent), pages.data_ptr(), table_p, lens_p,
                        _stream(cache, stream), ctypes.byref(ws.ptr))

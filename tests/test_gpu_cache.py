@@ -871,3 +871,41 @@ def test_a_negative_length_appends_nothing(cuda_lib):
     for pool, old in zip(pools, before):
         assert torch.equal(pool[0], old[0]) and torch.equal(pool[2], old[2])
         assert torch.equal(pool[1, 0, :2], new[0, :, 0]) and torch.equal(pool[1, 0, 2:], old[1, 0, 2:])
+
+
+# --- a stream of the caller's -----------------------------------------------------------
+
+def test_new_tensors_are_made_on_the_stream_of_the_call(cuda_lib):
+    """With ``stream=`` and no outputs given: the results are those of the current stream's calls, however busy that
+    one is meanwhile, and the memory of the new tensors is the given stream's."""
+    import torch
+    rng = np.random.default_rng(21)
+    ty = _types()["bf16"]
+    cache, _ = make_cache(rng, [700, 300], 2, 64, 16, ty, room=8, mean=True, poison=False)
+    out, _ = make_cache(rng, [0, 0], 2, 64, 16, ty, room=64, poison=False)
+    q, _ = tensor(rng, (2, 3, 4, 64), ty)
+    kv, _ = tensor(rng, (2, 3, 2, 64), ty)
+    side, ws = torch.cuda.Stream(), cuda_lib.Workspace()
+
+    def calls(stream):
+        o, lse, _ = cuda_lib.evisel_cache_attention(cache, q, kv, kv, ws=ws, stream=stream)
+        acc, _ = cuda_lib.evisel_cache_evidence(cache, q, lse, ws=ws, stream=stream)
+        kept, acc_out, _ = cuda_lib.evisel_cache_evict(cache, acc, out, 64, sink=1, recent=2, ws=ws, stream=stream)
+        view, pages, _ = cuda_lib.evisel_cache_select(cache, q, 5, ws=ws, stream=stream)
+        lens, _ = cuda_lib.evisel_cache_append(cache, kv, kv, ws=ws, stream=stream)
+        return [o, lse, acc, kept, acc_out, view.table, view.lens, pages, lens]
+
+    want = calls(None)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)               # the current stream is busy for about 0.1 s
+    got = calls(side)
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(want, got)):
+        assert torch.equal(a, b), i
+    # Freed while the side stream still runs, none of them may be handed to the current one.
+    sizes = [(x.shape, x.dtype, x.data_ptr()) for x in got]
+    where = {p for _, _, p in sizes}
+    del got
+    again = [torch.empty(s, dtype=t, device="cuda") for s, t, _ in sizes]
+    assert not where & {x.data_ptr() for x in again}
+    assert cuda_lib.evisel_status(ws) == 0
