@@ -224,10 +224,11 @@ def evisel_probe_attention(q, k, v, cu_seqlens, n_vis, tokens_per_frame, tile, r
         if not (t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.dim() == 3):
             raise ValueError("q, k, v must be contiguous CUDA bf16 tensors [N, H, d]")
     n, hq, d = q.shape
+    empty = _maker(torch.empty, stream)
     if o is None:
-        o = torch.empty((n, hq, d), dtype=torch.bfloat16, device=q.device)
+        o = empty((n, hq, d), dtype=torch.bfloat16, device=q.device)
     if lse is None:
-        lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
+        lse = empty((hq, n), dtype=torch.float32, device=q.device)
     if ws is None:
         ws = Workspace()
     args, keep = make_args(q, k, v, cu_seqlens, n_vis, tokens_per_frame, tile, row_ptr, col_idx, o, lse,
@@ -249,13 +250,14 @@ def evisel_evidence_reduce(ws, hq, n_vis, tokens_per_frame, num_videos, tok=None
         # The call overwrites every entry unless it accumulates (head and A_qf always).
         total_vis = _total(n_vis)
         total_frames = total_vis // int(tokens_per_frame)
-        new = torch.zeros if accumulate else torch.empty
+        zeros = _maker(torch.zeros, stream)
+        new = zeros if accumulate else _maker(torch.empty, stream)
         if tok is None:
             tok = new((hq, total_vis), dtype=torch.float32, device=device)
         if frame is None:
             frame = new((hq, total_frames), dtype=torch.float32, device=device)
         if head is None:
-            head = torch.zeros((num_videos, hq), dtype=torch.float32, device=device)
+            head = zeros((num_videos, hq), dtype=torch.float32, device=device)
         if aqf is None:
             aqf = new((total_frames,), dtype=torch.float32, device=device)
     _check(lib.evisel_evidence_reduce(ws.ptr, tok.data_ptr(), frame.data_ptr(), head.data_ptr(),
@@ -317,8 +319,8 @@ def evisel_intra_frame_evidence(q, k, v, cu_seqlens, n_vis, tokens_per_frame, ti
     n_vis_np = np.asarray(n_vis, dtype=np.int64)
     frames = int(np.sum(n_vis_np // int(tokens_per_frame)))
     if aif is None:
-        aif = torch.zeros((frames, int(tokens_per_frame), int(tokens_per_frame)), dtype=torch.float32,
-                          device=q.device)
+        aif = _maker(torch.zeros, stream)((frames, int(tokens_per_frame), int(tokens_per_frame)), dtype=torch.float32,
+                                          device=q.device)
     args, keep = make_args(q, k, v, cu_seqlens, n_vis, tokens_per_frame, tile, row_ptr, col_idx, o, lse,
                            softmax_scale)
     _check(lib.evisel_intra_frame_evidence(ctypes.byref(args), ws.ptr, aif.data_ptr(), int(bool(accumulate)),
@@ -339,10 +341,11 @@ def evisel_cross_frame_evidence(q, k, v, cu_seqlens, n_vis, tokens_per_frame, ti
     npf = int(tokens_per_frame)
     t = np.asarray(n_vis, dtype=np.int64) // npf
     n_aff = int(np.sum(np.maximum(t - 1, 0) ** 2))
+    empty = _maker(torch.empty, stream)
     if aff is None:
-        aff = torch.empty(n_aff, dtype=torch.float32, device=q.device)
+        aff = empty(n_aff, dtype=torch.float32, device=q.device)
     if eff is None:
-        eff = torch.empty(int(np.sum(t)), dtype=torch.float32, device=q.device)
+        eff = empty(int(np.sum(t)), dtype=torch.float32, device=q.device)
     args, keep = make_args(q, k, v, cu_seqlens, n_vis, tokens_per_frame, tile, row_ptr, col_idx, o, lse,
                            softmax_scale, True)
     _check(lib.evisel_cross_frame_evidence(ctypes.byref(args), ws.ptr, aff.data_ptr() if n_aff else None,
@@ -365,12 +368,13 @@ def evisel_topp_mask(q, k, cu_seqlens, n_vis, tokens_per_frame, tile, block, tau
     nb = nv // int(block) + -(-n_text // int(block))
     n, hq = int(q.shape[0]), int(q.shape[1])
     n_words = max(1, -(-int(nb.max() if nb.size else 0) // 32))
-    keep = torch.empty((hq, n_words, n), dtype=torch.int32, device=q.device)
+    empty = _maker(torch.empty, stream)
+    keep = empty((hq, n_words, n), dtype=torch.int32, device=q.device)
     n_vt = -(-nv // int(tile))
     uni = None
     if union:
-        uni = torch.empty((int(n_vt.sum()), max(1, -(-int(n_vt.max() if n_vt.size else 0) // 32))),
-                          dtype=torch.int32, device=q.device)
+        uni = empty((int(n_vt.sum()), max(1, -(-int(n_vt.max() if n_vt.size else 0) // 32))),
+                    dtype=torch.int32, device=q.device)
     if ws is None:
         ws = Workspace()
     dummy = torch.empty(0, device=q.device)
@@ -409,10 +413,11 @@ def evisel_coarse_evidence(q, k, cu_seqlens, n_vis, tokens_per_frame, tile, bloc
     total_vis = int(nv.sum())
     frames = int((nv // int(tokens_per_frame)).sum())
     dev = q.device
-    tok = torch.empty((hq, total_vis), device=dev) if tok is None else tok
-    frame = torch.empty((hq, frames), device=dev) if frame is None else frame
-    head = torch.empty((len(nv), hq), device=dev) if head is None else head
-    aqf = torch.empty((frames,), device=dev) if aqf is None else aqf
+    empty = _maker(torch.empty, stream)
+    tok = empty((hq, total_vis), device=dev) if tok is None else tok
+    frame = empty((hq, frames), device=dev) if frame is None else frame
+    head = empty((len(nv), hq), device=dev) if head is None else head
+    aqf = empty((frames,), device=dev) if aqf is None else aqf
     dummy = torch.empty(0, device=dev)
     args, keepalive = make_args(q, k, k, cu_seqlens, n_vis, tokens_per_frame, tile, [0], [], dummy, dummy,
                                 softmax_scale)
