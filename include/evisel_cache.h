@@ -20,8 +20,11 @@
  *     kernels: no access leaves the buffers, nothing is written to a page that
  *     the sequence's table does not hold, the results of that sequence are
  *     unspecified, and evisel_status() answers EVISEL_EBOUNDS.
- *   - A call allocates only when its workspace has to grow: not with the same
- *     or smaller sizes again (capture a graph after a first call).
+ *   - A call allocates only where it creates its workspace or an attention needs
+ *     more scratch than it holds, which is refused (EVISEL_EINVAL) while `stream`
+ *     is being captured: not with the same or smaller sizes again, so capture
+ *     after a first call. Scratch that a larger call outgrew stays until
+ *     evisel_free(), and with it the graphs that were captured before.
  */
 #ifndef EVISEL_CACHE_H
 #define EVISEL_CACHE_H
@@ -92,7 +95,7 @@ typedef struct {
  *   lse  device fp32 [hq, B, T], natural log (written)
  * The workspace keeps the fp32 partial results of ranges of cached keys: for
  * tiles of r = 16, 32, 128 or 256 rows (2 SMs + B * hkv * ceil(T * hq / hkv / r))
- * * r * (d + 2) * 4 bytes at most.
+ * * r * (d + 2) * 4 bytes; with what it outgrew at most 4.5 times as much.
  * Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED, EVISEL_ENOMEM, EVISEL_ECUDA. */
 int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft, void* o, float* lse, void* stream,
                            evisel_ws** ws_inout);

@@ -2,6 +2,8 @@
 // and their kernels. Not part of the public ABI.
 #pragma once
 
+#include <vector>
+
 #include "evisel_internal.h"
 
 struct evisel_ws;
@@ -138,11 +140,12 @@ cudaError_t launch_cache_attn_wide(const CacheAttnLaunch& L, cudaStream_t stream
 struct WsCache {
   void* buf = nullptr;              // scratch of the calls
   size_t bytes = 0;
+  std::vector<void*> outgrown;      // earlier ones, whose addresses graphs may hold
+  size_t held = 0;                  // bytes of all of them
 };
 int ws_acquire(evisel_ws** inout);  // creates one where *inout is null
 WsCache& ws_cache(evisel_ws* ws);
 int* ws_status(evisel_ws* ws);
-cudaStream_t ws_last_stream(evisel_ws* ws);
 void ws_ran_on(evisel_ws* ws, cudaStream_t stream);
 // 4-D map of `dims` with byte strides `strides` of dims 1..3, 128-byte swizzle; dtype as evisel_cache's.
 int encode_map4(CUtensorMap* map, const void* base, int dtype, const uint64_t (&dims)[4], const uint64_t (&strides)[3],

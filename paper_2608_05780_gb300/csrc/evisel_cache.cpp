@@ -205,20 +205,47 @@ int encode_queries(CUtensorMap* map, int* perm, QueryTile* tile, const evisel_ca
   return rc;
 }
 
+// Whether a call on `stream` may allocate now.
+int check_may_allocate(cudaStream_t stream, const char* what) {
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  const cudaError_t e = cudaStreamIsCapturing(stream, &capture);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return cuda_fail(e, "cudaStreamIsCapturing");
+  }
+  if (capture != cudaStreamCaptureStatusNone)
+    return fail(EVISEL_EINVAL, std::string(what) + " during a stream capture: make a call of this size before it, on the same workspace");
+  return EVISEL_OK;
+}
+
+// The caller's workspace, or a new one.
+int acquire(evisel_ws** ws_inout, cudaStream_t stream) {
+  if (!*ws_inout) {
+    const int rc = check_may_allocate(stream, "a workspace cannot be created");
+    if (rc != EVISEL_OK) return rc;
+  }
+  return ws_acquire(ws_inout);
+}
+
+// Scratch of `need` bytes. A smaller one stays until the workspace is freed: captured
+// graphs, and calls in flight, hold its address. Each is at least half as large again
+// as the one before it, so that all of them together are at most 4.5 times the largest need.
 int grow(evisel_ws* ws, size_t need, cudaStream_t stream) {
   WsCache& w = ws_cache(ws);
   if (need <= w.bytes) return EVISEL_OK;
-  cudaStreamSynchronize(ws_last_stream(ws));     // the old scratch may be in use
-  cudaStreamSynchronize(stream);
-  if (w.buf) cudaFree(w.buf);
-  w.buf = nullptr;
-  w.bytes = 0;
-  if (cudaMalloc(&w.buf, need) != cudaSuccess) {
+  const int rc = check_may_allocate(stream, "the workspace cannot grow");
+  if (rc != EVISEL_OK) return rc;
+  const size_t bytes = std::max(need, w.bytes + w.bytes / 2);
+  w.outgrown.reserve(w.outgrown.size() + 1);     // (what may throw, before the allocation)
+  void* buf = nullptr;
+  if (cudaMalloc(&buf, bytes) != cudaSuccess) {
     cudaGetLastError();
-    w.buf = nullptr;
-    return fail(EVISEL_ENOMEM, "cache scratch of " + std::to_string(need) + " bytes");
+    return fail(EVISEL_ENOMEM, "cache scratch of " + std::to_string(bytes) + " bytes");
   }
-  w.bytes = need;
+  if (w.buf) w.outgrown.push_back(w.buf);
+  w.buf = buf;
+  w.bytes = bytes;
+  w.held += bytes;
   return EVISEL_OK;
 }
 
@@ -278,8 +305,8 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
     if (problems * (tiles + L.lead) > kMaxUnits) return fail(EVISEL_EUNSUPPORTED, "too many units of work");
     const size_t parts = static_cast<size_t>(L.n_ctas) + problems;
     const size_t ml_bytes = align_up(parts * L.tile_rows * sizeof(float2), 256);
-    rc = ws_acquire(ws_inout);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    rc = acquire(ws_inout, stream);
     if (rc == EVISEL_OK) rc = grow(*ws_inout, ml_bytes + parts * L.tile_rows * cache->head_dim * sizeof(float), stream);
     if (rc == EVISEL_OK && cache->max_pages > 0) rc = encode_pages(&L.tm_k, &L.k_perm, cache->k, cache, cache->k_stride, L.box_rows);
     if (rc == EVISEL_OK && cache->max_pages > 0) rc = encode_pages(&L.tm_v, &L.v_perm, cache->v, cache, cache->v_stride, L.box_rows);
@@ -319,7 +346,8 @@ int evisel_cache_evidence(const evisel_cache* cache, const evisel_draft* draft, 
     L.has_q_map = draft->tokens > 0 && has_query_map(cache, draft);
     if (static_cast<int64_t>(cache->batch) * cache->hkv * ((static_cast<int64_t>(cache->max_pages) * cache->page + 127) / 128) > kMaxUnits)
       return fail(EVISEL_EUNSUPPORTED, "too many units of work");
-    rc = ws_acquire(ws_inout);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    rc = acquire(ws_inout, stream);
     if (rc == EVISEL_OK && L.has_q_map) rc = encode_pages(&L.tm_k, &L.k_perm, cache->k, cache, cache->k_stride, L.box_rows);
     if (rc == EVISEL_OK && L.has_q_map) rc = encode_queries(&L.tm_q, &L.q_perm, &L.qt, cache, draft);
     if (rc != EVISEL_OK) return rc;
@@ -329,7 +357,6 @@ int evisel_cache_evidence(const evisel_cache* cache, const evisel_draft* draft, 
     L.acc_len = acc_len;
     L.status = ws_status(*ws_inout);
     L.accumulate = accumulate != 0;
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     const cudaError_t e = launch_cache_evidence(L, stream);
     if (e != cudaSuccess) return cuda_fail(e, "cache evidence launch");
     ws_ran_on(*ws_inout, stream);
@@ -359,7 +386,8 @@ int evisel_cache_evict(const evisel_cache* cache, const float* acc, int64_t acc_
       return fail(EVISEL_EINVAL, "acc, kept and acc_out must be 4-byte aligned");
     if (acc == acc_out || out->lens == cache->lens || (out->k == cache->k && out->table == cache->table))
       return fail(EVISEL_EINVAL, "out and acc_out must not be the cache's own");
-    rc = ws_acquire(ws_inout);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    rc = acquire(ws_inout, stream);
     if (rc != EVISEL_OK) return rc;
     CacheEvictLaunch L{};
     L.c = view_of(cache);
@@ -377,7 +405,6 @@ int evisel_cache_evict(const evisel_cache* cache, const float* acc, int64_t acc_
     L.sink = sink;
     L.recent = recent;
     L.status = ws_status(*ws_inout);
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     const cudaError_t e = launch_cache_evict(L, stream);
     if (e != cudaSuccess) return cuda_fail(e, "cache eviction launch");
     ws_ran_on(*ws_inout, stream);
@@ -409,7 +436,8 @@ int evisel_cache_append(const evisel_cache* cache, const evisel_draft* draft, co
       if (rc == EVISEL_OK) rc = check_strides(draft->v_new_stride, sizes, 3, "v_new");
       if (rc != EVISEL_OK) return rc;
     }
-    rc = ws_acquire(ws_inout);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    rc = acquire(ws_inout, stream);
     if (rc != EVISEL_OK) return rc;
     CacheAppendLaunch L{};
     L.c = view_of(cache);
@@ -422,7 +450,6 @@ int evisel_cache_append(const evisel_cache* cache, const evisel_draft* draft, co
     L.counts = counts;
     L.lens_out = lens_out;
     L.status = ws_status(*ws_inout);
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     const cudaError_t e = launch_cache_append(L, stream);
     if (e != cudaSuccess) return cuda_fail(e, "cache append launch");
     ws_ran_on(*ws_inout, stream);
@@ -447,8 +474,8 @@ int evisel_cache_select(const evisel_cache* cache, const evisel_draft* draft, in
     if (misaligned(pages, 4) || misaligned(sel_table, 4) || misaligned(sel_lens, 4))
       return fail(EVISEL_EINVAL, "outputs must be 4-byte aligned");
     if (cache->max_pages > 0 && !cache->k_mean) return fail(EVISEL_EINVAL, "the cache has no k_mean");
-    rc = ws_acquire(ws_inout);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    rc = acquire(ws_inout, stream);
     if (rc != EVISEL_OK) return rc;
     CacheSelectLaunch L{};
     L.c = view_of(cache);

@@ -648,7 +648,6 @@ int ws_acquire(evisel_ws** inout) {
 }
 WsCache& ws_cache(evisel_ws* ws) { return ws->cache; }
 int* ws_status(evisel_ws* ws) { return ws->status; }
-cudaStream_t ws_last_stream(evisel_ws* ws) { return ws->last_stream; }
 void ws_ran_on(evisel_ws* ws, cudaStream_t stream) { ws->last_stream = stream; }
 
 int encode_map4(CUtensorMap* map, const void* base, int dtype, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
@@ -1159,6 +1158,7 @@ void evisel_free(evisel_ws* ws) {
   if (ws->topp_buf) cudaFree(ws->topp_buf);
   if (ws->coarse_buf) cudaFree(ws->coarse_buf);
   if (ws->cache.buf) cudaFree(ws->cache.buf);
+  for (void* p : ws->cache.outgrown) cudaFree(p);
   if (ws->topp_stage) cudaFreeHost(ws->topp_stage);
   if (ws->topp_done) cudaEventDestroy(ws->topp_done);
   if (prev >= 0 && prev != ws->device) cudaSetDevice(prev);
@@ -1207,7 +1207,7 @@ static const char kBuildIdString[] = "evisel-build-id:" EVISEL_BUILD_ID;
 const char* evisel_build_id(void) { return kBuildIdString + sizeof("evisel-build-id:") - 1; }
 
 int64_t evisel_workspace_bytes(const evisel_ws* ws) {
-  return ws ? static_cast<int64_t>(ws->arena_bytes + ws->cache.bytes) : 0;
+  return ws ? static_cast<int64_t>(ws->arena_bytes + ws->cache.held) : 0;
 }
 
 }  // extern "C"

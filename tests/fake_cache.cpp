@@ -35,3 +35,10 @@ CacheAttnShape cache_attn_shape(int rows, int, int64_t, int64_t, int, const Quer
 }
 
 }  // namespace evisel
+
+// A stream capture for the stand-in runtime.
+static int g_capturing = 0;
+extern "C" void fake_capture(int on) { g_capturing = on; }
+extern "C" cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
+  return *s = g_capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone, cudaSuccess;
+}

@@ -909,3 +909,46 @@ def test_new_tensors_are_made_on_the_stream_of_the_call(cuda_lib):
     again = [torch.empty(s, dtype=t, device="cuda") for s, t, _ in sizes]
     assert not where & {x.data_ptr() for x in again}
     assert cuda_lib.evisel_status(ws) == 0
+
+
+# --- graphs and workspaces that grow -----------------------------------------------------
+
+def test_a_graph_outlives_larger_calls_on_its_workspace(cuda_lib):
+    """Graphs of growing batches on one workspace, as a server captures them, replayed after all of them; and within a
+    capture a call that needs more scratch is refused, its neighbours are captured."""
+    import torch
+    rng = np.random.default_rng(23)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [300, 77, 0, 900, 5, 64], 2, 64, 16, ty, poison=False)
+    q, q_ref = tensor(rng, (6, 1, 4, 64), ty)
+    ws, graphs = cuda_lib.Workspace(), []
+    for batch in (1, 2, 6):
+        part = cache.view(cache.table[:batch], cache.lens[:batch])
+        o, lse, _ = cuda_lib.evisel_cache_attention(part, q[:batch], ws=ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cuda_lib.evisel_cache_attention(part, q[:batch], ws=ws, o=o, lse=lse)
+        graphs.append((graph, batch, o, lse))
+    long, _ = make_cache(rng, [3000] * 40, 2, 64, 64, ty, poison=False)
+    many, _ = tensor(rng, (40, 20, 4, 64), ty)
+    held, graph = ws.nbytes, torch.cuda.CUDAGraph()
+    o, lse = graphs[-1][2:]
+    with torch.cuda.graph(graph):
+        with pytest.raises(cuda_lib.EviselError, match="capture"):
+            cuda_lib.evisel_cache_attention(long, many, ws=ws)
+        with pytest.raises(cuda_lib.EviselError, match="capture"):
+            cuda_lib.evisel_cache_attention(cache, q)
+        cuda_lib.evisel_cache_attention(cache, q, ws=ws, o=o, lse=lse)
+    graphs.append((graph, 6, o, lse))
+    assert ws.nbytes == held
+    cuda_lib.evisel_cache_attention(long, many, ws=ws)       # outgrows what the graphs use
+    assert ws.nbytes > held
+    filler = torch.full((64 << 20,), float("nan"), device="cuda")
+    for graph, batch, o, lse in graphs + graphs[::-1]:
+        o.zero_(), lse.zero_()
+        graph.replay()
+        _status(cuda_lib, ws)
+        want = ref_cache.attention(dict(ref, lens=ref["lens"][:batch]), q_ref[:batch])
+        check_attention(o, lse, want, 64, ty, f"{batch} sequences")
+    assert torch.isnan(filler).all()
