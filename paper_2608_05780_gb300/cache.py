@@ -63,10 +63,10 @@ class Cache:
     stored [P, page, hkv, d] are passed transposed), ``table`` int32 [B, n] or [B, hkv, n] of page ids, ``lens`` int32
     [B] or [B, hkv] of cached tokens, and optionally ``k_mean`` [P, hkv, d] of the pages' mean keys.
 
-    The handle holds the tensors; assign ``lens`` or ``table`` to replace one.
+    The handle holds the tensors; assign one (``lens``, ``table``, ``k``, ``v``, ``k_mean``) to replace it.
     """
 
-    __slots__ = ("k", "v", "k_mean", "device", "dtype", "batch", "hkv", "page", "head_dim", "max_tokens", "_pool",
+    __slots__ = ("_k", "_v", "_k_mean", "device", "dtype", "batch", "hkv", "page", "head_dim", "max_tokens", "_pool",
                  "_table", "_lens", "_chosen", "_packed")
 
     def __init__(self, k, v, table, lens, k_mean=None):
@@ -82,7 +82,7 @@ class Cache:
         if k_mean is not None and not (k_mean.shape == (pages, hkv, d) and k_mean.dtype == k.dtype
                                        and k_mean.device == k.device and k_mean.is_contiguous()):
             _refuse("k_mean must be contiguous [P, hkv, d], of k's type and device")
-        self.k, self.v, self.k_mean, self.device, self.dtype = k, v, k_mean, k.device, k.dtype
+        self._k, self._v, self._k_mean, self.device, self.dtype = k, v, k_mean, k.device, k.dtype
         self.hkv, self.page, self.head_dim = hkv, page, d
         self._pool = (pages, c.dtypes[k.dtype], ks[:3], vs[:3], k.data_ptr(), v.data_ptr(),
                       0 if k_mean is None else k_mean.data_ptr())
@@ -127,9 +127,38 @@ class Cache:
     def lens(self, lens):
         self._set(self.table, lens)
 
+    def _replace_pages(self, k, v, k_mean):
+        new = Cache(k, v, *self._tensors(), k_mean)          # with its checks; this one stays as it was where they fail
+        for name in Cache.__slots__:
+            setattr(self, name, getattr(new, name))
+
+    @property
+    def k(self):
+        return self._k
+
+    @k.setter
+    def k(self, k):
+        self._replace_pages(k, self._v, self._k_mean)
+
+    @property
+    def v(self):
+        return self._v
+
+    @v.setter
+    def v(self, v):
+        self._replace_pages(self._k, v, self._k_mean)
+
+    @property
+    def k_mean(self):
+        return self._k_mean
+
+    @k_mean.setter
+    def k_mean(self, k_mean):
+        self._replace_pages(self._k, self._v, k_mean)
+
     def _same_pages(self):
         c = object.__new__(Cache)
-        c.k, c.v, c.k_mean, c.device, c.dtype = self.k, self.v, self.k_mean, self.device, self.dtype
+        c._k, c._v, c._k_mean, c.device, c.dtype = self._k, self._v, self._k_mean, self.device, self.dtype
         c.hkv, c.page, c.head_dim, c._pool = self.hkv, self.page, self.head_dim, self._pool
         return c
 

@@ -952,3 +952,39 @@ def test_a_graph_outlives_larger_calls_on_its_workspace(cuda_lib):
         want = ref_cache.attention(dict(ref, lens=ref["lens"][:batch]), q_ref[:batch])
         check_attention(o, lse, want, 64, ty, f"{batch} sequences")
     assert torch.isnan(filler).all()
+
+
+# --- the handle ---------------------------------------------------------------------------
+
+def test_assigned_pages_are_the_ones_that_calls_use(cuda_lib):
+    """k, v and k_mean of a handle, and of a view of chosen pages, replaced by assignment; what does not fit is refused
+    and changes nothing."""
+    import torch
+    rng = np.random.default_rng(29)
+    ty = _types()["bf16"]
+    cache, ref = make_cache(rng, [90, 33], 2, 64, 16, ty, room=8, mean=True, poison=False)
+    q, q_ref = tensor(rng, (2, 2, 4, 64), ty)
+    old_k, old_v, old_mean = cache.k, cache.v, cache.k_mean          # (alive throughout)
+    view, _, ws = cuda_lib.evisel_cache_select(cache, q, 3)
+    sel = dict(table=view.table.cpu().numpy(), lens=view.lens.cpu().numpy())
+    k, v = (torch.from_numpy(rng.standard_normal(tuple(old_k.shape))).to(ty).cuda() for _ in range(2))
+    mean = torch.zeros_like(old_mean)
+    for c, where in ((cache, ref), (view, sel)):
+        c.k, c.v = k, v
+        c.k_mean = mean
+        assert c.k is k and c.v is v and c.k_mean is mean
+        where.update(k=k.double().cpu().numpy(), v=v.double().cpu().numpy())
+        o, lse, _ = cuda_lib.evisel_cache_attention(c, q, ws=ws)
+        check_attention(o, lse, ref_cache.attention(where, q_ref), 64, ty)
+    before = [x.clone() for x in (old_k, old_v, old_mean)]
+    new, _ = tensor(rng, (2, 8, 2, 64), ty)
+    cuda_lib.evisel_cache_append(cache, new, new, ws=ws)
+    assert all(torch.equal(x, y) for x, y in zip((old_k, old_v, old_mean), before)) and bool((mean != 0).any())
+    cache.k_mean = None
+    with pytest.raises(cuda_lib.EviselError, match="k_mean"):
+        cuda_lib.evisel_cache_select(cache, q, 3, ws=ws)
+    for name, bad in (("k", k[1:]), ("v", v.float()), ("k", k.cpu()), ("v", v[..., :32]), ("k_mean", mean[:, :1])):
+        with pytest.raises(ValueError):
+            setattr(cache, name, bad)
+        assert cache.k is k and cache.v is v and cache.k_mean is None
+    _status(cuda_lib, ws)
