@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel
           ptx::fence_proxy_async_smem();
           __syncwarp();
         }
-        // Running max (log2 units), moved only when it grows by more than 2^8.
+        // Running max (log2 units, less the headroom), moved only when it grows by more than 2^8.
         float tm[MG][2];
         bool grows = false;
 #pragma unroll
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel
             float x = fmaxf(fmaxf(sc[g][0][2 * half], sc[g][0][2 * half + 1]), fmaxf(sc[g][1][2 * half], sc[g][1][2 * half + 1]));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-            tm[g][half] = x * L.d.scale_log2;
+            tm[g][half] = fmaf(x, L.d.scale_log2, -T::kHeadroom);
             grows = grows || tm[g][half] > m[g][half] + kRescaleThreshold;
           }
         if (__any_sync(0xffffffffu, grows)) {
@@ -345,6 +345,14 @@ __global__ void __launch_bounds__(32 * (kKeyWarps + 1), 2) cache_attn_few_kernel
 // max of its own. Dependent loads are the bound: 10 us by itself for 896 rows of 3 partials,
 // of which the drafted half runs before the kernel that it follows has ended.
 constexpr int kJoinWarps = 8;
+
+// LSE of a row sum l relative to 2^m.
+template <class T>
+__device__ __forceinline__ float row_lse(float m, float l) {
+  constexpr float kDown = T::kHeadroom > 0.f ? 0x1p-7f : 1.f;    // (lg2 is the more exact the nearer to 1)
+  static_assert(T::kHeadroom == 0.f || T::kHeadroom == 7.f, "kDown");
+  return l != 0.f ? ((m + T::kHeadroom) + __log2f(l * kDown)) * kLn2 : -INFINITY;
+}
 
 template <class T, int D>
 __global__ void __launch_bounds__(32 * kJoinWarps, 4) cache_join_kernel(const __grid_constant__ CacheAttnLaunch L, int wpr) {
@@ -519,7 +527,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 4) cache_join_kernel(const __
   else
     *reinterpret_cast<uint32_t*>(dst) = T::pack(acc[0] * inv, acc[1] * inv);
   if (lane == 0)
-    L.lse[(static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t] = l != 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+    L.lse[(static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t] = row_lse<T>(m, l);
 }
 
 // Many rows: 16 of them a warp as one side of mma.sync products, the drafted keys
@@ -542,6 +550,7 @@ __device__ __forceinline__ bool all_finite(const uint4& x) {
 template <class T, int D>
 __global__ void __launch_bounds__(32 * kTileWarps, 3) cache_join_tile_kernel(const __grid_constant__ CacheAttnLaunch L, int wpr) {
   constexpr int BLOCK = kChunk * 128, KB = D / 64;           // a 64-column block of a chunk
+  constexpr float kHeadroom = T::kHeadroom > 0.f ? T::kHeadroom + kRescaleThreshold : 0.f;  // (this maximum is never stale)
   __shared__ alignas(128) uint8_t tile[2 * KB * BLOCK];      // drafted keys and values, swizzled; then the warps' O
   __shared__ float2 join_ml[kTileWarps][16];
   __shared__ int scratch[40];
@@ -651,7 +660,7 @@ __global__ void __launch_bounds__(32 * kTileWarps, 3) cache_join_tile_kernel(con
             }
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          move_max(half, top);
+          move_max(half, top - kHeadroom);
           const float ref = m[half] == -INFINITY ? 0.f : m[half];
 #pragma unroll
           for (int j = 0; j < 2; ++j)
@@ -779,7 +788,7 @@ __global__ void __launch_bounds__(32 * kTileWarps, 3) cache_join_tile_kernel(con
 #pragma unroll
     for (int j = 0; j < D / 8; ++j) dst[4 * j] = T::pack(o[j][2 * half] * inv, o[j][2 * half + 1] * inv);
     if ((lane & 3) == 0)
-      L.lse[(static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t[half]] = l[half] != 0.f ? (m[half] + __log2f(l[half])) * kLn2 : -INFINITY;
+      L.lse[(static_cast<int64_t>(head) * L.c.batch + b) * L.d.tokens + t[half]] = row_lse<T>(m[half], l[half]);
   }
 }
 

@@ -293,7 +293,7 @@ __device__ __forceinline__ void softmax_rows(const CacheAttnLaunch& L, const Uni
       n += cnt;
       continue;
     }
-    float m = -INFINITY, l = 0.f;                // running max (log2 units), row sum
+    float m = -INFINITY, l = 0.f;                // running max (log2 units, less the headroom), row sum
     for (int j = 0; j < cnt; ++j, ++n) {
       const int b = two ? slot : j & 1;
       const int sb = two || b == 0 ? b : 2;
@@ -329,7 +329,7 @@ __device__ __forceinline__ void softmax_rows(const CacheAttnLaunch& L, const Uni
         mask32(rb, h * 64 + 32);
         max32(rb);
       }
-      const float tm = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * L.d.scale_log2;
+      const float tm = fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), L.d.scale_log2, -T::kHeadroom);
       const bool need = tm > m + kRescaleThreshold;
       if (__any_sync(0xffffffffu, need)) {
         const float alpha = need ? ptx::ex2(m - tm) : 1.f;

@@ -44,13 +44,20 @@ __device__ __forceinline__ int drafted_tokens(const DraftView& d, int b) {
 }
 
 // ---------------------------------------------------------------- 16-bit types
+// kHeadroom: log2 units by which a softmax's reference exponent stands below the
+// running maximum where weights are rounded to this type. fp16 ends at 2^-24: without
+// it weights below 2^-25 of the maximum were lost from O but not from the row sum
+// (16,000 keys at 2^-26: 2^-12 of the values). With 7, and a maximum that is up to
+// 2^8 stale, weights stay below 2^15 and are kept down to 2^-32.
 struct BF16 {
+  static constexpr float kHeadroom = 0.f;
   static constexpr uint32_t kFormat = 1;         // operand format of a kind::f16 tcgen05.mma
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return ptx::pack_bf16x2(lo, hi); }
   static __device__ __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
   static __device__ __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 };
 struct FP16 {
+  static constexpr float kHeadroom = 7.f;
   static constexpr uint32_t kFormat = 0;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     uint32_t r;

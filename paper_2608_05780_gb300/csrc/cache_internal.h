@@ -57,7 +57,7 @@ struct CacheAttnLaunch {
   void* o;
   float* lse;
   float* part_o;                    // [partials, tile_rows, d], unnormalised
-  float2* part_ml;                  // [partials, tile_rows]: running max (log2 units), row sum
+  float2* part_ml;                  // [partials, tile_rows]: running max (log2 units, less T::kHeadroom), row sum
   int* status;
   int k_perm, v_perm, q_perm;       // where token, head and page (sequence) stand in the maps' coordinates
   int box_rows;

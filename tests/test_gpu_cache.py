@@ -988,3 +988,54 @@ def test_assigned_pages_are_the_ones_that_calls_use(cuda_lib):
             setattr(cache, name, bad)
         assert cache.k is k and cache.v is v and cache.k_mean is None
     _status(cuda_lib, ws)
+
+
+# --- small weights in fp16 ------------------------------------------------------------------
+
+@pytest.mark.parametrize("lens,t,gq,d,roomy,drafted", [
+    ([4096, 1000], 1, 4, 64, False, False), ([4096], 1, 7, 128, False, False),       # few rows
+    ([4096], 6, 4, 64, True, False),                                                  # 32-row tiles
+    ([4096, 300], 40, 4, 64, True, False), ([2048], 20, 7, 128, True, False),         # many rows
+    ([0], 128, 4, 64, False, True),                                                   # drafted keys joined by tiles
+    ([0], 70, 8, 128, False, True), ([0, 0], 20, 2, 64, False, True),                 # and row by row
+])
+def test_small_weights_count_in_fp16(cuda_lib, lens, t, gq, d, roomy, drafted):
+    """Every sixteenth key has the row's maximum and a value of 0, the others weigh e^-18 = 2^-26 of it and hold all of
+    the values. A weight is kept to 2^-32 of the maximum at the least (half an fp16 step of 2^-24, 2^7 above it), so
+    that O = sum w v / sum w is off by 2^-32 sum |v| / sum w at most, beside the rounding of each weight and of O to
+    11 bits; v is large so that O does not fall among the type's last steps (2^-25 more)."""
+    import torch
+    rng = np.random.default_rng(t + d)
+    ty = torch.float16
+    cache, ref = make_cache(rng, lens, 1, d, 16, ty, poison=False)
+    batch = len(lens)
+
+    def fill(k, v, axis):                        # k = -18 e_0 but for every sixteenth, v positive but for those
+        at = [slice(None)] * k.dim()
+        at[axis] = slice(None, None, 16)
+        k.zero_(), v.copy_(v.abs() * 10_000 + 20_000).clamp_(max=60_000)
+        k[..., 0] = -18.0
+        k[tuple(at)] = 0.0
+        v[tuple(at)] = 0.0
+
+    fill(cache.k, cache.v, 2)
+    ref.update(k=cache.k.double().cpu().numpy(), v=cache.v.double().cpu().numpy())
+    q = torch.zeros((batch, t, gq, d), dtype=ty, device="cuda")
+    q[..., 0] = 1.0
+    k = v = None
+    if drafted:
+        k, v = (tensor(rng, (batch, t, 1, d), ty)[0] for _ in range(2))
+        fill(k, v, 1)
+    tree = tree_words(np.ones((batch, t, t), bool)) if drafted else None
+    o, lse, ws = cuda_lib.evisel_cache_attention(_roomy(cache) if roomy else cache, q, k, v, tree=tree, softmax_scale=1.0)
+    _status(cuda_lib, ws)
+    allowed = np.ones((batch, t, t), bool)
+    host = lambda x: None if x is None else x.double().cpu().numpy()  # noqa: E731
+    o_ref, lse_ref, size, values, _ = ref_cache.attention(ref, host(q), host(k), host(v), allowed, scale=1.0)
+    assert o_ref[0].min() > 2.0 ** -11           # the values' share is there to be seen
+    total = np.moveaxis(np.exp(lse_ref), 0, 2)[..., None]          # the maximum is e^0
+    bound = 2.0 ** -32 * values / total + 2.0 ** -10 * size + 2.0 ** -18 * size + 2.0 ** -25
+    err = np.abs(o.double().cpu().numpy() - o_ref)
+    assert np.all(err <= bound), f"O off by {err.max():.2e}, {np.max(err / bound):.2f} of the bound"
+    e = (d + 8) * 2.0 ** -24 * 18 + 2.0 ** -20
+    assert np.all(np.abs(lse.double().cpu().numpy() - lse_ref) <= e + 2.0 ** -22 * np.abs(lse_ref))
