@@ -110,6 +110,7 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
  *   use    device uint8 [B, T] or NULL: only rows whose byte is not 0 add (the
  *          accepted ones of a drafted tree)
  *   acc    device fp32 [B, hkv, acc_len] contiguous, acc_len >= the longest sequence
+ *          (NULL with acc_len = 0)
  *   accumulate  0: overwrite, 1: add
  * Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED, EVISEL_ENOMEM, EVISEL_ECUDA; a
  * sequence longer than acc_len shows as EVISEL_EBOUNDS in evisel_status(). */
@@ -120,7 +121,8 @@ int evisel_cache_evidence(const evisel_cache* cache, const evisel_draft* draft, 
  * there are no more; else the first `sink`, the last `recent` and, of the rest,
  * those with the largest acc (ties: the lower position; NaN counts as lowest),
  * in their order. They are copied to the first slots of out's pages.
- *   acc       device fp32 [B, hkv, acc_len], acc_len >= the longest sequence
+ *   acc       device fp32 [B, hkv, acc_len], acc_len >= the longest sequence (NULL
+ *             with acc_len = 0)
  *   out       another cache of the same batch, heads, head_dim and dtype, with
  *             room for budget tokens per sequence; its pages must not be among
  *             the cache's. k, v, lens and (if given) k_mean are written; page

@@ -334,7 +334,7 @@ int evisel_cache_evidence(const evisel_cache* cache, const evisel_draft* draft, 
     if (!ws_inout) return fail(EVISEL_EINVAL, "ws_inout is NULL");
     if (acc_len < 0) return fail(EVISEL_EINVAL, "acc_len is negative");
     if (cache->batch == 0 || cache->max_pages == 0) return EVISEL_OK;
-    if (!acc || (draft->tokens > 0 && !lse)) return fail(EVISEL_EINVAL, "acc or lse is NULL");
+    if ((acc_len > 0 && !acc) || (draft->tokens > 0 && !lse)) return fail(EVISEL_EINVAL, "acc or lse is NULL");
     if (misaligned(acc, 4) || misaligned(lse, 4)) return fail(EVISEL_EINVAL, "acc and lse must be 4-byte aligned");
     CacheEvidenceLaunch L{};
     L.c = view_of(cache);
@@ -381,7 +381,7 @@ int evisel_cache_evict(const evisel_cache* cache, const float* acc, int64_t acc_
     if (cache->batch == 0) return EVISEL_OK;
     if (cache->hkv > 1 && cache->lens_stride[1] != 0 && out->lens_stride[1] == 0)
       return fail(EVISEL_EINVAL, "lengths per head need lengths per head in out");
-    if (!acc || !kept || !acc_out) return fail(EVISEL_EINVAL, "acc, kept or acc_out is NULL");
+    if ((acc_len > 0 && !acc) || !kept || !acc_out) return fail(EVISEL_EINVAL, "acc, kept or acc_out is NULL");
     if (misaligned(acc, 4) || misaligned(kept, 4) || misaligned(acc_out, 4))
       return fail(EVISEL_EINVAL, "acc, kept and acc_out must be 4-byte aligned");
     if (acc == acc_out || out->lens == cache->lens || (out->k == cache->k && out->table == cache->table))

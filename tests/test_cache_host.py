@@ -332,3 +332,13 @@ def test_cache_handle_refuses_what_it_cannot_pass_on():
     for k, v in ((x, x[:2]), (x[0], x[0]), (x, x), (x.float(), x.float())):
         with pytest.raises(ValueError):
             ev.Cache(k, v, table, lens)
+
+
+def test_no_weights_of_empty_caches(fake):
+    """acc_len = 0 needs no acc: an empty tensor has no address. With one it does."""
+    ws = ctypes.c_void_p(None)
+    empty = _cache(max_pages=0, n_pages=0, k=0, v=0, table=0)
+    assert _evict(fake, ctypes.byref(ws), c=empty, n=0, acc=None) == 0
+    assert _evidence(fake, ctypes.byref(ws), n=0, acc=None) == 0
+    assert _evict(fake, ctypes.byref(ws), n=1, acc=None) == EINVAL and _evidence(fake, ctypes.byref(ws), n=1, acc=None) == EINVAL
+    fake.evisel_free(ws)

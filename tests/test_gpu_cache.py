@@ -1039,3 +1039,35 @@ def test_small_weights_count_in_fp16(cuda_lib, lens, t, gq, d, roomy, drafted):
     assert np.all(err <= bound), f"O off by {err.max():.2e}, {np.max(err / bound):.2f} of the bound"
     e = (d + 8) * 2.0 ** -24 * 18 + 2.0 ** -20
     assert np.all(np.abs(lse.double().cpu().numpy() - lse_ref) <= e + 2.0 ** -22 * np.abs(lse_ref))
+
+
+# --- caches without a page --------------------------------------------------------------------
+
+def test_every_call_on_a_cache_without_a_page(cuda_lib):
+    """No column in the table, as before a first append: evidence of nothing, an eviction that
+    keeps nothing, a choice of nothing; and a table with room whose sequences are empty, with weights of no length."""
+    import torch
+    rng = np.random.default_rng(31)
+    ty = _types()["bf16"]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pool = torch.zeros((1, 2, 16, 64), dtype=ty, device="cuda")
+    bare = cuda_lib.Cache(pool, pool, torch.zeros((3, 0), **i32), torch.zeros(3, **i32),
+                          torch.zeros((1, 2, 64), dtype=ty, device="cuda"))
+    room, _ = make_cache(rng, [0, 0, 0], 2, 64, 16, ty, room=32, poison=False)
+    q, _ = tensor(rng, (3, 2, 4, 64), ty)
+    lse = torch.zeros((4, 3, 2), device="cuda")
+    for cache in (bare, room):
+        none = torch.zeros((3, 2, 0), device="cuda")
+        acc, ws = cuda_lib.evisel_cache_evidence(cache, q, lse, acc=none)
+        assert acc is none
+        out, _ = make_cache(rng, [5, 6, 7], 2, 64, 16, ty, room=8, mean=True, poison=False)
+        before = out.k.clone(), out.v.clone(), out.k_mean.clone()
+        kept, acc_out, ws = cuda_lib.evisel_cache_evict(cache, none, out, 8, sink=1, recent=2, ws=ws)
+        assert torch.all(kept == -1) and torch.all(acc_out == 0) and out.lens.tolist() == [0, 0, 0]
+        assert all(torch.equal(x, y) for x, y in zip((out.k, out.v, out.k_mean), before))
+        _status(cuda_lib, ws)
+    view, pages, ws = cuda_lib.evisel_cache_select(bare, q, 3, ws=ws)
+    assert torch.all(pages == -1) and torch.all(view.lens == 0)
+    o, lse, ws = cuda_lib.evisel_cache_attention(view, q, ws=ws)
+    assert torch.all(o == 0) and torch.all(torch.isneginf(lse))
+    _status(cuda_lib, ws)
