@@ -58,6 +58,14 @@ def _refuse(what):
     raise ValueError(what)
 
 
+def _i32(x, what):
+    """A whole number for the C ABI (ctypes would wrap a larger one)."""
+    x = int(x)
+    if not -1 << 31 <= x < 1 << 31:
+        _refuse(f"{what} must fit 32 bits")
+    return x
+
+
 class Cache:
     """A paged cache: ``k`` and ``v`` pages [P, hkv, page, d] (bf16 or fp16, any strides with d contiguous: pages
     stored [P, page, hkv, d] are passed transposed), ``table`` int32 [B, n] or [B, hkv, n] of page ids, ``lens`` int32
@@ -293,7 +301,8 @@ def evisel_cache_evict(cache, acc, out, budget, sink=0, recent=0, kept=None, acc
     out.lens, and out.k_mean where there is one, are written.
 
     Returns (kept int32 [B, hkv, budget] with -1 past the tokens kept, acc_out [B, hkv, out.max_tokens], ws)."""
-    batch, hkv, budget = cache.batch, cache.hkv, int(budget)
+    batch, hkv = cache.batch, cache.hkv
+    budget, sink, recent = _i32(budget, "budget"), _i32(sink, "sink"), _i32(recent, "recent")
     n = acc.shape[-1] if acc.dim() else 0
     acc_p = _plain(cache, acc, _calls.f32, (batch, hkv, n), "acc")
     if not (out.device == cache.device and out.batch == batch and out.hkv == hkv):
@@ -313,7 +322,7 @@ def evisel_cache_evict(cache, acc, out, budget, sink=0, recent=0, kept=None, acc
         m = acc_out.shape[-1] if acc_out.dim() else 0
         acc_out_p = _plain(cache, acc_out, _calls.f32, (batch, hkv, m), "acc_out")
     ws = Workspace() if ws is None else ws
-    rc = _calls.evict(cache._packed, acc_p, n, out._packed, budget, int(sink), int(recent), kept_p, acc_out_p, m,
+    rc = _calls.evict(cache._packed, acc_p, n, out._packed, budget, sink, recent, kept_p, acc_out_p, m,
                       _stream(cache, stream), ctypes.byref(ws.ptr))
     if rc:
         _check(rc)
@@ -353,12 +362,13 @@ def evisel_cache_select(cache, q, n_select, sink=0, recent=1, drafted=None, ws=N
     Returns (view, pages, ws): a Cache of the chosen pages for evisel_cache_attention, and their logical numbers
     int32 [B, hkv, n_select], ascending, -1 past them."""
     draft = _draft(cache, q, None, None, None, drafted, 0.0)
-    n = max(0, int(n_select))
+    n_select, sink, recent = _i32(n_select, "n_select"), _i32(sink, "sink"), _i32(recent, "recent")
+    n = max(0, n_select)
     empty = _maker(_calls.empty, stream)
     pages = empty((cache.batch, cache.hkv, n), dtype=_calls.i32, device=cache.device)
     view, table_p, lens_p = cache._choice(n, empty)
     ws = Workspace() if ws is None else ws
-    rc = _calls.select(cache._packed, draft, int(n_select), int(sink), int(recent), pages.data_ptr(), table_p, lens_p,
+    rc = _calls.select(cache._packed, draft, n_select, sink, recent, pages.data_ptr(), table_p, lens_p,
                        _stream(cache, stream), ctypes.byref(ws.ptr))
     if rc:
         _check(rc)

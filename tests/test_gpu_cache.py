@@ -1071,3 +1071,25 @@ def test_every_call_on_a_cache_without_a_page(cuda_lib):
     o, lse, ws = cuda_lib.evisel_cache_attention(view, q, ws=ws)
     assert torch.all(o == 0) and torch.all(torch.isneginf(lse))
     _status(cuda_lib, ws)
+
+
+def test_numbers_past_32_bits_are_refused(cuda_lib):
+    """They would reach the library as what is left of them: 2^32 tokens to keep as none."""
+    import torch
+    rng = np.random.default_rng(37)
+    ty = _types()["bf16"]
+    cache, _ = make_cache(rng, [40], 1, 64, 16, ty, mean=True, poison=False)
+    out, _ = make_cache(rng, [0], 1, 64, 16, ty, room=8, poison=False)
+    q, _ = tensor(rng, (1, 1, 2, 64), ty)
+    acc = torch.rand((1, 1, cache.max_tokens), device="cuda")
+    for name in ("sink", "recent"):
+        for n in (1 << 32, -(1 << 32) + 1, 1 << 31):
+            with pytest.raises((ValueError, cuda_lib.EviselError)):
+                cuda_lib.evisel_cache_evict(cache, acc, out, 8, **{name: n})
+            with pytest.raises((ValueError, cuda_lib.EviselError)):
+                cuda_lib.evisel_cache_select(cache, q, 2, **{name: n})
+    for n in (1 << 31, (1 << 32) + 8):
+        with pytest.raises(ValueError, match="32 bits"):
+            cuda_lib.evisel_cache_evict(cache, acc, out, n)
+        with pytest.raises(ValueError, match="32 bits"):
+            cuda_lib.evisel_cache_select(cache, q, n)
