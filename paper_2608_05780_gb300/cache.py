@@ -58,12 +58,12 @@ def _refuse(what):
     raise ValueError(what)
 
 
-def _i32(x, what):
-    """A whole number for the C ABI (ctypes would wrap a larger one)."""
-    x = int(x)
-    if not -1 << 31 <= x < 1 << 31:
+def _i32(a, b, c, what):
+    """Three whole numbers for the C ABI, which refuses negative ones (ctypes would wrap those past 32 bits)."""
+    a, b, c = int(a), int(b), int(c)
+    if not -1 <= (a | b | c) >> 31 <= 0:
         _refuse(f"{what} must fit 32 bits")
-    return x
+    return a, b, c
 
 
 class Cache:
@@ -302,7 +302,7 @@ def evisel_cache_evict(cache, acc, out, budget, sink=0, recent=0, kept=None, acc
 
     Returns (kept int32 [B, hkv, budget] with -1 past the tokens kept, acc_out [B, hkv, out.max_tokens], ws)."""
     batch, hkv = cache.batch, cache.hkv
-    budget, sink, recent = _i32(budget, "budget"), _i32(sink, "sink"), _i32(recent, "recent")
+    budget, sink, recent = _i32(budget, sink, recent, "budget, sink and recent")
     n = acc.shape[-1] if acc.dim() else 0
     acc_p = _plain(cache, acc, _calls.f32, (batch, hkv, n), "acc")
     if not (out.device == cache.device and out.batch == batch and out.hkv == hkv):
@@ -362,7 +362,7 @@ def evisel_cache_select(cache, q, n_select, sink=0, recent=1, drafted=None, ws=N
     Returns (view, pages, ws): a Cache of the chosen pages for evisel_cache_attention, and their logical numbers
     int32 [B, hkv, n_select], ascending, -1 past them."""
     draft = _draft(cache, q, None, None, None, drafted, 0.0)
-    n_select, sink, recent = _i32(n_select, "n_select"), _i32(sink, "sink"), _i32(recent, "recent")
+    n_select, sink, recent = _i32(n_select, sink, recent, "n_select, sink and recent")
     n = max(0, n_select)
     empty = _maker(_calls.empty, stream)
     pages = empty((cache.batch, cache.hkv, n), dtype=_calls.i32, device=cache.device)
