@@ -151,12 +151,15 @@ def _maker(make, stream):
     if stream is None:
         return make
     import torch
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream)
 
-    def on_stream(*args, **kw):
-        with torch.cuda.stream(stream):
-            return make(*args, **kw)
+    def on_stream(*args, device, **kw):
+        if torch.device(device).type != "cuda":
+            return make(*args, device=device, **kw)
+        s = stream
+        if not isinstance(s, torch.cuda.Stream):             # another library's, by its handle; 0: the default stream
+            s = torch.cuda.ExternalStream(s.cuda_stream, device) if s.cuda_stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(s):
+            return make(*args, device=device, **kw)
     return on_stream
 
 
