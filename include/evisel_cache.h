@@ -143,7 +143,8 @@ int evisel_cache_evict(const evisel_cache* cache, const float* acc, int64_t acc_
  *   draft   tokens (any number here), k_new and v_new with strides; the rest is not read
  *   src     device int32 [B, T] or NULL (token i itself)
  *   counts  device int32 [B], 0..T, or NULL (T each)
- *   lens_out  device int32 [B], not cache->lens
+ *   lens_out  device int32 [B], not cache->lens, nor overlapping src or counts (other
+ *             blocks of the call still read them)
  * table and lens must be shared by the heads. A page may belong to one sequence
  * only where tokens go. Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED,
  * EVISEL_ENOMEM, EVISEL_ECUDA. */

@@ -30,6 +30,12 @@ int cuda_fail(cudaError_t e, const char* what) {
 
 bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
+// Whether two runs of 32-bit values share any.
+bool overlap(const int32_t* a, int64_t na, const int32_t* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + 4 * nb && y < x + 4 * na;
+}
+
 constexpr int64_t kMaxStride = int64_t(1) << 38;   // elements: a TMA stride is below 2^40 bytes
 constexpr int kMaxDrafted = 1024;
 constexpr int kMaxGroup = 128;
@@ -428,6 +434,9 @@ int evisel_cache_append(const evisel_cache* cache, const evisel_draft* draft, co
     if (!lens_out || lens_out == cache->lens) return fail(EVISEL_EINVAL, "lens_out is NULL or the cache's lens");
     if (misaligned(lens_out, 4) || misaligned(src, 4) || misaligned(counts, 4))
       return fail(EVISEL_EINVAL, "src, counts and lens_out must be 4-byte aligned");
+    if (overlap(lens_out, cache->batch, counts, cache->batch) ||
+        overlap(lens_out, cache->batch, src, static_cast<int64_t>(cache->batch) * draft->tokens))
+      return fail(EVISEL_EINVAL, "lens_out must not overlap counts or src");
     if (draft->tokens > 0) {
       if (!draft->k_new || !draft->v_new) return fail(EVISEL_EINVAL, "k_new or v_new is NULL");
       if (misaligned(draft->k_new) || misaligned(draft->v_new)) return fail(EVISEL_EINVAL, "k_new and v_new must be 16-byte aligned");

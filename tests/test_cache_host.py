@@ -342,3 +342,18 @@ def test_no_weights_of_empty_caches(fake):
     assert _evidence(fake, ctypes.byref(ws), n=0, acc=None) == 0
     assert _evict(fake, ctypes.byref(ws), n=1, acc=None) == EINVAL and _evidence(fake, ctypes.byref(ws), n=1, acc=None) == EINVAL
     fake.evisel_free(ws)
+
+
+def test_an_append_reads_its_counts_while_it_writes_the_lengths(fake):
+    """lens_out over counts or src (two sequences, three tokens each): other blocks would read what was written."""
+    at = lambda n: ctypes.c_void_p(FAKE + 4 * n)  # noqa: E731
+    ws = ctypes.c_void_p(None)
+    for lens_out, counts, src in ((4, 4, None), (5, 4, None), (4, 5, None), (4, None, 4), (9, None, 4), (4, None, 5)):
+        n = fake.fake_launches()
+        rc = _append(fake, ctypes.byref(ws), c=_cache(lens=FAKE + 8192), lens_out=at(lens_out),
+                     counts=None if counts is None else at(counts), src=None if src is None else at(src))
+        _refused(fake, rc, EINVAL, n, ws)
+    for lens_out, counts, src in ((6, 4, None), (4, 6, None), (10, None, 4), (4, None, 6)):
+        assert _append(fake, ctypes.byref(ws), c=_cache(lens=FAKE + 8192), lens_out=at(lens_out),
+                       counts=None if counts is None else at(counts), src=None if src is None else at(src)) == 0
+    fake.evisel_free(ws)
