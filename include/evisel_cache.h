@@ -91,6 +91,16 @@ typedef struct {
  * h / (hq / hkv). A row without any allowed key, and every row
  * t >= drafted[b], gets O = 0 and LSE = -inf. Values of keys that a row does
  * not attend never enter it, non-finite ones included.
+ * Logits, sums and O are held in 32 bits. Weights are rounded to the cache's
+ * type for their product with v (the tensor cores' operand type; against 64 bits
+ * O is off by 2.3e-3 in bf16 and 2.1e-4 in fp16, by 1.7e-3 and 2.0e-4 if they were
+ * not), those of drafted keys only where many drafted rows are joined by tiles;
+ * their sum, and so LSE, is not. In fp16 a weight counts down to 2^-32 of the
+ * largest. Which kernels run, and where a sequence's keys are cut, goes by the
+ * sizes of the whole call: the same call gives the same bits, the same
+ * sequence in another batch may differ in the last ones.
+ * The choice between few and many rows goes by what the tables could hold, not by
+ * the lengths. Queries repeated by a stride of 0 are attended 16 or 32 rows at a time.
  *   o    device [B, T, hq, d] contiguous, 16-byte aligned (written)
  *   lse  device fp32 [hq, B, T], natural log (written)
  * The workspace keeps the fp32 partial results of ranges of cached keys: for
@@ -104,7 +114,9 @@ int evisel_cache_attention(const evisel_cache* cache, const evisel_draft* draft,
  *   acc[b, h, m] (+)= sum_{t used} sum_{heads g of group h} exp(softmax_scale q[b, t, g] . k_m - LSE[g, b, t])
  * for m < the sequence's length (entries past it are left alone). With the LSE
  * of evisel_cache_attention() these are the probabilities of that call; rows
- * with LSE = -inf add nothing.
+ * with LSE = -inf add nothing. Queries repeated by a stride of 0 take a slow
+ * kernel without tensor cores (128 rows of 28 heads over 65,536 keys: 15 ms, not
+ * 0.07): copy them where there are many.
  *   draft  tokens, hq, softmax_scale, q and drafted (rows t >= drafted[b] add
  *          nothing); the rest is not read
  *   use    device uint8 [B, T] or NULL: only rows whose byte is not 0 add (the
@@ -154,7 +166,8 @@ int evisel_cache_append(const evisel_cache* cache, const evisel_draft* draft, co
 /* Chooses pages for every (sequence, KV head): all where there are at most
  * n_select; else the first `sink`, the last `recent` and, of the rest, those
  * with the largest score
- *   score_j = max over t < drafted[b] and the heads of the group of q . k_mean_j
+ *   score_j = max over t < drafted[b] and the heads of the group of q . k_mean_j,
+ * so that all drafted tokens and heads of a group share one choice
  * (fp32; ties: the lower page; a NaN product counts as -inf), in order. The result is a
  * cache view for evisel_cache_attention(): the cache with table = sel_table,
  * table_stride = {hkv * n_select, n_select}, max_pages = n_select, lens =

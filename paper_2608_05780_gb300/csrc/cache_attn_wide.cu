@@ -15,10 +15,11 @@
 // slot the other slot's S columns are a second S buffer.
 // A thread holds no row of S across its two passes (maximum, then P): in registers
 // it took as long. The running max moves only when it grows by more than 2^8; P is
-// rounded to 16 bits for its product with V, its sum is not.
+// rounded to 16 bits for its product with V (the MMA's operand type), its sum is not.
 // A slot's chain is the bound, S -> softmax (about 2,000 clocks) -> P.V and the
 // next S: 3,300 clocks a tile of two slots against 2,560 of tensor pipe. 64-token trees over
-// four caches of 65,664 tokens, 7 heads a KV head of 128: 204 us, 1,175 TFLOP/s.
+// four caches of 65,664 tokens, 7 heads a KV head of 128: 215 us from a cold L2, 1,115 TFLOP/s, the
+// tensor pipe 58% busy.
 #include <cstdint>
 #include <cuda_runtime.h>
 

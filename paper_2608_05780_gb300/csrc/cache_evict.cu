@@ -83,7 +83,9 @@ cudaError_t launch_d(const CacheEvictLaunch& L, cudaStream_t stream) {
   const int problems = L.c.batch * L.c.hkv;
   const int64_t room = static_cast<int64_t>(L.c.max_pages) * L.c.page;
   // What a CTA's registers hold it chooses from alone: both kernels, four heads, 8,192 scores 14.7 us (a cluster of
-  // eight 14.4, of two 15.7; eight sequences of them 17.8, with two 20.6), 16,384 31.9 us (eight 15.1).
+  // eight 14.4, of two 15.7; eight sequences of them 17.8, with two 20.6), 16,384 31.9 us (eight 15.1). Past what
+  // eight hold (65,536 scores) every pass reads them again: a call by itself, its launch and events (7 us) included,
+  // 34 us at 65,536, 57 at 65,664, 134 at 262,144.
   const int cluster = choose_cluster(problems, room < L.acc_len ? room : L.acc_len, kChooseThreads * 16, sm_count());
   const cudaError_t e = launch_clusters(cache_evict_choose_kernel, L, problems, kChooseThreads, cluster, stream);
   if (e != cudaSuccess) return e;
