@@ -29,10 +29,11 @@ LIB = os.path.join(HERE, "libevisel.so")
 SOURCES = ["probe_attn.cu", "attn_combine.cu", "evidence.cu", "evisel_capi.cpp", "evisel_noalloc.cu", "evisel_selftest.cu", "intra_frame.cu",
            "cross_frame.cu", "text_evidence.cu", "topp_mask.cu",
            "coarse_evidence.cu", "evisel_cache.cpp", "cache_attn.cu", "cache_attn_wide.cu", "cache_evidence.cu", "cache_evict.cu",
-           "cache_append.cu", "cache_select.cu"]
+           "cache_append.cu", "cache_select.cu", "evisel_decode.cpp", "rotary.cu", "cache_append_rotary.cu", "beam_select.cu",
+           "cache_reorder.cu"]
 HEADERS = ["evisel_internal.h", "evisel_plan.h", "sm103_ptx.cuh", "cache_internal.h", "cache_split.h", "cache_common.cuh",
-           "cache_attn.cuh", "cache_choose.cuh", "cache_pages.cuh"]
-PUBLIC = ["evisel.h", "evisel_cache.h"]
+           "cache_attn.cuh", "cache_choose.cuh", "cache_pages.cuh", "cache_host.h", "decode_internal.h", "rope.cuh"]
+PUBLIC = ["evisel.h", "evisel_cache.h", "evisel_decode.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", "-I" + INCLUDE, "-I" + CSRC]

@@ -8,35 +8,6 @@
 namespace evisel {
 namespace {
 
-struct NewTokens {
-  const CacheAppendLaunch& L;
-  int b, h, len, count;
-  __device__ __forceinline__ NewTokens(const CacheAppendLaunch& L_, int b_, int h_) : L(L_), b(b_), h(h_) {
-    len = cache_len(L.c, b, 0, L.status);
-    count = L.counts ? __ldg(L.counts + b) : L.d.tokens;
-    const int64_t room = (static_cast<int64_t>(L.c.max_pages) << L.c.log_page) - len;
-    if (count < 0 || count > L.d.tokens || count > room) {
-      record_bounds(L.status);
-      count = count < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(min(count, L.d.tokens)), room));
-    }
-    if (__ldg(L.c.lens + b * L.c.ls[0]) < 0) count = 0;   // the first pages may be another sequence's too
-  }
-  __device__ __forceinline__ int first() const { return len; }
-  __device__ __forceinline__ int end() const { return len + count; }
-  __device__ __forceinline__ void rows(int pos, const uint4*& k, const uint4*& v) const {
-    int i = pos - len;
-    if (L.src) {
-      i = __ldg(L.src + static_cast<int64_t>(b) * L.d.tokens + i);
-      if (static_cast<unsigned>(i) >= static_cast<unsigned>(L.d.tokens)) {
-        record_bounds(L.status);
-        i = 0;
-      }
-    }
-    k = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.k_new) + b * L.d.kns[0] + i * L.d.kns[1] + h * L.d.kns[2]);
-    v = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.v_new) + b * L.d.vns[0] + i * L.d.vns[1] + h * L.d.vns[2]);
-  }
-};
-
 template <class T, int D>
 __global__ void __launch_bounds__(kPageThreads, kPageBlocks) cache_append_kernel(const __grid_constant__ CacheAppendLaunch L) {
   const int h = blockIdx.y, b = blockIdx.z;

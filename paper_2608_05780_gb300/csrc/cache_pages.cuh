@@ -10,6 +10,47 @@ constexpr int kPageThreads = 256;
 // as many blocks as their registers leave, 43 with two and five.
 constexpr int kAtOnce = 2, kPageBlocks = 5;
 
+// The tokens that an append gives to (sequence, head): a page's source.
+struct NewTokens {
+  const CacheAppendLaunch& L;
+  int b, h, len, count;
+  __device__ __forceinline__ NewTokens(const CacheAppendLaunch& L_, int b_, int h_) : L(L_), b(b_), h(h_) {
+    len = cache_len(L.c, b, 0, L.status);
+    count = L.counts ? __ldg(L.counts + b) : L.d.tokens;
+    const int64_t room = (static_cast<int64_t>(L.c.max_pages) << L.c.log_page) - len;
+    if (count < 0 || count > L.d.tokens || count > room) {
+      record_bounds(L.status);
+      count = count < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(min(count, L.d.tokens)), room));
+    }
+    if (__ldg(L.c.lens + b * L.c.ls[0]) < 0) count = 0;   // the first pages may be another sequence's too
+  }
+  __device__ __forceinline__ int first() const { return len; }
+  __device__ __forceinline__ int end() const { return len + count; }
+  // The new token that goes to a position.
+  __device__ __forceinline__ int token(int pos) const {
+    int i = pos - len;
+    if (L.src) {
+      i = __ldg(L.src + static_cast<int64_t>(b) * L.d.tokens + i);
+      if (static_cast<unsigned>(i) >= static_cast<unsigned>(L.d.tokens)) {
+        record_bounds(L.status);
+        i = 0;
+      }
+    }
+    return i;
+  }
+  __device__ __forceinline__ const uint4* key(int i) const {
+    return reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.k_new) + b * L.d.kns[0] + i * L.d.kns[1] + h * L.d.kns[2]);
+  }
+  __device__ __forceinline__ const uint4* value(int i) const {
+    return reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.v_new) + b * L.d.vns[0] + i * L.d.vns[1] + h * L.d.vns[2]);
+  }
+  __device__ __forceinline__ void rows(int pos, const uint4*& k, const uint4*& v) const {
+    const int i = token(pos);
+    k = key(i);
+    v = value(i);
+  }
+};
+
 // Writes the page's slots at positions [src.first(), src.end()) and, with
 // `mean`, the mean of all its keys before src.end() (the older ones read back
 // from the page). A block of kPageThreads threads per (page, head, sequence); D / 8

@@ -1,0 +1,96 @@
+// Structures shared by the host side of the decoding-step calls
+// (evisel_decode.cpp) and their kernels. Not part of the public ABI.
+#pragma once
+
+#include "cache_internal.h"
+
+namespace evisel {
+
+struct RopeView {
+  uint64_t turn[64];                // 2^-64 turns per position of pair i
+  int pairs;                        // r / 2
+  int interleaved;
+  int border[2];                    // pairs below border[0] read axis 0, below border[1] axis 1, the others axis 2
+  float scale;
+};
+
+struct PositionView {
+  const int32_t* at;
+  const int32_t* first;
+  int64_t stride[2];                // axis, sequence
+};
+
+struct HeadsView {
+  const void* in;
+  void* out;
+  int64_t is[3], os[3];             // sequence, token, head (elements)
+  int heads;
+};
+
+struct RotaryLaunch {
+  RopeView rope;
+  PositionView pos;
+  HeadsView q, k;                   // k.heads = 0: none
+  int batch, tokens, head_dim, dtype;
+  int transpose;
+};
+
+struct AppendRotaryLaunch {
+  RopeView rope;
+  PositionView pos;
+  CacheAppendLaunch a;
+  HeadsView q;                      // heads = 0: none
+};
+
+constexpr int kMaxBeams = 64, kMaxBeamsOut = 64;
+
+struct BeamLaunch {
+  const void* logits;
+  int64_t ls[2];                    // sequence, beam (elements)
+  const float* scores;
+  const uint8_t* finished;
+  float* score_out;
+  int32_t* parent;
+  int32_t* token;
+  uint8_t* ended_out;
+  double* part_sum;                 // [rows, splits]: sum of exp(x - part_max)
+  float* part_max;                  // [rows, splits]
+  float* part_value;                // [rows, splits, n]: descending, -inf past the end
+  int32_t* part_index;              // [rows, splits, n]: token
+  int batch, beams, vocab, n, dtype, pad, eos;
+  int splits, part_vectors;         // a row is cut into `splits` parts of part_vectors 16-byte vectors
+};
+
+constexpr int kMaxStates = 8;
+
+struct ReorderLaunch {
+  CacheView c;
+  void* k;
+  void* v;
+  void* k_mean;
+  const int32_t* parent;
+  int32_t* table_out;
+  int32_t* lens_out;
+  int* status;
+  int beams, n_states;
+  const char* in[kMaxStates];
+  char* out[kMaxStates];
+  int64_t row_bytes[kMaxStates];
+  int first_block[kMaxStates + 1];  // state i's blocks, behind those of the cache
+  int chunks[kMaxStates];           // blocks of a row
+};
+
+// A row of logits cut into parts: enough for the SMs, none larger than a CTA's registers hold.
+struct BeamSplit {
+  int splits, part_vectors;
+};
+BeamSplit beam_split(int64_t rows, int vocab, int dtype, int n_sm);
+
+cudaError_t launch_rotary(const RotaryLaunch& L, cudaStream_t stream);
+cudaError_t launch_append_rotary(const AppendRotaryLaunch& L, cudaStream_t stream);
+cudaError_t launch_beams(const BeamLaunch& L, cudaStream_t stream);
+cudaError_t launch_reorder(const ReorderLaunch& L, cudaStream_t stream);
+// Bytes of a state row that a block copies.
+constexpr int kStateBytes = 16384;
+
+}  // namespace evisel

@@ -1,0 +1,386 @@
+// Host side of the decoding-step calls (evisel_decode.h): argument checks,
+// scratch of the workspace and kernel launches.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <string>
+
+#include <cuda_runtime.h>
+
+#include "../../include/evisel_decode.h"
+#include "cache_host.h"
+#include "decode_internal.h"
+
+using namespace evisel;
+using namespace evisel::host;
+
+namespace {
+
+constexpr int kMaxPairs = 64;
+constexpr int64_t kMaxTokens = int64_t(1) << 30;
+constexpr int64_t kMaxRows = 65535;              // of logits: a grid's second dimension
+constexpr int kMaxVocab = 1 << 24;
+
+// Bytes [begin, end) that a strided tensor reaches.
+struct Range {
+  uintptr_t begin, end;
+  bool meets(const Range& o) const { return begin < o.end && o.begin < end; }
+};
+
+Range range_of(const void* p, int64_t bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p);
+  return {x, x + (p ? static_cast<uintptr_t>(bytes) : 0)};
+}
+
+Range range_of(const void* p, const int64_t* stride, const int64_t* sizes, int head_dim) {
+  int64_t last = head_dim;
+  for (int i = 0; i < 3; ++i) last += sizes[i] > 1 ? (sizes[i] - 1) * stride[i] : 0;
+  return range_of(p, 2 * last);
+}
+
+int check_rope(const evisel_rope* r, int head_dim) {
+  if (!r) return fail(EVISEL_EINVAL, "rope is NULL");
+  if (r->rotary_dim < 16 || r->rotary_dim % 16 != 0 || r->rotary_dim > head_dim)
+    return fail(EVISEL_EUNSUPPORTED, "rotary_dim must be a multiple of 16 up to head_dim, got " + std::to_string(r->rotary_dim));
+  if (r->interleaved != 0 && r->interleaved != 1) return fail(EVISEL_EINVAL, "interleaved must be 0 or 1");
+  if (r->axes != 1 && r->axes != 3) return fail(EVISEL_EUNSUPPORTED, "axes must be 1 or 3");
+  if (r->axes == 3) {
+    const int32_t* s = r->section;
+    if (s[0] < 0 || s[1] < 0 || s[2] < 0 || static_cast<int64_t>(s[0]) + s[1] + s[2] != r->rotary_dim / 2)
+      return fail(EVISEL_EINVAL, "sections must not be negative, and rotary_dim / 2 together");
+  }
+  if (!std::isfinite(r->scale)) return fail(EVISEL_EINVAL, "scale must be finite");
+  if (r->reserved != 0) return fail(EVISEL_EINVAL, "reserved must be 0");
+  return EVISEL_OK;
+}
+
+RopeView view_of(const evisel_rope* r) {
+  RopeView v{};
+  v.pairs = r->rotary_dim / 2;
+  std::copy(r->turn, r->turn + v.pairs, v.turn);
+  v.interleaved = r->interleaved;
+  v.border[0] = r->axes == 3 ? r->section[0] : v.pairs;
+  v.border[1] = r->axes == 3 ? r->section[0] + r->section[1] : v.pairs;
+  v.scale = r->scale;
+  return v;
+}
+
+int check_positions(const evisel_positions* p) {
+  if (!p) return fail(EVISEL_EINVAL, "positions is NULL");
+  if (p->at && p->first) return fail(EVISEL_EINVAL, "positions: at or first, not both");
+  if (misaligned(p->at, 4) || misaligned(p->first, 4)) return fail(EVISEL_EINVAL, "positions must be 4-byte aligned");
+  if (p->at && (p->stride[0] < 0 || p->stride[1] < 0)) return fail(EVISEL_EINVAL, "position strides must not be negative");
+  return EVISEL_OK;
+}
+
+PositionView view_of(const evisel_positions* p) {
+  PositionView v{};
+  v.at = p->at;
+  v.first = p->first;
+  std::copy(p->stride, p->stride + 2, v.stride);
+  return v;
+}
+
+int check_heads(const evisel_heads* h, const char* what) {
+  if (!h) return fail(EVISEL_EINVAL, std::string(what) + " is NULL");
+  if (h->head_dim != 64 && h->head_dim != 128)
+    return fail(EVISEL_EUNSUPPORTED, "head_dim must be 64 or 128, got " + std::to_string(h->head_dim));
+  if (h->dtype != EVISEL_BF16 && h->dtype != EVISEL_FP16) return fail(EVISEL_EUNSUPPORTED, "dtype must be bf16 or fp16");
+  if (h->batch < 0 || h->tokens < 0 || h->heads < 0) return fail(EVISEL_EINVAL, "a size is negative");
+  if (h->reserved != 0) return fail(EVISEL_EINVAL, "reserved must be 0");
+  if (static_cast<int64_t>(h->batch) * h->tokens > kMaxTokens || h->heads > 65535)
+    return fail(EVISEL_EUNSUPPORTED, "batch * tokens must be at most 2^30, heads 65535");
+  if (h->batch == 0 || h->tokens == 0 || h->heads == 0) return EVISEL_OK;
+  if (!h->in || !h->out) return fail(EVISEL_EINVAL, std::string(what) + ": in or out is NULL");
+  if (misaligned(h->in) || misaligned(h->out)) return fail(EVISEL_EINVAL, std::string(what) + " must be 16-byte aligned");
+  const int64_t sizes[3] = {h->batch, h->tokens, h->heads};
+  int rc = check_strides(h->in_stride, sizes, 3, what);
+  if (rc == EVISEL_OK) rc = check_strides(h->out_stride, sizes, 3, what);
+  if (rc != EVISEL_OK) return rc;
+  bool same = h->in == h->out;
+  for (int i = 0; i < 3; ++i) {
+    if (sizes[i] > 1 && h->out_stride[i] < h->head_dim)
+      return fail(EVISEL_EINVAL, std::string(what) + ": strides of the output must be at least head_dim");
+    same = same && (sizes[i] <= 1 || h->in_stride[i] == h->out_stride[i]);
+  }
+  if (!same && range_of(h->in, h->in_stride, sizes, h->head_dim).meets(range_of(h->out, h->out_stride, sizes, h->head_dim)))
+    return fail(EVISEL_EINVAL, std::string(what) + ": out must be in itself with the same strides, or apart from it");
+  return EVISEL_OK;
+}
+
+HeadsView view_of(const evisel_heads* h) {
+  HeadsView v{};
+  v.in = h->in;
+  v.out = h->out;
+  std::copy(h->in_stride, h->in_stride + 3, v.is);
+  std::copy(h->out_stride, h->out_stride + 3, v.os);
+  v.heads = h->heads;
+  return v;
+}
+
+// One input's output over another input (each in its own place is the caller's to answer for: rows of one tensor).
+int check_apart(const evisel_heads* a, const evisel_heads* b) {
+  if (a->heads == 0 || b->heads == 0) return EVISEL_OK;
+  const int64_t na[3] = {a->batch, a->tokens, a->heads}, nb[3] = {b->batch, b->tokens, b->heads};
+  const Range out = range_of(a->out, a->out_stride, na, a->head_dim);
+  if (a->out != a->in && out.meets(range_of(b->in, b->in_stride, nb, b->head_dim)))
+    return fail(EVISEL_EINVAL, "an output lies over the other input");
+  if (a->out == b->out || (a->out != a->in && out.meets(range_of(b->out, b->out_stride, nb, b->head_dim))))
+    return fail(EVISEL_EINVAL, "the outputs lie over one another");
+  return EVISEL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int evisel_rope_init(evisel_rope* rope, int32_t rotary_dim, double base, double factor, double original, double low_turns,
+                     double high_turns, const double* freq_h) {
+  return guarded("evisel_rope_init", [&]() -> int {
+    constexpr double kTwoPi = 6.283185307179586476925286766559;
+    if (!rope) return fail(EVISEL_EINVAL, "rope is NULL");
+    if (rotary_dim < 16 || rotary_dim % 16 != 0 || rotary_dim > 2 * kMaxPairs)
+      return fail(EVISEL_EUNSUPPORTED, "rotary_dim must be a multiple of 16 up to 128, got " + std::to_string(rotary_dim));
+    if (!freq_h && !(base > 0.0 && std::isfinite(base))) return fail(EVISEL_EINVAL, "base must be positive and finite");
+    if (!(factor > 0.0 && std::isfinite(factor)) || !(original >= 0.0 && std::isfinite(original)))
+      return fail(EVISEL_EINVAL, "factor must be positive, original not negative, both finite");
+    if (original > 0.0 && !(std::isfinite(low_turns) && std::isfinite(high_turns) && low_turns < high_turns))
+      return fail(EVISEL_EINVAL, "low_turns must be below high_turns, both finite");
+    evisel_rope r{};
+    r.rotary_dim = rotary_dim;
+    r.axes = 1;
+    r.scale = 1.f;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+      double f = freq_h ? freq_h[i] : std::pow(base, -2.0 * i / rotary_dim);
+      if (original > 0.0) {
+        const double turns = original * f / kTwoPi;
+        const double keep = std::min(1.0, std::max(0.0, (turns - low_turns) / (high_turns - low_turns)));
+        f *= keep + (1.0 - keep) / factor;
+      } else {
+        f /= factor;
+      }
+      if (!std::isfinite(f)) return fail(EVISEL_EINVAL, "a frequency is not finite");
+      const double turn = f / kTwoPi, part = turn - std::floor(turn);
+      r.turn[i] = part < 1.0 ? static_cast<uint64_t>(std::ldexp(part, 64)) : 0;
+    }
+    *rope = r;
+    return EVISEL_OK;
+  });
+}
+
+int evisel_rotary(const evisel_rope* rope, const evisel_heads* q, const evisel_heads* k, const evisel_positions* positions,
+                  int transpose, void* stream) {
+  return guarded("evisel_rotary", [&]() -> int {
+    int rc = check_heads(q, "q");
+    if (rc == EVISEL_OK && k) rc = check_heads(k, "k");
+    if (rc == EVISEL_OK) rc = check_rope(rope, q->head_dim);
+    if (rc == EVISEL_OK) rc = check_positions(positions);
+    if (rc != EVISEL_OK) return rc;
+    if (k && (k->batch != q->batch || k->tokens != q->tokens || k->head_dim != q->head_dim || k->dtype != q->dtype))
+      return fail(EVISEL_EINVAL, "q and k must have the same batch, tokens, head_dim and dtype");
+    if (q->batch == 0 || q->tokens == 0 || q->heads + (k ? k->heads : 0) == 0) return EVISEL_OK;
+    if (k) rc = check_apart(q, k);
+    if (k && rc == EVISEL_OK) rc = check_apart(k, q);
+    if (rc != EVISEL_OK) return rc;
+    if (sm_count() <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
+    RotaryLaunch L{};
+    L.rope = view_of(rope);
+    L.pos = view_of(positions);
+    L.q = view_of(q);
+    if (k) L.k = view_of(k);
+    L.batch = q->batch;
+    L.tokens = q->tokens;
+    L.head_dim = q->head_dim;
+    L.dtype = q->dtype;
+    L.transpose = transpose != 0;
+    const cudaError_t e = launch_rotary(L, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e, "rotary launch") : EVISEL_OK;
+  });
+}
+
+int evisel_cache_append_rotary(const evisel_cache* cache, const evisel_rope* rope, const evisel_draft* draft,
+                               const evisel_positions* positions, const int32_t* src, const int32_t* counts,
+                               int32_t* lens_out, void* q_out, void* stream_ptr, evisel_ws** ws_inout) {
+  return guarded("evisel_cache_append_rotary", [&]() -> int {
+    int rc = check_append(cache, draft, src, counts, lens_out, ws_inout);
+    if (rc == EVISEL_OK) rc = check_rope(rope, cache->head_dim);
+    if (rc == EVISEL_OK) rc = check_positions(positions);
+    if (rc != EVISEL_OK) return rc;
+    if (cache->batch == 0) return EVISEL_OK;
+    if (overlap(lens_out, cache->batch, positions->first, cache->batch))
+      return fail(EVISEL_EINVAL, "lens_out must not overlap the positions");
+    if (positions->at && draft->tokens > 0) {
+      const int64_t span = positions->stride[0] * (rope->axes - 1) + positions->stride[1] * (cache->batch - 1) + draft->tokens;
+      if (overlap(lens_out, cache->batch, positions->at, span)) return fail(EVISEL_EINVAL, "lens_out must not overlap the positions");
+    }
+    AppendRotaryLaunch L{};
+    if (draft->q) {
+      if (src && !positions->at) return fail(EVISEL_EINVAL, "q beside src needs positions of its own (at)");
+      const evisel_heads h = {cache->batch, draft->tokens, draft->hq, cache->head_dim, cache->dtype, 0,
+                              {draft->q_stride[0], draft->q_stride[1], draft->q_stride[2]},
+                              {static_cast<int64_t>(draft->tokens) * draft->hq * cache->head_dim,
+                               static_cast<int64_t>(draft->hq) * cache->head_dim, cache->head_dim},
+                              draft->q, q_out};
+      if (draft->hq < 1) return fail(EVISEL_EINVAL, "hq must be positive");
+      rc = check_heads(&h, "q");
+      if (rc != EVISEL_OK) return rc;
+      if (draft->tokens > 0) {
+        const int64_t sizes[3] = {cache->batch, draft->tokens, cache->hkv};
+        const Range out = range_of(q_out, 2 * h.out_stride[0] * cache->batch);
+        if (out.meets(range_of(draft->k_new, draft->k_new_stride, sizes, cache->head_dim)) ||
+            out.meets(range_of(draft->v_new, draft->v_new_stride, sizes, cache->head_dim)))
+          return fail(EVISEL_EINVAL, "q_out lies over k_new or v_new");
+        L.q = view_of(&h);
+      }
+    }
+    const int n_sm = sm_count();
+    if (n_sm <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    rc = acquire(ws_inout, stream);
+    if (rc != EVISEL_OK) return rc;
+    L.rope = view_of(rope);
+    L.pos = view_of(positions);
+    L.a = append_of(cache, draft, src, counts, lens_out, *ws_inout);
+    const cudaError_t e = launch_append_rotary(L, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "rotated append launch");
+    ws_ran_on(*ws_inout, stream);
+    return EVISEL_OK;
+  });
+}
+
+int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* parent, int32_t* token, uint8_t* ended_out,
+                       void* stream_ptr, evisel_ws** ws_inout) {
+  return guarded("evisel_beam_select", [&]() -> int {
+    if (!beams) return fail(EVISEL_EINVAL, "beams is NULL");
+    if (!ws_inout) return fail(EVISEL_EINVAL, "ws_inout is NULL");
+    const evisel_beams& m = *beams;
+    if (m.dtype != EVISEL_BF16 && m.dtype != EVISEL_FP16 && m.dtype != EVISEL_FP32)
+      return fail(EVISEL_EUNSUPPORTED, "dtype must be bf16, fp16 or fp32");
+    if (m.batch < 0) return fail(EVISEL_EINVAL, "batch is negative");
+    if (m.beams < 1 || m.beams > kMaxBeams) return fail(EVISEL_EUNSUPPORTED, "beams must be 1 to " + std::to_string(kMaxBeams));
+    if (m.n_out < 1 || m.n_out > kMaxBeamsOut) return fail(EVISEL_EUNSUPPORTED, "n_out must be 1 to " + std::to_string(kMaxBeamsOut));
+    if (m.vocab < 1 || m.vocab > kMaxVocab) return fail(EVISEL_EUNSUPPORTED, "vocab must be 1 to 2^24");
+    if (m.pad < 0 || m.pad >= m.vocab) return fail(EVISEL_EINVAL, "pad must be a token");
+    if (m.reserved != 0) return fail(EVISEL_EINVAL, "reserved must be 0");
+    const int64_t rows = static_cast<int64_t>(m.batch) * m.beams;
+    if (rows > kMaxRows) return fail(EVISEL_EUNSUPPORTED, "batch * beams must be at most 65535");
+    if (m.batch == 0) return EVISEL_OK;
+    const int size = m.dtype == EVISEL_FP32 ? 4 : 2;
+    if (!m.logits || !score_out || !parent || !token) return fail(EVISEL_EINVAL, "logits or an output is NULL");
+    if (misaligned(m.logits, size) || misaligned(m.scores, 4) || misaligned(score_out, 4) || misaligned(parent, 4) || misaligned(token, 4))
+      return fail(EVISEL_EINVAL, "logits, scores and outputs must be aligned to their elements");
+    if (m.logits_stride[0] < 0 || m.logits_stride[1] < 0) return fail(EVISEL_EINVAL, "logits strides must not be negative");
+    const int64_t n = static_cast<int64_t>(m.batch) * m.n_out;
+    // Other sequences' blocks still read the scores and flags.
+    for (const Range& out : {range_of(score_out, 4 * n), range_of(parent, 4 * n), range_of(token, 4 * n), range_of(ended_out, n)})
+      if (out.meets(range_of(m.scores, 4 * rows)) || out.meets(range_of(m.finished, rows)))
+        return fail(EVISEL_EINVAL, "an output lies over scores or finished");
+    const int n_sm = sm_count();
+    if (n_sm <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
+    const BeamSplit split = beam_split(rows, m.vocab, m.dtype, n_sm);
+    const size_t parts = static_cast<size_t>(rows) * split.splits;
+    const size_t sums = align_up(parts * sizeof(double), 256), tops = align_up(parts * sizeof(float), 256),
+                 picks = align_up(parts * m.n_out * sizeof(float), 256);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    int rc = acquire(ws_inout, stream);
+    if (rc == EVISEL_OK) rc = grow(*ws_inout, sums + tops + 2 * picks, stream);
+    if (rc != EVISEL_OK) return rc;
+    char* buf = static_cast<char*>(ws_cache(*ws_inout).buf);
+    BeamLaunch L{};
+    L.logits = m.logits;
+    L.ls[0] = m.logits_stride[0];
+    L.ls[1] = m.logits_stride[1];
+    L.scores = m.scores;
+    L.finished = m.finished;
+    L.score_out = score_out;
+    L.parent = parent;
+    L.token = token;
+    L.ended_out = ended_out;
+    L.part_sum = reinterpret_cast<double*>(buf);
+    L.part_max = reinterpret_cast<float*>(buf + sums);
+    L.part_value = reinterpret_cast<float*>(buf + sums + tops);
+    L.part_index = reinterpret_cast<int32_t*>(buf + sums + tops + picks);
+    L.batch = m.batch;
+    L.beams = m.beams;
+    L.vocab = m.vocab;
+    L.n = m.n_out;
+    L.dtype = m.dtype;
+    L.pad = m.pad;
+    L.eos = m.eos;
+    L.splits = split.splits;
+    L.part_vectors = split.part_vectors;
+    const cudaError_t e = launch_beams(L, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "beam selection launch");
+    ws_ran_on(*ws_inout, stream);
+    return EVISEL_OK;
+  });
+}
+
+int evisel_cache_reorder(const evisel_cache* cache, const int32_t* parent, int32_t beams, const evisel_state* states,
+                         int32_t n_states, int32_t* table_out, int32_t* lens_out, void* stream_ptr, evisel_ws** ws_inout) {
+  return guarded("evisel_cache_reorder", [&]() -> int {
+    int rc = check_cache(cache, "cache");
+    if (rc != EVISEL_OK) return rc;
+    if (!ws_inout) return fail(EVISEL_EINVAL, "ws_inout is NULL");
+    if (beams < 1 || beams > kMaxBeams) return fail(EVISEL_EUNSUPPORTED, "beams must be 1 to " + std::to_string(kMaxBeams));
+    if (cache->batch % beams != 0) return fail(EVISEL_EINVAL, "the cache's batch must be a multiple of beams");
+    if (n_states < 0 || n_states > kMaxStates) return fail(EVISEL_EUNSUPPORTED, "at most " + std::to_string(kMaxStates) + " states");
+    if (n_states > 0 && !states) return fail(EVISEL_EINVAL, "states is NULL");
+    if (cache->hkv > 1 && (cache->table_stride[1] != 0 || cache->lens_stride[1] != 0))
+      return fail(EVISEL_EUNSUPPORTED, "a reordering needs a table and lengths that the heads share");
+    if (cache->batch == 0) return EVISEL_OK;
+    if (!parent || !lens_out || (cache->max_pages > 0 && !table_out)) return fail(EVISEL_EINVAL, "parent, table_out or lens_out is NULL");
+    if (misaligned(parent, 4) || misaligned(table_out, 4) || misaligned(lens_out, 4))
+      return fail(EVISEL_EINVAL, "parent, table_out and lens_out must be 4-byte aligned");
+    const int64_t batch = cache->batch, entries = batch * cache->max_pages;
+    const Range in[3] = {range_of(parent, 4 * batch),
+                         range_of(cache->table, cache->max_pages > 0 ? 4 * ((batch - 1) * cache->table_stride[0] + cache->max_pages) : 0),
+                         range_of(cache->lens, 4 * ((batch - 1) * cache->lens_stride[0] + 1))};
+    Range out[kMaxStates + 2] = {range_of(table_out, 4 * entries), range_of(lens_out, 4 * batch)};
+    ReorderLaunch L{};
+    L.first_block[0] = static_cast<int>(batch * cache->hkv);
+    int64_t blocks = L.first_block[0];
+    for (int i = 0; i < n_states; ++i) {
+      const evisel_state& s = states[i];
+      if (s.row_bytes < 0 || s.row_bytes >= (int64_t(1) << 40)) return fail(EVISEL_EINVAL, "row_bytes must be 0 to below 2^40");
+      if (s.row_bytes > 0 && (!s.in || !s.out)) return fail(EVISEL_EINVAL, "a state is NULL");
+      out[i + 2] = range_of(s.out, s.row_bytes * batch);
+      L.in[i] = static_cast<const char*>(s.in);
+      L.out[i] = static_cast<char*>(s.out);
+      L.row_bytes[i] = s.row_bytes;
+      const int64_t chunks = (s.row_bytes + kStateBytes - 1) / kStateBytes;
+      blocks += chunks * batch;
+      if (blocks > 0x7fffffff) return fail(EVISEL_EUNSUPPORTED, "the states are too large for one call");
+      L.chunks[i] = static_cast<int>(chunks);
+      L.first_block[i + 1] = static_cast<int>(blocks);
+    }
+    for (int i = 0; i < n_states + 2; ++i) {
+      for (const Range& r : in)
+        if (out[i].meets(r)) return fail(EVISEL_EINVAL, "an output lies over parent, the table or the lengths");
+      for (int j = 0; j < n_states; ++j)
+        if (out[i].meets(range_of(states[j].in, states[j].row_bytes * batch))) return fail(EVISEL_EINVAL, "an output lies over a state");
+      for (int j = 0; j < i; ++j)
+        if (out[i].meets(out[j])) return fail(EVISEL_EINVAL, "outputs lie over one another");
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    rc = acquire(ws_inout, stream);
+    if (rc != EVISEL_OK) return rc;
+    L.c = view_of(cache);
+    L.k = cache->k;
+    L.v = cache->v;
+    L.k_mean = cache->k_mean;
+    L.parent = parent;
+    L.table_out = table_out;
+    L.lens_out = lens_out;
+    L.status = ws_status(*ws_inout);
+    L.beams = beams;
+    L.n_states = n_states;
+    const cudaError_t e = launch_reorder(L, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "reordering launch");
+    ws_ran_on(*ws_inout, stream);
+    return EVISEL_OK;
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,42 @@
+// Position rotation of queries and keys: every element read and written once.
+#include "rope.cuh"
+
+namespace evisel {
+namespace {
+
+constexpr int kWarps = 8;
+
+template <class T, int D, bool INTER>
+__global__ void __launch_bounds__(kWarps * 32) rotary_kernel(const __grid_constant__ RotaryLaunch L, int share, int shares) {
+  __shared__ float2 mem[kWarps][D / 2];
+  const int warp = threadIdx.x >> 5;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
+  ptx::grid_wait();
+  ptx::grid_launch_next();
+  const int64_t n = item / shares;
+  if (n >= static_cast<int64_t>(L.batch) * L.tokens) return;
+  const int b = static_cast<int>(n / L.tokens), t = static_cast<int>(n - static_cast<int64_t>(b) * L.tokens);
+  const int heads = L.q.heads + L.k.heads, h0 = static_cast<int>(item - n * shares) * share;
+  int pos[3];
+  positions_of(L.rope, L.pos, b, t, 0, t, pos);
+  rotate_token<T, D, INTER>(L.rope, L.q, L.k, b, t, pos, L.transpose ? -1.f : 1.f, h0, min(heads, h0 + share), mem[warp]);
+}
+
+template <class T, int D>
+cudaError_t launch_d(const RotaryLaunch& L, cudaStream_t stream) {
+  const int64_t tokens = static_cast<int64_t>(L.batch) * L.tokens;
+  const int heads = L.q.heads + L.k.heads, share = rotary_heads_per_warp(tokens, heads, D, sm_count());
+  const int shares = (heads + share - 1) / share;
+  const unsigned grid = static_cast<unsigned>((tokens * shares + kWarps - 1) / kWarps);
+  return launch_after(L.rope.interleaved ? rotary_kernel<T, D, true> : rotary_kernel<T, D, false>, dim3(grid), kWarps * 32, 0,
+                      stream, L, share, shares);
+}
+
+}  // namespace
+
+cudaError_t launch_rotary(const RotaryLaunch& L, cudaStream_t stream) {
+  if (L.dtype == 0) return L.head_dim == 128 ? launch_d<BF16, 128>(L, stream) : launch_d<BF16, 64>(L, stream);
+  return L.head_dim == 128 ? launch_d<FP16, 128>(L, stream) : launch_d<FP16, 64>(L, stream);
+}
+
+}  // namespace evisel
