@@ -130,7 +130,7 @@ typedef struct {
  * Within a beam the order is that of the logits, exactly; between beams it goes by a
  * normaliser formed from fp32 exponentials, fp32 sums of up to 64 of them and 64-bit sums of those,
  * off by about 1e-7 at most, and 64-bit values. The same call gives the same bits.
- * The workspace keeps 8 n + 12 bytes for each part of a row, of 1,024 to 16,384 logits.
+ * The workspace keeps 8 bytes for every 1,024 logits (512 in fp32).
  * Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED, EVISEL_ENOMEM, EVISEL_ECUDA. */
 int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* parent, int32_t* token, uint8_t* ended_out,
                        void* stream, evisel_ws** ws_inout);

@@ -53,8 +53,9 @@ def continuations(logits, scores, finished=None, pad=0):
         if not math.isfinite(score) or np.isnan(row).any() or np.isposinf(row).any() or np.isneginf(row).all():
             continue
         top = row.max()
-        lse = top + math.log(math.fsum(np.exp(row - top)))
-        out += [(score + x - lse, k, v) for v, x in enumerate(row.tolist()) if x > -math.inf]
+        total = math.log(math.fsum(np.exp(row - top)))
+        # (x - top first: of logits near 1e38 nothing of score and total would be left)
+        out += [(score + ((x - top) - total), k, v) for v, x in enumerate(row.tolist()) if x > -math.inf]
     return sorted(out, key=lambda e: (-e[0], e[1], e[2]))
 
 

@@ -1,11 +1,9 @@
 // The highest continuations over a sequence's beams and the vocabulary, in two
-// launches: every part of every row of logits gives its maximum, its sum of exponentials
-// and its n highest logits; then a CTA per sequence forms the rows' normalisers and
-// chooses among the parts' winners.
-//
-// The n-th largest of the maxima of disjoint groups of elements is a lower bound of
-// the n-th largest element: what reaches it is a few more than n elements, which are
-// ranked by comparing all with all. Logits are read once; they stay in registers.
+// launches. A row of logits is cut into blocks of 1,024 (512 in 32 bits; powers of two more for
+// long rows); a warp streams a block and leaves its maximum and its sum of exponentials. Then a CTA per sequence forms
+// the rows' normalisers from the blocks' sums, takes the n highest blocks by their maxima (ties in
+// order), in which all of the n highest continuations lie, and reads those again: for any
+// continuation outside, each of the n blocks has one that stands before it.
 #include <algorithm>
 
 #include "cache_common.cuh"
@@ -14,376 +12,610 @@
 namespace evisel {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kPerThread = 8;                    // 16-byte vectors of a thread
-constexpr int kList = 512;                       // elements that reach the bound; beyond, one after the other
-constexpr float kLowest = -3.402823466e38f;
+constexpr int kThreads = 512, kWarps = kThreads / 32, kPerSm = 2;
+constexpr int kPerLane = 4;                      // 16-byte vectors of a lane's chunk; the next chunk is in flight
+constexpr int kChunk = 32 * kPerLane;
+constexpr int kMostBlocks = 4096;                // of a sequence, about
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eLow = 1.925963033500e-8f;  // log2 e - kLog2e
+
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  uint4 w;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(p));
+  return w;
+}
 
 struct F32 {};
 template <class T>
 struct Vec {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& w, float* f) {
-    float g[8];
-    unpack8<T>(w, g);
+  static constexpr uint32_t kNone = T::kFormat == 1 ? 0xff80ff80u : 0xfc00fc00u;   // -inf twice
+  static __device__ __forceinline__ void unpack(const uint4& w, float (&f)[8]) { unpack8<T>(w, f); }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if constexpr (T::kFormat == 1)
+      asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else
+      asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float element(const uint4* p, int i) { return T::lo(__ldg(reinterpret_cast<const uint16_t*>(p) + i)); }
+  static __device__ __forceinline__ float highest(const uint4& w) {
+    const uint32_t m = max2(max2(w.x, w.y), max2(w.z, w.w));
+    return fmaxf(T::lo(m), T::hi(m));
+  }
+  // The largest of the vectors' elements.
+  static __device__ __forceinline__ float highest(const uint4 (&w)[kPerLane]) {
+    uint32_t m = kNone;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = g[e];
+    for (int i = 0; i < kPerLane; ++i) m = max2(m, max2(max2(w[i].x, w[i].y), max2(w[i].z, w[i].w)));
+    return fmaxf(T::lo(m), T::hi(m));
   }
-  static __device__ __forceinline__ float one(const void* p, int64_t i) {
-    return T::lo(static_cast<const uint16_t*>(p)[i]);
-  }
-  // A vector of -inf with element e replaced.
-  static __device__ __forceinline__ uint32_t minus_inf() { return T::kFormat == 1 ? 0xff80ff80u : 0xfc00fc00u; }
-  static __device__ __forceinline__ void load_some(uint4& w, const void* p, int e0, int e1) {
+  // The elements [e0, e1) of a vector, -inf beside them.
+  static __device__ __forceinline__ uint4 load_some(const uint4* p, int e0, int e1) {
+    const uint16_t* s = reinterpret_cast<const uint16_t*>(p);
     uint32_t x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t none = minus_inf() & 0xffffu;
-      const uint32_t lo = 2 * i >= e0 && 2 * i < e1 ? static_cast<const uint16_t*>(p)[2 * i] : none;
-      const uint32_t hi = 2 * i + 1 >= e0 && 2 * i + 1 < e1 ? static_cast<const uint16_t*>(p)[2 * i + 1] : none;
+      const uint32_t lo = 2 * i >= e0 && 2 * i < e1 ? s[2 * i] : kNone & 0xffffu;
+      const uint32_t hi = 2 * i + 1 >= e0 && 2 * i + 1 < e1 ? s[2 * i + 1] : kNone & 0xffffu;
       x[i] = lo | hi << 16;
     }
-    w = make_uint4(x[0], x[1], x[2], x[3]);
+    return make_uint4(x[0], x[1], x[2], x[3]);
   }
 };
 template <>
 struct Vec<F32> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void unpack(const uint4& w, float* f) {
+  static constexpr uint32_t kNone = 0xff800000u;
+  static __device__ __forceinline__ void unpack(const uint4& w, float (&f)[4]) {
     f[0] = __uint_as_float(w.x), f[1] = __uint_as_float(w.y), f[2] = __uint_as_float(w.z), f[3] = __uint_as_float(w.w);
   }
-  static __device__ __forceinline__ uint32_t minus_inf() { return 0xff800000u; }
-  static __device__ __forceinline__ void load_some(uint4& w, const void* p, int e0, int e1) {
+  static __device__ __forceinline__ float element(const uint4* p, int i) { return __ldg(reinterpret_cast<const float*>(p) + i); }
+  static __device__ __forceinline__ float highest(const uint4& w) {
+    return fmaxf(ptx::max3(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z)), __uint_as_float(w.w));
+  }
+  static __device__ __forceinline__ float highest(const uint4 (&w)[kPerLane]) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i)
+      m = ptx::max3(m, ptx::max3(__uint_as_float(w[i].x), __uint_as_float(w[i].y), __uint_as_float(w[i].z)), __uint_as_float(w[i].w));
+    return m;
+  }
+  static __device__ __forceinline__ uint4 load_some(const uint4* p, int e0, int e1) {
+    const uint32_t* s = reinterpret_cast<const uint32_t*>(p);
     uint32_t x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = i >= e0 && i < e1 ? static_cast<const uint32_t*>(p)[i] : minus_inf();
-    w = make_uint4(x[0], x[1], x[2], x[3]);
+    for (int i = 0; i < 4; ++i) x[i] = i >= e0 && i < e1 ? s[i] : kNone;
+    return make_uint4(x[0], x[1], x[2], x[3]);
   }
 };
 
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
+// Order-preserving: larger for a larger value; 0 for none.
+__device__ __forceinline__ uint32_t order_bits(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);   // (-0 as 0)
+  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float from_order_bits(uint32_t b) { return __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b); }
+using Key = unsigned long long;
 
 // Whether (x, i) stands before (y, j): higher, or as high and earlier.
-template <class V>
-__device__ __forceinline__ bool before(V x, int i, V y, int j) {
-  return x > y || (x == y && i < j);
+__device__ __forceinline__ bool before(Key x, int i, Key y, int j) { return x > y || (x == y && i < j); }
+
+__device__ __forceinline__ float warp_max(float x) {
+  float m;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
+  return m;
 }
 
 // Whether a beam has continuations from its logits.
 __device__ __forceinline__ bool beam_is_live(const BeamLaunch& L, int row) {
-  if (L.finished && __ldg(L.finished + row)) return false;
-  const float s = L.scores ? __ldg(L.scores + row) : 0.f;
-  return isfinite(s);
+  const int ended = L.finished ? __ldg(L.finished + row) : 0;
+  const float score = L.scores ? __ldg(L.scores + row) : 0.f;
+  return ended == 0 && isfinite(score);
 }
 
 // Groups of threads whose maxima bound the n-th largest element.
 __device__ __forceinline__ int groups_for(int n) { return n <= 16 ? 64 : n <= 32 ? 128 : 256; }
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) beam_scan_kernel(const __grid_constant__ BeamLaunch L) {
-  constexpr int N = Vec<T>::N;
-  __shared__ __align__(16) float group_max[kThreads];
-  __shared__ float list_value[kList], bound;
-  __shared__ double warp_total[kWarps];
-  __shared__ int list_index[kList], count;
-  const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  ptx::grid_wait();
-  ptx::grid_launch_next();
-  const int64_t slot = static_cast<int64_t>(row) * L.splits + part;
-  if (!beam_is_live(L, row)) return;
-  const int b = row / L.beams, k = row - b * L.beams;
-  constexpr int kSize = 16 / N;
-  const char* base = static_cast<const char*>(L.logits) + (b * L.ls[0] + k * L.ls[1]) * kSize;
-  const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(base) & 15) / kSize);   // elements before the row in its first vector
-  const uint4* vectors = reinterpret_cast<const uint4*>(base - skew * kSize);
-  const int v0 = part * L.part_vectors, v1 = min(v0 + L.part_vectors, (skew + L.vocab + N - 1) / N);
-  if (tid == 0) count = 0;
-
-  uint4 w[kPerThread];
-  float best = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    const int v = v0 + tid + i * kThreads;
-    w[i] = make_uint4(Vec<T>::minus_inf(), Vec<T>::minus_inf(), Vec<T>::minus_inf(), Vec<T>::minus_inf());
-    if (v < v1) {
-      const int e0 = skew - v * N, e1 = skew + L.vocab - v * N;   // the row's elements of the vector
-      if (e0 <= 0 && e1 >= N) w[i] = __ldg(vectors + v);
-      else Vec<T>::load_some(w[i], vectors + v, e0, e1);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    float x[N];
-    Vec<T>::unpack(w[i], x);
-#pragma unroll
-    for (int e = 0; e < N; ++e) best = fmaxf(best, x[e]);
-  }
-  const int groups = groups_for(L.n), width = kThreads / groups;
-  float g = best;
-  for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
-  if (tid % width == 0) group_max[tid / width] = g;
+// A lower bound of the n-th largest of the values whose maxima by thread are `x`:
+// the n-th largest of `groups` groups' maxima. The threads of a group share the comparisons. Two barriers.
+template <int kBlock>
+__device__ __forceinline__ uint32_t bound_of(uint32_t x, uint32_t* group_max, uint32_t* bound, int n, int groups) {
+  const int tid = threadIdx.x, width = kBlock / groups, group = tid / width, share = groups / width;
+  for (int o = 1; o < width; o <<= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+  if (tid % width == 0) group_max[group] = x;
   __syncthreads();
-
-  // The part's maximum, and its sum of exponentials from there.
-  float top = -INFINITY;
-  for (int i = lane; i < groups; i += 32) top = fmaxf(top, group_max[i]);
-  top = warp_max(top);
-  const float shift = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
+  const int first = tid % width * share;
+  int rank = 0;
+  for (int i = first; i < first + share; i += 8) {
 #pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    float x[N];
-    Vec<T>::unpack(w[i], x);
-#pragma unroll
-    for (int e = 0; e < N; ++e) sum += ptx::ex2((x[e] - shift) * 1.4426950408889634f);
+    for (int j = i; j < i + 8; ++j) rank += group_max[j] > x || (group_max[j] == x && j < group) ? 1 : 0;
   }
-  double total = sum;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if (lane == 0) warp_total[warp] = total;
-  if (tid < groups) {
-    const float mine = group_max[tid];
-    int rank = 0;
-    for (int i = 0; i < groups; ++i) rank += before(group_max[i], i, mine, tid) ? 1 : 0;
-    if (rank == L.n - 1) bound = fmaxf(mine, kLowest);
-  }
+  for (int o = 1; o < width; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+  if (rank == n - 1) *bound = x;
   __syncthreads();
-
-  if (tid == 0) {
-    double s = 0.0;
-    for (int i = 0; i < kWarps; ++i) s += warp_total[i];
-    L.part_sum[slot] = s;
-    L.part_max[slot] = shift;
-  }
-  const float least = bound;
-  if (best >= least) {
-#pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-      float x[N];
-      Vec<T>::unpack(w[i], x);
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (x[e] >= least) {
-          const int at = atomicAdd(&count, 1);
-          if (at < kList) {
-            list_value[at] = x[e];
-            list_index[at] = (v0 + tid + i * kThreads) * N + e - skew;
-          }
-        }
-    }
-  }
-  __syncthreads();
-  float* value = L.part_value + slot * L.n;
-  int32_t* index = L.part_index + slot * L.n;
-  const int found = count;
-  if (found <= kList) {
-    for (int i = tid; i < found; i += kThreads) {
-      const float x = list_value[i];
-      const int at = list_index[i];
-      int rank = 0;
-      for (int j = 0; j < found; ++j) rank += before(list_value[j], list_index[j], x, at) ? 1 : 0;
-      if (rank < L.n) value[rank] = x, index[rank] = at;
-    }
-    for (int i = found + tid; i < L.n; i += kThreads) value[i] = -INFINITY, index[i] = -1;
-    return;
-  }
-  // Many as high as one another (a row of few values): the next one after the last, n times.
-  float last = INFINITY;
-  int last_at = -1;
-  for (int r = 0; r < L.n; ++r) {
-    float x_best = -INFINITY;
-    int at_best = 0x7fffffff;
-#pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-      float x[N];
-      Vec<T>::unpack(w[i], x);
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int at = (v0 + tid + i * kThreads) * N + e - skew;
-        if (x[e] > -INFINITY && before(last, last_at, x[e], at) && before(x[e], at, x_best, at_best)) x_best = x[e], at_best = at;
-      }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float y = __shfl_xor_sync(0xffffffffu, x_best, o);
-      const int yi = __shfl_xor_sync(0xffffffffu, at_best, o);
-      if (before(y, yi, x_best, at_best)) x_best = y, at_best = yi;
-    }
-    __syncthreads();
-    if (lane == 0) list_value[warp] = x_best, list_index[warp] = at_best;
-    __syncthreads();
-    for (int i = 0; i < kWarps; ++i)
-      if (before(list_value[i], list_index[i], x_best, at_best)) x_best = list_value[i], at_best = list_index[i];
-    last = x_best, last_at = at_best;
-    if (tid == 0) value[r] = x_best, index[r] = x_best > -INFINITY ? at_best : -1;
-  }
+  return *bound;
 }
 
-// ---------------------------------------------------------------- the choice among the parts' winners
-constexpr int kMergeThreads = 512, kMergeWarps = kMergeThreads / 32;
-constexpr int kMergeList = 1024;
+// A block's exponentials are 2^(x kLog2e - c), each exponent rounded once, with c = top kLog2e as it was rounded:
+// their sum is in units of 2^(c + top kLog2eLow). Beyond 2^20, where c's rounding would be a large exponent by itself,
+// they are 2^((x - top) kLog2e), in units of e^top.
+__device__ __forceinline__ bool is_near(float top) { return fabsf(top) < 1048576.f; }
+__device__ __forceinline__ float offset_c(float top) { return is_near(top) ? top * kLog2e : 0.f; }
 
-struct Candidates {
-  const BeamLaunch& L;
-  const double* offset;             // score - normaliser of a beam; NaN: no continuations from its logits
-  int b, per_beam, listed;
-  __device__ __forceinline__ int total() const { return listed + L.beams; }
-  // Value and flat index (beam, token) of candidate i; -inf where it is none.
-  __device__ __forceinline__ void get(int i, double& value, int& flat) const {
-    value = -INFINITY;
-    flat = 0x7fffffff;
-    if (i < listed) {
-      const int k = i / per_beam;
-      if (!(offset[k] == offset[k])) return;
-      const int64_t at = static_cast<int64_t>(b) * listed + i;
-      const float x = L.part_value[at];
-      if (!(x > -INFINITY)) return;
-      value = offset[k] + static_cast<double>(x);
-      flat = k * L.vocab + L.part_index[at];
-    } else {                                     // an ended beam as it is
-      const int k = i - listed, row = b * L.beams + k;
-      if (!L.finished || !__ldg(L.finished + row)) return;
-      const float s = L.scores ? __ldg(L.scores + row) : 0.f;
-      if (!isfinite(s)) return;
-      value = s;
-      flat = k * L.vocab + L.pad;
+// log2 of the units of (top, c) in units of (to, to_c).
+__device__ __forceinline__ float units_between(float top, float c, float to, float to_c) {
+  if (is_near(top) && is_near(to)) return fmaf(top - to, kLog2eLow, c - to_c);
+  return (top - to) * kLog2e + (is_near(top) ? fmaf(-top, kLog2e, c) : 0.f) - (is_near(to) ? fmaf(-to, kLog2e, to_c) : 0.f);
+}
+
+template <class T, bool kFar>
+__device__ __forceinline__ float sum_of(const uint4 (&w)[kPerLane], float top, float c) {
+  const uint64_t shift = ptx::f2(-top, -top), minus_c = ptx::f2(-c, -c), log2e = ptx::f2(kLog2e, kLog2e);
+  uint64_t acc = 0;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    float x[Vec<T>::N];
+    Vec<T>::unpack(w[i], x);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::N; e += 2) {
+      uint64_t y = ptx::f2(x[e], x[e + 1]);
+      if constexpr (kFar) y = ptx::add2(y, shift);
+      float a, b;
+      ptx::unf2(ptx::fma2(y, log2e, minus_c), a, b);
+      acc = ptx::add2(acc, ptx::f2(ptx::ex2(a), ptx::ex2(b)));
     }
+  }
+  float a, b;
+  ptx::unf2(acc, a, b);
+  return a + b;
+}
+
+// A row's 16-byte vectors, from the one that holds its first element on.
+template <class T>
+struct Row {
+  static constexpr int N = Vec<T>::N;
+  const uint4* vectors;
+  int skew;                         // elements of the first vector before the row
+  Row() = default;
+  __device__ __forceinline__ Row(const BeamLaunch& L, int row) {
+    constexpr int kSize = 16 / N;
+    const int b = row / L.beams, k = row - b * L.beams;
+    const char* base = static_cast<const char*>(L.logits) + (b * L.ls[0] + k * L.ls[1]) * kSize;
+    skew = static_cast<int>((reinterpret_cast<uintptr_t>(base) & 15) / kSize);
+    vectors = reinterpret_cast<const uint4*>(base - skew * kSize);
+  }
+  // Vector v of the row, -inf beside it.
+  __device__ __forceinline__ uint4 vector(int v, int vocab) const {
+    if (v * N >= skew && (v + 1) * N <= skew + vocab) return __ldg(vectors + v);
+    return Vec<T>::load_some(vectors + v, skew - v * N, skew + vocab - v * N);
+  }
+  // The chunk at vector `at`, -inf beside the row; kOnce: nothing of it is read again by this SM.
+  template <bool kOnce>
+  __device__ __forceinline__ void load(uint4 (&w)[kPerLane], int at, int vocab) const {
+    const int lane = threadIdx.x & 31, inner0 = skew > 0 ? 1 : 0, inner1 = (skew + vocab) / N, last = (skew + vocab + N - 1) / N;
+    if (at >= inner0 && at + kChunk <= inner1) {
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) w[i] = kOnce ? load_once(vectors + at + lane + i * 32) : __ldg(vectors + at + lane + i * 32);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+      const int v = at + lane + i * 32;
+      w[i] = v < last ? vector(v, vocab) : make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+    }
+  }
+  __device__ __forceinline__ float element(int token) const { return Vec<T>::element(vectors, token + skew); }
+  __device__ __forceinline__ int token(int at, int i, int e) const {
+    return (at + static_cast<int>(threadIdx.x & 31) + i * 32) * N + e - skew;
   }
 };
 
-__global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_constant__ BeamLaunch L) {
-  __shared__ double offset[kMaxBeams], group_max[256], list_value[kMergeList], bound;
-  __shared__ int list_flat[kMergeList], count;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+template <class T>
+__global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __grid_constant__ BeamLaunch L) {
+  const unsigned step = gridDim.x * kWarps;
+  unsigned u = blockIdx.x * kWarps + (threadIdx.x >> 5);           // a block of all rows' blocks
   ptx::grid_wait();
   ptx::grid_launch_next();
-  if (tid == 0) count = 0;
-  for (int k = warp; k < L.beams; k += kMergeWarps) {
-    const int row = b * L.beams + k;
-    const bool live = beam_is_live(L, row);
-    double lse = 0.0;
-    if (live) {
-      const int64_t first = static_cast<int64_t>(row) * L.splits;
-      float top = -INFINITY;
-      for (int i = lane; i < L.splits; i += 32)
-        if (L.part_sum[first + i] != 0.0) top = fmaxf(top, L.part_max[first + i]);
-      top = warp_max(top);
-      double sum = 0.0;
-      for (int i = lane; i < L.splits; i += 32) {
-        const double s = L.part_sum[first + i];
-        const float m = L.part_max[first + i];
-        sum += s == 0.0 ? 0.0 : m == top ? s : s * exp(static_cast<double>(m) - static_cast<double>(top));
+  Row<T> row;
+  int at = 0, end = 0;
+  // The next block that is to be read.
+  auto find = [&]() {
+    for (; u < L.total; u += step) {
+      const int r = static_cast<int>(u / L.blocks);
+      if (!beam_is_live(L, r)) continue;
+      row = Row<T>(L, r);
+      at = (u - r * L.blocks) * L.block_vectors;
+      end = min(at + L.block_vectors, L.row_vectors);
+      return true;
+    }
+    return false;
+  };
+  uint4 next[kPerLane];
+  bool more = find();
+  if (more) row.template load<true>(next, at, L.vocab);
+  float top = -INFINITY, c = 0.f, sum = 0.f, low = 0.f;            // the sum is sum + low
+  while (more) {
+    uint4 w[kPerLane];
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) w[i] = next[i];
+    const unsigned now = u;
+    const bool last = at + kChunk >= end;
+    if (!last) {
+      at += kChunk;
+      row.template load<true>(next, at, L.vocab);
+    } else {
+      u += step;
+      if ((more = find())) row.template load<true>(next, at, L.vocab);
+    }
+    const float highest = warp_max(Vec<T>::highest(w));
+    if (highest > top) {            // (the whole warp)
+      const float to = offset_c(highest);
+      if (sum != 0.f) {
+        const float f = ptx::ex2(units_between(top, c, highest, to));
+        sum *= f, low *= f;
       }
+      top = highest, c = to;
+    }
+    const float add = is_near(top) || top == -INFINITY ? sum_of<T, false>(w, top, c) : sum_of<T, true>(w, top, 0.f);
+    const float both = __fadd_rn(sum, add), rest = both - sum;
+    low += (sum - (both - rest)) + (add - rest);
+    sum = both;
+    if (last) {
+      sum += low;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      lse = static_cast<double>(top) + log(sum);
+      if ((threadIdx.x & 31) == 0) L.part[now] = make_float2(top, sum);
+      top = -INFINITY, c = 0.f, sum = 0.f, low = 0.f;
     }
-    // A sum that is no number makes every value NaN; a row of -inf has none above it.
-    const double score = L.scores ? static_cast<double>(__ldg(L.scores + row)) : 0.0;
-    if (lane == 0) offset[k] = live && isfinite(lse) ? score - lse : NAN;
   }
-  __syncthreads();
-  const Candidates c{L, offset, b, L.splits * L.n, L.beams * L.splits * L.n};
-  const int total = c.total(), groups = groups_for(L.n), width = kMergeThreads / groups;
-  double best = -INFINITY;
-  for (int i = tid; i < total; i += kMergeThreads) {
-    double x;
-    int f;
-    c.get(i, x, f);
-    best = fmax(best, x);
+}
+
+// ---------------------------------------------------------------- the choice
+constexpr int kMergeThreads = 512, kMergeWarps = kMergeThreads / 32;
+constexpr int kList = 512;
+constexpr int kHeld = 4;                         // blocks of a thread that stay in registers
+
+// A value of 48 bits as the sum of two floats, the second at most half a step of the first.
+struct Two {
+  float hi, lo;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {
+  const float s = a + b, t = s - a;
+  return {s, (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ Two add(Two a, Two b) {
+  const Two s = two_sum(a.hi, b.hi), t = two_sum(a.lo, b.lo);
+  Two r = two_sum(s.hi, s.lo + t.hi);
+  return two_sum(r.hi, r.lo + t.lo);
+}
+__device__ __forceinline__ Two add(Two a, float b) {
+  const Two s = two_sum(a.hi, b);
+  return two_sum(s.hi, s.lo + a.lo);
+}
+
+__device__ __forceinline__ Key order_key(Two x) {           // 0: none, beyond the numbers
+  return !(fabsf(x.hi) < INFINITY) ? 0 : static_cast<Key>(order_bits(x.hi)) << 32 | order_bits(x.lo);
+}
+__device__ __forceinline__ float value_of(Key key) {    // the value rounded to fp32
+  return key == 0 ? -INFINITY : from_order_bits(static_cast<uint32_t>(key >> 32));
+}
+
+constexpr float kLn2 = 0.693147182f, kLn2Low = -1.90465421e-09f;
+// ln of s > 0 (s.hi a normal number) times 2^exponent, to about 2^-31: s = 2^e (1 + z + y), 1 + z from 1/sqrt 2 to sqrt 2,
+// ln(1 + z + y) = 2 artanh t, t = (z + y) / (2 + z + y), the series from t^3 on and what t's rounding leaves in 32 bits.
+__device__ __forceinline__ Two ln(Two s, int exponent) {
+  const uint32_t bits = __float_as_uint(s.hi);
+  int e = static_cast<int>(bits >> 23) - 127;
+  float z = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u) - 1.f;
+  float y = s.lo * __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+  if (z > 0.414213562f) z = fmaf(z, 0.5f, -0.5f), y *= 0.5f, ++e;
+  const float below = __fadd_rn(2.f, z), by = __frcp_rn(below), cut = z - __fadd_rn(below, -2.f), t = z * by;
+  const float left = fmaf(-t, below, z) + fmaf(-t, cut, fmaf(-t, y, y));   // z + y - t (2 + z + y), 2 + z = below + cut
+  const float t2 = t * t, rest = fmaf(fmaf(fmaf(fmaf(t2, 2.f / 11.f, 2.f / 9.f), t2, 2.f / 7.f), t2, 0.4f), t2, 2.f / 3.f) * t2 * t;
+  const float n = static_cast<float>(e + exponent), q = __fmul_rn(n, kLn2);
+  return add(Two{q, fmaf(n, kLn2Low, fmaf(n, kLn2, -q))}, two_sum(2.f * t, fmaf(fmaf(2.f, t2, 2.f) * by, left, rest)));   // (artanh' = 1 + t^2 + ..)
+}
+
+// A continuation's place: by value, then by beam, logit and token.
+struct Place {
+  Key value, rest;
+  __device__ __forceinline__ bool operator>(const Place& o) const { return value > o.value || (value == o.value && rest > o.rest); }
+};
+__device__ __forceinline__ Key rest_of(int k, float x, int token) {
+  return static_cast<Key>(63 - k) << 56 | static_cast<Key>(order_bits(x)) << 24 | static_cast<uint32_t>(0xffffff - token);
+}
+__device__ __forceinline__ int beam_of(Key rest) { return 63 - static_cast<int>(rest >> 56); }
+__device__ __forceinline__ int token_of(Key rest) { return 0xffffff - static_cast<int>(rest & 0xffffff); }
+
+struct MergeShared {
+  Two offset[kMaxBeams];                         // score - normaliser; NaN: no continuations from the logits
+  float ended_score[kMaxBeams];                  // of a beam that has ended; NaN: it has not, or has none
+  Key listed_value[kList], value[kList], rest[kList];
+  int id[kList], chosen[kMaxBeamsOut];           // blocks
+  uint32_t group_max[256], bound;
+  Key least, warp_value[kMergeWarps], warp_rest[kMergeWarps];
+  int listed, count;
+  uint8_t ended[kMaxBeams];
+};
+
+// A row's normaliser in 64 bits, by a warp; NaN: none. (Apart, so that the usual path is short: what a launch of
+// a few microseconds spends is also the fetching of its instructions.)
+__device__ __noinline__ Two far_normaliser(const float2* part, int blocks) {
+  float top = -INFINITY;
+  for (int j = threadIdx.x & 31; j < blocks; j += 32) top = fmaxf(top, part[j].x);
+  top = warp_max(top);
+  double far = 0.0;
+  for (int j = threadIdx.x & 31; j < blocks; j += 32) {
+    const float2 p = part[j];
+    if (p.x == -INFINITY) continue;
+    const double c = offset_c(p.x);
+    const double from = is_near(p.x) ? 0.693147180559945309417 * (c + static_cast<double>(p.x) * static_cast<double>(kLog2eLow)) : static_cast<double>(p.x);
+    far += static_cast<double>(p.y) * exp(from - static_cast<double>(top));
   }
-  double g = best;
-  for (int o = 1; o < width; o <<= 1) g = fmax(g, __shfl_xor_sync(0xffffffffu, g, o));
-  if (tid % width == 0) group_max[tid / width] = g;
-  __syncthreads();
-  if (tid < groups) {
-    const double mine = group_max[tid];
-    int rank = 0;
-    for (int i = 0; i < groups; ++i) rank += before(group_max[i], i, mine, tid) ? 1 : 0;
-    if (rank == L.n - 1) bound = fmax(mine, -1.7976931348623157e308);
+  for (int o = 16; o > 0; o >>= 1) far += __shfl_xor_sync(0xffffffffu, far, o);
+  const double x = log(far);
+  const float hi = static_cast<float>(x);
+  return isfinite(x) && isfinite(top) ? add(two_sum(hi, static_cast<float>(x - static_cast<double>(hi))), top) : Two{NAN, NAN};
+}
+
+// A row's normaliser, by a warp; NaN: none. The blocks' sums are added in 48 bits, so that the rows of one logit that
+// are cut differently (one begins inside a vector) have one normaliser.
+__device__ __forceinline__ Two normaliser(const float2* part, int blocks) {
+  constexpr int kBatch = 8;                      // loads on their way at once
+  float exponent = -INFINITY;
+  Two sum = {0.f, 0.f};                          // the sum is sum 2^exponent
+  bool far = false;
+  for (int j0 = threadIdx.x & 31; j0 - static_cast<int>(threadIdx.x & 31) < blocks; j0 += kBatch * 32) {
+    float2 p[kBatch];
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) p[i] = j0 + i * 32 < blocks ? part[j0 + i * 32] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) top = fmaxf(top, p[i].x), far = far || (!is_near(p[i].x) && p[i].x != -INFINITY);
+    top = warp_max(top);
+    const float to = fmaxf(exponent, is_near(top) ? ceilf(top * kLog2e) : 0.f);
+    const float down = ptx::ex2(exponent - to);
+    sum.hi *= down, sum.lo *= down;
+    exponent = to;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float by = p[i].x == -INFINITY ? -INFINITY : fmaf(p[i].x, kLog2eLow, offset_c(p[i].x) - exponent);
+      const float f = ptx::ex2(by), product = __fmul_rn(p[i].y, f);
+      const Two s = two_sum(sum.hi, product);
+      sum.hi = s.hi, sum.lo += s.lo + fmaf(p[i].y, f, -product);
+    }
   }
-  __syncthreads();
-  const double least = bound;
-  if (best >= least)
-    for (int i = tid; i < total; i += kMergeThreads) {
-      double x;
-      int f;
-      c.get(i, x, f);
-      if (x >= least) {
-        const int at = atomicAdd(&count, 1);
-        if (at < kMergeList) list_value[at] = x, list_flat[at] = f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const Two s = two_sum(sum.hi, __shfl_xor_sync(0xffffffffu, sum.hi, o));
+    sum.hi = s.hi, sum.lo += s.lo + __shfl_xor_sync(0xffffffffu, sum.lo, o);
+  }
+  if (__any_sync(0xffffffffu, far)) return far_normaliser(part, blocks);
+  return sum.hi > 0.f && sum.hi < INFINITY ? ln(two_sum(sum.hi, sum.lo), static_cast<int>(exponent)) : Two{NAN, NAN};
+}
+
+// The blocks of a sequence, and the beams that have ended, which are blocks of one.
+struct Blocks {
+  const BeamLaunch& L;
+  const MergeShared& s;
+  const float2* part;               // of the sequence
+  int row0;
+  __device__ __forceinline__ int beam(int id) const { return L.blocks == 1 ? id : static_cast<int>(__umulhi(id, L.inverse_blocks)); }
+  // What block `id` has at most, its maximum being x.
+  __device__ __forceinline__ Key key(int id, float x) const {
+    const int k = beam(id);
+    const Two offset = s.offset[k];
+    if (offset.hi == offset.hi) return x > -INFINITY ? order_key(add(offset, x)) : 0;
+    return id == k * static_cast<int>(L.blocks) ? ended(k) : 0;
+  }
+  __device__ __forceinline__ Key ended(int k) const {
+    const float score = s.ended_score[k];
+    return score == score ? order_key({score, 0.f}) : 0;
+  }
+};
+
+// The chosen blocks' continuations of `least` and above, a warp to a block. Vectors that hold one are few: they are
+// found by their maxima and read again.
+template <class T, class F>
+__device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key least, F&& take) {
+  constexpr int N = Vec<T>::N;
+  const BeamLaunch& L = all.L;
+  const float value = value_of(least);
+  for (int r = threadIdx.x >> 5; r < chosen; r += kMergeWarps) {
+    const int id = all.s.chosen[r], k = all.beam(id);
+    const Two offset = all.s.offset[k];
+    if (!(offset.hi == offset.hi)) {
+      const Key key = all.ended(k);
+      if ((threadIdx.x & 31) == 0 && key >= least) take(Place{key, rest_of(k, 0.f, L.pad)});
+      continue;
+    }
+    const Row<T> row(L, all.row0 + k);
+    // A logit below this is not of `least`, which the two roundings leave in doubt by less than 2^-22 of either.
+    const float lowest = least > 1 ? value - offset.hi - (fabsf(value) + fabsf(offset.hi)) * 0x1p-20f : -INFINITY;
+    const int first = (id - k * L.blocks) * L.block_vectors, end = min(first + L.block_vectors, L.row_vectors);
+    for (int at = first; at < end; at += kChunk) {
+      uint4 w[kPerLane];
+      row.template load<false>(w, at, L.vocab);
+      unsigned held = 0;
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) held |= Vec<T>::highest(w[i]) >= lowest ? 1u << i : 0u;
+      for (; held; held &= held - 1) {
+        const int i = __ffs(held) - 1, t0 = row.token(at, i, 0);
+        const uint4 again = row.vector(at + (static_cast<int>(threadIdx.x) & 31) + i * 32, L.vocab);
+        float x[N];
+        Vec<T>::unpack(again, x);
+        unsigned takes = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) takes |= x[e] >= lowest && x[e] > -INFINITY ? 1u << e : 0u;
+        for (; takes; takes &= takes - 1) {
+          const int t = t0 + __ffs(takes) - 1;
+          const float y = row.element(t);
+          const Key key = order_key(add(offset, y));
+          if (key >= least) take(Place{key, rest_of(k, y, t)});
+        }
       }
     }
-  __syncthreads();
-  auto put = [&](int rank, double x, int f) {
-    const int64_t at = static_cast<int64_t>(b) * L.n + rank;
-    const bool some = x > -INFINITY;
-    const int k = some ? f / L.vocab : -1, v = some ? f - k * L.vocab : -1;
-    L.score_out[at] = static_cast<float>(x);
-    L.parent[at] = k;
-    L.token[at] = v;
-    if (L.ended_out) L.ended_out[at] = !some || v == L.eos || (L.finished && __ldg(L.finished + b * L.beams + k)) ? 1 : 0;
-  };
-  const int found = count;
-  if (found <= kMergeList) {
-    for (int i = tid; i < found; i += kMergeThreads) {
-      const double x = list_value[i];
-      const int f = list_flat[i];
-      int rank = 0;
-      for (int j = 0; j < found; ++j) rank += before(list_value[j], list_flat[j], x, f) ? 1 : 0;
-      if (rank < L.n) put(rank, x, f);
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __grid_constant__ BeamLaunch L) {
+  __shared__ MergeShared s;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const Blocks all{L, s, L.part + static_cast<int64_t>(b) * L.beams * L.blocks, b * L.beams};
+  if (tid == 0) s.count = s.listed = 0;
+  ptx::grid_wait();
+  ptx::grid_launch_next();
+  // Each row's normaliser, by a warp; the first blocks' maxima on their way meanwhile.
+  const int ids = L.beams * L.blocks;
+  float first[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int id = tid + i * kMergeThreads;
+    first[i] = id < ids ? all.part[id].x : -INFINITY;              // (of ended beams not used)
+  }
+  for (int k = warp; k < L.beams; k += kMergeWarps) {
+    const int ended = L.finished ? __ldg(L.finished + all.row0 + k) : 0;
+    const float score = L.scores ? __ldg(L.scores + all.row0 + k) : 0.f;
+    const bool live = ended == 0 && isfinite(score);
+    const Two lse = live ? normaliser(all.part + k * static_cast<int64_t>(L.blocks), L.blocks) : Two{NAN, NAN};
+    if (lane == 0) {
+      s.offset[k] = add({-lse.hi, -lse.lo}, score);
+      s.ended_score[k] = ended && isfinite(score) ? score : NAN;
+      s.ended[k] = ended ? 1 : 0;
     }
-    for (int i = found + tid; i < L.n; i += kMergeThreads) put(i, -INFINITY, 0);
+  }
+  __syncthreads();
+
+  // The n highest blocks.
+  Key held[kHeld], best = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int id = tid + i * kMergeThreads;
+    held[i] = id < ids ? all.key(id, first[i]) : 0;
+    best = max(best, held[i]);
+  }
+  for (int id = tid + kHeld * kMergeThreads; id < ids; id += kMergeThreads) best = max(best, all.key(id, all.part[id].x));
+  const Key bound = max(static_cast<Key>(bound_of<kMergeThreads>(static_cast<uint32_t>(best >> 32), s.group_max, &s.bound, L.n, groups_for(L.n))) << 32, Key(1));
+  if (best >= bound) {
+    auto list = [&](int id, Key key) {
+      if (key < bound) return;
+      const int to = atomicAdd(&s.listed, 1);
+      if (to < kList) s.listed_value[to] = key, s.id[to] = id;
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) list(tid + i * kMergeThreads, held[i]);
+    for (int id = tid + kHeld * kMergeThreads; id < ids; id += kMergeThreads) list(id, all.key(id, all.part[id].x));
+  }
+  __syncthreads();
+  const int listed = s.listed, chosen = min(listed, L.n);
+  if (listed <= kList) {
+    for (int i = tid; i < listed; i += kMergeThreads) {
+      const Key key = s.listed_value[i];
+      const int id = s.id[i];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < listed; ++j) rank += before(s.listed_value[j], s.id[j], key, id) ? 1 : 0;
+      if (rank < L.n) s.chosen[rank] = id;
+      if (rank == L.n - 1) s.least = key;
+    }
+  } else {
+    // Many as high as one another: the next one after the last, n times.
+    Key last = ~Key(0);
+    int last_id = -1;
+    for (int r = 0; r < L.n; ++r) {
+      Key y = 0;
+      int f = 0x7fffffff;
+      for (int i = tid; i < ids; i += kMergeThreads) {
+        const Key key = all.key(i, all.part[i].x);
+        if (key >= bound && before(last, last_id, key, i) && before(key, i, y, f)) y = key, f = i;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const Key z = __shfl_xor_sync(0xffffffffu, y, o);
+        const int g = __shfl_xor_sync(0xffffffffu, f, o);
+        if (before(z, g, y, f)) y = z, f = g;
+      }
+      if (lane == 0) s.warp_value[warp] = y, s.warp_rest[warp] = f;
+      __syncthreads();
+      for (int i = 0; i < kMergeWarps; ++i)
+        if (before(s.warp_value[i], static_cast<int>(s.warp_rest[i]), y, f)) y = s.warp_value[i], f = static_cast<int>(s.warp_rest[i]);
+      last = y, last_id = f;
+      if (tid == 0) s.chosen[r] = f, s.least = y;
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+
+  // Their continuations down to the n-th block's highest.
+  const Key least = listed >= L.n ? s.least : Key(1);
+  read_chosen<T>(all, chosen, least, [&](Place p) {
+    const int to = atomicAdd(&s.count, 1);
+    if (to < kList) s.value[to] = p.value, s.rest[to] = p.rest;
+  });
+  __syncthreads();
+  auto put = [&](int rank, Place p) {
+    const int64_t to = static_cast<int64_t>(b) * L.n + rank;
+    const int k = p.value ? beam_of(p.rest) : -1, v = p.value ? token_of(p.rest) : -1;
+    L.score_out[to] = value_of(p.value);
+    L.parent[to] = k;
+    L.token[to] = v;
+    if (L.ended_out) L.ended_out[to] = !p.value || v == L.eos || s.ended[k] ? 1 : 0;
+  };
+  const int count = s.count;
+  if (count <= kList) {
+    for (int i = tid; i < count; i += kMergeThreads) {
+      const Place p{s.value[i], s.rest[i]};
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < count; ++j) rank += Place{s.value[j], s.rest[j]} > p ? 1 : 0;
+      if (rank < L.n) put(rank, p);
+    }
+    for (int i = count + tid; i < L.n; i += kMergeThreads) put(i, {0, 0});
     return;
   }
-  double last = INFINITY;
-  int last_flat = -1;
+  Place last{~Key(0), ~Key(0)};
   for (int r = 0; r < L.n; ++r) {
-    double x_best = -INFINITY;
-    int f_best = 0x7fffffff;
-    for (int i = tid; i < total; i += kMergeThreads) {
-      double x;
-      int f;
-      c.get(i, x, f);
-      if (x > -INFINITY && before(last, last_flat, x, f) && before(x, f, x_best, f_best)) x_best = x, f_best = f;
-    }
+    Place y{0, 0};
+    read_chosen<T>(all, chosen, least, [&](Place p) {
+      if (last > p && p > y) y = p;
+    });
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      const double y = __shfl_xor_sync(0xffffffffu, x_best, o);
-      const int yf = __shfl_xor_sync(0xffffffffu, f_best, o);
-      if (before(y, yf, x_best, f_best)) x_best = y, f_best = yf;
+      const Place z{__shfl_xor_sync(0xffffffffu, y.value, o), __shfl_xor_sync(0xffffffffu, y.rest, o)};
+      if (z > y) y = z;
     }
+    if (lane == 0) s.warp_value[warp] = y.value, s.warp_rest[warp] = y.rest;
     __syncthreads();
-    if (lane == 0) list_value[warp] = x_best, list_flat[warp] = f_best;
+    for (int i = 0; i < kMergeWarps; ++i) {
+      const Place z{s.warp_value[i], s.warp_rest[i]};
+      if (z > y) y = z;
+    }
+    last = y;
+    if (tid == 0) put(r, y);
     __syncthreads();
-    for (int i = 0; i < kMergeWarps; ++i)
-      if (before(list_value[i], list_flat[i], x_best, f_best)) x_best = list_value[i], f_best = list_flat[i];
-    last = x_best, last_flat = f_best;
-    if (tid == 0) put(r, x_best, f_best);
   }
 }
 
 template <class T>
 cudaError_t launch_t(const BeamLaunch& L, cudaStream_t stream) {
-  const cudaError_t e = launch_after(beam_scan_kernel<T>, dim3(L.splits, L.batch * L.beams), kThreads, 0, stream, L);
-  return e != cudaSuccess ? e : launch_after(beam_merge_kernel, dim3(L.batch), kMergeThreads, 0, stream, L);
+  const cudaError_t e = launch_after(beam_scan_kernel<T>, dim3(L.ctas), kThreads, 0, stream, L);
+  return e != cudaSuccess ? e : launch_after(beam_choice_kernel<T>, dim3(L.batch), kMergeThreads, 0, stream, L);
 }
 
 }  // namespace
 
-BeamSplit beam_split(int64_t rows, int vocab, int dtype, int n_sm) {
+BeamSplit beam_split(int64_t rows, int beams, int vocab, int dtype, int n_sm) {
   const int per = dtype == 2 ? 4 : 8;
-  const int vectors = (vocab + per - 1) / per + 1;               // (a row may begin inside one)
-  const int most = kThreads * kPerThread;
-  int64_t each = (rows * vectors + 2 * n_sm - 1) / (2 * n_sm);   // two CTAs to an SM, where rows are few
-  each = std::max<int64_t>(kThreads, std::min<int64_t>(most, (each + kThreads - 1) / kThreads * kThreads));
   BeamSplit s;
-  s.splits = static_cast<int>((vectors + each - 1) / each);
-  s.part_vectors = (vectors + s.splits - 1) / s.splits;
+  s.row_vectors = (vocab + per - 1) / per + 1;   // (a row may begin inside one)
+  s.block_vectors = kChunk;
+  while (static_cast<int64_t>(beams) * s.row_vectors > static_cast<int64_t>(kMostBlocks) * s.block_vectors) s.block_vectors *= 2;
+  s.blocks = (s.row_vectors + s.block_vectors - 1) / s.block_vectors;
+  const int64_t most = static_cast<int64_t>(n_sm) * kPerSm;
+  s.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, (rows * s.blocks + kWarps - 1) / kWarps)));
   return s;
 }
 

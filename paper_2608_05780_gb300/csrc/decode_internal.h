@@ -53,12 +53,11 @@ struct BeamLaunch {
   int32_t* parent;
   int32_t* token;
   uint8_t* ended_out;
-  double* part_sum;                 // [rows, splits]: sum of exp(x - part_max)
-  float* part_max;                  // [rows, splits]
-  float* part_value;                // [rows, splits, n]: descending, -inf past the end
-  int32_t* part_index;              // [rows, splits, n]: token
+  float2* part;                     // [rows, blocks]: maximum, sum of exponentials
   int batch, beams, vocab, n, dtype, pad, eos;
-  int splits, part_vectors;         // a row is cut into `splits` parts of part_vectors 16-byte vectors
+  int row_vectors, block_vectors, ctas;   // as BeamSplit's
+  unsigned blocks, total;                            // of a row, of all rows
+  unsigned inverse_blocks;                           // 2^32 / blocks, rounded up: i / blocks = umulhi(i, inverse_blocks)
 };
 
 constexpr int kMaxStates = 8;
@@ -80,11 +79,11 @@ struct ReorderLaunch {
   int chunks[kMaxStates];           // blocks of a row
 };
 
-// A row of logits cut into parts: enough for the SMs, none larger than a CTA's registers hold.
+// A row of row_vectors 16-byte vectors as `blocks` blocks of block_vectors, which the warps of `ctas` CTAs take in turn.
 struct BeamSplit {
-  int splits, part_vectors;
+  int row_vectors, block_vectors, blocks, ctas;
 };
-BeamSplit beam_split(int64_t rows, int vocab, int dtype, int n_sm);
+BeamSplit beam_split(int64_t rows, int beams, int vocab, int dtype, int n_sm);
 
 cudaError_t launch_rotary(const RotaryLaunch& L, cudaStream_t stream);
 cudaError_t launch_append_rotary(const AppendRotaryLaunch& L, cudaStream_t stream);

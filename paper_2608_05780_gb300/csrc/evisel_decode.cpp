@@ -270,7 +270,8 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
     if (!m.logits || !score_out || !parent || !token) return fail(EVISEL_EINVAL, "logits or an output is NULL");
     if (misaligned(m.logits, size) || misaligned(m.scores, 4) || misaligned(score_out, 4) || misaligned(parent, 4) || misaligned(token, 4))
       return fail(EVISEL_EINVAL, "logits, scores and outputs must be aligned to their elements");
-    if (m.logits_stride[0] < 0 || m.logits_stride[1] < 0) return fail(EVISEL_EINVAL, "logits strides must not be negative");
+    if (m.logits_stride[0] < 0 || m.logits_stride[1] < 0 || std::max(m.logits_stride[0], m.logits_stride[1]) >= kMaxStride)
+      return fail(EVISEL_EINVAL, "logits strides must be 0 to below 2^38");
     const int64_t n = static_cast<int64_t>(m.batch) * m.n_out;
     // Other sequences' blocks still read the scores and flags.
     for (const Range& out : {range_of(score_out, 4 * n), range_of(parent, 4 * n), range_of(token, 4 * n), range_of(ended_out, n)})
@@ -278,15 +279,13 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
         return fail(EVISEL_EINVAL, "an output lies over scores or finished");
     const int n_sm = sm_count();
     if (n_sm <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
-    const BeamSplit split = beam_split(rows, m.vocab, m.dtype, n_sm);
-    const size_t parts = static_cast<size_t>(rows) * split.splits;
-    const size_t sums = align_up(parts * sizeof(double), 256), tops = align_up(parts * sizeof(float), 256),
-                 picks = align_up(parts * m.n_out * sizeof(float), 256);
+    const BeamSplit split = beam_split(rows, m.beams, m.vocab, m.dtype, n_sm);
+    if (rows > 0x7fffffff / split.blocks) return fail(EVISEL_EUNSUPPORTED, "batch * beams * vocab is beyond the blocks that are counted in 31 bits");
+    const size_t parts = static_cast<size_t>(rows) * split.blocks;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     int rc = acquire(ws_inout, stream);
-    if (rc == EVISEL_OK) rc = grow(*ws_inout, sums + tops + 2 * picks, stream);
+    if (rc == EVISEL_OK) rc = grow(*ws_inout, parts * sizeof(float2), stream);
     if (rc != EVISEL_OK) return rc;
-    char* buf = static_cast<char*>(ws_cache(*ws_inout).buf);
     BeamLaunch L{};
     L.logits = m.logits;
     L.ls[0] = m.logits_stride[0];
@@ -297,10 +296,7 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
     L.parent = parent;
     L.token = token;
     L.ended_out = ended_out;
-    L.part_sum = reinterpret_cast<double*>(buf);
-    L.part_max = reinterpret_cast<float*>(buf + sums);
-    L.part_value = reinterpret_cast<float*>(buf + sums + tops);
-    L.part_index = reinterpret_cast<int32_t*>(buf + sums + tops + picks);
+    L.part = static_cast<float2*>(ws_cache(*ws_inout).buf);
     L.batch = m.batch;
     L.beams = m.beams;
     L.vocab = m.vocab;
@@ -308,8 +304,12 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
     L.dtype = m.dtype;
     L.pad = m.pad;
     L.eos = m.eos;
-    L.splits = split.splits;
-    L.part_vectors = split.part_vectors;
+    L.row_vectors = split.row_vectors;
+    L.block_vectors = split.block_vectors;
+    L.ctas = split.ctas;
+    L.blocks = split.blocks;
+    L.total = static_cast<unsigned>(parts);
+    L.inverse_blocks = static_cast<unsigned>(((uint64_t(1) << 32) + split.blocks - 1) / split.blocks);
     const cudaError_t e = launch_beams(L, stream);
     if (e != cudaSuccess) return cuda_fail(e, "beam selection launch");
     ws_ran_on(*ws_inout, stream);
