@@ -14,8 +14,9 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32, kPerSm = 2;
 constexpr int kPerLane = 4;                      // 16-byte vectors of a lane's chunk; the next chunk is in flight
-constexpr int kChunk = 32 * kPerLane;
-constexpr int kMostBlocks = 4096;                // of a sequence, about
+constexpr int kChunkShift = 7, kChunk = 32 * kPerLane;
+static_assert(kChunk == 1 << kChunkShift);
+constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLog2eLow = 1.925963033500e-8f;  // log2 e - kLog2e
 
@@ -179,9 +180,8 @@ struct Row {
   const uint4* vectors;
   int skew;                         // elements of the first vector before the row
   Row() = default;
-  __device__ __forceinline__ Row(const BeamLaunch& L, int row) {
+  __device__ __forceinline__ Row(const BeamLaunch& L, int b, int k) {
     constexpr int kSize = 16 / N;
-    const int b = row / L.beams, k = row - b * L.beams;
     const char* base = static_cast<const char*>(L.logits) + (b * L.ls[0] + k * L.ls[1]) * kSize;
     skew = static_cast<int>((reinterpret_cast<uintptr_t>(base) & 15) / kSize);
     vectors = reinterpret_cast<const uint4*>(base - skew * kSize);
@@ -191,10 +191,11 @@ struct Row {
     if (v * N >= skew && (v + 1) * N <= skew + vocab) return __ldg(vectors + v);
     return Vec<T>::load_some(vectors + v, skew - v * N, skew + vocab - v * N);
   }
+  __device__ __forceinline__ int vectors_of(int vocab) const { return (skew + vocab + N - 1) / N; }
   // The chunk at vector `at`, -inf beside the row; kOnce: nothing of it is read again by this SM.
   template <bool kOnce>
   __device__ __forceinline__ void load(uint4 (&w)[kPerLane], int at, int vocab) const {
-    const int lane = threadIdx.x & 31, inner0 = skew > 0 ? 1 : 0, inner1 = (skew + vocab) / N, last = (skew + vocab + N - 1) / N;
+    const int lane = threadIdx.x & 31, inner0 = skew > 0 ? 1 : 0, inner1 = (skew + vocab) / N, last = vectors_of(vocab);
     if (at >= inner0 && at + kChunk <= inner1) {
 #pragma unroll
       for (int i = 0; i < kPerLane; ++i) w[i] = kOnce ? load_once(vectors + at + lane + i * 32) : __ldg(vectors + at + lane + i * 32);
@@ -207,26 +208,33 @@ struct Row {
     }
   }
   __device__ __forceinline__ float element(int token) const { return Vec<T>::element(vectors, token + skew); }
-  __device__ __forceinline__ int token(int at, int i, int e) const {
-    return (at + static_cast<int>(threadIdx.x & 31) + i * 32) * N + e - skew;
-  }
 };
 
 template <class T>
 __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __grid_constant__ BeamLaunch L) {
-  const unsigned step = gridDim.x * kWarps;
-  unsigned u = blockIdx.x * kWarps + (threadIdx.x >> 5);           // a block of all rows' blocks
+  // A block of all rows' blocks, and where it lies: sequence b, beam k, block j. (Counted on without divisions, which
+  // would cost as much as the exponentials.)
+  unsigned u = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const unsigned r = u / L.blocks;
+  int j = u - r * L.blocks, b = r / L.beams, k = r - b * L.beams;
   ptx::grid_wait();
   ptx::grid_launch_next();
   Row<T> row;
   int at = 0, end = 0;
-  // The next block that is to be read.
+  // The block, or the next one after it, that is to be read.
+  auto advance = [&]() {
+    u += L.step;
+    j += L.step_block;
+    k += L.step_beam;
+    b += L.step_batch;
+    if (j >= static_cast<int>(L.blocks)) j -= L.blocks, ++k;
+    if (k >= L.beams) k -= L.beams, ++b;         // (k was below beams and grew by beams at most)
+  };
   auto find = [&]() {
-    for (; u < L.total; u += step) {
-      const int r = static_cast<int>(u / L.blocks);
-      if (!beam_is_live(L, r)) continue;
-      row = Row<T>(L, r);
-      at = (u - r * L.blocks) * L.block_vectors;
+    for (; u < L.total; advance()) {
+      if (!beam_is_live(L, b * L.beams + k)) continue;
+      row = Row<T>(L, b, k);
+      at = j * L.block_vectors;
       end = min(at + L.block_vectors, L.row_vectors);
       return true;
     }
@@ -246,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __gri
       at += kChunk;
       row.template load<true>(next, at, L.vocab);
     } else {
-      u += step;
+      advance();
       if ((more = find())) row.template load<true>(next, at, L.vocab);
     }
     const float highest = warp_max(Vec<T>::highest(w));
@@ -274,7 +282,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __gri
 
 // ---------------------------------------------------------------- the choice
 constexpr int kMergeThreads = 512, kMergeWarps = kMergeThreads / 32;
-constexpr int kList = 512;
+constexpr int kList = 1024;                      // a chunk, at which the threads' maxima may bound nothing
+constexpr int kRanked = 160;                     // entries that are ranked by comparing all with all as they are
 constexpr int kHeld = 4;                         // blocks of a thread that stay in registers
 
 // A value of 48 bits as the sum of two floats, the second at most half a step of the first.
@@ -334,7 +343,7 @@ struct MergeShared {
   float ended_score[kMaxBeams];                  // of a beam that has ended; NaN: it has not, or has none
   Key listed_value[kList], value[kList], rest[kList];
   int id[kList], chosen[kMaxBeamsOut];           // blocks
-  uint32_t group_max[256], bound;
+  uint32_t group_max[kMergeThreads], bound;
   Key least, warp_value[kMergeWarps], warp_rest[kMergeWarps];
   int listed, count;
   uint8_t ended[kMaxBeams];
@@ -416,45 +425,43 @@ struct Blocks {
   }
 };
 
-// The chosen blocks' continuations of `least` and above, a warp to a block. Vectors that hold one are few: they are
+// The chosen blocks' continuations of `least` and above, a warp to a chunk. Vectors that hold one are few: they are
 // found by their maxima and read again.
 template <class T, class F>
 __device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key least, F&& take) {
   constexpr int N = Vec<T>::N;
   const BeamLaunch& L = all.L;
+  const int lane = threadIdx.x & 31, shift = L.block_shift - kChunkShift;
   const float value = value_of(least);
-  for (int r = threadIdx.x >> 5; r < chosen; r += kMergeWarps) {
-    const int id = all.s.chosen[r], k = all.beam(id);
+  for (int u = threadIdx.x >> 5; u < chosen << shift; u += kMergeWarps) {
+    const int r = u >> shift, id = all.s.chosen[r], k = all.beam(id);
     const Two offset = all.s.offset[k];
-    if (!(offset.hi == offset.hi)) {
+    if (!(offset.hi == offset.hi)) {             // a beam that has ended
       const Key key = all.ended(k);
-      if ((threadIdx.x & 31) == 0 && key >= least) take(Place{key, rest_of(k, 0.f, L.pad)});
+      if (lane == 0 && u == r << shift && key >= least) take(Place{key, rest_of(k, 0.f, L.pad)});
       continue;
     }
-    const Row<T> row(L, all.row0 + k);
     // A logit below this is not of `least`, which the two roundings leave in doubt by less than 2^-22 of either.
-    const float lowest = least > 1 ? value - offset.hi - (fabsf(value) + fabsf(offset.hi)) * 0x1p-20f : -INFINITY;
-    const int first = (id - k * L.blocks) * L.block_vectors, end = min(first + L.block_vectors, L.row_vectors);
-    for (int at = first; at < end; at += kChunk) {
-      uint4 w[kPerLane];
-      row.template load<false>(w, at, L.vocab);
-      unsigned held = 0;
+    const float lowest = least > 1 ? value - offset.hi - (fabsf(value) + fabsf(offset.hi)) * 0x1p-20f : kLowest;
+    const Row<T> row(L, blockIdx.x, k);
+    const int at = ((id - k * static_cast<int>(L.blocks)) << L.block_shift) + ((u - (r << shift)) << kChunkShift);
+    uint4 w[kPerLane];
+    row.template load<false>(w, at, L.vocab);
+    unsigned held = 0;
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) held |= Vec<T>::highest(w[i]) >= lowest ? 1u << i : 0u;
-      for (; held; held &= held - 1) {
-        const int i = __ffs(held) - 1, t0 = row.token(at, i, 0);
-        const uint4 again = row.vector(at + (static_cast<int>(threadIdx.x) & 31) + i * 32, L.vocab);
-        float x[N];
-        Vec<T>::unpack(again, x);
-        unsigned takes = 0;
+    for (int i = 0; i < kPerLane; ++i) held |= Vec<T>::highest(w[i]) >= lowest ? 1u << i : 0u;
+    for (; held; held &= held - 1) {
+      const int v = at + lane + (__ffs(held) - 1) * 32;
+      float x[N];
+      Vec<T>::unpack(row.vector(v, L.vocab), x);
+      unsigned takes = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e) takes |= x[e] >= lowest && x[e] > -INFINITY ? 1u << e : 0u;
-        for (; takes; takes &= takes - 1) {
-          const int t = t0 + __ffs(takes) - 1;
-          const float y = row.element(t);
-          const Key key = order_key(add(offset, y));
-          if (key >= least) take(Place{key, rest_of(k, y, t)});
-        }
+      for (int e = 0; e < N; ++e) takes |= x[e] >= lowest ? 1u << e : 0u;
+      for (; takes; takes &= takes - 1) {
+        const int t = v * N - row.skew + __ffs(takes) - 1;
+        const float y = row.element(t);
+        const Key key = order_key(add(offset, y));
+        if (key >= least) take(Place{key, rest_of(k, y, t)});
       }
     }
   }
@@ -549,13 +556,26 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
   }
   __syncthreads();
 
-  // Their continuations down to the n-th block's highest.
-  const Key least = listed >= L.n ? s.least : Key(1);
-  read_chosen<T>(all, chosen, least, [&](Place p) {
-    const int to = atomicAdd(&s.count, 1);
-    if (to < kList) s.value[to] = p.value, s.rest[to] = p.rest;
-  });
-  __syncthreads();
+  // Their continuations down to the n-th block's highest; where those are too many, or blocks too few, down to a bound
+  // from the continuations themselves.
+  Key least = listed >= L.n ? s.least : Key(1);
+  for (int tries = listed >= L.n ? 0 : 1;; ++tries) {
+    if (tries == 1) {
+      best = 0;
+      read_chosen<T>(all, chosen, least, [&](Place p) { best = max(best, p.value); });
+      const uint32_t high = bound_of<kMergeThreads>(static_cast<uint32_t>(best >> 32), s.group_max, &s.bound, L.n, kMergeThreads);
+      least = max(least, static_cast<Key>(high) << 32);
+      if (tid == 0) s.count = 0;
+      __syncthreads();
+    }
+    read_chosen<T>(all, chosen, least, [&](Place p) {
+      const int to = atomicAdd(&s.count, 1);
+      if (to < kList) s.value[to] = p.value, s.rest[to] = p.rest;
+    });
+    __syncthreads();
+    if (s.count <= kList || tries > 0) break;
+    __syncthreads();
+  }
   auto put = [&](int rank, Place p) {
     const int64_t to = static_cast<int64_t>(b) * L.n + rank;
     const int k = p.value ? beam_of(p.rest) : -1, v = p.value ? token_of(p.rest) : -1;
@@ -564,8 +584,30 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
     L.token[to] = v;
     if (L.ended_out) L.ended_out[to] = !p.value || v == L.eos || s.ended[k] ? 1 : 0;
   };
-  const int count = s.count;
+  int count = s.count;
   if (count <= kList) {
+    if (count > kRanked) {          // few of them, by a bound from the list itself
+      constexpr int kOwn = kList / kMergeThreads;
+      Place own[kOwn];
+      best = 0;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        const int j = tid + i * kMergeThreads;
+        own[i] = j < count ? Place{s.value[j], s.rest[j]} : Place{0, 0};
+        best = max(best, own[i].value);
+      }
+      const uint32_t high = bound_of<kMergeThreads>(static_cast<uint32_t>(best >> 32), s.group_max, &s.bound, L.n, kMergeThreads);
+      if (tid == 0) s.count = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i)
+        if (own[i].value >> 32 >= high && own[i].value > 0) {
+          const int to = atomicAdd(&s.count, 1);
+          s.value[to] = own[i].value, s.rest[to] = own[i].rest;
+        }
+      __syncthreads();
+      count = s.count;
+    }
     for (int i = tid; i < count; i += kMergeThreads) {
       const Place p{s.value[i], s.rest[i]};
       int rank = 0;
@@ -607,15 +649,20 @@ cudaError_t launch_t(const BeamLaunch& L, cudaStream_t stream) {
 
 }  // namespace
 
-BeamSplit beam_split(int64_t rows, int beams, int vocab, int dtype, int n_sm) {
+BeamSplit beam_split(int64_t rows, int beams, int vocab, int n, int dtype, int n_sm) {
   const int per = dtype == 2 ? 4 : 8;
   BeamSplit s;
   s.row_vectors = (vocab + per - 1) / per + 1;   // (a row may begin inside one)
-  s.block_vectors = kChunk;
-  while (static_cast<int64_t>(beams) * s.row_vectors > static_cast<int64_t>(kMostBlocks) * s.block_vectors) s.block_vectors *= 2;
+  // As many bytes of maxima as of chosen blocks to read, within the powers of two: block^2 = 2 beams vocab / n.
+  for (s.block_shift = kChunkShift; s.block_shift < 14; ++s.block_shift) {
+    const int64_t block = static_cast<int64_t>(per) << s.block_shift;
+    if (block * block * n >= 2 * static_cast<int64_t>(beams) * vocab) break;
+  }
+  s.block_vectors = 1 << s.block_shift;
   s.blocks = (s.row_vectors + s.block_vectors - 1) / s.block_vectors;
   const int64_t most = static_cast<int64_t>(n_sm) * kPerSm;
   s.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, (rows * s.blocks + kWarps - 1) / kWarps)));
+  s.warps = s.ctas * kWarps;
   return s;
 }
 

@@ -55,8 +55,10 @@ struct BeamLaunch {
   uint8_t* ended_out;
   float2* part;                     // [rows, blocks]: maximum, sum of exponentials
   int batch, beams, vocab, n, dtype, pad, eos;
-  int row_vectors, block_vectors, ctas;   // as BeamSplit's
+  int row_vectors, block_vectors, block_shift, ctas;   // as BeamSplit's
   unsigned blocks, total;                            // of a row, of all rows
+  unsigned step;                                     // warps: step_batch sequences, step_beam beams and step_block blocks
+  int step_batch, step_beam, step_block;
   unsigned inverse_blocks;                           // 2^32 / blocks, rounded up: i / blocks = umulhi(i, inverse_blocks)
 };
 
@@ -79,11 +81,11 @@ struct ReorderLaunch {
   int chunks[kMaxStates];           // blocks of a row
 };
 
-// A row of row_vectors 16-byte vectors as `blocks` blocks of block_vectors, which the warps of `ctas` CTAs take in turn.
+// A row of row_vectors 16-byte vectors as `blocks` blocks of block_vectors, which `warps` warps of `ctas` CTAs take in turn.
 struct BeamSplit {
-  int row_vectors, block_vectors, blocks, ctas;
+  int row_vectors, block_vectors, block_shift, blocks, ctas, warps;   // block_vectors = 1 << block_shift
 };
-BeamSplit beam_split(int64_t rows, int beams, int vocab, int dtype, int n_sm);
+BeamSplit beam_split(int64_t rows, int beams, int vocab, int n, int dtype, int n_sm);
 
 cudaError_t launch_rotary(const RotaryLaunch& L, cudaStream_t stream);
 cudaError_t launch_append_rotary(const AppendRotaryLaunch& L, cudaStream_t stream);

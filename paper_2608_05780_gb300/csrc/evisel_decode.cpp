@@ -279,7 +279,7 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
         return fail(EVISEL_EINVAL, "an output lies over scores or finished");
     const int n_sm = sm_count();
     if (n_sm <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
-    const BeamSplit split = beam_split(rows, m.beams, m.vocab, m.dtype, n_sm);
+    const BeamSplit split = beam_split(rows, m.beams, m.vocab, m.n_out, m.dtype, n_sm);
     if (rows > 0x7fffffff / split.blocks) return fail(EVISEL_EUNSUPPORTED, "batch * beams * vocab is beyond the blocks that are counted in 31 bits");
     const size_t parts = static_cast<size_t>(rows) * split.blocks;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
@@ -306,8 +306,13 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
     L.eos = m.eos;
     L.row_vectors = split.row_vectors;
     L.block_vectors = split.block_vectors;
+    L.block_shift = split.block_shift;
     L.ctas = split.ctas;
     L.blocks = split.blocks;
+    L.step = split.warps;
+    L.step_block = split.warps % split.blocks;
+    L.step_beam = split.warps / split.blocks % m.beams;
+    L.step_batch = split.warps / split.blocks / m.beams;
     L.total = static_cast<unsigned>(parts);
     L.inverse_blocks = static_cast<unsigned>(((uint64_t(1) << 32) + split.blocks - 1) / split.blocks);
     const cudaError_t e = launch_beams(L, stream);
