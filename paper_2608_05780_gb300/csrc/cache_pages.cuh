@@ -38,11 +38,12 @@ struct NewTokens {
     }
     return i;
   }
-  __device__ __forceinline__ const uint4* key(int i) const {
-    return reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.k_new) + b * L.d.kns[0] + i * L.d.kns[1] + h * L.d.kns[2]);
+  // The token's key and value, of the head or one behind it.
+  __device__ __forceinline__ const uint4* key(int i, int behind = 0) const {
+    return reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.k_new) + b * L.d.kns[0] + i * L.d.kns[1] + (h + behind) * L.d.kns[2]);
   }
-  __device__ __forceinline__ const uint4* value(int i) const {
-    return reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.v_new) + b * L.d.vns[0] + i * L.d.vns[1] + h * L.d.vns[2]);
+  __device__ __forceinline__ const uint4* value(int i, int behind = 0) const {
+    return reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(L.d.v_new) + b * L.d.vns[0] + i * L.d.vns[1] + (h + behind) * L.d.vns[2]);
   }
   __device__ __forceinline__ void rows(int pos, const uint4*& k, const uint4*& v) const {
     const int i = token(pos);

@@ -4,7 +4,7 @@ rotated append, beam selection, reordering, and a run of them together.
 Bounds, u the rounding of the 16-bit type (2^-8 bf16, 2^-11 fp16):
 
   rotation  the angle comes from 32 bits of a turn that is exact modulo 1 up to |p| 2^-51 turns, rounded to fp32 (2^-25 of
-            a half turn: 2^-23.3 radians); sincospif adds 2^-23, the scale 2^-24, two products and a sum 2^-23:
+            a half turn: 2^-23.3 radians); sine and cosine add 2^-24, the scale 2^-24, two products and a sum 2^-23:
             (2^-21 + |p| 2^-48) (|x1| + |x2|) + u |y|, and 2^-25 for fp16's smallest numbers
   beams     exponentials off by 2^-22 + 2^-23 |x - max| relative, of which ln V covers the mean over the row; up to 64
             of them added in fp32 by one thread, 2^-18 relative at worst; the rest in 64 bits. value: 2^-18 + 2^-22 +
@@ -280,6 +280,64 @@ def test_rotated_append_checks_device_memory(cuda_lib):
         mine = torch.zeros(cache.k.shape[0], dtype=torch.bool, device="cuda")
         mine[owned] = True
         assert torch.equal(cache.k[~mine], before[~mine]), what
+
+
+@pytest.mark.parametrize("dtype,layout,d,page,interleaved,r", [
+    ("bf16", "nhd", 128, 16, False, 128), ("fp16", "hnd", 64, 16, True, 48), ("bf16", "hnd", 128, 64, True, 128)])
+def test_rotated_append_of_many_pages(cuda_lib, dtype, layout, d, page, interleaved, r):
+    """As many pages as the kernel needs to take two heads at a time: keys, values and means as from single heads; pages that
+    are none of the pool leave everything else as it is."""
+    import torch
+    ev, rng, dtype = cuda_lib, np.random.default_rng(page + d), _types()[dtype]
+    tokens, hkv = 480 * page + 5, 4
+    rope = ev.Rotary(d, r, interleaved=interleaved)
+    (k, _), (v, _) = (tensor(rng, (1, tokens, hkv, d), dtype) for _ in range(2))
+    cache, _ = make_cache(rng, [page + 3], hkv, d, page, dtype, layout, room=tokens, mean=True, poison=False)
+    start = {n: getattr(cache, n).clone() for n in ("k", "v", "k_mean")}
+    plain = ev.Cache(cache.k.clone(), cache.v.clone(), cache.table, cache.lens, cache.k_mean.clone())
+    k_rot, _ = ev.evisel_rotary(rope, k, first=cache.lens)
+    want, ws = ev.evisel_cache_append(plain, k_rot, v)
+    got, _, _ = ev.evisel_cache_append_rotary(cache, rope, k, v, ws=ws)
+    assert torch.equal(got, want) and torch.equal(cache.k, plain.k) and torch.equal(cache.v, plain.v)
+    table = cache.table[0].long()
+    n, pages = int(got[0]), -(-int(got[0]) // page)
+    held = torch.tensor([min(page, n - j * page) for j in range(pages)], device="cuda")
+    live = (torch.arange(page, device="cuda") < held[:, None])[:, None, :, None]
+    x = torch.where(live, cache.k[table[:pages]].double(), 0.0)
+    m, size = x.sum(2) / held[:, None, None], x.abs().sum(2) / held[:, None, None]
+    err = (cache.k_mean[table[1:pages]].double() - m[1:]).abs()
+    assert bool((err <= (page + 8) * 2.0 ** -24 * size[1:] + u_of(dtype) * m[1:].abs() + 2.0 ** -25).all())
+    assert torch.equal(cache.k_mean[table[0]], start["k_mean"][table[0]]) and ev.evisel_status(ws) == 0
+    # Every other page is none.
+    for name, x in start.items():
+        getattr(cache, name).copy_(x)
+    broken = cache.table.clone()
+    broken[0, 1::2] = torch.tensor([-1, cache.k.shape[0], 1 << 30], dtype=torch.int32,
+                                   device="cuda")[torch.arange(broken[0, 1::2].numel(), device="cuda") % 3]
+    cache.table = broken
+    _, _, ws = ev.evisel_cache_append_rotary(cache, rope, k, v)
+    assert ev.evisel_status(ws) == -7
+    lost = torch.ones(cache.k.shape[0], dtype=torch.bool, device="cuda")
+    lost[table[2::2]] = False
+    for name in ("k", "v", "k_mean"):
+        now = getattr(cache, name)
+        assert torch.equal(now[lost], start[name][lost]) 
+    assert torch.equal(cache.k[table[2:pages:2]][:, :, :3], plain.k[table[2:pages:2]][:, :, :3])
+
+
+def test_rotated_append_of_few_tokens_to_no_page(cuda_lib):
+    """Most threads of a block have no token then: pages and means stay as they are."""
+    import torch
+    ev, rng, dtype = cuda_lib, np.random.default_rng(8), torch.bfloat16
+    for tokens in (1, 3, 17):
+        k, _ = tensor(rng, (2, tokens, 3, 128), dtype)
+        cache, _ = make_cache(rng, [0, 70], 3, 128, 64, dtype, room=tokens, mean=True, poison=False)
+        before = [x.clone() for x in (cache.k, cache.v, cache.k_mean)]
+        cache.table = torch.where(cache.table >= 0, cache.table + 1000, cache.table)
+        _, _, ws = ev.evisel_cache_append_rotary(cache, ev.Rotary(128), k, k)
+        assert ev.evisel_status(ws) == -7
+        for x, y in zip((cache.k, cache.v, cache.k_mean), before):
+            assert torch.equal(x, y)
 
 
 # --- beams -------------------------------------------------------------------------
