@@ -458,6 +458,59 @@ def test_beams_that_ended_or_never_were(cuda_lib):
     assert ev.evisel_beam_select(dev[0][:0], dev[1][:0], 3)[0].shape == (0, 3)
 
 
+@pytest.mark.parametrize("dtype,beams,vocab,n", [
+    ("bf16", 2, 300001, 1), ("fp32", 3, 150003, 2), ("fp16", 1, 700001, 3), ("bf16", 1, 32000, 64), ("fp32", 1, 20003, 50),
+    ("bf16", 2, 2047, 64), ("fp16", 64, 2500, 1)])
+def test_beam_blocks(cuda_lib, dtype, beams, vocab, n):
+    """Blocks of several chunks, fewer blocks than continuations, a block at a row's end that is empty."""
+    import torch
+    ev, dt, rng = cuda_lib, _types()[dtype], np.random.default_rng(vocab)
+    x = torch.from_numpy(rng.standard_normal((1, beams, vocab)) * 2.5).to(dt)
+    x[0, 0, vocab - 1] = x[0, 0, vocab - 5] = x[0, beams - 1, 0] = 13.0
+    scores = (-3 * rng.random((1, beams))).astype(np.float32)
+    out = ev.evisel_beam_select(x.cuda(), torch.from_numpy(scores).cuda(), n)
+    _check_beams(out, x.double().numpy(), scores, n)
+    x[:] = 0.5                          # every block's highest is its first of very many
+    scores[:] = -1
+    out = ev.evisel_beam_select(x.cuda(), torch.from_numpy(scores).cuda(), n)
+    m = min(n, vocab)
+    assert out[1][0, :m].tolist() == [0] * m and out[2][0, :m].tolist() == list(range(m))
+    assert (out[0][0, :m].double().cpu() + 1 + math.log(vocab)).abs().max() <= 2.0 ** -18 + 2.0 ** -24 * 16
+
+
+def test_more_equal_blocks_than_are_listed(cuda_lib):
+    import torch
+    x = torch.full((2, 64, 32768), -2.0, dtype=torch.bfloat16, device="cuda")
+    x[1, 63, 32767] = -1.0
+    scores, parent, token, _, _ = cuda_lib.evisel_beam_select(x, None, 5)
+    assert parent[0].tolist() == [0] * 5 and token[0].tolist() == [0, 1, 2, 3, 4]
+    assert parent[1].tolist() == [63, 0, 0, 0, 0] and token[1].tolist() == [32767, 0, 1, 2, 3]
+    assert (scores[0].double().cpu() + math.log(32768)).abs().max() <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("vocab", [300, 5000, 200003])
+@pytest.mark.parametrize("kind", ["far above", "far below", "one block far", "across", "huge"])
+def test_beam_logits_far_from_zero(cuda_lib, kind, vocab):
+    """Beyond 2^20, where the exponents are formed in another way: whole rows, some of a row's blocks, chunks on both sides."""
+    import torch
+    ev, rng = cuda_lib, np.random.default_rng(vocab)
+    x = rng.standard_normal((1, 3, vocab)) * 3
+    if kind == "far above":
+        x += 3e6
+    elif kind == "far below":
+        x[:, 1:] -= 5e7
+    elif kind == "one block far":
+        x[:, :, :min(vocab // 2, 1024)] -= 2e6
+    elif kind == "across":
+        x += 2.0 ** 20
+    else:
+        x *= 1e37
+    x = torch.from_numpy(x).to(torch.float32)
+    scores = np.float32([[-1, -2, -1.5]])
+    out = ev.evisel_beam_select(x.cuda(), torch.from_numpy(scores).cuda(), 2 if vocab > 9999 else 7)
+    _check_beams(out, x.double().numpy(), scores, out[0].shape[1], label=kind)
+
+
 # --- reordering --------------------------------------------------------------------
 
 def _beam_cache(rng, ev, prompts, grown, beams, hkv, d, page, dtype, layout, mean, slack=1, width=0):
