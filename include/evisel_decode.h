@@ -127,9 +127,10 @@ typedef struct {
  *   token      device int32 [B, n]: v, -1 past them
  *   ended_out  device uint8 [B, n] or NULL: 1 where the parent had ended, where v is
  *              eos, and past them
- * Within a beam the order is that of the logits, exactly; between beams it goes by a
- * normaliser formed from fp32 exponentials, fp32 sums of up to 64 of them and 64-bit sums of those,
- * off by about 1e-7 at most, and 64-bit values. The same call gives the same bits.
+ * Within a beam the order is that of the logits, exactly; between beams it goes by values of 48
+ * bits whose normaliser is formed from fp32 exponentials, fp32 sums of blocks of 1,024 of them (512 of fp32 logits; powers of
+ * two more for long rows) and 48-bit sums of those: off by 2^-18 at most, 1e-7 as a rule. Equal rows have the
+ * same normaliser wherever they lie, and the same call gives the same bits. Rows that begin on 16 bytes are read fastest.
  * The workspace keeps 8 bytes for every 1,024 logits (512 in fp32).
  * Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED, EVISEL_ENOMEM, EVISEL_ECUDA. */
 int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* parent, int32_t* token, uint8_t* ended_out,

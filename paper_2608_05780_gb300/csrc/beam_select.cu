@@ -26,6 +26,13 @@ __device__ __forceinline__ uint4 load_once(const uint4* p) {
   return w;
 }
 
+// The 16 bytes that begin `by` words (0 to 3) into a and end in b.
+__device__ __forceinline__ uint4 shifted_words(uint4 a, uint4 b, int by) {
+  if (by & 2) a = make_uint4(a.z, a.w, b.x, b.y), b = make_uint4(b.z, b.w, 0, 0);
+  if (by & 1) a = make_uint4(a.y, a.z, a.w, b.x);
+  return a;
+}
+
 struct F32 {};
 template <class T>
 struct Vec {
@@ -52,6 +59,14 @@ struct Vec {
     for (int i = 0; i < kPerLane; ++i) m = max2(m, max2(max2(w[i].x, w[i].y), max2(w[i].z, w[i].w)));
     return fmaxf(T::lo(m), T::hi(m));
   }
+  // The vector that begins `by` elements into a (by < N) and ends in b.
+  static __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int by) {
+    const uint4 w = shifted_words(a, b, by >> 1);
+    const uint32_t x = shifted_words(b, b, by >> 1).x;             // the word behind
+    const uint32_t bits = (by & 1) * 16;
+    return make_uint4(__funnelshift_r(w.x, w.y, bits), __funnelshift_r(w.y, w.z, bits), __funnelshift_r(w.z, w.w, bits),
+                      __funnelshift_r(w.w, x, bits));
+  }
   // The elements [e0, e1) of a vector, -inf beside them.
   static __device__ __forceinline__ uint4 load_some(const uint4* p, int e0, int e1) {
     const uint16_t* s = reinterpret_cast<const uint16_t*>(p);
@@ -73,6 +88,7 @@ struct Vec<F32> {
     f[0] = __uint_as_float(w.x), f[1] = __uint_as_float(w.y), f[2] = __uint_as_float(w.z), f[3] = __uint_as_float(w.w);
   }
   static __device__ __forceinline__ float element(const uint4* p, int i) { return __ldg(reinterpret_cast<const float*>(p) + i); }
+  static __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int by) { return shifted_words(a, b, by); }
   static __device__ __forceinline__ float highest(const uint4& w) {
     return fmaxf(ptx::max3(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z)), __uint_as_float(w.w));
   }
@@ -173,44 +189,62 @@ __device__ __forceinline__ float sum_of(const uint4 (&w)[kPerLane], float top, f
   return a + b;
 }
 
-// A row's 16-byte vectors, from the one that holds its first element on.
-template <class T>
+// A row's vectors of N tokens, -inf beside it. kSkewed: rows may begin inside 16 bytes; a vector is then put together from
+// the two that hold it, so that blocks and lanes have the same tokens, and equal rows one sum, wherever they lie.
+template <class T, bool kSkewed>
 struct Row {
   static constexpr int N = Vec<T>::N;
-  const uint4* vectors;
-  int skew;                         // elements of the first vector before the row
+  const uint4* vectors;             // from the 16 bytes that hold its first element on
+  int skew;                         // elements of those before the row
   Row() = default;
   __device__ __forceinline__ Row(const BeamLaunch& L, int b, int k) {
     constexpr int kSize = 16 / N;
     const char* base = static_cast<const char*>(L.logits) + (b * L.ls[0] + k * L.ls[1]) * kSize;
-    skew = static_cast<int>((reinterpret_cast<uintptr_t>(base) & 15) / kSize);
+    skew = kSkewed ? static_cast<int>((reinterpret_cast<uintptr_t>(base) & 15) / kSize) : 0;
     vectors = reinterpret_cast<const uint4*>(base - skew * kSize);
   }
-  // Vector v of the row, -inf beside it.
-  __device__ __forceinline__ uint4 vector(int v, int vocab) const {
-    if (v * N >= skew && (v + 1) * N <= skew + vocab) return __ldg(vectors + v);
-    return Vec<T>::load_some(vectors + v, skew - v * N, skew + vocab - v * N);
+  static __device__ __forceinline__ uint4 none() { return make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone); }
+  // 16 bytes of memory; what lies beside the row is not read.
+  template <bool kOnce>
+  __device__ __forceinline__ uint4 aligned(int v, int vocab) const {
+    const int before = skew - v * N, after = skew + vocab - v * N;
+    if (before <= 0 && after >= N) return kOnce ? load_once(vectors + v) : __ldg(vectors + v);
+    return after > 0 ? Vec<T>::load_some(vectors + v, before, after) : none();
   }
-  __device__ __forceinline__ int vectors_of(int vocab) const { return (skew + vocab + N - 1) / N; }
-  // The chunk at vector `at`, -inf beside the row; kOnce: nothing of it is read again by this SM.
+  // The chunk at vector `at`; kOnce: nothing of it is read again by this SM.
   template <bool kOnce>
   __device__ __forceinline__ void load(uint4 (&w)[kPerLane], int at, int vocab) const {
-    const int lane = threadIdx.x & 31, inner0 = skew > 0 ? 1 : 0, inner1 = (skew + vocab) / N, last = vectors_of(vocab);
-    if (at >= inner0 && at + kChunk <= inner1) {
+    const int lane = threadIdx.x & 31, v = at + lane;
+    if (!kSkewed || skew == 0) {
+      if ((at + kChunk) * N <= vocab) {
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) w[i] = kOnce ? load_once(vectors + at + lane + i * 32) : __ldg(vectors + at + lane + i * 32);
+        for (int i = 0; i < kPerLane; ++i) w[i] = kOnce ? load_once(vectors + v + i * 32) : __ldg(vectors + v + i * 32);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) w[i] = aligned<kOnce>(v + i * 32, vocab);
+      }
       return;
     }
+    if constexpr (kSkewed) {
+      uint4 a[kPerLane + 1];
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i) {
-      const int v = at + lane + i * 32;
-      w[i] = v < last ? vector(v, vocab) : make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+      for (int i = 0; i < kPerLane; ++i) a[i] = aligned<kOnce>(v + i * 32, vocab);
+      a[kPerLane] = lane == 0 ? aligned<kOnce>(at + kChunk, vocab) : none();
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) {
+        // The next lane's vector; the last lane's next is the first one's of the vectors behind.
+        const uint4 give = lane == 0 ? a[i + 1] : a[i];
+        const int from = (lane + 1) & 31;
+        const uint4 after = make_uint4(__shfl_sync(0xffffffffu, give.x, from), __shfl_sync(0xffffffffu, give.y, from),
+                                       __shfl_sync(0xffffffffu, give.z, from), __shfl_sync(0xffffffffu, give.w, from));
+        w[i] = Vec<T>::shifted(a[i], after, skew);
+      }
     }
   }
   __device__ __forceinline__ float element(int token) const { return Vec<T>::element(vectors, token + skew); }
 };
 
-template <class T>
+template <class T, bool kSkewed>
 __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __grid_constant__ BeamLaunch L) {
   // A block of all rows' blocks, and where it lies: sequence b, beam k, block j. (Counted on without divisions, which
   // would cost as much as the exponentials.)
@@ -219,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __gri
   int j = u - r * L.blocks, b = r / L.beams, k = r - b * L.beams;
   ptx::grid_wait();
   ptx::grid_launch_next();
-  Row<T> row;
+  Row<T, kSkewed> row;
   int at = 0, end = 0;
   // The block, or the next one after it, that is to be read.
   auto advance = [&]() {
@@ -233,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __gri
   auto find = [&]() {
     for (; u < L.total; advance()) {
       if (!beam_is_live(L, b * L.beams + k)) continue;
-      row = Row<T>(L, b, k);
+      row = Row<T, kSkewed>(L, b, k);
       at = j * L.block_vectors;
       end = min(at + L.block_vectors, L.row_vectors);
       return true;
@@ -369,8 +403,8 @@ __device__ __noinline__ Two far_normaliser(const float2* part, int blocks) {
   return isfinite(x) && isfinite(top) ? add(two_sum(hi, static_cast<float>(x - static_cast<double>(hi))), top) : Two{NAN, NAN};
 }
 
-// A row's normaliser, by a warp; NaN: none. The blocks' sums are added in 48 bits, so that the rows of one logit that
-// are cut differently (one begins inside a vector) have one normaliser.
+// A row's normaliser, by a warp; NaN: none. The blocks' sums are added in 48 bits, so that rounding to them is
+// not seen beside the blocks' own.
 __device__ __forceinline__ Two normaliser(const float2* part, int blocks) {
   constexpr int kBatch = 8;                      // loads on their way at once
   float exponent = -INFINITY;
@@ -427,7 +461,7 @@ struct Blocks {
 
 // The chosen blocks' continuations of `least` and above, a warp to a chunk. Vectors that hold one are few: they are
 // found by their maxima and read again.
-template <class T, class F>
+template <class T, bool kSkewed, class F>
 __device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key least, F&& take) {
   constexpr int N = Vec<T>::N;
   const BeamLaunch& L = all.L;
@@ -443,7 +477,7 @@ __device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key l
     }
     // A logit below this is not of `least`, which the two roundings leave in doubt by less than 2^-22 of either.
     const float lowest = least > 1 ? value - offset.hi - (fabsf(value) + fabsf(offset.hi)) * 0x1p-20f : kLowest;
-    const Row<T> row(L, blockIdx.x, k);
+    const Row<T, kSkewed> row(L, blockIdx.x, k);
     const int at = ((id - k * static_cast<int>(L.blocks)) << L.block_shift) + ((u - (r << shift)) << kChunkShift);
     uint4 w[kPerLane];
     row.template load<false>(w, at, L.vocab);
@@ -451,14 +485,12 @@ __device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key l
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) held |= Vec<T>::highest(w[i]) >= lowest ? 1u << i : 0u;
     for (; held; held &= held - 1) {
-      const int v = at + lane + (__ffs(held) - 1) * 32;
-      float x[N];
-      Vec<T>::unpack(row.vector(v, L.vocab), x);
+      const int t0 = (at + lane + (__ffs(held) - 1) * 32) * N;
       unsigned takes = 0;
 #pragma unroll
-      for (int e = 0; e < N; ++e) takes |= x[e] >= lowest ? 1u << e : 0u;
+      for (int e = 0; e < N; ++e) takes |= t0 + e < L.vocab && row.element(t0 + e) >= lowest ? 1u << e : 0u;
       for (; takes; takes &= takes - 1) {
-        const int t = v * N - row.skew + __ffs(takes) - 1;
+        const int t = t0 + __ffs(takes) - 1;
         const float y = row.element(t);
         const Key key = order_key(add(offset, y));
         if (key >= least) take(Place{key, rest_of(k, y, t)});
@@ -467,7 +499,7 @@ __device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key l
   }
 }
 
-template <class T>
+template <class T, bool kSkewed>
 __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __grid_constant__ BeamLaunch L) {
   __shared__ MergeShared s;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -562,13 +594,13 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
   for (int tries = listed >= L.n ? 0 : 1;; ++tries) {
     if (tries == 1) {
       best = 0;
-      read_chosen<T>(all, chosen, least, [&](Place p) { best = max(best, p.value); });
+      read_chosen<T, kSkewed>(all, chosen, least, [&](Place p) { best = max(best, p.value); });
       const uint32_t high = bound_of<kMergeThreads>(static_cast<uint32_t>(best >> 32), s.group_max, &s.bound, L.n, kMergeThreads);
       least = max(least, static_cast<Key>(high) << 32);
       if (tid == 0) s.count = 0;
       __syncthreads();
     }
-    read_chosen<T>(all, chosen, least, [&](Place p) {
+    read_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
       const int to = atomicAdd(&s.count, 1);
       if (to < kList) s.value[to] = p.value, s.rest[to] = p.rest;
     });
@@ -621,7 +653,7 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
   Place last{~Key(0), ~Key(0)};
   for (int r = 0; r < L.n; ++r) {
     Place y{0, 0};
-    read_chosen<T>(all, chosen, least, [&](Place p) {
+    read_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
       if (last > p && p > y) y = p;
     });
 #pragma unroll
@@ -641,10 +673,18 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
   }
 }
 
+template <class T, bool kSkewed>
+cudaError_t launch_both(const BeamLaunch& L, cudaStream_t stream) {
+  const cudaError_t e = launch_after(beam_scan_kernel<T, kSkewed>, dim3(L.ctas), kThreads, 0, stream, L);
+  return e != cudaSuccess ? e : launch_after(beam_choice_kernel<T, kSkewed>, dim3(L.batch), kMergeThreads, 0, stream, L);
+}
+
 template <class T>
 cudaError_t launch_t(const BeamLaunch& L, cudaStream_t stream) {
-  const cudaError_t e = launch_after(beam_scan_kernel<T>, dim3(L.ctas), kThreads, 0, stream, L);
-  return e != cudaSuccess ? e : launch_after(beam_choice_kernel<T>, dim3(L.batch), kMergeThreads, 0, stream, L);
+  constexpr int64_t kSize = 16 / Vec<T>::N;
+  const bool skewed =
+      ((reinterpret_cast<uintptr_t>(L.logits) | (L.batch > 1 ? L.ls[0] * kSize : 0) | (L.beams > 1 ? L.ls[1] * kSize : 0)) & 15) != 0;
+  return skewed ? launch_both<T, true>(L, stream) : launch_both<T, false>(L, stream);
 }
 
 }  // namespace
@@ -652,7 +692,7 @@ cudaError_t launch_t(const BeamLaunch& L, cudaStream_t stream) {
 BeamSplit beam_split(int64_t rows, int beams, int vocab, int n, int dtype, int n_sm) {
   const int per = dtype == 2 ? 4 : 8;
   BeamSplit s;
-  s.row_vectors = (vocab + per - 1) / per + 1;   // (a row may begin inside one)
+  s.row_vectors = (vocab + per - 1) / per;
   // As many bytes of maxima as of chosen blocks to read, within the powers of two: block^2 = 2 beams vocab / n.
   for (s.block_shift = kChunkShift; s.block_shift < 14; ++s.block_shift) {
     const int64_t block = static_cast<int64_t>(per) << s.block_shift;

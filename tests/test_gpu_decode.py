@@ -6,8 +6,9 @@ Bounds, u the rounding of the 16-bit type (2^-8 bf16, 2^-11 fp16):
   rotation  the angle comes from 32 bits of a turn that is exact modulo 1 up to |p| 2^-51 turns, rounded to fp32 (2^-25 of
             a half turn: 2^-23.3 radians); sine and cosine add 2^-24, the scale 2^-24, two products and a sum 2^-23:
             (2^-21 + |p| 2^-48) (|x1| + |x2|) + u |y|, and 2^-25 for fp16's smallest numbers
-  beams     exponentials off by 2^-22 + 2^-23 |x - max| relative, of which ln V covers the mean over the row; up to 64
-            of them added in fp32 by one thread, 2^-18 relative at worst; the rest in 64 bits. value: 2^-18 + 2^-22 +
+  beams     exponentials off by 2^-22 + 2^-23 |x - max| relative, of which ln V covers the mean over the row; added in
+            fp32 by a lane (17 roundings, chunks of a block without loss) and a warp (6), 2^-19.4 relative at worst; the rest in
+            48 bits. value: 2^-18 + 2^-22 +
             2^-23 (ln V + 1); rounded once to fp32, 2^-24 |value|
   means     fp32 sums over the stored keys: (n + 8) 2^-24 mean |k| + u |mean|
 """
@@ -476,6 +477,24 @@ def test_beam_blocks(cuda_lib, dtype, beams, vocab, n):
     m = min(n, vocab)
     assert out[1][0, :m].tolist() == [0] * m and out[2][0, :m].tolist() == list(range(m))
     assert (out[0][0, :m].double().cpu() + 1 + math.log(vocab)).abs().max() <= 2.0 ** -18 + 2.0 ** -24 * 16
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("vocab", [777, 3001, 50257])
+def test_equal_beams_tie(cuda_lib, dtype, vocab):
+    """Equal rows have one normaliser wherever they begin in memory: ties go to the lower beam, bit by bit."""
+    import torch
+    ev, dt, rng = cuda_lib, _types()[dtype], np.random.default_rng(vocab)
+    row = torch.from_numpy(rng.permutation(vocab) / vocab * 60 - 30).to(dt).cuda()
+    want = torch.sort(row.float(), descending=True, stable=True).indices[:4].tolist()
+    for stride in (vocab, vocab + 1, vocab + 3):
+        x = torch.zeros(9 * stride + 1, dtype=dt, device="cuda")[1:].as_strided((1, 9, vocab), (0, stride, 1))
+        x.copy_(row)
+        scores, parent, token, _, _ = ev.evisel_beam_select(x, None, 36)
+        same = [[v for v, y in enumerate(row.tolist()) if y == row[w].item()] for w in want[:1]][0]
+        first = [(k, v) for k in range(9) for v in same][:36]           # 16-bit logits may tie within a row too
+        assert list(zip(parent[0].tolist(), token[0].tolist()))[:len(first)] == first
+        assert scores[0, :len(first)].unique().numel() == 1
 
 
 def test_more_equal_blocks_than_are_listed(cuda_lib):
