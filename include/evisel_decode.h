@@ -58,7 +58,7 @@ int evisel_rope_init(evisel_rope* rope, int32_t rotary_dim, double base, double 
 typedef struct {
   const int32_t* at;               /* device or NULL                                  */
   const int32_t* first;            /* device [B] or NULL; not with at                 */
-  int64_t stride[2];               /* of at, in elements: axis, sequence; >= 0        */
+  int64_t stride[2];               /* of at, in elements: axis, sequence; 0 to below 2^38 */
 } evisel_positions;
 
 /* Heads [B, T, heads, d] to rotate. */
@@ -110,7 +110,7 @@ typedef struct {
   int32_t pad;                     /* token of an ended beam, 0 <= pad < V            */
   int32_t eos;                     /* token that ends a beam; -1: none                */
   int32_t reserved;                /* 0                                               */
-  int64_t logits_stride[2];        /* sequence, beam, in elements, >= 0               */
+  int64_t logits_stride[2];        /* sequence, beam, in elements, 0 to below 2^38    */
   const void* logits;              /* device [B, K, V], V contiguous                  */
   const float* scores;             /* device [B, K]: summed log-probabilities, or NULL: 0 */
   const uint8_t* finished;         /* device [B, K] or NULL: not 0 where a beam has ended */
@@ -122,6 +122,7 @@ typedef struct {
  * one continuation, (k, pad) with its score; its logits are not read. A value that is
  * -inf or NaN is none: a forbidden token (-inf), a beam without a score (-inf), all
  * of a row with a NaN or +inf logit, a beam whose score is NaN or +inf.
+ * Outputs are apart from the inputs and from one another; B K is at most 65,535.
  *   score_out  device fp32 [B, n] (written), -inf past the continuations there are
  *   parent     device int32 [B, n]: k, -1 past them
  *   token      device int32 [B, n]: v, -1 past them

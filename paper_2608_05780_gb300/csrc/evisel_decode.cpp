@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kMaxPairs = 64;
 constexpr int64_t kMaxTokens = int64_t(1) << 30;
-constexpr int64_t kMaxRows = 65535;              // of logits: a grid's second dimension
+constexpr int64_t kMaxRows = 65535;              // of logits, as many as a cache has sequences
 constexpr int kMaxVocab = 1 << 24;
 
 // Bytes [begin, end) that a strided tensor reaches.
@@ -70,7 +70,8 @@ int check_positions(const evisel_positions* p) {
   if (!p) return fail(EVISEL_EINVAL, "positions is NULL");
   if (p->at && p->first) return fail(EVISEL_EINVAL, "positions: at or first, not both");
   if (misaligned(p->at, 4) || misaligned(p->first, 4)) return fail(EVISEL_EINVAL, "positions must be 4-byte aligned");
-  if (p->at && (p->stride[0] < 0 || p->stride[1] < 0)) return fail(EVISEL_EINVAL, "position strides must not be negative");
+  if (p->at && (std::min(p->stride[0], p->stride[1]) < 0 || std::max(p->stride[0], p->stride[1]) >= kMaxStride))
+    return fail(EVISEL_EINVAL, "position strides must be 0 to below 2^38");
   return EVISEL_OK;
 }
 
@@ -273,10 +274,16 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
     if (m.logits_stride[0] < 0 || m.logits_stride[1] < 0 || std::max(m.logits_stride[0], m.logits_stride[1]) >= kMaxStride)
       return fail(EVISEL_EINVAL, "logits strides must be 0 to below 2^38");
     const int64_t n = static_cast<int64_t>(m.batch) * m.n_out;
-    // Other sequences' blocks still read the scores and flags.
-    for (const Range& out : {range_of(score_out, 4 * n), range_of(parent, 4 * n), range_of(token, 4 * n), range_of(ended_out, n)})
-      if (out.meets(range_of(m.scores, 4 * rows)) || out.meets(range_of(m.finished, rows)))
-        return fail(EVISEL_EINVAL, "an output lies over scores or finished");
+    // Other sequences' blocks still read the inputs, the chosen blocks of the logits again.
+    const int64_t reach = (m.batch - 1) * m.logits_stride[0] + (m.beams - 1) * m.logits_stride[1] + m.vocab;
+    const Range in[3] = {range_of(m.logits, reach * size), range_of(m.scores, 4 * rows), range_of(m.finished, rows)};
+    const Range out[4] = {range_of(score_out, 4 * n), range_of(parent, 4 * n), range_of(token, 4 * n), range_of(ended_out, n)};
+    for (int i = 0; i < 4; ++i) {
+      for (const Range& r : in)
+        if (out[i].meets(r)) return fail(EVISEL_EINVAL, "an output lies over logits, scores or finished");
+      for (int j = 0; j < i; ++j)
+        if (out[i].meets(out[j])) return fail(EVISEL_EINVAL, "outputs lie over one another");
+    }
     const int n_sm = sm_count();
     if (n_sm <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
     const BeamSplit split = beam_split(rows, m.beams, m.vocab, m.n_out, m.dtype, n_sm);

@@ -123,7 +123,7 @@ BAD_ROPE = [(dict(rotary_dim=0), EUNSUPPORTED), (dict(rotary_dim=24), EUNSUPPORT
             (dict(interleaved=2), EINVAL), (dict(axes=2), EUNSUPPORTED), (dict(axes=3), EINVAL),
             (dict(axes=3, section=(-1, 33, 32)), EINVAL), (dict(axes=3, section=(1 << 30, 1 << 30, 1 << 30)), EINVAL),
             (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(reserved=1), EINVAL)]
-BAD_POS = [(dict(first=FAKE), EINVAL), (dict(at=FAKE + 2), EINVAL), (dict(at=0, first=FAKE + 1), EINVAL), (dict(stride=(-1, 3)), EINVAL),
+BAD_POS = [(dict(first=FAKE), EINVAL), (dict(at=FAKE + 2), EINVAL), (dict(at=0, first=FAKE + 1), EINVAL), (dict(stride=(-1, 3)), EINVAL), (dict(stride=(1 << 38, 3)), EINVAL), (dict(stride=(0, 1 << 38)), EINVAL),
            (dict(stride=(6, -3)), EINVAL)]
 
 
@@ -171,6 +171,9 @@ Q1, K1 = FAKE, FAKE + (2 << 20)
     ("select", dict(m=_sel(logits=FAKE + 1)), EINVAL), ("select", dict(m=_sel(dtype=2, logits=FAKE + 2)), EINVAL),
     ("select", dict(m=_sel(logits_stride=(-1, 32000))), EINVAL), ("select", dict(score=None), EINVAL), ("select", dict(parent=None), EINVAL),
     ("select", dict(token=_at((6 << 20) + 2)), EINVAL), ("select", dict(score=_at(1 << 20)), EINVAL), ("select", dict(ended=_at(2 << 20)), EINVAL),
+    ("select", dict(parent=_at(511996)), EINVAL), ("select", dict(ended=_at(511999)), EINVAL), ("select", dict(token=_at((5 << 20) + 60)), EINVAL),
+    ("select", dict(ended=_at((4 << 20) + 63)), EINVAL), ("select", dict(m=_sel(logits_stride=(1 << 38, 32000))), EINVAL),
+    ("select", dict(m=_sel(logits_stride=(128000, 1 << 38))), EINVAL), ("select", dict(m=_sel(logits_stride=(1 << 24, 32000))), EINVAL),
     ("reorder", dict(c=None), EINVAL), ("reorder", dict(beams=0), EUNSUPPORTED), ("reorder", dict(beams=65), EUNSUPPORTED),
     ("reorder", dict(beams=3), EINVAL), ("reorder", dict(parent=None), EINVAL), ("reorder", dict(table=None), EINVAL),
     ("reorder", dict(lens=None), EINVAL), ("reorder", dict(lens=_at((3 << 20) + 2)), EINVAL), ("reorder", dict(n=-1), EUNSUPPORTED),
@@ -230,7 +233,7 @@ def test_failures_are_reported(fake):
     ws = P(None)
     assert _select(fake, ctypes.byref(ws)) == 0
     held = fake.evisel_workspace_bytes(ws)
-    large = _sel(batch=64, n_out=64, scores=0, finished=0)
+    large = _sel(batch=64, n_out=64, scores=0, finished=0, logits=FAKE + (64 << 20))
     fake.fake_fail(b"cudaMalloc", 0)
     assert _select(fake, ctypes.byref(ws), m=large) == ENOMEM
     fake.fake_capture(1)
