@@ -105,17 +105,22 @@ def _positions(rope, positions, first, shape, device):
     return _POSITIONS.pack(0, first.data_ptr(), 0, 0)
 
 
-def _heads(rope, x, out, batch, tokens, what, c):
-    """The packed heads x [B, T, H, d] (or [T, H, d]) and their output."""
-    s, o = x.stride(), out.stride()
-    if not (x.shape[-1] == rope.head_dim and x.dtype in c.dtypes and x.is_cuda and (s[-1] == 1 or x.numel() == 0)):
-        _refuse(f"{what} must be CUDA [B, T, H, {rope.head_dim}] or [T, H, {rope.head_dim}] of bf16 or fp16, d contiguous")
-    if out is not x and not (out.shape == x.shape and out.dtype == x.dtype and out.device == x.device
-                             and (o[-1] == 1 or x.numel() == 0)):
-        _refuse(f"the output of {what} must have its shape, type and device, d contiguous")
-    s, o = (s, o) if len(s) == 4 else ((0, *s), (0, *o))
-    return _HEADS.pack(batch, tokens, x.shape[-2], rope.head_dim, c.dtypes[x.dtype], 0, s[0], s[1], s[2], o[0], o[1], o[2],
-                       x.data_ptr(), out.data_ptr())
+def _heads(rope, x, out, shape, batch, tokens, empty, what, c):
+    """(the output, made where there is none, the packed heads x [B, T, H, d] or [T, H, d])."""
+    s, dtype, d = x.stride(), x.dtype, rope.head_dim
+    heads = shape[-2]
+    if not (shape[-1] == d and dtype in c.dtypes and x.is_cuda and (s[-1] == 1 or 0 in shape)):
+        _refuse(f"{what} must be CUDA [B, T, H, {d}] or [T, H, {d}] of bf16 or fp16, d contiguous")
+    if out is None:
+        out = empty(shape, dtype=dtype, device=x.device)
+        o0, o1, o2 = tokens * heads * d, heads * d, d
+    else:
+        o = out.stride()
+        if out is not x and not (out.shape == shape and out.dtype == dtype and out.device == x.device and (o[-1] == 1 or 0 in shape)):
+            _refuse(f"the output of {what} must have its shape, type and device, d contiguous")
+        o0, o1, o2 = o[:3] if len(o) == 4 else (0, o[0], o[1])
+    s0, s1, s2 = s[:3] if len(s) == 4 else (0, s[0], s[1])
+    return out, _HEADS.pack(batch, tokens, heads, d, c.dtypes[dtype], 0, s0, s1, s2, o0, o1, o2, x.data_ptr(), out.data_ptr())
 
 
 def evisel_rotary(rope, q, k=None, positions=None, first=None, transpose=False, q_out=None, k_out=None, stream=None):
@@ -126,22 +131,19 @@ def evisel_rotary(rope, q, k=None, positions=None, first=None, transpose=False, 
 
     Returns (q_out, k_out), None without k."""
     c = _decode()
-    if q.dim() not in (3, 4) or (k is not None and (k.dim() != q.dim() or k.shape[:-2] != q.shape[:-2]
-                                                    or k.dtype != q.dtype or k.device != q.device)):
+    shape, k_shape = q.shape, None if k is None else k.shape
+    if len(shape) not in (3, 4) or (k is not None and not (len(k_shape) == len(shape) and k_shape[:-2] == shape[:-2]
+                                                           and k.dtype == q.dtype and k.device == q.device)):
         _refuse("q and k must be [B, T, H, d] or [T, H, d], of one batch, tokens, type and device")
-    batch, tokens = (1, q.shape[0]) if q.dim() == 3 else q.shape[:2]
-    if q.dim() == 3 and positions is not None and positions.dim():
+    batch, tokens = (1, shape[0]) if len(shape) == 3 else shape[:2]
+    if len(shape) == 3 and positions is not None and positions.dim():
         positions = positions.unsqueeze(-2)
     pos = _positions(rope, positions, first, (batch, tokens), q.device)
     empty = _maker(c.empty, stream)
-    if q_out is None:
-        q_out = empty(q.shape, dtype=q.dtype, device=q.device)
-    packed = _heads(rope, q, q_out, batch, tokens, "q", c)
+    q_out, packed = _heads(rope, q, q_out, shape, batch, tokens, empty, "q", c)
     k_packed = None
     if k is not None:
-        if k_out is None:
-            k_out = empty(k.shape, dtype=k.dtype, device=k.device)
-        k_packed = _heads(rope, k, k_out, batch, tokens, "k", c)
+        k_out, k_packed = _heads(rope, k, k_out, k_shape, batch, tokens, empty, "k", c)
     elif k_out is not None:
         _refuse("k_out without k")
     rc = c.rotary(rope._packed, packed, k_packed, pos, 1 if transpose else 0, _stream(q, stream))
