@@ -216,33 +216,34 @@ struct Row {
     if (before <= 0 && after >= N) return kOnce ? load_once(vectors + v) : __ldg(vectors + v);
     return after > 0 ? Vec<T>::load_some(vectors + v, before, after) : none();
   }
-  // The chunk at vector `at`; kOnce: nothing of it is read again by this SM.
+  // The chunk at vector `at` as it lies in memory, kSkewed: with the first vector behind it in the first lane; kOnce:
+  // nothing of it is read again by this SM.
+  static constexpr int kLoads = kPerLane + (kSkewed ? 1 : 0);
   template <bool kOnce>
-  __device__ __forceinline__ void load(uint4 (&w)[kPerLane], int at, int vocab) const {
+  __device__ __forceinline__ void load(uint4 (&a)[kLoads], int at, int vocab) const {
     const int lane = threadIdx.x & 31, v = at + lane;
-    if (!kSkewed || skew == 0) {
-      if ((at + kChunk) * N <= vocab) {
+    if ((at + kChunk) * N <= skew + vocab && (at > 0 || skew == 0)) {
 #pragma unroll
-        for (int i = 0; i < kPerLane; ++i) w[i] = kOnce ? load_once(vectors + v + i * 32) : __ldg(vectors + v + i * 32);
-      } else {
-#pragma unroll
-        for (int i = 0; i < kPerLane; ++i) w[i] = aligned<kOnce>(v + i * 32, vocab);
-      }
-      return;
-    }
-    if constexpr (kSkewed) {
-      uint4 a[kPerLane + 1];
+      for (int i = 0; i < kPerLane; ++i) a[i] = kOnce ? load_once(vectors + v + i * 32) : __ldg(vectors + v + i * 32);
+    } else {
 #pragma unroll
       for (int i = 0; i < kPerLane; ++i) a[i] = aligned<kOnce>(v + i * 32, vocab);
-      a[kPerLane] = lane == 0 ? aligned<kOnce>(at + kChunk, vocab) : none();
+    }
+    if constexpr (kSkewed) a[kPerLane] = lane == 0 ? aligned<kOnce>(at + kChunk, vocab) : none();
+  }
+  // Its vectors of tokens, by the whole warp.
+  __device__ __forceinline__ void put_together(uint4 (&w)[kPerLane], const uint4 (&a)[kLoads]) const {
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) {
-        // The next lane's vector; the last lane's next is the first one's of the vectors behind.
+    for (int i = 0; i < kPerLane; ++i) {
+      if constexpr (kSkewed) {
+        // The next lane's vector; the last lane's next is the first lane's of the vectors behind.
+        const int lane = threadIdx.x & 31, from = (lane + 1) & 31;
         const uint4 give = lane == 0 ? a[i + 1] : a[i];
-        const int from = (lane + 1) & 31;
         const uint4 after = make_uint4(__shfl_sync(0xffffffffu, give.x, from), __shfl_sync(0xffffffffu, give.y, from),
                                        __shfl_sync(0xffffffffu, give.z, from), __shfl_sync(0xffffffffu, give.w, from));
         w[i] = Vec<T>::shifted(a[i], after, skew);
+      } else {
+        w[i] = a[i];
       }
     }
   }
@@ -279,14 +280,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __gri
     }
     return false;
   };
-  uint4 next[kPerLane];
+  uint4 next[Row<T, kSkewed>::kLoads];
   bool more = find();
   if (more) row.template load<true>(next, at, L.vocab);
   float top = -INFINITY, c = 0.f, sum = 0.f, low = 0.f;            // the sum is sum + low
   while (more) {
     uint4 w[kPerLane];
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) w[i] = next[i];
+    row.put_together(w, next);
     const unsigned now = u;
     const bool last = at + kChunk >= end;
     if (!last) {
@@ -484,8 +484,9 @@ __device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key l
     const float lowest = least > 1 ? value - offset.hi - (fabsf(value) + fabsf(offset.hi)) * 0x1p-20f : kLowest;
     const Row<T, kSkewed> row(L, blockIdx.x, k);
     const int at = ((id - k * static_cast<int>(L.blocks)) << L.block_shift) + ((u - (r << shift)) << kChunkShift);
-    uint4 w[kPerLane];
-    row.template load<false>(w, at, L.vocab);
+    uint4 w[kPerLane], a[Row<T, kSkewed>::kLoads];
+    row.template load<false>(a, at, L.vocab);
+    row.put_together(w, a);
     unsigned held = 0;
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) held |= Vec<T>::highest(w[i]) >= lowest ? 1u << i : 0u;
