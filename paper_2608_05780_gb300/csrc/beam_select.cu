@@ -464,45 +464,57 @@ struct Blocks {
   }
 };
 
-// The chosen blocks' continuations of `least` and above, a warp to a chunk. Vectors that hold one are few: they are
-// found by their maxima and read again.
-template <class T, bool kSkewed, class F>
-__device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, Key least, F&& take) {
-  constexpr int N = Vec<T>::N;
+// The chosen blocks' chunks, a warp to each: chunk(beam, row, at, vectors), and ended(beam) of beams that have ended.
+template <class T, bool kSkewed, class C, class E>
+__device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, C&& chunk, E&& ended) {
   const BeamLaunch& L = all.L;
-  const int lane = threadIdx.x & 31, shift = L.block_shift - kChunkShift;
-  const float value = value_of(least);
+  const int shift = L.block_shift - kChunkShift;
   for (int u = threadIdx.x >> 5; u < chosen << shift; u += kMergeWarps) {
     const int r = u >> shift, id = all.s.chosen[r], k = all.beam(id);
-    const Two offset = all.s.offset[k];
-    if (!(offset.hi == offset.hi)) {             // a beam that has ended
-      const Key key = all.ended(k);
-      if (lane == 0 && u == r << shift && key >= least) take(Place{key, rest_of(k, 0.f, L.pad)});
+    if (!(all.s.offset[k].hi == all.s.offset[k].hi)) {
+      if ((threadIdx.x & 31) == 0 && u == r << shift) ended(k);
       continue;
     }
-    // A logit below this is not of `least`, which the two roundings leave in doubt by less than 2^-22 of either.
-    const float lowest = least > 1 ? value - offset.hi - (fabsf(value) + fabsf(offset.hi)) * 0x1p-20f : kLowest;
     const Row<T, kSkewed> row(L, blockIdx.x, k);
     const int at = ((id - k * static_cast<int>(L.blocks)) << L.block_shift) + ((u - (r << shift)) << kChunkShift);
     uint4 w[kPerLane], a[Row<T, kSkewed>::kLoads];
     row.template load<false>(a, at, L.vocab);
     row.put_together(w, a);
-    unsigned held = 0;
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) held |= Vec<T>::highest(w[i]) >= lowest ? 1u << i : 0u;
-    for (; held; held &= held - 1) {
-      const int t0 = (at + lane + (__ffs(held) - 1) * 32) * N;
-      unsigned takes = 0;
-#pragma unroll
-      for (int e = 0; e < N; ++e) takes |= t0 + e < L.vocab && row.element(t0 + e) >= lowest ? 1u << e : 0u;
-      for (; takes; takes &= takes - 1) {
-        const int t = t0 + __ffs(takes) - 1;
-        const float y = row.element(t);
-        const Key key = order_key(add(offset, y));
-        if (key >= least) take(Place{key, rest_of(k, y, t)});
-      }
-    }
+    chunk(k, row, at, w);
   }
+}
+
+// Their continuations of `least` and above. Vectors that hold one are few: they are found by their maxima and read again.
+template <class T, bool kSkewed, class F>
+__device__ __forceinline__ void take_chosen(const Blocks& all, int chosen, Key least, F&& take) {
+  constexpr int N = Vec<T>::N;
+  const float value = value_of(least);
+  read_chosen<T, kSkewed>(
+      all, chosen,
+      [&](int k, const Row<T, kSkewed>& row, int at, const uint4 (&w)[kPerLane]) {
+        const Two offset = all.s.offset[k];
+        // A logit below this is not of `least`, which the two roundings leave in doubt by less than 2^-22 of either.
+        const float lowest = least > 1 ? value - offset.hi - (fabsf(value) + fabsf(offset.hi)) * 0x1p-20f : kLowest;
+        unsigned held = 0;
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) held |= Vec<T>::highest(w[i]) >= lowest ? 1u << i : 0u;
+        for (; held; held &= held - 1) {
+          const int t0 = (at + static_cast<int>(threadIdx.x & 31) + (__ffs(held) - 1) * 32) * N;
+          unsigned takes = 0;
+#pragma unroll
+          for (int e = 0; e < N; ++e) takes |= t0 + e < all.L.vocab && row.element(t0 + e) >= lowest ? 1u << e : 0u;
+          for (; takes; takes &= takes - 1) {
+            const int t = t0 + __ffs(takes) - 1;
+            const float y = row.element(t);
+            const Key key = order_key(add(offset, y));
+            if (key >= least) take(Place{key, rest_of(k, y, t)});
+          }
+        }
+      },
+      [&](int k) {
+        const Key key = all.ended(k);
+        if (key >= least) take(Place{key, rest_of(k, 0.f, all.L.pad)});
+      });
 }
 
 template <class T, bool kSkewed>
@@ -600,13 +612,19 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
   for (int tries = listed >= L.n ? 0 : 1;; ++tries) {
     if (tries == 1) {
       best = 0;
-      read_chosen<T, kSkewed>(all, chosen, least, [&](Place p) { best = max(best, p.value); });
+      read_chosen<T, kSkewed>(
+          all, chosen,
+          [&](int k, const Row<T, kSkewed>&, int, const uint4 (&w)[kPerLane]) {
+            const float x = Vec<T>::highest(w);
+            if (x > -INFINITY) best = max(best, order_key(add(s.offset[k], x)));
+          },
+          [&](int k) { best = max(best, all.ended(k)); });
       const uint32_t high = bound_of<kMergeThreads>(static_cast<uint32_t>(best >> 32), s.group_max, &s.bound, L.n, kMergeThreads);
       least = max(least, static_cast<Key>(high) << 32);
       if (tid == 0) s.count = 0;
       __syncthreads();
     }
-    read_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
+    take_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
       const int to = atomicAdd(&s.count, 1);
       if (to < kList) s.value[to] = p.value, s.rest[to] = p.rest;
     });
@@ -659,7 +677,7 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
   Place last{~Key(0), ~Key(0)};
   for (int r = 0; r < L.n; ++r) {
     Place y{0, 0};
-    read_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
+    take_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
       if (last > p && p > y) y = p;
     });
 #pragma unroll
