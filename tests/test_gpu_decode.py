@@ -497,6 +497,20 @@ def test_equal_beams_tie(cuda_lib, dtype, vocab):
         assert scores[0, :len(first)].unique().numel() == 1
 
 
+def test_beam_rows_past_32_bits(cuda_lib):
+    """Strides of sequences and beams beyond 2^31 elements, from an odd one."""
+    import torch
+    rng, far = np.random.default_rng(6), (1 << 31) + 5
+    pool = torch.empty(3 * far + 9000, dtype=torch.bfloat16, device="cuda")
+    scores = np.float32([[-1, -2], [-0.5, -3]])
+    for strides in ((2 * far, far), (far, 4096), (5, far)):
+        x = pool[1:].as_strided((2, 2, 4001) if strides[0] > 5 else (1, 2, 4001), (*strides, 1))
+        y = torch.from_numpy(rng.standard_normal(tuple(x.shape)) * 3).to(torch.bfloat16)
+        x.copy_(y)
+        out = cuda_lib.evisel_beam_select(x, torch.from_numpy(scores[:len(y)]).cuda(), 9)
+        _check_beams(out, y.double().numpy(), scores, 9, label=str(strides))
+
+
 def test_more_equal_blocks_than_are_listed(cuda_lib):
     import torch
     x = torch.full((2, 64, 32768), -2.0, dtype=torch.bfloat16, device="cuda")

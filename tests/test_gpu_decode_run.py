@@ -200,3 +200,34 @@ def test_calls_at_once_on_their_own_streams(cuda_lib):
         for got in both[i][1]:
             for a, b in zip(got, want):
                 assert torch.equal(a, b)
+
+
+def test_graphs_that_share_a_workspace(cuda_lib):
+    """Selections of two sizes captured on one workspace, which grows in between: replayed in any order, each as before."""
+    import torch
+    ev = cuda_lib
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    ws, made = ev.Workspace(), []
+    for batch, vocab, n in ((1, 5000, 4), (16, 70001, 10)):
+        x = torch.randn((batch, 3, vocab), device="cuda", generator=gen).to(torch.bfloat16)
+        call = lambda x=x, n=n: ev.evisel_beam_select(x, None, n, ws=ws)[:4]  # noqa: E731
+        want = call()
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            got = call()
+        made.append((graph, got, [a.clone() for a in want]))
+    for i in (0, 1, 1, 0, 1, 0):
+        graph, got, want = made[i]
+        for a in got:
+            a.zero_()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+    assert ev.evisel_status(ws) == 0
+    x = torch.randn((64, 3, 200001), device="cuda", generator=gen).to(torch.bfloat16)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with pytest.raises(ev.EviselError, match="capture"):
+        with torch.cuda.graph(graph):
+            ev.evisel_beam_select(x, None, 10, ws=ws)           # the workspace would have to grow
+    assert torch.equal(ev.evisel_beam_select(x[:1], None, 1, ws=ws)[2][0, 0].cpu(), x[0].float().log_softmax(-1).max(0).values.argmax().int().cpu())
