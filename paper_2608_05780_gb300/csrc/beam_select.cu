@@ -11,6 +11,7 @@
 // The choice is a chain of dependent steps: 7 us more there, 4.5 of the 6.6 us that four beams over 32,000 tokens take.
 #include <algorithm>
 
+#include "cache_choose.cuh"
 #include "cache_common.cuh"
 #include "decode_internal.h"
 
@@ -18,6 +19,7 @@ namespace evisel {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32, kPerSm = 2;
+constexpr int kCluster = 8, kSmallBlocks = 2;     // CTAs of a sequence whose blocks are few: so many to a warp at most
 constexpr int kPerLane = 4;                      // 16-byte vectors of a lane's chunk; the next chunk is in flight
 constexpr int kChunkShift = 7, kChunk = 32 * kPerLane;
 static_assert(kChunk == 1 << kChunkShift);
@@ -250,15 +252,12 @@ struct Row {
   __device__ __forceinline__ float element(int token) const { return Vec<T>::element(vectors, token + skew); }
 };
 
+// The blocks u, u + L.step, .. below `limit` of all rows' blocks, by a warp. (Counted on without divisions, which
+// would cost as much as the exponentials.)
 template <class T, bool kSkewed>
-__global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __grid_constant__ BeamLaunch L) {
-  // A block of all rows' blocks, and where it lies: sequence b, beam k, block j. (Counted on without divisions, which
-  // would cost as much as the exponentials.)
-  unsigned u = blockIdx.x * kWarps + (threadIdx.x >> 5);
+__device__ __forceinline__ void scan(const BeamLaunch& L, unsigned u, unsigned limit) {
   const unsigned r = u / L.blocks;
-  int j = u - r * L.blocks, b = r / L.beams, k = r - b * L.beams;
-  ptx::grid_wait();
-  ptx::grid_launch_next();
+  int j = u - r * L.blocks, b = r / L.beams, k = r - b * L.beams;  // where block u lies
   Row<T, kSkewed> row;
   int at = 0, end = 0;
   // The block, or the next one after it, that is to be read.
@@ -271,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __gri
     if (k >= L.beams) k -= L.beams, ++b;         // (k was below beams and grew by beams at most)
   };
   auto find = [&]() {
-    for (; u < L.total; advance()) {
+    for (; u < limit; advance()) {
       if (!beam_is_live(L, b * L.beams + k)) continue;
       row = Row<T, kSkewed>(L, b, k);
       at = j * L.block_vectors;
@@ -317,6 +316,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __gri
       top = -INFINITY, c = 0.f, sum = 0.f, low = 0.f;
     }
   }
+}
+
+template <class T, bool kSkewed>
+__global__ void __launch_bounds__(kThreads, kPerSm) beam_scan_kernel(const __grid_constant__ BeamLaunch L) {
+  ptx::grid_wait();
+  ptx::grid_launch_next();
+  scan<T, kSkewed>(L, blockIdx.x * kWarps + (threadIdx.x >> 5), L.total);
 }
 
 // ---------------------------------------------------------------- the choice
@@ -449,7 +455,7 @@ struct Blocks {
   const BeamLaunch& L;
   const MergeShared& s;
   const float2* part;               // of the sequence
-  int row0;
+  int row0, b;
   __device__ __forceinline__ int beam(int id) const { return L.blocks == 1 ? id : static_cast<int>(__umulhi(id, L.inverse_blocks)); }
   // What block `id` has at most, its maximum being x.
   __device__ __forceinline__ Key key(int id, float x) const {
@@ -475,7 +481,7 @@ __device__ __forceinline__ void read_chosen(const Blocks& all, int chosen, C&& c
       if ((threadIdx.x & 31) == 0 && u == r << shift) ended(k);
       continue;
     }
-    const Row<T, kSkewed> row(L, blockIdx.x, k);
+    const Row<T, kSkewed> row(L, all.b, k);
     const int at = ((id - k * static_cast<int>(L.blocks)) << L.block_shift) + ((u - (r << shift)) << kChunkShift);
     uint4 w[kPerLane], a[Row<T, kSkewed>::kLoads];
     row.template load<false>(a, at, L.vocab);
@@ -517,14 +523,11 @@ __device__ __forceinline__ void take_chosen(const Blocks& all, int chosen, Key l
       });
 }
 
+// The choice for sequence b, by a CTA; s.listed and s.count are 0.
 template <class T, bool kSkewed>
-__global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __grid_constant__ BeamLaunch L) {
-  __shared__ MergeShared s;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Blocks all{L, s, L.part + static_cast<int64_t>(b) * L.beams * L.blocks, b * L.beams};
-  if (tid == 0) s.count = s.listed = 0;
-  ptx::grid_wait();
-  ptx::grid_launch_next();
+__device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int b) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const Blocks all{L, s, L.part + static_cast<int64_t>(b) * L.beams * L.blocks, b * L.beams, b};
   // Each row's normaliser, by a warp; the first blocks' maxima on their way meanwhile.
   const int ids = L.beams * L.blocks;
   float first[kHeld];
@@ -698,7 +701,35 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
 }
 
 template <class T, bool kSkewed>
+__global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __grid_constant__ BeamLaunch L) {
+  __shared__ MergeShared s;
+  if (threadIdx.x == 0) s.count = s.listed = 0;
+  __syncthreads();
+  ptx::grid_wait();
+  ptx::grid_launch_next();
+  choose<T, kSkewed>(L, s, blockIdx.x);
+}
+
+// Both for few blocks, at most two to a warp: a cluster per sequence scans its blocks, and its first CTA chooses. The device
+// takes as long (6.7 us for four beams over 32,000 tokens, 0.7 more than two launches at two blocks a warp), the host
+// 2.5 us less of a call's 19; with four blocks a warp the device lost that again (8.6 to 11.9 us for eight beams over 50,264).
+template <class T, bool kSkewed>
+__global__ void __launch_bounds__(kThreads, kPerSm) beam_small_kernel(const __grid_constant__ BeamLaunch L) {
+  static_assert(kThreads == kMergeThreads);
+  __shared__ MergeShared s;
+  const unsigned rank = ptx::cluster_rank(), b = blockIdx.x / kCluster, first = b * L.beams * L.blocks;
+  if (threadIdx.x == 0) s.count = s.listed = 0;
+  ptx::grid_wait();
+  ptx::grid_launch_next();
+  scan<T, kSkewed>(L, first + rank * kWarps + (threadIdx.x >> 5), first + L.beams * L.blocks);
+  __syncwarp();
+  ptx::cluster_sync();              // (the blocks' maxima and sums are seen behind it)
+  if (rank == 0) choose<T, kSkewed>(L, s, b);
+}
+
+template <class T, bool kSkewed>
 cudaError_t launch_both(const BeamLaunch& L, cudaStream_t stream) {
+  if (L.small) return launch_clusters(beam_small_kernel<T, kSkewed>, L, L.batch, kThreads, kCluster, stream);
   const cudaError_t e = launch_after(beam_scan_kernel<T, kSkewed>, dim3(L.ctas), kThreads, 0, stream, L);
   return e != cudaSuccess ? e : launch_after(beam_choice_kernel<T, kSkewed>, dim3(L.batch), kMergeThreads, 0, stream, L);
 }
@@ -726,7 +757,8 @@ BeamSplit beam_split(int64_t rows, int beams, int vocab, int n, int dtype, int n
   s.blocks = (s.row_vectors + s.block_vectors - 1) / s.block_vectors;
   const int64_t most = static_cast<int64_t>(n_sm) * kPerSm;
   s.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, (rows * s.blocks + kWarps - 1) / kWarps)));
-  s.warps = s.ctas * kWarps;
+  s.small = static_cast<int64_t>(beams) * s.blocks <= kCluster * kWarps * kSmallBlocks && rows / beams * kCluster <= most;
+  s.warps = s.small ? kCluster * kWarps : s.ctas * kWarps;
   return s;
 }
 

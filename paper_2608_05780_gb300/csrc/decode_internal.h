@@ -55,7 +55,7 @@ struct BeamLaunch {
   uint8_t* ended_out;
   float2* part;                     // [rows, blocks]: maximum, sum of exponentials
   int batch, beams, vocab, n, dtype, pad, eos;
-  int row_vectors, block_vectors, block_shift, ctas;   // as BeamSplit's
+  int row_vectors, block_vectors, block_shift, ctas, small;   // as BeamSplit's
   unsigned blocks, total;                            // of a row, of all rows
   unsigned step;                                     // warps: step_batch sequences, step_beam beams and step_block blocks
   int step_batch, step_beam, step_block;
@@ -84,6 +84,7 @@ struct ReorderLaunch {
 // A row of row_vectors 16-byte vectors as `blocks` blocks of block_vectors, which `warps` warps of `ctas` CTAs take in turn.
 struct BeamSplit {
   int row_vectors, block_vectors, block_shift, blocks, ctas, warps;   // block_vectors = 1 << block_shift
+  int small;                                         // one launch: the warps are those of a sequence's cluster
 };
 BeamSplit beam_split(int64_t rows, int beams, int vocab, int n, int dtype, int n_sm);
 

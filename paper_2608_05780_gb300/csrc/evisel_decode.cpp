@@ -315,6 +315,7 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
     L.block_vectors = split.block_vectors;
     L.block_shift = split.block_shift;
     L.ctas = split.ctas;
+    L.small = split.small;
     L.blocks = split.blocks;
     L.step = split.warps;
     L.step_block = split.warps % split.blocks;

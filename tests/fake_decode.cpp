@@ -18,7 +18,7 @@ cudaError_t launch_rotary(const RotaryLaunch& L, cudaStream_t) { return g_rotary
 cudaError_t launch_append_rotary(const AppendRotaryLaunch&, cudaStream_t) { return launched(); }
 cudaError_t launch_beams(const BeamLaunch&, cudaStream_t) { return launched(); }
 cudaError_t launch_reorder(const ReorderLaunch& L, cudaStream_t) { return g_reorder = L, launched(); }
-BeamSplit beam_split(int64_t, int, int vocab, int, int, int) { return {vocab / 8 + 1, 128, 7, vocab / 1024 + 1, 304, 4864}; }
+BeamSplit beam_split(int64_t, int, int vocab, int, int, int) { return {vocab / 8 + 1, 128, 7, vocab / 1024 + 1, 304, 4864, 0}; }
 }  // namespace evisel
 
 extern "C" {
