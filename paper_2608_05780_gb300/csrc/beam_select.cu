@@ -1,5 +1,5 @@
 // The highest continuations over a sequence's beams and the vocabulary, in two
-// launches. A row of logits is cut into blocks of 1,024 tokens (512 in 32 bits; powers of two more for
+// launches (or, of few logits, one). A row of logits is cut into blocks of 1,024 tokens (512 in 32 bits; powers of two more for
 // long rows); a warp streams a block and leaves its maximum and its sum of exponentials. Then a CTA per sequence forms
 // the rows' normalisers from the blocks' sums, takes the n highest blocks by their maxima (ties in
 // order), in which all of the n highest continuations lie, and reads those again: for any

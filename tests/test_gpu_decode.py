@@ -497,6 +497,21 @@ def test_equal_beams_tie(cuda_lib, dtype, vocab):
         assert scores[0, :len(first)].unique().numel() == 1
 
 
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 8192), ("fp16", 5001), ("fp32", 3003)])
+def test_beams_of_a_batch_and_alone(cuda_lib, dtype, vocab):
+    """A sequence's continuations are the same bits in a batch of two launches, in one of one launch, and by itself."""
+    import torch
+    ev, dt = cuda_lib, _types()[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    x = (torch.randn((45, 5, vocab), device="cuda", generator=gen) * 3).to(dt)
+    scores = -torch.rand((45, 5), device="cuda", generator=gen)
+    ended = torch.rand((45, 5), device="cuda", generator=gen) < 0.2
+    whole = ev.evisel_beam_select(x, scores, 12, finished=ended, eos=2)[:4]
+    for first, last in ((0, 1), (7, 27), (44, 45)):
+        part = ev.evisel_beam_select(x[first:last], scores[first:last].contiguous(), 12, finished=ended[first:last].contiguous(), eos=2)[:4]
+        assert all(torch.equal(a[first:last], b) for a, b in zip(whole, part)), first
+
+
 def test_beam_rows_past_32_bits(cuda_lib):
     """Strides of sequences and beams beyond 2^31 elements, from an odd one."""
     import torch
