@@ -6,6 +6,8 @@
 // written) take 45.6 us, 87% of a plain copy's rate, with 128 threads, five blocks per SM and two heads a block; 52 us with 256
 // threads and two blocks, 55 with one head (the angles twice), 77 with the library's sincospif in every head, one
 // token of a thread at a time and the means through unpadded columns of shared memory.
+// Pages of 16 with eight heads of 64: 57.6 us, 76.8 while half of the threads had no token; one head of 128: 34.6 for half the
+// bytes, bound by the angles (formed from a thread's own registers 31.5, but a step's one token of 32 sequences 4.3 for 3.7).
 #include "cache_pages.cuh"
 #include "rope.cuh"
 
@@ -16,30 +18,38 @@ constexpr int kThreads = 128, kWarps = kThreads / 32, kBlocks = 5;
 
 // As fill_page(), but D / 16 threads share a token, each with the two pieces of a head that hold its pairs, and a
 // block has HEADS heads: two where blocks are many, so that a token's turns are formed once for both, else one and
-// two tokens of it at a time. Either way a thread has eight loads on their way.
+// two tokens of it at a time. Either way a thread has eight loads on their way. Pages of 16 tokens with heads of 64
+// keep half of the threads busy: the other half takes the next heads.
+constexpr int groups_of(int d) { return kThreads / (d / 16); }       // of threads, with a token each
+template <int D>
+__host__ __device__ __forceinline__ int parts_of(int page) { return groups_of(D) > 16 && page == 16 ? 2 : 1; }
+
 template <class T, int D, bool INTER, int HEADS>
-__device__ __forceinline__ void fill_page_rotated(const AppendRotaryLaunch& L, int b, int h0, int page, const NewTokens& src,
+__device__ __forceinline__ void fill_page_rotated(const AppendRotaryLaunch& L, int b, int first_head, int page, const NewTokens& src,
                                                   float* mem) {
-  constexpr int LANES = D / 16, GROUPS = kThreads / LANES, TOKENS = 2 / HEADS;
+  constexpr int LANES = D / 16, TOKENS = 2 / HEADS;
+  static_assert(groups_of(D) <= 32);             // (two parts at most: pages have 16 tokens or more)
   const CacheView& c = L.a.c;
+  const int parts = parts_of<D>(c.page), groups = groups_of(D) / parts, part = threadIdx.x / LANES / groups;
+  const int behind = part * HEADS, h0 = first_head + behind;
   const int p0 = page << c.log_page, p1 = min(p0 + c.page, src.end());
   if (p1 <= p0 || p1 <= src.first()) return;     // (the whole block)
   // The page (the heads share a table), which the loads of new tokens need not wait for.
   const int64_t id = __ldg(c.table + b * c.ts[0] + page);
   uint16_t* k = static_cast<uint16_t*>(const_cast<void*>(c.k)) + h0 * c.ks[1];
   uint16_t* v = static_cast<uint16_t*>(const_cast<void*>(c.v)) + h0 * c.vs[1];
-  const int j = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+  const int j = threadIdx.x % LANES, grp = threadIdx.x / LANES - part * groups;
   const bool rotates = 8 * j < L.rope.pairs;
   int lo, hi;
   lane_pieces(L.rope, j, lo, hi);
   float sum_lo[HEADS][8] = {}, sum_hi[HEADS][8] = {};
-  for (int base = p0 + grp; base < p1; base += GROUPS * TOKENS) {
+  for (int base = h0 < c.hkv ? p0 + grp : p1; base < p1; base += groups * TOKENS) {
     uint4 a[2], w[2], x[2], y[2];
     bool fresh[TOKENS], in[TOKENS];
     int at[TOKENS][3];
 #pragma unroll
     for (int t = 0; t < TOKENS; ++t) {
-      const int pos = base + t * GROUPS;
+      const int pos = base + t * groups;
       fresh[t] = pos < p1 && pos >= src.first();
       in[t] = fresh[t] || (pos < p1 && c.k_mean);                  // an older token is read for the mean only
       const int i = fresh[t] ? src.token(pos) : 0;
@@ -48,7 +58,7 @@ __device__ __forceinline__ void fill_page_rotated(const AppendRotaryLaunch& L, i
         const int n = t * HEADS + u;
         a[n] = w[n] = make_uint4(0, 0, 0, 0);
         if (fresh[t]) {
-          const uint4 *kr = src.key(i, u), *vr = src.value(i, u);
+          const uint4 *kr = src.key(i, behind + u), *vr = src.value(i, behind + u);
           a[n] = kr[lo], w[n] = kr[hi], x[n] = vr[lo], y[n] = vr[hi];
         }
       }
@@ -57,7 +67,7 @@ __device__ __forceinline__ void fill_page_rotated(const AppendRotaryLaunch& L, i
     if (static_cast<uint64_t>(id) >= static_cast<uint64_t>(c.n_pages)) break;
 #pragma unroll
     for (int t = 0; t < TOKENS; ++t) {
-      const int slot = base + t * GROUPS - p0;
+      const int slot = base + t * groups - p0;
       if (in[t] && !fresh[t]) {
 #pragma unroll
         for (int u = 0; u < HEADS; ++u) {
@@ -97,7 +107,7 @@ __device__ __forceinline__ void fill_page_rotated(const AppendRotaryLaunch& L, i
   }
   if (!c.k_mean) return;
   // A warp's tokens by shuffles, the warps' sums through shared memory.
-  constexpr int WARPS = kThreads / 32;
+  const int warps = kWarps / parts;              // of a part
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
   for (int u = 0; u < HEADS; ++u) {
@@ -109,7 +119,7 @@ __device__ __forceinline__ void fill_page_rotated(const AppendRotaryLaunch& L, i
         sum_hi[u][e] += __shfl_xor_sync(0xffffffffu, sum_hi[u][e], o);
       }
     if (lane < LANES) {
-      float4* m = reinterpret_cast<float4*>(mem + (u * WARPS + warp) * D);
+      float4* m = reinterpret_cast<float4*>(mem + ((behind + u) * warps + warp - part * warps) * D);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         m[lo * 2 + e] = make_float4(sum_lo[u][4 * e], sum_lo[u][4 * e + 1], sum_lo[u][4 * e + 2], sum_lo[u][4 * e + 3]);
@@ -119,12 +129,13 @@ __device__ __forceinline__ void fill_page_rotated(const AppendRotaryLaunch& L, i
   }
   __syncthreads();
   const float n = static_cast<float>(p1 - p0);
-  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(const_cast<void*>(c.k_mean)) + (id * c.hkv + h0) * D);
-  for (int i = threadIdx.x; i < HEADS * D / 2; i += kThreads) {
-    const float* m = mem + (i / (D / 2) * WARPS) * D + i % (D / 2) * 2;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(const_cast<void*>(c.k_mean)) + (id * c.hkv + first_head) * D);
+  for (int i = threadIdx.x; i < min(HEADS * parts, c.hkv - first_head) * (D / 2); i += kThreads) {
+    const float* m = mem + (i / (D / 2) * warps) * D + i % (D / 2) * 2;
     float p = 0.f, q = 0.f;
 #pragma unroll
-    for (int g = 0; g < WARPS; ++g) p += m[g * D], q += m[g * D + 1];
+    for (int g = 0; g < kWarps; ++g)
+      if (g < warps) p += m[g * D], q += m[g * D + 1];
     dst[i] = T::pack(p / n, q / n);
   }
 }
@@ -134,11 +145,12 @@ __global__ void __launch_bounds__(kThreads, kBlocks) cache_append_rotary_kernel(
                                                                            int share, int shares) {
   __shared__ __align__(16) float mem[kThreads * 16];
   const CacheView& c = L.a.c;
-  const int64_t kv_blocks = static_cast<int64_t>(pages) * (c.hkv / HEADS) * c.batch;
+  const int heads = HEADS * parts_of<D>(c.page), head_blocks = (c.hkv + heads - 1) / heads;
+  const int64_t kv_blocks = static_cast<int64_t>(pages) * head_blocks * c.batch;
   ptx::grid_wait();
   ptx::grid_launch_next();
   if (blockIdx.x < kv_blocks) {
-    const int x = blockIdx.x % pages, bh = blockIdx.x / pages, b = bh / (c.hkv / HEADS), h = (bh - b * (c.hkv / HEADS)) * HEADS;
+    const int x = blockIdx.x % pages, bh = blockIdx.x / pages, b = bh / head_blocks, h = (bh - b * head_blocks) * heads;
     const NewTokens src(L.a, b, h);
     if (x == 0 && h == 0 && threadIdx.x == 0) L.a.lens_out[b] = src.end();
     fill_page_rotated<T, D, INTER, HEADS>(L, b, h, (src.len >> c.log_page) + x, src, mem);
@@ -162,7 +174,8 @@ cudaError_t launch_d(const AppendRotaryLaunch& L, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(L.a.c.batch) * tokens;
   int64_t grid = static_cast<int64_t>(pages) * L.a.c.hkv * L.a.c.batch;
   const int heads = L.a.c.hkv % 2 == 0 && grid >= kBlocks * 2 * static_cast<int64_t>(sm_count()) ? 2 : 1;
-  grid /= heads;
+  const int block_heads = heads * parts_of<D>(L.a.c.page);
+  grid = static_cast<int64_t>(pages) * ((L.a.c.hkv + block_heads - 1) / block_heads) * L.a.c.batch;
   int share = 1, shares = 1;
   if (L.q.heads > 0 && rows > 0) {
     share = rotary_heads_per_warp(rows, L.q.heads, D, sm_count());
