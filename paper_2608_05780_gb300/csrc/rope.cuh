@@ -83,28 +83,22 @@ constexpr int kHeadsAtOnce = 4;                  // passes whose loads are in fl
 
 // Heads [h0, h1) of the q and k heads of token t of sequence b, by one warp: the
 // lanes form the token's turns once (mem: D / 2 entries of the warp's own) and every
-// D / 16 lanes rotate a head.
-template <class T, int D, bool INTER>
+// D / 16 lanes rotate a head, AT of them at a time.
+template <class T, int D, bool INTER, int AT = kHeadsAtOnce>
 __device__ __forceinline__ void rotate_token(const RopeView& r, const HeadsView& q, const HeadsView& k, int b, int t,
                                              const int (&pos)[3], float sign, int h0, int h1, float2* mem) {
   constexpr int LANES = D / 16, HEADS = 32 / LANES;
   const int lane = threadIdx.x & 31, j = lane % LANES;
-  for (int i = lane; i < r.pairs; i += 32) mem[i] = pair_turn(r, pos, i, sign);
-  __syncwarp();
-  const bool rotates = 8 * j < r.pairs;
-  float2 cs[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) cs[e] = rotates ? mem[8 * j + e] : make_float2(1.f, 0.f);
   int lo, hi;
   lane_pieces(r, j, lo, hi);
   const uint16_t* q_in = static_cast<const uint16_t*>(q.in) + b * q.is[0] + t * q.is[1];
   const uint16_t* k_in = static_cast<const uint16_t*>(k.in) + b * k.is[0] + t * k.is[1];
   uint16_t* q_out = static_cast<uint16_t*>(q.out) + b * q.os[0] + t * q.os[1];
   uint16_t* k_out = static_cast<uint16_t*>(k.out) + b * k.os[0] + t * k.os[1];
-  for (int base = h0 + lane / LANES; base < h1; base += HEADS * kHeadsAtOnce) {
-    uint4 a[kHeadsAtOnce], c[kHeadsAtOnce];
+  uint4 a[AT], c[AT];
+  auto load = [&](int base) {
 #pragma unroll
-    for (int i = 0; i < kHeadsAtOnce; ++i) {
+    for (int i = 0; i < AT; ++i) {
       const int h = base + i * HEADS;
       if (h < h1) {
         const uint4* row = reinterpret_cast<const uint4*>(h < q.heads ? q_in + h * q.is[2] : k_in + (h - q.heads) * k.is[2]);
@@ -112,8 +106,18 @@ __device__ __forceinline__ void rotate_token(const RopeView& r, const HeadsView&
         c[i] = row[hi];
       }
     }
+  };
+  int base = h0 + lane / LANES;
+  load(base);                       // on their way while the turns are formed
+  for (int i = lane; i < r.pairs; i += 32) mem[i] = pair_turn(r, pos, i, sign);
+  __syncwarp();
+  const bool rotates = 8 * j < r.pairs;
+  float2 cs[8];
 #pragma unroll
-    for (int i = 0; i < kHeadsAtOnce; ++i) {
+  for (int e = 0; e < 8; ++e) cs[e] = rotates ? mem[8 * j + e] : make_float2(1.f, 0.f);
+  while (base < h1) {
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
       const int h = base + i * HEADS;
       if (h < h1) {
         uint4* row = reinterpret_cast<uint4*>(h < q.heads ? q_out + h * q.os[2] : k_out + (h - q.heads) * k.os[2]);
@@ -122,6 +126,8 @@ __device__ __forceinline__ void rotate_token(const RopeView& r, const HeadsView&
         row[hi] = c[i];
       }
     }
+    base += HEADS * AT;
+    load(base);
   }
 }
 
