@@ -385,6 +385,7 @@ __device__ __forceinline__ int token_of(Key rest) { return 0xffffff - static_cas
 
 struct MergeShared {
   Two offset[kMaxBeams];                         // score - normaliser; NaN: no continuations from the logits
+  float score[kMaxBeams];                        // of a beam that goes on from its logits, else NaN
   float ended_score[kMaxBeams];                  // of a beam that has ended; NaN: it has not, or has none
   Key listed_value[kList], value[kList], rest[kList];
   int id[kList], chosen[kMaxBeamsOut];           // blocks
@@ -455,7 +456,7 @@ struct Blocks {
   const BeamLaunch& L;
   const MergeShared& s;
   const float2* part;               // of the sequence
-  int row0, b;
+  int b;
   __device__ __forceinline__ int beam(int id) const { return L.blocks == 1 ? id : static_cast<int>(__umulhi(id, L.inverse_blocks)); }
   // What block `id` has at most, its maximum being x.
   __device__ __forceinline__ Key key(int id, float x) const {
@@ -523,11 +524,23 @@ __device__ __forceinline__ void take_chosen(const Blocks& all, int chosen, Key l
       });
 }
 
-// The choice for sequence b, by a CTA; s.listed and s.count are 0.
+// What choose() needs of the inputs. (They were there before the scan was: nothing to wait for.)
+__device__ __forceinline__ void begin(const BeamLaunch& L, MergeShared& s, int b) {
+  if (threadIdx.x == 0) s.count = s.listed = 0;
+  for (int k = threadIdx.x; k < L.beams; k += kMergeThreads) {
+    const int ended = L.finished ? __ldg(L.finished + b * L.beams + k) : 0;
+    const float score = L.scores ? __ldg(L.scores + b * L.beams + k) : 0.f;
+    s.score[k] = ended == 0 && isfinite(score) ? score : NAN;
+    s.ended_score[k] = ended && isfinite(score) ? score : NAN;
+    s.ended[k] = ended ? 1 : 0;
+  }
+}
+
+// The choice for sequence b, by a CTA, behind begin() and a barrier.
 template <class T, bool kSkewed>
 __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int b) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Blocks all{L, s, L.part + static_cast<int64_t>(b) * L.beams * L.blocks, b * L.beams, b};
+  const Blocks all{L, s, L.part + static_cast<int64_t>(b) * L.beams * L.blocks, b};
   // Each row's normaliser, by a warp; the first blocks' maxima on their way meanwhile.
   const int ids = L.beams * L.blocks;
   float first[kHeld];
@@ -537,15 +550,9 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
     first[i] = id < ids ? all.part[id].x : -INFINITY;              // (of ended beams not used)
   }
   for (int k = warp; k < L.beams; k += kMergeWarps) {
-    const int ended = L.finished ? __ldg(L.finished + all.row0 + k) : 0;
-    const float score = L.scores ? __ldg(L.scores + all.row0 + k) : 0.f;
-    const bool live = ended == 0 && isfinite(score);
-    const Two lse = live ? normaliser(all.part + k * static_cast<int64_t>(L.blocks), L.blocks) : Two{NAN, NAN};
-    if (lane == 0) {
-      s.offset[k] = add({-lse.hi, -lse.lo}, score);
-      s.ended_score[k] = ended && isfinite(score) ? score : NAN;
-      s.ended[k] = ended ? 1 : 0;
-    }
+    const float score = s.score[k];
+    const Two lse = score == score ? normaliser(all.part + k * static_cast<int64_t>(L.blocks), L.blocks) : Two{NAN, NAN};
+    if (lane == 0) s.offset[k] = add({-lse.hi, -lse.lo}, score);
   }
   __syncthreads();
 
@@ -703,7 +710,7 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
 template <class T, bool kSkewed>
 __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __grid_constant__ BeamLaunch L) {
   __shared__ MergeShared s;
-  if (threadIdx.x == 0) s.count = s.listed = 0;
+  begin(L, s, blockIdx.x);
   __syncthreads();
   ptx::grid_wait();
   ptx::grid_launch_next();
@@ -718,9 +725,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm) beam_small_kernel(const __gr
   static_assert(kThreads == kMergeThreads);
   __shared__ MergeShared s;
   const unsigned rank = ptx::cluster_rank(), b = blockIdx.x / kCluster, first = b * L.beams * L.blocks;
-  if (threadIdx.x == 0) s.count = s.listed = 0;
   ptx::grid_wait();
   ptx::grid_launch_next();
+  begin(L, s, b);
   scan<T, kSkewed>(L, first + rank * kWarps + (threadIdx.x >> 5), first + L.beams * L.blocks);
   __syncwarp();
   ptx::cluster_sync();              // (the blocks' maxima and sums are seen behind it)
