@@ -404,7 +404,10 @@ __device__ __noinline__ Two far_normaliser(const float2* part, int blocks) {
   double far = 0.0;
   for (int j = threadIdx.x & 31; j < blocks; j += 32) {
     const float2 p = part[j];
-    if (p.x == -INFINITY) continue;
+    if (p.x == -INFINITY) {
+      far += p.y;                   // 0, or not a number
+      continue;
+    }
     const double c = offset_c(p.x);
     const double from = is_near(p.x) ? 0.693147180559945309417 * (c + static_cast<double>(p.x) * static_cast<double>(kLog2eLow)) : static_cast<double>(p.x);
     far += static_cast<double>(p.y) * exp(from - static_cast<double>(top));
@@ -430,6 +433,11 @@ __device__ __forceinline__ Two normaliser(const float2* part, int blocks) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) top = fmaxf(top, p[i].x), far = far || (!is_near(p[i].x) && p[i].x != -INFINITY);
     top = warp_max(top);
+    if (top == -INFINITY) {         // sums of 0, or of what is no number; no exponent yet
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) sum.hi += p[i].y;
+      continue;
+    }
     const float to = fmaxf(exponent, is_near(top) ? ceilf(top * kLog2e) : 0.f);
     const float down = ptx::ex2(exponent - to);
     sum.hi *= down, sum.lo *= down;

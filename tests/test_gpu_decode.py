@@ -497,6 +497,39 @@ def test_equal_beams_tie(cuda_lib, dtype, vocab):
         assert scores[0, :len(first)].unique().numel() == 1
 
 
+@pytest.mark.parametrize("level", [-3.0, -300.0, -20000.0])
+def test_beam_rows_that_begin_with_forbidden_tokens(cuda_lib, level):
+    """More forbidden tokens than a warp has blocks at once, and then logits far below zero."""
+    import torch
+    rng = np.random.default_rng(9)
+    x = np.full((1, 2, 400000), -np.inf)
+    x[0, 0, 300000:] = rng.standard_normal(100000) + level
+    x[0, 1, ::2] = rng.standard_normal(200000) + level
+    x = torch.from_numpy(x).to(torch.float32)
+    scores = np.float32([[-1, -2]])
+    out = cuda_lib.evisel_beam_select(x.cuda(), torch.from_numpy(scores).cuda(), 64)
+    _check_beams(out, x.double().numpy(), scores, 64, label=str(level))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("far", [False, True])
+def test_beam_rows_with_a_block_that_is_no_number(cuda_lib, dtype, far):
+    """A NaN anywhere takes the whole row out, also where a block has nothing else and the row is far from zero."""
+    import torch
+    dt = _types()[dtype]
+    x = torch.randn((1, 4, 9000), device="cuda")
+    if far:
+        x[:, :3] += 3e6
+    x = x.to(dt)
+    x[0, 0, 2048:4096] = float("nan")
+    x[0, 1, 2048:4096] = float("-inf")
+    x[0, 1, 3000] = float("nan")
+    x[0, 2, 8999] = float("nan")
+    out = cuda_lib.evisel_beam_select(x, None, 9)
+    assert out[1][0].tolist() == [3] * 9
+    _check_beams(out, x.double().cpu().numpy(), np.zeros((1, 4)), 9)
+
+
 @pytest.mark.parametrize("dtype,vocab", [("bf16", 8192), ("fp16", 5001), ("fp32", 3003)])
 def test_beams_of_a_batch_and_alone(cuda_lib, dtype, vocab):
     """A sequence's continuations are the same bits in a batch of two launches, in one of one launch, and by itself."""
