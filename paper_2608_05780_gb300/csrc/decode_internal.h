@@ -74,6 +74,7 @@ struct ReorderLaunch {
   int32_t* lens_out;
   int* status;
   int beams, n_states;
+  int heads;                        // of a block
   const char* in[kMaxStates];
   char* out[kMaxStates];
   int64_t row_bytes[kMaxStates];
@@ -92,7 +93,7 @@ cudaError_t launch_rotary(const RotaryLaunch& L, cudaStream_t stream);
 cudaError_t launch_append_rotary(const AppendRotaryLaunch& L, cudaStream_t stream);
 cudaError_t launch_beams(const BeamLaunch& L, cudaStream_t stream);
 cudaError_t launch_reorder(const ReorderLaunch& L, cudaStream_t stream);
-// Bytes of a state row that a block copies.
-constexpr int kStateBytes = 16384;
+// Bytes of a state row that a block copies, and of a page's keys and values at most where it takes several heads.
+constexpr int kStateBytes = 16384, kPageBytes = 32768;
 
 }  // namespace evisel

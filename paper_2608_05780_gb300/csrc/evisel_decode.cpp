@@ -352,7 +352,8 @@ int evisel_cache_reorder(const evisel_cache* cache, const int32_t* parent, int32
                          range_of(cache->lens, 4 * ((batch - 1) * cache->lens_stride[0] + 1))};
     Range out[kMaxStates + 2] = {range_of(table_out, 4 * entries), range_of(lens_out, 4 * batch)};
     ReorderLaunch L{};
-    L.first_block[0] = static_cast<int>(batch * cache->hkv);
+    L.heads = std::min(cache->hkv, std::max(1, kPageBytes / (cache->page * cache->head_dim * 4)));
+    L.first_block[0] = static_cast<int>(batch * ((cache->hkv + L.heads - 1) / L.heads));
     int64_t blocks = L.first_block[0];
     for (int i = 0; i < n_states; ++i) {
       const evisel_state& s = states[i];

@@ -39,7 +39,7 @@ class _Calls:
         base = _get()
         self.empty, self.i32, self.f32, self.masks, self.dtypes = base.empty, base.i32, base.f32, base.masks, base.dtypes
         self.logits = {**base.dtypes, torch.float32: 2}
-        self.u8, self.bool = torch.uint8, torch.bool
+        self.bool = torch.bool
 
 
 def _decode():

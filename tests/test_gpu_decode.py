@@ -653,6 +653,15 @@ def test_reordering(cuda_lib, beams, grown, page, dtype, layout, d, mean):
     _check_reorder(ev, cache, parent, states)
 
 
+@pytest.mark.parametrize("hkv,d,page,layout", [(5, 128, 16, "nhd"), (9, 64, 16, "hnd"), (3, 64, 64, "nhd"), (1, 64, 32, "hnd")])
+def test_reordering_of_heads_in_groups(cuda_lib, hkv, d, page, layout):
+    """Heads that do not divide into the groups that a block copies; values and means of every head."""
+    import torch
+    rng = np.random.default_rng(hkv)
+    cache = _beam_cache(rng, cuda_lib, [page + 5, 3 * page - 1, 7], 4, 6, hkv, d, page, torch.bfloat16, layout, True)
+    _check_reorder(cuda_lib, cache, rng.integers(-1, 6, (3, 6)))
+
+
 def test_reordering_again_and_again(cuda_lib):
     """Many steps of appends and reorderings: every sequence's tokens are those of its line of parents, as plain lists."""
     import torch
