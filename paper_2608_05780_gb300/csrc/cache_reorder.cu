@@ -1,8 +1,9 @@
 // The beams that go on: tables and lengths by parent, the pages in progress of
-// further children copied, other states by row: a block per sequence and head (or several of up to 32 KB of
-// their pages together: 512 sequences of eight heads of 64, pages of 16, 8.1 us for 10.8) and per 16 KB of a state's row, all in one launch. Each block finds out by itself whose pages its sequence takes (64 parents are two registers of a warp),
-// rather than wait for another kernel. Small calls are its dependent loads (parents, lengths, table, page): 3.9 us for four beams; 128
-// beams with 135 KB of states each take 9.0, 70% of a plain copy's rate.
+// further children copied, other states by row, all in one launch: a block per sequence and head
+// (or several heads, of up to 32 KB of a page: 512 sequences of eight heads of 64 with pages of 16 take 8.1 us, 10.8 head by
+// head) and per 16 KB of a state's row. Each block finds out by itself whose pages its sequence takes (64 parents are two
+// registers of a warp), rather than wait for another kernel. Small calls are its dependent loads (parents, lengths, table, page):
+// 3.9 us for four beams; 128 beams with 135 KB of states each take 9.0, 70% of a plain copy's rate.
 #include "cache_common.cuh"
 #include "decode_internal.h"
 
