@@ -1,8 +1,9 @@
 // The highest continuations over a sequence's beams and the vocabulary, in two
 // launches (or, of few logits, one). A row of logits is cut into blocks of 1,024 tokens (512 in 32 bits; powers of two more for
 // long rows); a warp streams a block and leaves its maximum and its sum of exponentials. Then a CTA per sequence forms
-// the rows' normalisers from the blocks' sums, takes the n highest blocks by their maxima (ties in
-// order), in which all of the n highest continuations lie, and reads those again: for any
+// the rows' normalisers from the blocks' sums, takes the n highest blocks by where their highest continuations
+// stand (their values, then beam, logit and place: different logits may have the same value), in which
+// all of the n highest continuations lie, and reads those again: for any
 // continuation outside, each of the n blocks has one that stands before it.
 //
 // So the pass over the logits keeps no lists, and warps wait for nothing but their loads. What it costs beside the
@@ -122,9 +123,6 @@ __device__ __forceinline__ uint32_t order_bits(float x) {
 }
 __device__ __forceinline__ float from_order_bits(uint32_t b) { return __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b); }
 using Key = unsigned long long;
-
-// Whether (x, i) stands before (y, j): higher, or as high and earlier.
-__device__ __forceinline__ bool before(Key x, int i, Key y, int j) { return x > y || (x == y && i < j); }
 
 __device__ __forceinline__ float warp_max(float x) {
   float m;
@@ -372,10 +370,16 @@ __device__ __forceinline__ Two ln(Two s, int exponent) {
   return add(Two{q, fmaf(n, kLn2Low, fmaf(n, kLn2, -q))}, two_sum(2.f * t, fmaf(fmaf(2.f, t2, 2.f) * by, left, rest)));   // (artanh' = 1 + t^2 + ..)
 }
 
-// A continuation's place: by value, then by beam, logit and token.
-struct Place {
-  Key value, rest;
-  __device__ __forceinline__ bool operator>(const Place& o) const { return value > o.value || (value == o.value && rest > o.rest); }
+// A continuation's place: by value, then by beam, logit and token. A value may leave less of a logit than it has (fp32 logits
+// beside a score of -1e9, or near zero), so that the logit decides among equal ones of a beam. (One number of 128 bits, read in one
+// load: compared key by key, 64 sequences of 8 beams over 152,064 tokens took 33.6 us, and 32.4 so.)
+struct alignas(16) Place {
+  Key rest, value;
+  Place() = default;
+  __device__ __forceinline__ Place(Key value_, Key rest_) : rest(rest_), value(value_) {}
+  __device__ __forceinline__ bool operator>(const Place& o) const {
+    return (static_cast<unsigned __int128>(value) << 64 | rest) > (static_cast<unsigned __int128>(o.value) << 64 | o.rest);
+  }
 };
 __device__ __forceinline__ Key rest_of(int k, float x, int token) {
   return static_cast<Key>(63 - k) << 56 | static_cast<Key>(order_bits(x)) << 24 | static_cast<uint32_t>(0xffffff - token);
@@ -387,10 +391,11 @@ struct MergeShared {
   Two offset[kMaxBeams];                         // score - normaliser; NaN: no continuations from the logits
   float score[kMaxBeams];                        // of a beam that goes on from its logits, else NaN
   float ended_score[kMaxBeams];                  // of a beam that has ended; NaN: it has not, or has none
-  Key listed_value[kList], value[kList], rest[kList];
-  int id[kList], chosen[kMaxBeamsOut];           // blocks
+  Place place[kList];                            // of the listed blocks, then of continuations
+  int chosen[kMaxBeamsOut];                      // blocks
   uint32_t group_max[kMergeThreads], bound;
-  Key least, warp_value[kMergeWarps], warp_rest[kMergeWarps];
+  Place warp_place[kMergeWarps];
+  Key least;
   int listed, count;
   uint8_t ended[kMaxBeams];
 };
@@ -473,6 +478,8 @@ struct Blocks {
     if (offset.hi == offset.hi) return x > -INFINITY ? order_key(add(offset, x)) : 0;
     return id == k * static_cast<int>(L.blocks) ? ended(k) : 0;
   }
+  // Where its highest continuation stands among those of other blocks: within a beam, blocks are in the order of tokens.
+  __device__ __forceinline__ Place place(int id, float x, Key value) const { return {value, rest_of(beam(id), x, id)}; }
   __device__ __forceinline__ Key ended(int k) const {
     const float score = s.ended_score[k];
     return score == score ? order_key({score, 0.f}) : 0;
@@ -532,6 +539,22 @@ __device__ __forceinline__ void take_chosen(const Blocks& all, int chosen, Key l
       });
 }
 
+// The highest of the CTA's places. (Another barrier before the next call.)
+__device__ __forceinline__ Place highest_of(MergeShared& s, Place y) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const Place z{__shfl_xor_sync(0xffffffffu, y.value, o), __shfl_xor_sync(0xffffffffu, y.rest, o)};
+    if (z > y) y = z;
+  }
+  if ((threadIdx.x & 31) == 0) s.warp_place[threadIdx.x >> 5] = y;
+  __syncthreads();
+  for (int i = 0; i < kMergeWarps; ++i) {
+    const Place z = s.warp_place[i];
+    if (z > y) y = z;
+  }
+  return y;
+}
+
 // What choose() needs of the inputs. (They were there before the scan was: nothing to wait for.)
 __device__ __forceinline__ void begin(const BeamLaunch& L, MergeShared& s, int b) {
   if (threadIdx.x == 0) s.count = s.listed = 0;
@@ -575,50 +598,41 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
   for (int id = tid + kHeld * kMergeThreads; id < ids; id += kMergeThreads) best = max(best, all.key(id, all.part[id].x));
   const Key bound = max(static_cast<Key>(bound_of<kMergeThreads>(static_cast<uint32_t>(best >> 32), s.group_max, &s.bound, L.n, groups_for(L.n))) << 32, Key(1));
   if (best >= bound) {
-    auto list = [&](int id, Key key) {
+    auto list = [&](int id, float x, Key key) {
       if (key < bound) return;
       const int to = atomicAdd(&s.listed, 1);
-      if (to < kList) s.listed_value[to] = key, s.id[to] = id;
+      if (to < kList) s.place[to] = all.place(id, x, key);
     };
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) list(tid + i * kMergeThreads, held[i]);
-    for (int id = tid + kHeld * kMergeThreads; id < ids; id += kMergeThreads) list(id, all.key(id, all.part[id].x));
+    for (int i = 0; i < kHeld; ++i) list(tid + i * kMergeThreads, first[i], held[i]);
+    for (int id = tid + kHeld * kMergeThreads; id < ids; id += kMergeThreads) {
+      const float x = all.part[id].x;
+      list(id, x, all.key(id, x));
+    }
   }
   __syncthreads();
   const int listed = s.listed, chosen = min(listed, L.n);
   if (listed <= kList) {
     for (int i = tid; i < listed; i += kMergeThreads) {
-      const Key key = s.listed_value[i];
-      const int id = s.id[i];
+      const Place p = s.place[i];
       int rank = 0;
 #pragma unroll 8
-      for (int j = 0; j < listed; ++j) rank += before(s.listed_value[j], s.id[j], key, id) ? 1 : 0;
-      if (rank < L.n) s.chosen[rank] = id;
-      if (rank == L.n - 1) s.least = key;
+      for (int j = 0; j < listed; ++j) rank += s.place[j] > p ? 1 : 0;
+      if (rank < L.n) s.chosen[rank] = token_of(p.rest);
+      if (rank == L.n - 1) s.least = p.value;
     }
   } else {
     // Many as high as one another: the next one after the last, n times.
-    Key last = ~Key(0);
-    int last_id = -1;
+    Place last{~Key(0), ~Key(0)};
     for (int r = 0; r < L.n; ++r) {
-      Key y = 0;
-      int f = 0x7fffffff;
+      Place y{0, 0};
       for (int i = tid; i < ids; i += kMergeThreads) {
-        const Key key = all.key(i, all.part[i].x);
-        if (key >= bound && before(last, last_id, key, i) && before(key, i, y, f)) y = key, f = i;
+        const float x = all.part[i].x;
+        const Place p = all.place(i, x, all.key(i, x));
+        if (p.value >= bound && last > p && p > y) y = p;
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const Key z = __shfl_xor_sync(0xffffffffu, y, o);
-        const int g = __shfl_xor_sync(0xffffffffu, f, o);
-        if (before(z, g, y, f)) y = z, f = g;
-      }
-      if (lane == 0) s.warp_value[warp] = y, s.warp_rest[warp] = f;
-      __syncthreads();
-      for (int i = 0; i < kMergeWarps; ++i)
-        if (before(s.warp_value[i], static_cast<int>(s.warp_rest[i]), y, f)) y = s.warp_value[i], f = static_cast<int>(s.warp_rest[i]);
-      last = y, last_id = f;
-      if (tid == 0) s.chosen[r] = f, s.least = y;
+      last = y = highest_of(s, y);
+      if (tid == 0) s.chosen[r] = token_of(y.rest), s.least = y.value;
       __syncthreads();
     }
   }
@@ -644,7 +658,7 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
     }
     take_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
       const int to = atomicAdd(&s.count, 1);
-      if (to < kList) s.value[to] = p.value, s.rest[to] = p.rest;
+      if (to < kList) s.place[to] = p;
     });
     __syncthreads();
     if (s.count <= kList || tries > 0) break;
@@ -667,7 +681,7 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) {
         const int j = tid + i * kMergeThreads;
-        own[i] = j < count ? Place{s.value[j], s.rest[j]} : Place{0, 0};
+        own[i] = j < count ? s.place[j] : Place{0, 0};
         best = max(best, own[i].value);
       }
       const uint32_t high = bound_of<kMergeThreads>(static_cast<uint32_t>(best >> 32), s.group_max, &s.bound, L.n, kMergeThreads);
@@ -677,16 +691,16 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
       for (int i = 0; i < kOwn; ++i)
         if (own[i].value >> 32 >= high && own[i].value > 0) {
           const int to = atomicAdd(&s.count, 1);
-          s.value[to] = own[i].value, s.rest[to] = own[i].rest;
+          s.place[to] = own[i];
         }
       __syncthreads();
       count = s.count;
     }
     for (int i = tid; i < count; i += kMergeThreads) {
-      const Place p{s.value[i], s.rest[i]};
+      const Place p = s.place[i];
       int rank = 0;
 #pragma unroll 8
-      for (int j = 0; j < count; ++j) rank += Place{s.value[j], s.rest[j]} > p ? 1 : 0;
+      for (int j = 0; j < count; ++j) rank += s.place[j] > p ? 1 : 0;
       if (rank < L.n) put(rank, p);
     }
     for (int i = count + tid; i < L.n; i += kMergeThreads) put(i, {0, 0});
@@ -698,18 +712,7 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
     take_chosen<T, kSkewed>(all, chosen, least, [&](Place p) {
       if (last > p && p > y) y = p;
     });
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const Place z{__shfl_xor_sync(0xffffffffu, y.value, o), __shfl_xor_sync(0xffffffffu, y.rest, o)};
-      if (z > y) y = z;
-    }
-    if (lane == 0) s.warp_value[warp] = y.value, s.warp_rest[warp] = y.rest;
-    __syncthreads();
-    for (int i = 0; i < kMergeWarps; ++i) {
-      const Place z{s.warp_value[i], s.warp_rest[i]};
-      if (z > y) y = z;
-    }
-    last = y;
+    last = y = highest_of(s, y);
     if (tid == 0) put(r, y);
     __syncthreads();
   }
