@@ -152,8 +152,11 @@ typedef struct {
  * The pages from the one in progress on are a sequence's own: the first child of p
  * keeps p's, the e-th of a group's further children takes those of its e-th sequence without
  * a child, and gets the tokens of p's page in progress (keys, values and, with
- * k_mean, its mean) copied into its first. No page is lost or used twice, and none
- * is allocated. A sequence without a child may be shorter than the parent whose child
+ * k_mean, its mean) copied into its first. So from the pages in progress on no page is
+ * lost or used twice, and none is allocated. Before them the children of a parent share its pages, and full
+ * pages of a sequence without a child are in no table any more, unless others share them: a caller that
+ * gives pages back counts the tables that name them, and finds those that left as the pages that a
+ * group's rows of `table` name and its rows of table_out do not. A sequence without a child may be shorter than the parent whose child
  * takes its pages (the empty slots beside a prompt); longer by whole pages shows as EVISEL_EBOUNDS,
  * as does a parent >= K, which counts as negative, and the group's result is unspecified.
  *   cache      table and lens shared by the heads; batch a multiple of beams

@@ -242,8 +242,9 @@ def evisel_beam_select(logits, scores=None, n_out=None, finished=None, eos=-1, p
 def evisel_cache_reorder(cache, parent, states=(), table_out=None, lens_out=None, states_out=None, ws=None, stream=None):
     """The beams that go on: ``parent`` int32 [G, K] names, for each of the cache's G groups of K sequences, the one
     of its group that sequence j takes over from (negative: itself). Full pages are shared, the page in progress is
-    copied into a page of a sequence without a child, so that every sequence keeps pages of its own to append to. Each of ``states``
-    (contiguous tensors [G K, ...]) is gathered by parent.
+    copied into a page of a sequence without a child, so that every sequence keeps pages of its own to append to. Full pages
+    that only a sequence without a child had are in the cache's table, but not in the new one: free for whoever keeps
+    count of pages. Each of ``states`` (contiguous tensors [G K, ...]) is gathered by parent.
 
     Returns (table int32 [G K, n], lens int32 [G K], states, ws), to be assigned to the cache."""
     c = _decode()

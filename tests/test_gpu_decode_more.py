@@ -5,6 +5,8 @@ import math
 import numpy as np
 import pytest
 
+from test_gpu_decode import _beam_cache
+
 pytestmark = pytest.mark.gpu
 
 
@@ -52,3 +54,33 @@ def test_beam_logits_closer_than_a_value_tells(cuda_lib, dtype, batch, beams, vo
     out = cuda_lib.evisel_beam_select(x.to(dt).cuda(), scores.cuda(), n)
     _check_own_order(out, x.double().numpy(), n)
     assert cuda_lib.evisel_status(out[4]) == 0
+
+
+# --- reordering --------------------------------------------------------------------
+
+def test_pages_that_leave_the_tables(cuda_lib):
+    """Steps over several page ends: from the page in progress on every page stays in one table of its group; the full pages
+    that leave are those that only sequences without a child had, and are what the old table names and the new one does not."""
+    import torch
+    ev, rng, dt = cuda_lib, np.random.default_rng(12), torch.bfloat16
+    beams, page, prompts, steps, left = 4, 16, [5, 16, 31], 40, 0
+    cache, ws = _beam_cache(rng, ev, prompts, 0, beams, 2, 64, page, dt, "hnd", False, slack=steps), ev.Workspace()
+    new = torch.zeros((len(prompts) * beams, 1, 2, 64), dtype=dt, device="cuda")
+    for step in range(steps):
+        cache.lens, _ = ev.evisel_cache_append(cache, new, new, ws=ws)
+        old, lens = cache.table.cpu().numpy(), cache.lens.cpu().numpy()
+        parent = rng.integers(-1, beams, (len(prompts), beams)).astype(np.int32)
+        cache.table, cache.lens, _, _ = ev.evisel_cache_reorder(cache, torch.from_numpy(parent).cuda(), ws=ws)
+        now = cache.table.cpu().numpy()
+        for g in range(len(prompts)):
+            rows, goes_on = slice(g * beams, (g + 1) * beams), {p if p >= 0 else j for j, p in enumerate(parent[g].tolist())}
+            full = int(lens[g * beams]) // page
+            a, b = old[rows], now[rows]
+            own = [x[:, full:][x[:, full:] >= 0].tolist() for x in (a, b)]
+            assert sorted(own[0]) == sorted(own[1]) and len(set(own[1])) == len(own[1])
+            gone = set(a[a >= 0].tolist()) - set(b[b >= 0].tolist())
+            lines = [set(a[j, :full].tolist()) for j in range(beams)]
+            assert gone == set().union(*lines) - set().union(*(lines[j] for j in goes_on)), step
+            assert not set(b[b >= 0].tolist()) - set(a[a >= 0].tolist())
+            left += len(gone)
+    assert left > 0 and ev.evisel_status(ws) == 0
