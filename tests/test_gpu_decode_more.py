@@ -5,7 +5,9 @@ import math
 import numpy as np
 import pytest
 
-from test_gpu_decode import _beam_cache
+from cache_helpers import make_cache, tensor
+from oracle import decode as ref
+from test_gpu_decode import _beam_cache, _check_rotated, _rope
 
 pytestmark = pytest.mark.gpu
 
@@ -13,6 +15,55 @@ pytestmark = pytest.mark.gpu
 def _types():
     import torch
     return {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+# --- rotation ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,d,r,interleaved,batch,tokens,hq,hkv", [
+    ("bf16", 128, 128, False, 2, 2451, 28, 4), ("fp16", 128, 96, True, 1, 4901, 6, 2), ("bf16", 64, 64, False, 3, 1701, 16, 8),
+    ("fp16", 64, 32, True, 1, 4869, 9, 4), ("bf16", 128, 112, True, 1, 4873, 13, 5), ("fp16", 64, 48, False, 2, 2441, 4, 2),
+    ("bf16", 128, 128, False, 1, 1500, 28, 4), ("bf16", 128, 128, True, 2, 750, 13, 5), ("fp16", 64, 64, False, 1, 700, 65, 0)])
+def test_rotation_of_prompts(cuda_lib, dtype, d, r, interleaved, batch, tokens, hq, hkv):
+    """So many tokens that a warp has all heads of one, in several passes, or a share of them in two: forth, back, in place."""
+    import torch
+    ev, dtype, rng = cuda_lib, _types()[dtype], np.random.default_rng(tokens)
+    rope, freqs = _rope(ev, d, r, interleaved)
+    q, qr = tensor(rng, (batch, tokens, hq, d), dtype)
+    k, kr = tensor(rng, (batch, tokens, hkv, d), dtype) if hkv else (None, None)
+    pos = rng.integers(0, 70000, (batch, tokens)).astype(np.int32)
+    p = torch.from_numpy(pos).cuda()
+    for back in (False, True):
+        got = ev.evisel_rotary(rope, q, k, positions=p, transpose=back)
+        for y, x in zip(got, (qr, kr)):
+            if x is not None:
+                _check_rotated(y, *ref.rotate(x, pos, freqs, interleaved, transpose=back), 70000, dtype, f"back {back}")
+    ev.evisel_rotary(rope, q, k, positions=p, transpose=True, q_out=q, k_out=k)
+    assert torch.equal(q, got[0]) and (k is None or torch.equal(k, got[1]))
+
+
+# --- append ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,layout,d,page,interleaved,r,batch,tokens,hq,hkv", [
+    ("bf16", "hnd", 128, 64, False, 128, 3, 1700, 28, 4), ("fp16", "nhd", 64, 16, True, 32, 2, 2500, 40, 5),
+    ("bf16", "nhd", 128, 32, True, 96, 1, 1300, 21, 3)])
+def test_rotated_append_of_a_prompt_with_its_queries(cuda_lib, dtype, layout, d, page, interleaved, r, batch, tokens, hq, hkv):
+    """A warp then has all queries of a token, in several passes: they, keys and values as by evisel_rotary and
+    evisel_cache_append, bit by bit."""
+    import torch
+    ev, dtype, rng = cuda_lib, _types()[dtype], np.random.default_rng(tokens)
+    rope = ev.Rotary(d, r, interleaved=interleaved)
+    (k, _), (v, _), (q, _) = (tensor(rng, (batch, tokens, h, d), dtype) for h in (hkv, hkv, hq))
+    lens = [page + 3, 0, 5 * page][:batch]
+    place = torch.from_numpy((np.array(lens)[:, None] + np.arange(tokens)).astype(np.int32)).cuda()
+    at = torch.from_numpy(rng.integers(0, 9000, (batch, tokens)).astype(np.int32)).cuda()
+    for kw, p in ((dict(), place), (dict(positions=at), at)):
+        cache, _ = make_cache(rng, lens, hkv, d, page, dtype, layout, room=tokens, poison=False)
+        plain = ev.Cache(cache.k.clone(), cache.v.clone(), cache.table, cache.lens)
+        q_rot, k_rot = ev.evisel_rotary(rope, q, k, positions=p)
+        want, ws = ev.evisel_cache_append(plain, k_rot, v)
+        got, q_out, _ = ev.evisel_cache_append_rotary(cache, rope, k, v, q=q, ws=ws, **kw)
+        assert torch.equal(got, want) and torch.equal(cache.k, plain.k) and torch.equal(cache.v, plain.v)
+        assert torch.equal(q_out, q_rot) and ev.evisel_status(ws) == 0
 
 
 # --- beams -------------------------------------------------------------------------
@@ -56,6 +107,41 @@ def test_beam_logits_closer_than_a_value_tells(cuda_lib, dtype, batch, beams, vo
     assert cuda_lib.evisel_status(out[4]) == 0
 
 
+@pytest.mark.parametrize("dtype,batch,beams,vocab,n,ended", [
+    ("bf16", 200, 3, 20011, 6, 0.0), ("fp16", 200, 3, 20008, 6, 0.2), ("fp32", 90, 4, 20012, 8, 0.2), ("fp32", 90, 4, 20013, 8, 0.0),
+    ("bf16", 700, 17, 1025, 17, 0.1), ("bf16", 2, 16, 152064, 16, 0.0), ("fp16", 3, 16, 152065, 32, 0.2), ("fp32", 2, 64, 20001, 40, 0.1)])
+def test_beams_of_many_blocks(cuda_lib, dtype, batch, beams, vocab, n, ended):
+    """More blocks than warps, which then carry on to other beams and sequences; more blocks of a sequence than its threads
+    hold. Against sorted values in 64 bits, within twice the bound of test_gpu_decode; a beam's own order exactly."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    x = (torch.randn((batch, beams, vocab), device="cuda", generator=gen) * 2.5).to(_types()[dtype])
+    scores = -5 * torch.rand((batch, beams), device="cuda", generator=gen)
+    done = torch.rand((batch, beams), device="cuda", generator=gen) < ended
+    got_s, parent, token, finished, ws = cuda_lib.evisel_beam_select(x, scores, n, finished=done, eos=3, pad=1)
+    value = scores[..., None].double() + torch.log_softmax(x.double(), -1)
+    value[done] = -math.inf
+    value[..., 1][done] = scores[done].double()
+    # (Of beams that have all ended there may be fewer than n.)
+    there = torch.arange(n, device="cuda") < (value > -math.inf).sum((1, 2))[:, None]
+    assert cuda_lib.evisel_status(ws) == 0 and torch.equal(parent >= 0, there) and torch.equal(token >= 0, there)
+    assert bool((got_s[~there] == -math.inf).all()) and bool(finished[~there].all())
+    e = 2.0 ** -18 + 2.0 ** -22 + 2.0 ** -23 * (math.log(vocab) + 1)
+    k, v = parent.clamp(min=0).long(), token.clamp(min=0).long()
+    mine = value.flatten(1).gather(1, k * vocab + v)
+    assert bool(((mine - value.flatten(1).topk(n).values).abs() <= 2 * e)[there].all())
+    assert bool(((got_s - mine).abs() <= e + 2.0 ** -24 * mine.abs())[there].all())
+    assert torch.equal(finished[there], ((token == 3) | done.gather(1, k))[there])
+    # The j-th of a beam's own is the j-th of its logits (so that none comes twice).
+    x = x.masked_fill(done[..., None], -math.inf)
+    x[..., 1][done] = 0
+    order = torch.sort(x, descending=True, stable=True).indices[..., :n]
+    same = parent[:, :, None] == parent[:, None, :]
+    rank = (same & torch.ones((n, n), dtype=torch.bool, device="cuda").tril(-1)).sum(2)
+    rows = torch.arange(batch, device="cuda")[:, None]
+    assert torch.equal(order[rows, k, rank].int()[there], token[there])
+
+
 # --- reordering --------------------------------------------------------------------
 
 def test_pages_that_leave_the_tables(cuda_lib):
@@ -84,3 +170,41 @@ def test_pages_that_leave_the_tables(cuda_lib):
             assert not set(b[b >= 0].tolist()) - set(a[a >= 0].tolist())
             left += len(gone)
     assert left > 0 and ev.evisel_status(ws) == 0
+
+
+@pytest.mark.parametrize("what", ["parent", "lens", "page"])
+def test_reordering_writes_no_other_page(cuda_lib, what):
+    """Parents, lengths and pages out of range: every page but those that valid copies of the other slots go to stays as it
+    was, the other group's table and lengths are right."""
+    import torch
+    ev, rng = cuda_lib, np.random.default_rng(8)
+    cache = _beam_cache(rng, ev, [40, 40], 3, 3, 2, 64, 16, torch.bfloat16, "hnd", True, slack=20)
+    before = {n: getattr(cache, n).clone() for n in ("k", "v", "k_mean")}
+    lens, table = cache.lens.clone(), cache.table.clone()
+    own = table[:, 2].tolist()              # the pages in progress of 43 tokens
+    parent = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    source = {own[4]: own[3], own[5]: own[3]}
+    if what == "parent":
+        parent[0] = torch.tensor([0, 3, 0])
+        source[own[2]] = own[0]             # 3 counts as negative: the second slot stays
+    elif what == "lens":
+        lens[0] = 1 << 20
+    else:
+        table[0, 2], table[4, 2] = 1 << 20, -7
+        del source[own[4]]
+    cache.lens, cache.table = lens, table
+    got_table, got_lens, _, ws = ev.evisel_cache_reorder(cache, parent)
+    assert ev.evisel_status(ws) == -7
+    for name, old in before.items():
+        want = old.clone()
+        for to, at in source.items():
+            if name == "k_mean":
+                want[to] = old[at]
+            else:
+                want[to][:, :11] = old[at][:, :11]
+        now = getattr(cache, name)
+        changed = [i for i in range(len(old)) if not torch.equal(now[i], want[i])]
+        assert not changed, (name, changed)
+    want = table[3:].clone()
+    want[1:, :2] = table[3, :2]
+    assert torch.equal(got_table[3:], want) and got_lens[3:].tolist() == [43] * 3
