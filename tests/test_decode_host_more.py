@@ -1,4 +1,5 @@
 """Host side of the decoding-step calls, continued: pages that leave the tables."""
+import numpy as np
 
 from oracle import decode as ref
 
