@@ -94,7 +94,8 @@ int evisel_rotary(const evisel_rope* rope, const evisel_heads* q, const evisel_h
  *   draft  tokens, k_new and v_new with strides; hq, q and q_stride, or q == NULL
  *   q_out  device [B, T, hq, d] contiguous, 16-byte aligned: q itself where that is
  *          contiguous, or memory apart from every input (written); NULL without q
- * Everything else as in evisel_cache_append(): src, counts, lens_out, what is refused.
+ * Everything else as in evisel_cache_append(): src, counts, lens_out (here refused over the
+ * table and the positions, too).
  * Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED, EVISEL_ENOMEM, EVISEL_ECUDA. */
 int evisel_cache_append_rotary(const evisel_cache* cache, const evisel_rope* rope, const evisel_draft* draft,
                                const evisel_positions* positions, const int32_t* src, const int32_t* counts,

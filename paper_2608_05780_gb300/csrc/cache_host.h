@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdint>
 #include <string>
+#include <utility>
 
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
@@ -30,6 +31,52 @@ inline int cuda_fail(cudaError_t e, const char* what) {
 }
 
 inline bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+// Bytes [begin, end).
+struct Range {
+  uintptr_t begin, end;
+  bool meets(const Range& o) const { return begin < o.end && o.begin < end; }
+};
+
+inline Range range_of(const void* p, int64_t bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p);
+  return {x, x + (p ? static_cast<uintptr_t>(bytes) : 0)};
+}
+
+// A strided tensor: runs of `width` elements of `size` bytes, by up to three dimensions (strides in elements, not negative).
+struct Strided {
+  const void* p;
+  int size;
+  int64_t width;
+  int n;
+  int64_t sizes[3], strides[3];
+};
+
+// Whether the bytes of `r` hold any of t's own, not of what lies between its runs: in each dimension, outermost
+// first, only the first and the last place that reach into r can be there in part. (A dimension inside which another steps further than
+// its own step counts as one piece.)
+inline bool meets(const Range& r, Strided t) {
+  using Wide = __int128;            // strides may be any number
+  if (!t.p || r.begin >= r.end || t.width <= 0) return false;
+  Wide inner[4] = {static_cast<Wide>(t.width) * t.size};          // bytes of the dimensions inside
+  for (int i = 0; i < t.n; ++i) {
+    if (t.sizes[i] <= 0) return false;
+    if (t.sizes[i] == 1) t.strides[i] = 0;
+    for (int j = i; j > 0 && t.strides[j] < t.strides[j - 1]; --j) std::swap(t.strides[j], t.strides[j - 1]), std::swap(t.sizes[j], t.sizes[j - 1]);
+  }
+  for (int i = 0; i < t.n; ++i) inner[i + 1] = inner[i] + static_cast<Wide>(t.sizes[i] - 1) * t.strides[i] * t.size;
+  const auto found = [&](const auto& self, Wide base, int i) -> bool {
+    if (base >= r.end || base + inner[i] <= r.begin) return false;
+    const Wide step = i > 0 ? static_cast<Wide>(t.strides[i - 1]) * t.size : 0;
+    if (i == 0 || base >= r.begin || (step > 0 && step < inner[i - 1])) return true;
+    if (step == 0) return self(self, base, i - 1);
+    const Wide behind = static_cast<Wide>(r.begin) - base - inner[i - 1], before = static_cast<Wide>(r.end) - base - 1;
+    const Wide first = behind < 0 ? 0 : behind / step + 1, last = std::min<Wide>(t.sizes[i - 1] - 1, before / step);
+    if (last - first >= 2) return true;
+    return first <= last && (self(self, base + first * step, i - 1) || self(self, base + last * step, i - 1));
+  };
+  return found(found, reinterpret_cast<uintptr_t>(t.p), t.n);
+}
 
 // Whether two runs of 32-bit values share any.
 inline bool overlap(const int32_t* a, int64_t na, const int32_t* b, int64_t nb) {
@@ -100,6 +147,10 @@ inline CacheView view_of(const evisel_cache* c) {
   return v;
 }
 
+// Lengths and table that the heads share.
+inline Strided lens_of(const evisel_cache* c) { return {c->lens, 4, 1, 1, {c->batch}, {c->lens_stride[0]}}; }
+inline Strided table_of(const evisel_cache* c) { return {c->table, 4, c->max_pages, 1, {c->batch}, {c->table_stride[0]}}; }
+
 // What an append needs of its arguments.
 inline int check_append(const evisel_cache* cache, const evisel_draft* draft, const int32_t* src, const int32_t* counts,
                         const int32_t* lens_out, evisel_ws** ws_inout) {
@@ -119,6 +170,9 @@ inline int check_append(const evisel_cache* cache, const evisel_draft* draft, co
   if (overlap(lens_out, cache->batch, counts, cache->batch) ||
       overlap(lens_out, cache->batch, src, static_cast<int64_t>(cache->batch) * draft->tokens))
     return fail(EVISEL_EINVAL, "lens_out must not overlap counts or src");
+  // Other blocks still read the lengths.
+  if (meets(range_of(lens_out, 4 * static_cast<int64_t>(cache->batch)), lens_of(cache)))
+    return fail(EVISEL_EINVAL, "lens_out must not overlap the cache's lens");
   if (draft->tokens > 0) {
     if (!draft->k_new || !draft->v_new) return fail(EVISEL_EINVAL, "k_new or v_new is NULL");
     if (misaligned(draft->k_new) || misaligned(draft->v_new)) return fail(EVISEL_EINVAL, "k_new and v_new must be 16-byte aligned");

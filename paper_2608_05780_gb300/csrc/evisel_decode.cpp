@@ -22,18 +22,8 @@ constexpr int64_t kMaxTokens = int64_t(1) << 30;
 constexpr int64_t kMaxRows = 65535;              // of logits, as many as a cache has sequences
 constexpr int kMaxVocab = 1 << 24;
 
-// Bytes [begin, end) that a strided tensor reaches.
-struct Range {
-  uintptr_t begin, end;
-  bool meets(const Range& o) const { return begin < o.end && o.begin < end; }
-};
-
-Range range_of(const void* p, int64_t bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(p);
-  return {x, x + (p ? static_cast<uintptr_t>(bytes) : 0)};
-}
-
-Range range_of(const void* p, const int64_t* stride, const int64_t* sizes, int head_dim) {
+// All that a strided tensor reaches.
+Range reach_of(const void* p, const int64_t* stride, const int64_t* sizes, int head_dim) {
   int64_t last = head_dim;
   for (int i = 0; i < 3; ++i) last += sizes[i] > 1 ? (sizes[i] - 1) * stride[i] : 0;
   return range_of(p, 2 * last);
@@ -105,7 +95,7 @@ int check_heads(const evisel_heads* h, const char* what) {
       return fail(EVISEL_EINVAL, std::string(what) + ": strides of the output must be at least head_dim");
     same = same && (sizes[i] <= 1 || h->in_stride[i] == h->out_stride[i]);
   }
-  if (!same && range_of(h->in, h->in_stride, sizes, h->head_dim).meets(range_of(h->out, h->out_stride, sizes, h->head_dim)))
+  if (!same && reach_of(h->in, h->in_stride, sizes, h->head_dim).meets(reach_of(h->out, h->out_stride, sizes, h->head_dim)))
     return fail(EVISEL_EINVAL, std::string(what) + ": out must be in itself with the same strides, or apart from it");
   return EVISEL_OK;
 }
@@ -124,10 +114,10 @@ HeadsView view_of(const evisel_heads* h) {
 int check_apart(const evisel_heads* a, const evisel_heads* b) {
   if (a->heads == 0 || b->heads == 0) return EVISEL_OK;
   const int64_t na[3] = {a->batch, a->tokens, a->heads}, nb[3] = {b->batch, b->tokens, b->heads};
-  const Range out = range_of(a->out, a->out_stride, na, a->head_dim);
-  if (a->out != a->in && out.meets(range_of(b->in, b->in_stride, nb, b->head_dim)))
+  const Range out = reach_of(a->out, a->out_stride, na, a->head_dim);
+  if (a->out != a->in && out.meets(reach_of(b->in, b->in_stride, nb, b->head_dim)))
     return fail(EVISEL_EINVAL, "an output lies over the other input");
-  if (a->out == b->out || (a->out != a->in && out.meets(range_of(b->out, b->out_stride, nb, b->head_dim))))
+  if (a->out == b->out || (a->out != a->in && out.meets(reach_of(b->out, b->out_stride, nb, b->head_dim))))
     return fail(EVISEL_EINVAL, "the outputs lie over one another");
   return EVISEL_OK;
 }
@@ -209,6 +199,8 @@ int evisel_cache_append_rotary(const evisel_cache* cache, const evisel_rope* rop
     if (rc == EVISEL_OK) rc = check_positions(positions);
     if (rc != EVISEL_OK) return rc;
     if (cache->batch == 0) return EVISEL_OK;
+    if (meets(range_of(lens_out, 4 * static_cast<int64_t>(cache->batch)), table_of(cache)))
+      return fail(EVISEL_EINVAL, "lens_out must not overlap the cache's table");
     if (overlap(lens_out, cache->batch, positions->first, cache->batch))
       return fail(EVISEL_EINVAL, "lens_out must not overlap the positions");
     if (positions->at && draft->tokens > 0) {
@@ -229,8 +221,8 @@ int evisel_cache_append_rotary(const evisel_cache* cache, const evisel_rope* rop
       if (draft->tokens > 0) {
         const int64_t sizes[3] = {cache->batch, draft->tokens, cache->hkv};
         const Range out = range_of(q_out, 2 * h.out_stride[0] * cache->batch);
-        if (out.meets(range_of(draft->k_new, draft->k_new_stride, sizes, cache->head_dim)) ||
-            out.meets(range_of(draft->v_new, draft->v_new_stride, sizes, cache->head_dim)))
+        if (out.meets(reach_of(draft->k_new, draft->k_new_stride, sizes, cache->head_dim)) ||
+            out.meets(reach_of(draft->v_new, draft->v_new_stride, sizes, cache->head_dim)))
           return fail(EVISEL_EINVAL, "q_out lies over k_new or v_new");
         L.q = view_of(&h);
       }

@@ -1,8 +1,106 @@
-"""Host side of the decoding-step calls, continued: pages that leave the tables."""
+"""Host side of the decoding-step calls, continued: outputs over what a call reads, pages that leave the tables."""
+import ctypes
+import itertools
+import os
+import subprocess
+
 import numpy as np
+import pytest
 
 from oracle import decode as ref
+from paper_2608_05780_gb300.build import CSRC, INCLUDE, nvcc
+from test_cache_host import FAKE, _append as _plain_append, _cache, _draft
+from test_decode_host import _append, _at, fake  # noqa: F401
 
+EINVAL = -1
+MB = 1 << 20
+
+
+def _run(fake, f):
+    """The call's return code; nothing was launched where it was refused."""
+    ws, n = ctypes.c_void_p(None), (fake.fake_launches(), fake.fake_decode_launches())
+    rc = f(ctypes.byref(ws))
+    assert (rc == 0) != ((fake.fake_launches(), fake.fake_decode_launches()) == n), fake.evisel_last_error()
+    fake.evisel_free(ws)
+    return rc
+
+
+# --- ranges ---------------------------------------------------------------------------
+
+def _bytes(p, size, width, sizes, strides):
+    out = set()
+    for at in itertools.product(*map(range, sizes)):
+        first = p + size * sum(a * s for a, s in zip(at, strides))
+        out.update(range(first, first + size * width))
+    return out
+
+
+def test_ranges(tmp_path):
+    """Against all bytes one by one: nested dimensions in any order, repeated ones, of one place and of none; dimensions
+    that step into one another count as one piece at least where they meet."""
+    out = str(tmp_path / "libranges.so")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    here = os.path.dirname(os.path.abspath(__file__))
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-I" + INCLUDE, "-I" + CSRC, "-I" + cuda,
+                    os.path.join(here, "fake_ranges.cpp"), "-o", out], check=True)
+    lib = ctypes.CDLL(out)
+    U64, I64 = ctypes.c_uint64, ctypes.c_int64
+    lib.ranges_meet.argtypes = [U64, U64, U64, ctypes.c_int, I64, ctypes.c_int, ctypes.POINTER(I64), ctypes.POINTER(I64)]
+    rng, met = np.random.default_rng(0), 0
+    for _ in range(4000):
+        n, size, width, p = int(rng.integers(0, 4)), int(rng.choice([1, 2, 4])), int(rng.integers(1, 5)), int(rng.integers(40, 60))
+        sizes, strides, step = rng.integers(1, 4, n).tolist(), [], width
+        nested = rng.random() < 0.8
+        for s in sizes:
+            step += int(rng.integers(0, 4))
+            strides.append(step if nested else int(rng.integers(0, 9)))
+            step += (s - 1) * step
+            if nested and rng.random() < 0.2:
+                strides[-1] = 0
+        if n and rng.random() < 0.1:
+            sizes[int(rng.integers(n))] = 0
+        order = rng.permutation(n)
+        sizes, strides = [sizes[i] for i in order], [strides[i] for i in order]
+        all_ = _bytes(p, size, width, sizes, strides)
+        for _ in range(12):
+            begin = int(rng.integers(30, max(all_, default=60) + 10))
+            end = begin + int(rng.integers(0, 12))
+            want = any(begin <= x < end for x in all_)
+            got = lib.ranges_meet(begin, end, p, size, width, n, (I64 * 3)(*sizes), (I64 * 3)(*strides))
+            assert bool(got) == want if nested else bool(got) >= want, (begin, end, p, size, width, sizes, strides)
+            met += want
+    assert met > 1000
+    far = (I64 * 3)(1 << 50, 1 << 62, 1 << 40)               # strides that no memory has
+    assert lib.ranges_meet(40, 50, 40, 4, 1, 3, (I64 * 3)(7, 7, 7), far) == 1
+    assert lib.ranges_meet(50, 60, 40, 4, 1, 3, (I64 * 3)(7, 7, 7), far) == 0
+    assert lib.ranges_meet(0, 60, 0, 4, 1, 1, (I64 * 3)(7), (I64 * 3)(1)) == 0          # no tensor
+
+
+# --- outputs over what a call reads ------------------------------------------------------
+
+LENS, TABLE = FAKE + 30 * MB, FAKE + 40 * MB
+
+
+@pytest.mark.parametrize("call", [_plain_append, _append])
+@pytest.mark.parametrize("stride,batch,at,code", [
+    (1, 2, 1, EINVAL), (1, 2, -1, EINVAL), (1, 2, 0, EINVAL), (1, 2, 2, 0), (1, 2, -2, 0), (5, 2, 1, 0), (5, 2, 4, EINVAL), (5, 2, 5, EINVAL),
+    (5, 2, 6, 0), (0, 2, 1, 0), (0, 2, -1, EINVAL), (0, 1, 1, 0)])
+def test_lengths_over_lengths(fake, call, stride, batch, at, code):  # noqa: F811
+    """An append writes lens_out while its other blocks still read the cache's lengths."""
+    kw = dict(c=_cache(lens=LENS, table=TABLE, lens_stride=(stride, 0), batch=batch), d=_draft(k_new=FAKE + 5 * MB, v_new=FAKE + 6 * MB),
+              lens_out=ctypes.c_void_p(LENS + 4 * at), src=_at(8 * MB), counts=_at(9 * MB))
+    assert _run(fake, lambda ws: call(fake, ws, **kw)) == code
+
+
+@pytest.mark.parametrize("stride,at,code", [
+    (50, 49, EINVAL), (50, 99, EINVAL), (50, -1, EINVAL), (50, 100, 0), (50, -2, 0), (60, 52, 0), (60, 59, EINVAL), (0, 50, 0), (0, 49, EINVAL)])
+def test_lengths_over_the_table(fake, stride, at, code):  # noqa: F811
+    """And the table, of 50 pages to a sequence."""
+    c = _cache(lens=LENS, table=TABLE, table_stride=(stride, 0))
+    assert _run(fake, lambda ws: _append(fake, ws, c=c, lens_out=ctypes.c_void_p(TABLE + 4 * at))) == code
+
+
+# --- the oracle's pins -------------------------------------------------------------------
 
 def test_oracle_pages_that_leave():
     """Two beams of 36 tokens that share a page of 16: the second's full page of its own is in no table afterwards, the
