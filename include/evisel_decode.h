@@ -92,8 +92,8 @@ int evisel_rotary(const evisel_rope* rope, const evisel_heads* q, const evisel_h
  * rotated in the same launch, all T of each sequence, token t as token t (without
  * `at` this needs src == NULL).
  *   draft  tokens, k_new and v_new with strides; hq, q and q_stride, or q == NULL
- *   q_out  device [B, T, hq, d] contiguous, 16-byte aligned: q itself where that is
- *          contiguous, or memory apart from every input (written); NULL without q
+ *   q_out  device [B, T, hq, d] contiguous, 16-byte aligned (written): q itself where that
+ *          is contiguous, or memory apart from every input, lens_out and the cache; NULL without q
  * Everything else as in evisel_cache_append(): src, counts, lens_out (here refused over the
  * table and the positions, too).
  * Errors: EVISEL_EINVAL, EVISEL_EUNSUPPORTED, EVISEL_ENOMEM, EVISEL_ECUDA. */

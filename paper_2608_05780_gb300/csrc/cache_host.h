@@ -150,6 +150,10 @@ inline CacheView view_of(const evisel_cache* c) {
 // Lengths and table that the heads share.
 inline Strided lens_of(const evisel_cache* c) { return {c->lens, 4, 1, 1, {c->batch}, {c->lens_stride[0]}}; }
 inline Strided table_of(const evisel_cache* c) { return {c->table, 4, c->max_pages, 1, {c->batch}, {c->table_stride[0]}}; }
+// The pool's keys or values.
+inline Strided pages_of(const evisel_cache* c, const void* p, const int64_t* stride) {
+  return {p, 2, c->head_dim, 3, {c->n_pages, c->hkv, c->page}, {stride[0], stride[1], stride[2]}};
+}
 
 // What an append needs of its arguments.
 inline int check_append(const evisel_cache* cache, const evisel_draft* draft, const int32_t* src, const int32_t* counts,

@@ -65,6 +65,11 @@ int check_positions(const evisel_positions* p) {
   return EVISEL_OK;
 }
 
+// Whether the bytes hold any of the positions that a call reads.
+bool meets_positions(const Range& out, const evisel_positions* p, int axes, int64_t batch, int64_t tokens) {
+  return meets(out, {p->at, 4, tokens, 2, {axes, batch}, {p->stride[0], p->stride[1]}}) || out.meets(range_of(p->first, 4 * batch));
+}
+
 PositionView view_of(const evisel_positions* p) {
   PositionView v{};
   v.at = p->at;
@@ -219,11 +224,21 @@ int evisel_cache_append_rotary(const evisel_cache* cache, const evisel_rope* rop
       rc = check_heads(&h, "q");
       if (rc != EVISEL_OK) return rc;
       if (draft->tokens > 0) {
-        const int64_t sizes[3] = {cache->batch, draft->tokens, cache->hkv};
+        const int64_t sizes[3] = {cache->batch, draft->tokens, cache->hkv}, rows = static_cast<int64_t>(cache->batch) * draft->tokens;
         const Range out = range_of(q_out, 2 * h.out_stride[0] * cache->batch);
         if (out.meets(reach_of(draft->k_new, draft->k_new_stride, sizes, cache->head_dim)) ||
             out.meets(reach_of(draft->v_new, draft->v_new_stride, sizes, cache->head_dim)))
           return fail(EVISEL_EINVAL, "q_out lies over k_new or v_new");
+        // (In its own place it lies where q was: the caller's to answer for.)
+        if (q_out != draft->q) {
+          if (meets(out, lens_of(cache)) || meets(out, table_of(cache)) || out.meets(range_of(src, 4 * rows)) ||
+              out.meets(range_of(counts, 4 * static_cast<int64_t>(cache->batch))) || meets_positions(out, positions, rope->axes, cache->batch, draft->tokens))
+            return fail(EVISEL_EINVAL, "q_out lies over lens, the table, src, counts or the positions");
+          if (out.meets(range_of(lens_out, 4 * static_cast<int64_t>(cache->batch))) || meets(out, pages_of(cache, cache->k, cache->k_stride)) ||
+              meets(out, pages_of(cache, cache->v, cache->v_stride)) ||
+              out.meets(range_of(cache->k_mean, 2 * static_cast<int64_t>(cache->n_pages) * cache->hkv * cache->head_dim)))
+            return fail(EVISEL_EINVAL, "q_out lies over lens_out or the cache's pages or means");
+        }
         L.q = view_of(&h);
       }
     }

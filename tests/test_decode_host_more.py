@@ -10,7 +10,7 @@ import pytest
 from oracle import decode as ref
 from paper_2608_05780_gb300.build import CSRC, INCLUDE, nvcc
 from test_cache_host import FAKE, _append as _plain_append, _cache, _draft
-from test_decode_host import _append, _at, fake  # noqa: F401
+from test_decode_host import _append, _at, _pos, _rope, fake  # noqa: F401
 
 EINVAL = -1
 MB = 1 << 20
@@ -98,6 +98,35 @@ def test_lengths_over_the_table(fake, stride, at, code):  # noqa: F811
     """And the table, of 50 pages to a sequence."""
     c = _cache(lens=LENS, table=TABLE, table_stride=(stride, 0))
     assert _run(fake, lambda ws: _append(fake, ws, c=c, lens_out=ctypes.c_void_p(TABLE + 4 * at))) == code
+
+
+SRC, COUNTS, LENS_OUT, AT, K, V, MEAN, Q_OUT = (FAKE + i * MB for i in (41, 42, 43, 44, 50, 60, 70, 80))
+Q_BYTES = 2 * 3 * 28 * 128 * 2      # of two sequences, three tokens, 28 heads of 128
+
+
+@pytest.mark.parametrize("over,at,code", [
+    (dict(), Q_OUT, 0), (dict(), LENS + 4, EINVAL), (dict(), LENS - Q_BYTES, 0), (dict(), LENS - Q_BYTES + 16, EINVAL), (dict(), LENS + 16, 0),
+    (dict(), TABLE + 384, EINVAL), (dict(), TABLE + 400, 0), (dict(), SRC, EINVAL), (dict(), SRC + 32, 0), (dict(), COUNTS, EINVAL),
+    (dict(), COUNTS + 16, 0), (dict(), LENS_OUT - 16, EINVAL), (dict(), LENS_OUT + 16, 0), (dict(), AT - Q_BYTES + 16, EINVAL),
+    (dict(pos=dict(at=AT, stride=(0, 65536))), AT + 16, 0), (dict(pos=dict(at=AT, stride=(0, 65536))), AT + 4 * 65536 - 16, EINVAL),
+    (dict(pos=dict(at=AT, stride=(65536, 3)), axes=3), AT + 8 * 65536, EINVAL), (dict(pos=dict(at=AT, stride=(65536, 3)), axes=3), AT + 4 * 65536 + 32, 0),
+    (dict(pos=dict(at=AT, stride=(65536, 3))), AT + 8 * 65536, 0), (dict(pos=dict(at=0, first=AT), src=0), AT, EINVAL),
+    (dict(pos=dict(at=0, first=AT), src=0), AT + 16, 0),
+    (dict(), K, EINVAL), (dict(), K + 100 * 65536, 0), (dict(), K + 100 * 65536 - 16, EINVAL), (dict(), V + 99 * 65536, EINVAL), (dict(), MEAN + 102384, EINVAL),
+    (dict(), MEAN + 102400, 0), (dict(mean=0), MEAN, 0),
+    (dict(k_stride=(131072, 8192, 128)), K + 65536, 0), (dict(k_stride=(131072, 8192, 128)), K + 262144 - 16, EINVAL),   # every second page of 64 KB
+    (dict(k_stride=(131072, 256, 1024)), K + 131072, 0), (dict(k_stride=(131072, 256, 1024)), K + 131072 - 512, EINVAL)])
+def test_queries_over_what_an_append_reads(fake, over, at, code):  # noqa: F811
+    """Rotated queries are written while other blocks read lengths, tables and positions and write pages; gaps between them
+    are nobody's."""
+    over = dict(over)
+    pos = _pos(**{**dict(at=AT, stride=(0, 3)), **over.pop("pos", {})})
+    rope = _rope(axes=3, section=(16, 24, 24)) if over.pop("axes", 1) == 3 else _rope()
+    src = ctypes.c_void_p(over.pop("src", SRC))
+    c = _cache(**{**dict(lens=LENS, table=TABLE, k=K, v=V, k_mean=over.pop("mean", MEAN)), **over})
+    kw = dict(c=c, rope=rope, pos=pos, src=src, counts=ctypes.c_void_p(COUNTS), lens_out=ctypes.c_void_p(LENS_OUT),
+              q_out=ctypes.c_void_p(at))
+    assert _run(fake, lambda ws: _append(fake, ws, **kw)) == code
 
 
 # --- the oracle's pins -------------------------------------------------------------------
