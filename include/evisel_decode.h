@@ -71,7 +71,7 @@ typedef struct {
   int64_t out_stride[3];           /* likewise, and not 0                             */
   const void* in;                  /* device, 16-byte aligned                         */
   void* out;                       /* device; `in` itself with the same strides, or memory
-                                      apart from it                                   */
+                                      apart from it; apart from the positions         */
 } evisel_heads;
 
 /* Rotates q and (unless NULL) k, which have the same batch, tokens, head_dim and

@@ -115,6 +115,25 @@ HeadsView view_of(const evisel_heads* h) {
   return v;
 }
 
+// Rotated heads over positions that other blocks still read. (Runs one by one where all that positions reach is
+// met: sequences' rows may hold their heads and, apart from them, their position.)
+int check_positions_apart(const evisel_heads* h, const evisel_positions* p, int axes) {
+  constexpr int64_t kRuns = 1 << 16, kFar = int64_t(1) << 61;
+  if (h->heads == 0) return EVISEL_OK;
+  const Strided out = {h->out, 2, h->head_dim, 3, {h->batch, h->tokens, h->heads}, {h->out_stride[0], h->out_stride[1], h->out_stride[2]}};
+  bool met = meets(range_of(p->first, 4 * static_cast<int64_t>(h->batch)), out);
+  if (p->at) {
+    const __int128 reach = static_cast<__int128>(p->stride[0]) * (axes - 1) + static_cast<__int128>(p->stride[1]) * (h->batch - 1) + h->tokens;
+    met = meets(range_of(p->at, static_cast<int64_t>(std::min<__int128>(4 * reach, kFar))), out);
+    if (met && static_cast<int64_t>(axes) * h->batch <= kRuns) {
+      met = false;
+      for (int64_t i = 0; i < static_cast<int64_t>(axes) * h->batch && !met; ++i)
+        met = meets(range_of(p->at + i / h->batch * p->stride[0] + i % h->batch * p->stride[1], 4 * static_cast<int64_t>(h->tokens)), out);
+    }
+  }
+  return met ? fail(EVISEL_EINVAL, "an output lies over the positions") : EVISEL_OK;
+}
+
 // One input's output over another input (each in its own place is the caller's to answer for: rows of one tensor).
 int check_apart(const evisel_heads* a, const evisel_heads* b) {
   if (a->heads == 0 || b->heads == 0) return EVISEL_OK;
@@ -178,6 +197,8 @@ int evisel_rotary(const evisel_rope* rope, const evisel_heads* q, const evisel_h
     if (q->batch == 0 || q->tokens == 0 || q->heads + (k ? k->heads : 0) == 0) return EVISEL_OK;
     if (k) rc = check_apart(q, k);
     if (k && rc == EVISEL_OK) rc = check_apart(k, q);
+    if (rc == EVISEL_OK) rc = check_positions_apart(q, positions, rope->axes);
+    if (k && rc == EVISEL_OK) rc = check_positions_apart(k, positions, rope->axes);
     if (rc != EVISEL_OK) return rc;
     if (sm_count() <= 0) return fail(EVISEL_ECUDA, "the device's multiprocessors cannot be counted");
     RotaryLaunch L{};

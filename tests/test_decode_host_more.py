@@ -10,7 +10,7 @@ import pytest
 from oracle import decode as ref
 from paper_2608_05780_gb300.build import CSRC, INCLUDE, nvcc
 from test_cache_host import FAKE, _append as _plain_append, _cache, _draft
-from test_decode_host import _append, _at, _pos, _rope, fake  # noqa: F401
+from test_decode_host import _append, _at, _heads, _pos, _rope, _rotary, fake  # noqa: F401
 
 EINVAL = -1
 MB = 1 << 20
@@ -127,6 +127,30 @@ def test_queries_over_what_an_append_reads(fake, over, at, code):  # noqa: F811
     kw = dict(c=c, rope=rope, pos=pos, src=src, counts=ctypes.c_void_p(COUNTS), lens_out=ctypes.c_void_p(LENS_OUT),
               q_out=ctypes.c_void_p(at))
     assert _run(fake, lambda ws: _append(fake, ws, **kw)) == code
+
+
+ROW = 2 * (28 * 128 + 8)            # of a sequence: 28 heads of 128, and 16 bytes that hold its position
+
+
+@pytest.mark.parametrize("pos,axes,heads,code", [
+    (dict(at=AT, stride=(6, 3)), 1, {}, 0), (dict(at=Q_OUT, stride=(6, 3)), 1, {}, EINVAL), (dict(at=Q_OUT + Q_BYTES - 4, stride=(6, 3)), 1, {}, EINVAL),
+    (dict(at=Q_OUT + Q_BYTES, stride=(6, 3)), 1, {}, 0), (dict(at=Q_OUT - 24, stride=(6, 3)), 1, {}, 0), (dict(at=Q_OUT - 20, stride=(6, 3)), 1, {}, EINVAL),
+    (dict(at=Q_OUT - 4096, stride=(1024, 3)), 3, {}, EINVAL), (dict(at=Q_OUT - 4096, stride=(20000, 3)), 3, {}, 0),
+    (dict(at=0, first=Q_OUT + 4), 1, {}, EINVAL), (dict(at=0, first=Q_OUT - 8), 1, {}, 0), (dict(at=0, first=Q_OUT - 4), 1, {}, EINVAL),
+    (dict(at=Q_OUT, stride=(6, 3)), 1, dict(heads=0), 0),
+    # one token of each of 200 sequences, whose rows hold queries and position
+    (dict(at=Q_OUT + ROW - 16, stride=(0, ROW // 4)), 1, dict(batch=200, tokens=1, out_stride=(ROW // 2, 0, 128)), 0),
+    (dict(at=Q_OUT + ROW - 20, stride=(0, ROW // 4)), 1, dict(batch=200, tokens=1, out_stride=(ROW // 2, 0, 128)), EINVAL)])
+def test_rotated_heads_over_positions(fake, pos, axes, heads, code):  # noqa: F811
+    """Of queries, then of keys."""
+    rope, pos = _rope(axes=3, section=(16, 24, 24)) if axes == 3 else _rope(), _pos(**pos)
+    mine = _heads(**{**dict(out=Q_OUT), **heads})
+    far = _heads(**{n: x for n, x in heads.items() if n != "heads"}, out=FAKE + (1 << 44))
+    assert _rotary(fake, None, rope, mine, None, pos) == code
+    assert _rotary(fake, None, rope, far, None, pos) == 0 and _rotary(fake, None, rope, far, mine, pos) == code
+    # Too many sequences to look at one by one, with strides that no memory has.
+    many, wide = _heads(out=Q_OUT, batch=1 << 28, tokens=4, out_stride=(1 << 30, 4096, 128)), _pos(at=Q_OUT - 4096, stride=(0, (1 << 38) - 1))
+    assert _rotary(fake, None, _rope(), many, None, wide) == EINVAL
 
 
 # --- the oracle's pins -------------------------------------------------------------------
