@@ -22,11 +22,43 @@ constexpr int64_t kMaxTokens = int64_t(1) << 30;
 constexpr int64_t kMaxRows = 65535;              // of logits, as many as a cache has sequences
 constexpr int kMaxVocab = 1 << 24;
 
-// All that a strided tensor reaches.
-Range reach_of(const void* p, const int64_t* stride, const int64_t* sizes, int head_dim) {
-  int64_t last = head_dim;
-  for (int i = 0; i < 3; ++i) last += sizes[i] > 1 ? (sizes[i] - 1) * stride[i] : 0;
-  return range_of(p, 2 * last);
+Strided heads_of(const void* p, const int64_t* stride, const int64_t* sizes, int head_dim) {
+  return {p, 2, head_dim, 3, {sizes[0], sizes[1], sizes[2]}, {stride[0], stride[1], stride[2]}};
+}
+
+// Heads [batch, token, head, d] in memory.
+struct HeadsAt {
+  const void* p;
+  const int64_t* stride;
+  int64_t heads;
+};
+
+// Whether two of them, of the same batch and tokens, share no memory: apart as wholes, or parts of the rows of
+// one tensor, where dimensions of one stride step over both.
+bool apart(const HeadsAt& a, const HeadsAt& b, int64_t batch, int64_t tokens, int head_dim) {
+  using Wide = __int128;
+  const Wide from = static_cast<Wide>(reinterpret_cast<uintptr_t>(b.p)) - reinterpret_cast<uintptr_t>(a.p);
+  const int64_t sizes[2] = {batch, tokens};
+  const auto step = [&](const HeadsAt& h, int i) { return 2 * (sizes[i] > 1 ? static_cast<Wide>(h.stride[i]) : 0); };
+  for (int rows = 0; rows < 4; ++rows) {         // the dimensions that step over both: bit 0 the batch's, bit 1 the tokens'
+    const auto reach = [&](const HeadsAt& h) {
+      Wide bytes = 2 * (head_dim + (h.heads > 1 ? (h.heads - 1) * static_cast<Wide>(h.stride[2]) : 0));
+      for (int i = 0; i < 2; ++i) bytes += rows >> i & 1 ? 0 : (sizes[i] - 1) * step(h, i);
+      return bytes;
+    };
+    const Wide ends[2] = {reach(a), from + reach(b)};
+    if (from < ends[0] && 0 < ends[1]) continue;
+    Wide both = std::max(ends[0], ends[1]) - std::min<Wide>(0, from);
+    bool nested = true;
+    const int inner = step(a, 0) < step(a, 1) ? 0 : 1;
+    for (const int i : {inner, 1 - inner}) {
+      if (!(rows >> i & 1) || sizes[i] <= 1) continue;
+      nested = nested && step(a, i) == step(b, i) && both <= step(a, i);
+      both += (sizes[i] - 1) * step(a, i);
+    }
+    if (nested) return true;
+  }
+  return false;
 }
 
 int check_rope(const evisel_rope* r, int head_dim) {
@@ -100,7 +132,7 @@ int check_heads(const evisel_heads* h, const char* what) {
       return fail(EVISEL_EINVAL, std::string(what) + ": strides of the output must be at least head_dim");
     same = same && (sizes[i] <= 1 || h->in_stride[i] == h->out_stride[i]);
   }
-  if (!same && reach_of(h->in, h->in_stride, sizes, h->head_dim).meets(reach_of(h->out, h->out_stride, sizes, h->head_dim)))
+  if (!same && !apart({h->in, h->in_stride, h->heads}, {h->out, h->out_stride, h->heads}, h->batch, h->tokens, h->head_dim))
     return fail(EVISEL_EINVAL, std::string(what) + ": out must be in itself with the same strides, or apart from it");
   return EVISEL_OK;
 }
@@ -120,7 +152,8 @@ HeadsView view_of(const evisel_heads* h) {
 int check_positions_apart(const evisel_heads* h, const evisel_positions* p, int axes) {
   constexpr int64_t kRuns = 1 << 16, kFar = int64_t(1) << 61;
   if (h->heads == 0) return EVISEL_OK;
-  const Strided out = {h->out, 2, h->head_dim, 3, {h->batch, h->tokens, h->heads}, {h->out_stride[0], h->out_stride[1], h->out_stride[2]}};
+  const int64_t sizes[3] = {h->batch, h->tokens, h->heads};
+  const Strided out = heads_of(h->out, h->out_stride, sizes, h->head_dim);
   bool met = meets(range_of(p->first, 4 * static_cast<int64_t>(h->batch)), out);
   if (p->at) {
     const __int128 reach = static_cast<__int128>(p->stride[0]) * (axes - 1) + static_cast<__int128>(p->stride[1]) * (h->batch - 1) + h->tokens;
@@ -137,11 +170,10 @@ int check_positions_apart(const evisel_heads* h, const evisel_positions* p, int 
 // One input's output over another input (each in its own place is the caller's to answer for: rows of one tensor).
 int check_apart(const evisel_heads* a, const evisel_heads* b) {
   if (a->heads == 0 || b->heads == 0) return EVISEL_OK;
-  const int64_t na[3] = {a->batch, a->tokens, a->heads}, nb[3] = {b->batch, b->tokens, b->heads};
-  const Range out = reach_of(a->out, a->out_stride, na, a->head_dim);
-  if (a->out != a->in && out.meets(reach_of(b->in, b->in_stride, nb, b->head_dim)))
+  const HeadsAt out = {a->out, a->out_stride, a->heads};
+  if (a->out != a->in && !apart(out, {b->in, b->in_stride, b->heads}, a->batch, a->tokens, a->head_dim))
     return fail(EVISEL_EINVAL, "an output lies over the other input");
-  if (a->out == b->out || (a->out != a->in && out.meets(reach_of(b->out, b->out_stride, nb, b->head_dim))))
+  if (a->out == b->out || (a->out != a->in && !apart(out, {b->out, b->out_stride, b->heads}, a->batch, a->tokens, a->head_dim)))
     return fail(EVISEL_EINVAL, "the outputs lie over one another");
   return EVISEL_OK;
 }
@@ -247,8 +279,8 @@ int evisel_cache_append_rotary(const evisel_cache* cache, const evisel_rope* rop
       if (draft->tokens > 0) {
         const int64_t sizes[3] = {cache->batch, draft->tokens, cache->hkv}, rows = static_cast<int64_t>(cache->batch) * draft->tokens;
         const Range out = range_of(q_out, 2 * h.out_stride[0] * cache->batch);
-        if (out.meets(reach_of(draft->k_new, draft->k_new_stride, sizes, cache->head_dim)) ||
-            out.meets(reach_of(draft->v_new, draft->v_new_stride, sizes, cache->head_dim)))
+        if (meets(out, heads_of(draft->k_new, draft->k_new_stride, sizes, cache->head_dim)) ||
+            meets(out, heads_of(draft->v_new, draft->v_new_stride, sizes, cache->head_dim)))
           return fail(EVISEL_EINVAL, "q_out lies over k_new or v_new");
         // (In its own place it lies where q was: the caller's to answer for.)
         if (q_out != draft->q) {

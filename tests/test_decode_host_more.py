@@ -10,7 +10,7 @@ import pytest
 from oracle import decode as ref
 from paper_2608_05780_gb300.build import CSRC, INCLUDE, nvcc
 from test_cache_host import FAKE, _append as _plain_append, _cache, _draft
-from test_decode_host import _append, _at, _heads, _pos, _rope, _rotary, fake  # noqa: F401
+from test_decode_host import _append, _at, _heads, _keys, _pos, _rope, _rotary, fake  # noqa: F401
 
 EINVAL = -1
 MB = 1 << 20
@@ -151,6 +151,29 @@ def test_rotated_heads_over_positions(fake, pos, axes, heads, code):  # noqa: F8
     # Too many sequences to look at one by one, with strides that no memory has.
     many, wide = _heads(out=Q_OUT, batch=1 << 28, tokens=4, out_stride=(1 << 30, 4096, 128)), _pos(at=Q_OUT - 4096, stride=(0, (1 << 38) - 1))
     assert _rotary(fake, None, _rope(), many, None, wide) == EINVAL
+
+
+def test_rotated_heads_in_the_rows_of_one_tensor(fake):  # noqa: F811
+    """Outputs that share rows, and an output beside its input there, share no memory; where they do they are refused."""
+    rows = (3 * 4608, 4608, 128)            # two sequences, three tokens, 36 heads
+    at = lambda head: Q_OUT + 256 * head    # noqa: E731
+    q = lambda head, **kw: _heads(**{**dict(out=at(head), out_stride=rows), **kw})  # noqa: E731
+    k = lambda head, **kw: _keys(**{**dict(out=at(head), out_stride=rows), **kw})  # noqa: E731
+    run = lambda *a: _rotary(fake, None, _rope(), *a, _pos(at=AT))  # noqa: E731
+    assert run(q(0), k(28)) == run(q(0), k(32)) == run(q(8), k(0)) == run(q(8), k(4)) == 0
+    assert run(q(0), k(27)) == run(q(8), k(5)) == run(q(0), k(33)) == run(q(0), k(0)) == EINVAL
+    assert run(q(0), k(36)) == EINVAL       # the second token's row
+    inside = dict(in_stride=rows)
+    assert run(q(0), k(28, src=at(32), **inside)) == run(q(0, src=FAKE), k(28, src=at(28), **inside)) == 0
+    assert run(q(0), k(28, src=at(30), **inside)) == run(q(0), k(28, src=at(20), **inside)) == EINVAL
+    wide = dict(in_stride=(3 * 9216, 9216, 128), out_stride=(3 * 9216, 9216, 128))
+    assert run(q(28, src=at(0), **wide), None) == 0 and run(q(27, src=at(0), **wide), None) == EINVAL
+    # Heads outside the tokens: 36 x 3 rows of a sequence.
+    inner = (3 * 4608, 128, 384)
+    assert run(q(0, out_stride=inner), k(3 * 28, out_stride=inner)) == 0
+    assert run(q(0, out_stride=inner), k(3 * 28 - 1, out_stride=inner)) == EINVAL
+    assert run(q(0), k(3 * 28, out_stride=inner)) == EINVAL         # rows of other strides
+    assert run(q(0, out_stride=(10752, 3584, 128)), k(28)) == EINVAL
 
 
 # --- the oracle's pins -------------------------------------------------------------------

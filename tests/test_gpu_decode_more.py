@@ -41,6 +41,25 @@ def test_rotation_of_prompts(cuda_lib, dtype, d, r, interleaved, batch, tokens, 
     assert torch.equal(q, got[0]) and (k is None or torch.equal(k, got[1]))
 
 
+@pytest.mark.parametrize("tokens", [1, 37, 5000])
+def test_rotation_into_the_rows_of_one_tensor(cuda_lib, tokens):
+    """Queries and keys side by side, and rotated rows beside the plain ones: the same bits, and nothing else written."""
+    import torch
+    ev, rng, dtype = cuda_lib, np.random.default_rng(3), torch.bfloat16
+    rope = ev.Rotary(64, 48)
+    (q, _), (k, _) = (tensor(rng, (2, tokens, h, 64), dtype) for h in (5, 2))
+    want = ev.evisel_rotary(rope, q, k)
+    rows = torch.zeros((2, tokens, 9, 64), dtype=dtype, device="cuda")
+    got = ev.evisel_rotary(rope, q, k, q_out=rows[:, :, :5], k_out=rows[:, :, 5:7])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(rows[:, :, :7], torch.cat(want, 2)) and not rows[:, :, 7:].any()
+    rows = torch.cat([q, torch.zeros_like(q)], 2)
+    ev.evisel_rotary(rope, rows[:, :, :5], q_out=rows[:, :, 5:])
+    assert torch.equal(rows[:, :, :5], q) and torch.equal(rows[:, :, 5:], want[0])
+    heads = torch.zeros((2, 7, tokens, 64), dtype=dtype, device="cuda").transpose(1, 2)
+    ev.evisel_rotary(rope, q, k, q_out=heads[:, :, :5], k_out=heads[:, :, 5:])
+    assert torch.equal(heads, torch.cat(want, 2))
+
+
 # --- append ------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,layout,d,page,interleaved,r,batch,tokens,hq,hkv", [
