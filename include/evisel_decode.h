@@ -37,7 +37,8 @@ typedef struct {
   int32_t reserved;                /* 0                                               */
   uint64_t turn[64];               /* f_i / 2 pi modulo 1, in units of 2^-64 of a turn:
                                       p * turn[i] modulo 2^64 is the angle of any 32-bit
-                                      position, off by at most |p| 2^-53 turns         */
+                                      position, off from p f_i / 2 pi (f_i in fp64) by at
+                                      most |p| max(1, |f_i| / 2 pi) 2^-52 turns        */
 } evisel_rope;
 
 /* Frequencies f_i = base^(-2 i / r), in radians per position; or freq_h[i] (host,

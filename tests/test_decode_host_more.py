@@ -1,8 +1,10 @@
 """Host side of the decoding-step calls, continued: outputs over what a call reads, pages that leave the tables."""
 import ctypes
 import itertools
+import math
 import os
 import subprocess
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -10,7 +12,7 @@ import pytest
 from oracle import decode as ref
 from paper_2608_05780_gb300.build import CSRC, INCLUDE, nvcc
 from test_cache_host import FAKE, _append as _plain_append, _cache, _draft
-from test_decode_host import _append, _at, _heads, _keys, _pos, _rope, _rotary, fake  # noqa: F401
+from test_decode_host import _append, _at, _heads, _keys, _pos, _rope, _rotary, _turns, PI, fake  # noqa: F401
 
 EINVAL = -1
 MB = 1 << 20
@@ -174,6 +176,24 @@ def test_rotated_heads_in_the_rows_of_one_tensor(fake):  # noqa: F811
     assert run(q(0, out_stride=inner), k(3 * 28 - 1, out_stride=inner)) == EINVAL
     assert run(q(0), k(3 * 28, out_stride=inner)) == EINVAL         # rows of other strides
     assert run(q(0, out_stride=(10752, 3584, 128)), k(28)) == EINVAL
+
+
+# --- turns -----------------------------------------------------------------------------
+
+def test_turns_are_as_near_as_documented(fake):  # noqa: F811
+    """f / 2 pi: 2 pi in fp64 is off by 0.35 x 2^-53 relative, the quotient by 2^-53 of itself, a negative one's fraction by
+    2^-54, the cut by 2^-64; whole turns are dropped exactly. Together below max(1, |f| / 2 pi) 2^-52."""
+    rng = np.random.default_rng(0)
+    freqs = [0.0, 1.0, -1.0, 2 * math.pi, 7.5, 100.0, -100.0, 1e4, 12345.678, -1e9, 1e-9, -1e-300, 3e-18, 1e15]
+    freqs += (rng.standard_normal(498) * 10.0 ** rng.uniform(-6, 8, 498)).tolist()
+    for i in range(0, len(freqs), 64):
+        part = freqs[i:i + 64]
+        for t, f in zip(_turns(fake, 2 * len(part), base=float("nan"), freqs=part), part):
+            exact = Fraction(f) / (2 * PI)
+            bound = max(Fraction(1), abs(exact)) / 2 ** 52
+            for p in (1, -1, 70001, (1 << 31) - 1, -(1 << 31)):
+                off = (Fraction((p * t) % 2 ** 64, 2 ** 64) - p * exact) % 1
+                assert min(off, 1 - off) <= abs(p) * bound, (f, p)
 
 
 # --- the oracle's pins -------------------------------------------------------------------
