@@ -371,15 +371,14 @@ __device__ __forceinline__ Two ln(Two s, int exponent) {
 }
 
 // A continuation's place: by value, then by beam, logit and token. A value may leave less of a logit than it has (fp32 logits
-// beside a score of -1e9, or near zero), so that the logit decides among equal ones of a beam. (One number of 128 bits, read in one
-// load: compared key by key, 64 sequences of 8 beams over 152,064 tokens took 33.6 us, and 32.4 so.)
+// beside a score of -1e9, or near zero), so that the logit decides among equal ones of a beam. (Lists are ranked by it as one number of
+// 128 bits, read in one load: 64 sequences of 8 beams over 152,064 tokens take 32.0 us, 33.6 compared key by key.)
 struct alignas(16) Place {
   Key rest, value;
   Place() = default;
   __device__ __forceinline__ Place(Key value_, Key rest_) : rest(rest_), value(value_) {}
-  __device__ __forceinline__ bool operator>(const Place& o) const {
-    return (static_cast<unsigned __int128>(value) << 64 | rest) > (static_cast<unsigned __int128>(o.value) << 64 | o.rest);
-  }
+  __device__ __forceinline__ bool operator>(const Place& o) const { return value > o.value || (value == o.value && rest > o.rest); }
+  __device__ __forceinline__ unsigned __int128 number() const { return static_cast<unsigned __int128>(value) << 64 | rest; }
 };
 __device__ __forceinline__ Key rest_of(int k, float x, int token) {
   return static_cast<Key>(63 - k) << 56 | static_cast<Key>(order_bits(x)) << 24 | static_cast<uint32_t>(0xffffff - token);
@@ -617,7 +616,7 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
       const Place p = s.place[i];
       int rank = 0;
 #pragma unroll 8
-      for (int j = 0; j < listed; ++j) rank += s.place[j] > p ? 1 : 0;
+      for (int j = 0; j < listed; ++j) rank += s.place[j].number() > p.number() ? 1 : 0;
       if (rank < L.n) s.chosen[rank] = token_of(p.rest);
       if (rank == L.n - 1) s.least = p.value;
     }
@@ -626,10 +625,16 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
     Place last{~Key(0), ~Key(0)};
     for (int r = 0; r < L.n; ++r) {
       Place y{0, 0};
-      for (int i = tid; i < ids; i += kMergeThreads) {
-        const float x = all.part[i].x;
-        const Place p = all.place(i, x, all.key(i, x));
-        if (p.value >= bound && last > p && p > y) y = p;
+      auto look = [&](int id, float x, Key key) {
+        if (key < bound || key > last.value || key < y.value) return;
+        const Place p = all.place(id, x, key);
+        if (last > p && p > y) y = p;
+      };
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) look(tid + i * kMergeThreads, first[i], held[i]);
+      for (int id = tid + kHeld * kMergeThreads; id < ids; id += kMergeThreads) {
+        const float x = all.part[id].x;
+        look(id, x, all.key(id, x));
       }
       last = y = highest_of(s, y);
       if (tid == 0) s.chosen[r] = token_of(y.rest), s.least = y.value;
@@ -700,7 +705,7 @@ __device__ __forceinline__ void choose(const BeamLaunch& L, MergeShared& s, int 
       const Place p = s.place[i];
       int rank = 0;
 #pragma unroll 8
-      for (int j = 0; j < count; ++j) rank += s.place[j] > p ? 1 : 0;
+      for (int j = 0; j < count; ++j) rank += s.place[j].number() > p.number() ? 1 : 0;
       if (rank < L.n) put(rank, p);
     }
     for (int i = count + tid; i < L.n; i += kMergeThreads) put(i, {0, 0});
