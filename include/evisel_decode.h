@@ -130,7 +130,8 @@ typedef struct {
  *   token      device int32 [B, n]: v, -1 past them
  *   ended_out  device uint8 [B, n] or NULL: 1 where the parent had ended, where v is
  *              eos, and past them
- * Within a beam the order is that of the logits, exactly; between beams it goes by values of 48
+ * Within a beam the order is that of the logits, exactly, also where a large score leaves less of
+ * them in their values; between beams it goes by values of 48
  * bits whose normaliser is formed from fp32 exponentials, fp32 sums of blocks of 1,024 of them (512 of fp32 logits; powers of
  * two more for long rows) and 48-bit sums of those: off by 2^-18 at most, 1e-7 as a rule. Equal rows have the
  * same normaliser wherever they lie, and the same call gives the same bits. Rows that begin on 16 bytes are read fastest.
@@ -142,7 +143,8 @@ int evisel_beam_select(const evisel_beams* beams, float* score_out, int32_t* par
 /* One array of states by sequence: row c of `out` becomes the row of c's parent. */
 typedef struct {
   const void* in;                  /* device [batch, row_bytes]                       */
-  void* out;                       /* device [batch, row_bytes], apart from every input */
+  void* out;                       /* device [batch, row_bytes], apart from every input and
+                                      (not refused) from the cache's pages and means    */
   int64_t row_bytes;
 } evisel_state;
 

@@ -9,7 +9,7 @@
 // So the pass over the logits keeps no lists, and warps wait for nothing but their loads. What it costs beside the
 // memory is instructions: 64 sequences of 8 beams over 152,064 tokens (156 MB) take 25.5 us (6.1 TB/s, 90% of a plain copy's rate,
 // the schedulers 71% busy), 29.5 with two divisions a block, 42 with lists of candidates by CTA and their bounds.
-// The choice is a chain of dependent steps: 7 us more there, 4.5 of the 6.6 us that four beams over 32,000 tokens take.
+// The choice is a chain of dependent steps: 6.5 us more there, 4.5 of the 6.5 us that four beams over 32,000 tokens take.
 #include <algorithm>
 
 #include "cache_choose.cuh"
@@ -734,8 +734,8 @@ __global__ void __launch_bounds__(kMergeThreads, 2) beam_choice_kernel(const __g
 }
 
 // Both for few blocks, at most two to a warp: a cluster per sequence scans its blocks, and its first CTA chooses. The device
-// takes as long (6.7 us for four beams over 32,000 tokens, 0.7 more than two launches at two blocks a warp), the host
-// 2.5 us less of a call's 19; with four blocks a warp the device lost that again (8.6 to 11.9 us for eight beams over 50,264).
+// takes as long as for two launches (6.4 us for four beams over 32,000 tokens), the host 4 us less of a call's
+// 20; with four blocks a warp the device lost that again (8.6 to 11.9 us for eight beams over 50,264).
 template <class T, bool kSkewed>
 __global__ void __launch_bounds__(kThreads, kPerSm) beam_small_kernel(const __grid_constant__ BeamLaunch L) {
   static_assert(kThreads == kMergeThreads);

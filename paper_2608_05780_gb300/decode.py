@@ -127,7 +127,8 @@ def evisel_rotary(rope, q, k=None, positions=None, first=None, transpose=False, 
     """Queries q [B, T, hq, d] and keys k [B, T, hkv, d] (or [T, H, d] each, of any strides with d contiguous) rotated
     to their positions: int32 ``positions`` [B, T] (or [T]; with a rope of three sections [3, B, T], [3, T]), or
     ``first`` int32 [B] (or [1]) and on, or 0 and on. ``transpose`` applies the transposed matrix: the gradients of q
-    and k from those of the results. ``q_out`` and ``k_out`` may be q and k themselves.
+    and k from those of the results. The call records none by itself: what it returns does not require one, also where q
+    and k do. ``q_out`` and ``k_out`` may be q and k themselves.
 
     Returns (q_out, k_out), None without k."""
     c = _decode()
